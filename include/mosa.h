@@ -252,6 +252,129 @@ int mosa_backward_timed(const mosa_shape* s, const void* X, const mosa_weights* 
 int mosa_forward_noalloc(const mosa_shape* s, const void* X, const mosa_weights* w, void* Y, int accumulate,
                          int32_t* I_out, float* r_out, void* saved, size_t saved_bytes, void* stream);
 
+/* ---------------------------------------------------------------------------
+ * Operators of the dense heads: what a model runs around and beside the layer's
+ * heads when it trains them with normalised queries and keys, lets a local
+ * window keep the first tokens, or answers token by token.
+ *
+ * Conventions, besides those at the top of this file
+ *   - Rows come as `mosa_rows`: d_head contiguous values at
+ *       data + b batch_stride + h head_stride + t row_stride  (elements),
+ *     so that [B, H, T, dh], [B, T, H, dh] and slices of packed rows (the
+ *     layer's saved Q | K | V among them) are read and written as they lie.
+ *     `data` is 16-byte aligned and every stride a multiple of 16 bytes and not
+ *     negative; the stride of an axis of one entry is not read.  An input's
+ *     strides may be 0 (a broadcast input); the rows of an output may not
+ *     overlap (an output's strides are checked against that).
+ *   - d_head is 32, 64 or 128; q_heads is a multiple of kv_heads, and query
+ *     head h goes with key head h / (q_heads / kv_heads).
+ *   - Arrays of int32 on the device (lengths, positions, page tables) cannot be
+ *     checked before the call returns; what a value out of range does is said
+ *     at each of them, and no value makes a kernel leave its tensors.
+ *   - Results are reproducible: no sum depends on the order in which workgroups
+ *     run.  A call that is captured into a graph records kernels only.  Calls
+ *     that may overlap in time need scratch buffers of their own.
+ * ------------------------------------------------------------------------- */
+typedef struct mosa_rows {
+    void* data;
+    int64_t batch_stride, head_stride, row_stride;
+} mosa_rows;
+
+/* Norm and rotation of query and key rows.
+ *   y = R(p) n,  n = w x / sqrt(mean(x^2) + eps)
+ * for every row x of q (weights wq [d_head]) and k (wk), p the token's
+ * position.  R(p) turns the first rope_dim columns in rope_dim / 2 pairs, pair j
+ * by the angle p rope_base^(-2 j / rope_dim): columns 2j and 2j + 1
+ * (MOSA_PAIRS_ADJACENT, as in the layer), or j and j + rope_dim / 2
+ * (MOSA_PAIRS_HALVES).  rope_dim 0 turns nothing; otherwise it is even, at most
+ * d_head, and a multiple of 16 with MOSA_PAIRS_HALVES. */
+#define MOSA_PAIRS_ADJACENT 0
+#define MOSA_PAIRS_HALVES 1
+typedef struct mosa_norm_shape {
+    int32_t batch, seq_len, q_heads, kv_heads, d_head, dtype, rope_dim, rope_pairs;
+    float rope_base, eps;
+} mosa_norm_shape;
+
+/* Scratch of mosa_qk_norm_rope_backward (0 is possible only for an error). */
+int mosa_norm_scratch_size(const mosa_norm_shape* s, size_t* scratch_bytes);
+/* positions: int32 [batch, seq_len], any value, or NULL for 0 .. seq_len - 1.
+ * A NULL weight stands for ones.  An output may be its input (same address and
+ * strides). */
+int mosa_qk_norm_rope(const mosa_norm_shape* s, const mosa_rows* q, const mosa_rows* k, const void* wq,
+                      const void* wk, const int32_t* positions, const mosa_rows* q_out, const mosa_rows* k_out,
+                      void* stream);
+/* From q, k as they went in and the outputs' gradients dq_out, dk_out: dq, dk,
+ * and dwq, dwk [d_head] (each may be NULL where it is not needed).  dq may be
+ * dq_out and dk may be dk_out. */
+int mosa_qk_norm_rope_backward(const mosa_norm_shape* s, const mosa_rows* q, const mosa_rows* k, const void* wq,
+                               const void* wk, const int32_t* positions, const mosa_rows* dq_out,
+                               const mosa_rows* dk_out, const mosa_rows* dq, const mosa_rows* dk, void* dwq,
+                               void* dwk, void* scratch, size_t scratch_bytes, void* stream);
+
+/* Causal attention with a sliding window and first tokens that stay visible.
+ * Sequence b has Q queries and N keys, the last query at the last key's
+ * position: query i sits at p = N - Q + i and sees key j iff
+ *   j <= p  and  (window == 0 or p - j < window or j < sinks).
+ * out = softmax(scale q k^T) v over the keys that it sees; a query that sees
+ * none (Q > N) gives zeros.  lse: natural logarithm of the sum of exp(scale q k)
+ * (-inf for such a query).  Keys that a query does not see do not reach its
+ * output or gradient, whatever they hold. */
+typedef struct mosa_attn_shape {
+    int32_t batch, q_heads, kv_heads, q_len, kv_len, d_head, dtype, window, sinks;
+    float scale;
+} mosa_attn_shape;
+
+/* Scratch of the forward (over rows or over the 4-bit cache) and of the backward. */
+int mosa_attn_scratch_size(const mosa_attn_shape* s, size_t* forward_bytes, size_t* backward_bytes);
+/* q_lens, kv_lens: int32 [batch], Q and N of every sequence (taken into
+ * 0 .. q_len and 0 .. kv_len), or NULL for q_len and kv_len.  Rows past them are
+ * not read; out is 0 and lse -inf there.  lse: float [batch, q_heads, q_len], or
+ * NULL. */
+int mosa_window_attention(const mosa_attn_shape* s, const mosa_rows* q, const mosa_rows* k, const mosa_rows* v,
+                          const int32_t* q_lens, const int32_t* kv_lens, const mosa_rows* out, float* lse,
+                          void* scratch, size_t scratch_bytes, void* stream);
+/* With out and lse of the forward and d_out: dq, dk and dv, summed over the
+ * query heads of a key head; 0 past the lengths. */
+int mosa_window_attention_backward(const mosa_attn_shape* s, const mosa_rows* q, const mosa_rows* k,
+                                   const mosa_rows* v, const mosa_rows* out, const float* lse,
+                                   const mosa_rows* d_out, const int32_t* q_lens, const int32_t* kv_lens,
+                                   const mosa_rows* dq, const mosa_rows* dk, const mosa_rows* dv, void* scratch,
+                                   size_t scratch_bytes, void* stream);
+
+/* A paged cache of key and value rows held in 4 bits.
+ * Groups of 32 values of a row share m, their least value, and s = (greatest -
+ * m) / 15, both in bf16; a value is held as the integer 0 .. 15 nearest to
+ * (x - m) / s (ties to even; differences in fp32) and stands for m + s code.  A
+ * group whose s is below 2^-126 has s = 0; a group with a value that is not
+ * finite, or whose spread is not, stands for NaN throughout.
+ * Position t of sequence b lies in page page_table[b, t / page_size], an int32
+ * of 0 .. pages - 1; page_table is [batch, max_pages].  page_size is a multiple
+ * of 16, at most 1024.  Sequences may share pages that are only read.
+ * `dtype` is the type of the rows that go in and out. */
+typedef struct mosa_cache_shape {
+    int32_t batch, kv_heads, d_head, dtype, pages, page_size, max_pages;
+} mosa_cache_shape;
+
+int mosa_cache4_size(const mosa_cache_shape* s, size_t* cache_bytes);
+/* Rows t < lens[b] of k and v [batch, kv_heads, rows, d_head] become positions
+ * start[b] + t.  start NULL: 0; lens NULL: rows (taken into 0 .. rows).  A
+ * position below 0, past the table, or on a page that does not exist is not
+ * written. */
+int mosa_cache4_append(const mosa_cache_shape* s, void* cache, const int32_t* page_table, const int32_t* start,
+                       const int32_t* lens, int rows, const mosa_rows* k, const mosa_rows* v, void* stream);
+/* The values of positions start[b] + t, t < lens[b], as rows; 0 past lens and
+ * where mosa_cache4_append would not write. */
+int mosa_cache4_read(const mosa_cache_shape* s, const void* cache, const int32_t* page_table, const int32_t* start,
+                     const int32_t* lens, int rows, const mosa_rows* k, const mosa_rows* v, void* stream);
+/* mosa_window_attention over the cache's positions 0 .. kv_lens[b] - 1 (kv_lens
+ * is required, q_lens may be NULL; s->kv_len bounds kv_lens and is at most
+ * max_pages page_size).  Keys on pages that do not exist are not seen; pages
+ * that no query's window or sinks reach are not read. */
+int mosa_cache4_attention(const mosa_attn_shape* s, const mosa_cache_shape* c, const mosa_rows* q,
+                          const void* cache, const int32_t* page_table, const int32_t* q_lens,
+                          const int32_t* kv_lens, const mosa_rows* out, float* lse, void* scratch,
+                          size_t scratch_bytes, void* stream);
+
 /* Static text for a status code (never NULL). */
 const char* mosa_status_string(int status);
 

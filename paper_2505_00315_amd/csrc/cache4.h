@@ -1,0 +1,64 @@
+// Layout of the 4-bit cache and access to single values of it.
+//
+// A page holds, for every key head, a block of page_size positions:
+//   codes of K   page_size rows of dh / 2 bytes
+//   codes of V   page_size / 4 groups of 4 positions, 2 dh bytes each
+//   meta of K    page_size rows of dh / 32 words, s in the low and m in the high half (bf16)
+//   meta of V    the same
+// A K row is dh / 8 words; word kg dh / 32 + g holds columns 32 g + 8 kg .. + 7,
+// column 2 i in nibble i and column 2 i + 1 in nibble i + 4: lane group kg of a
+// matrix instruction over the 32 columns of a group reads its words of all
+// groups with one load, and a shift and a mask give a pair of neighbours.
+// V is kept in 16-bit pieces of 4 columns of one position, the pieces of 4
+// neighbouring positions next to each other, so that a word holds the same
+// columns of two positions: there the matrix instruction runs over positions.
+#pragma once
+
+#include "heads.h"
+
+namespace mosa {
+
+struct CacheBlock {
+    size_t at;  // byte offset of the block
+    int ps, dh;
+    __device__ __forceinline__ size_t kword(int t, int w) const { return at + (size_t)t * (dh / 2) + 4 * w; }
+    __device__ __forceinline__ size_t vpiece(int t, int u) const {
+        return at + (size_t)ps * (dh / 2) + 2 * (((t >> 2) * (dh / 4) + u) * 4 + (t & 3));
+    }
+    __device__ __forceinline__ size_t kmeta(int t, int g) const { return at + (size_t)ps * dh + 4 * (t * (dh / 32) + g); }
+    __device__ __forceinline__ size_t vmeta(int t, int g) const {
+        return kmeta(t, g) + (size_t)ps * (dh / 32) * 4;
+    }
+};
+__host__ __device__ inline size_t cache_block_bytes(int ps, int dh) { return (size_t)ps * (dh + dh / 32 * 8); }
+
+// The block and the place in it of position t of sequence b, head h; false
+// where the table ends or names no page.
+__device__ __forceinline__ bool cache_find(const CacheArgs& c, int b, int h, int t, CacheBlock& blk, int& tl) {
+    const int e = t / c.ps;
+    if (t < 0 || e >= c.per) return false;
+    const int page = c.table[(size_t)b * c.per + e];
+    if (page < 0 || page >= c.pages) return false;
+    blk.at = ((size_t)page * c.H + h) * cache_block_bytes(c.ps, c.dh);
+    blk.ps = c.ps;
+    blk.dh = c.dh;
+    tl = t - e * c.ps;
+    return true;
+}
+
+// m + s code: the product is exact in fp32 (8 and 4 bits), so there is one rounding.
+__device__ __forceinline__ float cache_value(uint32_t meta, uint32_t code) {
+    return __builtin_fmaf((float)code, __uint_as_float(meta << 16), __uint_as_float(meta & 0xffff0000u));
+}
+__device__ __forceinline__ float cache_k(const CacheArgs& c, const CacheBlock& blk, int tl, int d) {
+    const int g = d >> 5, kg = (d >> 3) & 3, i = d & 7;
+    const uint32_t w = *reinterpret_cast<const uint32_t*>(c.cache + blk.kword(tl, kg * (c.dh / 32) + g));
+    return cache_value(*reinterpret_cast<const uint32_t*>(c.cache + blk.kmeta(tl, g)),
+                       (w >> (4 * ((i >> 1) + 4 * (i & 1)))) & 15);
+}
+__device__ __forceinline__ float cache_v(const CacheArgs& c, const CacheBlock& blk, int tl, int d) {
+    const uint32_t w = *reinterpret_cast<const uint16_t*>(c.cache + blk.vpiece(tl, d >> 2));
+    return cache_value(*reinterpret_cast<const uint32_t*>(c.cache + blk.vmeta(tl, d >> 5)), (w >> (4 * (d & 3))) & 15);
+}
+
+}  // namespace mosa

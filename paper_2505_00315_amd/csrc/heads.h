@@ -1,0 +1,114 @@
+// Operators of the dense heads (norm and rotation, windowed attention, the
+// 4-bit cache): arguments shared by their kernels and the host layer.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+#include "common.h"
+#include "kernels.h"
+
+namespace mosa {
+
+// Rows of one head: d_head contiguous values every `row` elements; the strides
+// of axes of one entry are 0 here.
+struct Rows {
+    char* p;
+    int64_t batch, head, row;
+};
+template <typename ST>
+__device__ __forceinline__ ST* row_ptr(const Rows& r, int b, int h, int64_t t) {
+    return reinterpret_cast<ST*>(r.p) + b * r.batch + h * r.head + t * r.row;
+}
+
+// f(storage value, integral constant d_head) for the type and head size of a call.
+template <typename F>
+inline int heads_by_type(int dtype, int dh, F f) {
+    if (dtype == kBF16) {
+        if (dh == 32) return f(uint16_t{}, std::integral_constant<int, 32>{});
+        if (dh == 64) return f(uint16_t{}, std::integral_constant<int, 64>{});
+        return f(uint16_t{}, std::integral_constant<int, 128>{});
+    }
+    if (dh == 32) return f(float{}, std::integral_constant<int, 32>{});
+    if (dh == 64) return f(float{}, std::integral_constant<int, 64>{});
+    return f(float{}, std::integral_constant<int, 128>{});
+}
+
+// ---------------------------------------------------------------------------
+// norm and rotation
+// ---------------------------------------------------------------------------
+constexpr int kMaxTurns = 64;  // pairs of a row of 128
+struct Turns {                 // theta_j / (2 pi): the turns of pair j per position
+    double t[kMaxTurns];
+};
+struct NormArgs {
+    int B, T, Hq, Hkv, dh, rope, halves;
+    float eps;
+    Rows q, k, qo, ko, dq, dk;  // forward: q, k -> qo, ko; backward: q, k and the gradients qo, ko -> dq, dk
+    const void *wq, *wk;
+    const int32_t* pos;
+    Turns turns;
+};
+size_t norm_partial_bytes(int64_t tokens, int dh);
+int launch_qk_norm(int dtype, const NormArgs& a, hipStream_t stream);
+int launch_qk_norm_bwd(int dtype, const NormArgs& a, void* dwq, void* dwk, float* partial, hipStream_t stream);
+
+// ---------------------------------------------------------------------------
+// windowed attention
+// ---------------------------------------------------------------------------
+struct AttnArgs {
+    int B, Hq, Hkv, G, Tq, N, W, S;  // W: 0 or a window below N; S: sinks, at most N
+    float scale;
+    Rows q, k, v, out, dout, dq, dk, dv;
+    const int32_t *ql, *kl;
+    float* lse;  // [B, Hq, Tq] (forward: may be nullptr)
+    float* D;    // backward: sum(out dout) of every query row
+};
+
+// Lengths of sequence b, taken into the tensors.
+__device__ __forceinline__ int seq_len_of(const int32_t* lens, int b, int most) {
+    return lens ? min(max(lens[b], 0), most) : most;
+}
+
+// The visibility rule (positions p, j of the query and the key).
+__device__ __forceinline__ bool sees(const AttnArgs& a, int p, int j) {
+    return j <= p && (a.W == 0 || p - j < a.W || j < a.S);
+}
+
+// Keys that some query of positions p0 .. p1 sees: 0 .. s - 1 and lo .. hi - 1
+// (s <= lo), as one list of `count` keys: entry e is key e below s, lo + e - s above.
+struct KeyList {
+    int s, lo, count;
+    __device__ __forceinline__ int key(int e) const { return e < s ? e : e - s + lo; }
+};
+__device__ __forceinline__ KeyList keys_of(const AttnArgs& a, int p0, int p1, int kn) {
+    KeyList l;
+    const int hi = min(p1 + 1, kn);
+    l.lo = a.W ? min(max(p0 - a.W + 1, 0), max(hi, 0)) : 0;
+    l.s = min(a.S, l.lo);
+    l.count = hi <= 0 ? 0 : l.s + hi - l.lo;
+    return l;
+}
+
+size_t attn_fwd_scratch(int dtype, int dh, const AttnArgs& a);
+size_t attn_bwd_scratch(const AttnArgs& a);
+int launch_window_attn(int dtype, int dh, const AttnArgs& a, float* part, hipStream_t stream);
+int launch_window_attn_bwd(int dtype, int dh, const AttnArgs& a, hipStream_t stream);
+
+// ---------------------------------------------------------------------------
+// the 4-bit cache
+// ---------------------------------------------------------------------------
+struct CacheArgs {
+    int B, H, dh, pages, ps, per;  // ps: positions per page, per: table entries per sequence
+    unsigned char* cache;
+    const int32_t *table, *start, *lens;
+    int rows;
+    Rows k, v;
+};
+int launch_cache4_append(int dtype, const CacheArgs& a, hipStream_t stream);
+int launch_cache4_read(int dtype, const CacheArgs& a, hipStream_t stream);
+size_t cache4_attn_scratch(int dtype, int dh, const AttnArgs& a);
+int launch_cache4_attn(int dtype, const AttnArgs& a, const CacheArgs& c, float* part, hipStream_t stream);
+
+}  // namespace mosa

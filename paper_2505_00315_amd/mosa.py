@@ -22,7 +22,11 @@ MOSA_BF16 = 1
 
 SYMBOLS = ("mosa_workspace_size", "mosa_saved_offsets", "mosa_forward", "mosa_backward",
            "mosa_forward_timed", "mosa_backward_timed", "mosa_status_string", "mosa_adaptive_k",
-           "mosa_forward_noalloc")
+           "mosa_forward_noalloc",
+           # operators of the dense heads (ops.py)
+           "mosa_norm_scratch_size", "mosa_qk_norm_rope", "mosa_qk_norm_rope_backward", "mosa_attn_scratch_size",
+           "mosa_window_attention", "mosa_window_attention_backward", "mosa_cache4_size", "mosa_cache4_append",
+           "mosa_cache4_read", "mosa_cache4_attention")
 NOALLOC_SCRATCH_MAX = 64 << 20  # MOSA_NOALLOC_SCRATCH_MAX
 MAX_STAGES = 32
 
