@@ -175,11 +175,7 @@ __global__ __launch_bounds__(256) void cache4_rows_kernel(AttnArgs a, CacheArgs 
         row_attend<DH>(a, CacheKeys<DH>{c, b, h / a.G}, [&](int e) { return list.key(e); }, 0, list.count, p, kn, q, lane,
                        m, l, o);
     }
-    const float f = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;
-#pragma unroll
-    for (int n = 0; n < RowLanes<DH>::N; ++n)
-        if (RowLanes<DH>::has(lane)) st1<ST>(row_ptr<ST>(a.out, b, h, i) + lane + 64 * n, o[n] * f);
-    if (a.lse && lane == 0) a.lse[row] = l == 0.f ? -__builtin_inff() : m * kLn2 + logf(l);
+    row_finish<ST, DH>(a, b, h, i, row, lane, m, l, o, nullptr, nullptr);
 }
 
 template <class K>

@@ -57,8 +57,24 @@ int launch_qk_norm_bwd(int dtype, const NormArgs& a, void* dwq, void* dwk, float
 // ---------------------------------------------------------------------------
 // windowed attention
 // ---------------------------------------------------------------------------
+// Division of x < 2^31 by n: the product with the reciprocal, rounded up, is at
+// most one too large.
+struct UDiv {
+    uint32_t n, m;
+    __device__ __forceinline__ int div(int x) const {
+        const uint32_t q = m ? (uint32_t)(((uint64_t)(uint32_t)x * m) >> 32) : (uint32_t)x;
+        return (int)(q * n > (uint32_t)x ? q - 1 : q);
+    }
+};
+inline UDiv make_udiv(uint32_t n) { return {n, n == 1 ? 0u : (uint32_t)((((uint64_t)1 << 32) + n - 1) / n)}; }
+
+// The query rows of a key head are taken as one list, the G heads of a query
+// next to each other: row r is query r / G of head r % G of the group.  A block
+// of rows then spans few positions, so the keys that it walks are close to those
+// that each of its rows sees, and the group's heads share every key that is read.
 struct AttnArgs {
     int B, Hq, Hkv, G, Tq, N, W, S;  // W: 0 or a window below N; S: sinks, at most N
+    UDiv gd;                         // by G
     float scale;
     Rows q, k, v, out, dout, dq, dk, dv;
     const int32_t *ql, *kl;
@@ -90,6 +106,33 @@ __device__ __forceinline__ KeyList keys_of(const AttnArgs& a, int p0, int p1, in
     l.count = hi <= 0 ? 0 : l.s + hi - l.lo;
     return l;
 }
+
+// Row r of the list of (b, key head hk): its query index, and its address in a
+// tensor of query rows.
+template <typename ST>
+__device__ __forceinline__ ST* qrow_ptr(const AttnArgs& a, const Rows& t, int b, int hk, int r, int i) {
+    return row_ptr<ST>(t, b, hk * a.G + (r - i * a.G), i);
+}
+// The same row among [B, Hq, Tq].
+__device__ __forceinline__ int64_t qrow_index(const AttnArgs& a, int b, int hk, int r, int i) {
+    return ((int64_t)b * a.Hq + hk * a.G + (r - i * a.G)) * a.Tq + i;
+}
+
+// Results over a part of a row's keys, for every row of [B, Hq, Tq]: the
+// unnormalised sum o, the running maximum m (log2 units) and the sum l of the
+// weights 2^(score - m); merge_parts joins them in the order of the parts.
+struct Parts {
+    float *o, *ml;  // [parts][rows][DH], [parts][rows][2]
+};
+inline size_t parts_bytes(int parts, int64_t rows, int dh) {
+    return parts > 1 ? (size_t)parts * (size_t)rows * (size_t)(dh + 2) * sizeof(float) : 0;
+}
+inline Parts make_parts(float* buf, int parts, int64_t rows, int dh) {
+    return {buf, buf + (size_t)parts * (size_t)rows * (size_t)dh};
+}
+size_t wattn_tiled_scratch(int dh, const AttnArgs& a);  // bf16
+int launch_wattn_tiled(int dh, const AttnArgs& a, float* part, hipStream_t stream);
+int launch_merge_parts(int dtype, int dh, const AttnArgs& a, int parts, const Parts& p, hipStream_t stream);
 
 size_t attn_fwd_scratch(int dtype, int dh, const AttnArgs& a);
 size_t attn_bwd_scratch(const AttnArgs& a);

@@ -90,6 +90,7 @@ int check_attn(const mosa_attn_shape* s) {
 AttnArgs attn_args(const mosa_attn_shape* s, const int32_t* q_lens, const int32_t* kv_lens) {
     AttnArgs a{};
     a.B = s->batch, a.Hq = s->q_heads, a.Hkv = s->kv_heads, a.G = s->q_heads / s->kv_heads;
+    a.gd = make_udiv((uint32_t)a.G);
     a.Tq = s->q_len, a.N = s->kv_len;
     a.W = s->window < s->kv_len ? s->window : 0;  // a window of every key is none
     a.S = s->sinks < s->kv_len ? s->sinks : s->kv_len;

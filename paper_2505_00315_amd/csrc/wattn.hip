@@ -29,8 +29,7 @@ __global__ __launch_bounds__(256) void wattn_rows_kernel(AttnArgs a, uint32_t fi
         row_attend<DH>(a, WideKeys<ST, DH>{a, b, h / a.G}, [&](int e) { return list.key(e); }, 0, list.count, p, kn, q,
                        lane, m, l, o);
     }
-    row_store<ST, DH>(row_ptr<ST>(a.out, b, h, i), lane, o, l > 0.f ? 1.f / l : l == 0.f ? 0.f : l);
-    if (a.lse && lane == 0) a.lse[row] = l == 0.f ? -__builtin_inff() : m * kLn2 + logf(l);
+    row_finish<ST, DH>(a, b, h, i, row, lane, m, l, o, nullptr, nullptr);
 }
 
 // D = sum(out dout) of a query row (0 past the length).
@@ -130,10 +129,13 @@ int bwd_t(const AttnArgs& a, hipStream_t stream) {
 
 }  // namespace
 
-size_t attn_fwd_scratch(int, int, const AttnArgs&) { return 0; }
+size_t attn_fwd_scratch(int dtype, int dh, const AttnArgs& a) {
+    return dtype == kBF16 ? wattn_tiled_scratch(dh, a) : 0;
+}
 size_t attn_bwd_scratch(const AttnArgs& a) { return (size_t)a.B * a.Hq * a.Tq * sizeof(float); }
 
-int launch_window_attn(int dtype, int dh, const AttnArgs& a, float*, hipStream_t stream) {
+int launch_window_attn(int dtype, int dh, const AttnArgs& a, float* part, hipStream_t stream) {
+    if (dtype == kBF16) return launch_wattn_tiled(dh, a, part, stream);
     return heads_by_type(dtype, dh, [&](auto st, auto d) {
         return launch_rows(wattn_rows_kernel<decltype(st), decltype(d)::value>, (int64_t)a.B * a.Hq * a.Tq, a, stream);
     });

@@ -1,0 +1,422 @@
+// Causal attention with a sliding window and first tokens that stay visible:
+// the forward over rows in bf16.
+//
+// One pass over the keys with the running maximum and sum of the softmax.  A
+// workgroup of 4 waves owns 64 QN rows of a key head's row list (16 QN per
+// wave) and walks the keys that some row of the block sees, sinks first, in
+// tiles of 64 through an LDS ring filled by direct global-to-LDS loads:
+//   S^T = K Q^T  (query in the lane),  p = 2^(s c - m),  O^T += V^T P^T
+// with P^T as it lies in the registers of S^T and V^T read transposed from the
+// row-major tile.  The products cost 4 d_head operations per pair and the
+// exponential about as much issue time as a quarter of them; a wave of 32 rows
+// reads each K and V fragment once per 2 matrix instructions, which is what the
+// LDS can deliver at their full rate.
+#include "attn_lds.h"
+#include "heads.h"
+#include "launch_parts.h"
+#include "rowattn.h"
+
+namespace mosa {
+
+namespace {
+
+constexpr int kKB = 64;  // keys per tile
+
+template <int DH>
+__device__ __forceinline__ int wk_swz(int r) {  // K tile: unit permutation of row r
+    if constexpr (DH == 128) return r & 15;
+    else return kswz(r, DH / 8);
+}
+template <int DH>
+__device__ __forceinline__ int wv_swz(int r) {  // V tile (even: transposed reads take unit pairs)
+    if constexpr (DH == 128) return 2 * (r & 7);
+    else return vt_swz<DH / 8>(r);
+}
+template <int DH>
+constexpr int stages() { return DH == 128 ? 2 : 4; }  // 64 KB of ring (32 KB for 32-wide heads): two workgroups per CU
+
+// Launch geometry: blocks of QB rows, nb per (b, key head), each cut into parts.
+struct FwdGeom {
+    int nb, parts;
+};
+
+template <int DH, int QN>
+__global__ __launch_bounds__(256, 2) void wattn_fwd_kernel(AttnArgs a, FwdGeom G, Parts part, uint32_t first) {
+    using ST = uint16_t;
+    constexpr int U = DH / 8, KB = kKB, QB = 64 * QN, STG = stages<DH>(), NS = DH / 32, ND = DH / 16;
+    constexpr int TILE = KB * DH * 2, STAGE = 2 * TILE, LD = TILE / 4096;  // LD: loads per wave and operand tile
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, c16 = lane & 15;
+
+    // Workgroups of one XCD take neighbouring blocks: the blocks of a key head
+    // share its keys.  Without a window later blocks are longer and go first.
+    const uint32_t per = (uint32_t)G.nb * G.parts;
+    uint32_t id = first ? first + blockIdx.x : (uint32_t)xcd_logical_id(blockIdx.x, gridDim.x);
+    const int bh = (int)(id / per), b = bh / a.Hkv, hk = bh % a.Hkv;
+    id %= per;
+    const int pt = (int)(id % G.parts), blk = a.W ? (int)(id / G.parts) : G.nb - 1 - (int)(id / G.parts);
+    const int R = a.Tq * a.G, r0 = blk * QB, wr0 = r0 + 16 * QN * wave;
+    const int qn = seq_len_of(a.ql, b, a.Tq), kn = seq_len_of(a.kl, b, a.N), off = kn - qn;
+    const int rn = qn * a.G;  // rows of this sequence
+
+    // keys of the block's rows, and this part's tiles of them
+    KeyList list{0, 0, 0};
+    if (r0 < rn) list = keys_of(a, off + a.gd.div(r0), off + a.gd.div(min(r0 + QB, rn) - 1), kn);
+    const int all = (list.count + KB - 1) / KB, share = (all + G.parts - 1) / G.parts;
+    const int tbeg = min(pt * share, all), ntile = min(all, tbeg + share) - tbeg;
+
+    // this wave's rows: query index and position of row wr0 + 16 qs + c16
+    int qi[QN], pos[QN];
+#pragma unroll
+    for (int qs = 0; qs < QN; ++qs) {
+        qi[qs] = a.gd.div(min(wr0 + 16 * qs + c16, R - 1));
+        pos[qs] = off + qi[qs];
+    }
+    float m_run[QN], l_run[QN];
+    f32x4 o[QN][ND];
+#pragma unroll
+    for (int qs = 0; qs < QN; ++qs) {
+        m_run[qs] = -__builtin_inff();
+        l_run[qs] = 0.f;
+#pragma unroll
+        for (int db = 0; db < ND; ++db) o[qs][db] = zero4();
+    }
+
+    if (ntile > 0) {
+        // positions of the wave's first and last row, for the tests of whole tiles
+        const int pw0 = off + a.gd.div(min(wr0, rn - 1)), pw1 = off + a.gd.div(min(wr0 + 16 * QN, rn) - 1);
+        // query fragments (B operand): columns 32 st + 8 g .. + 7 (rows past the
+        // sequence are clamped to its last one; they are not written)
+        Frag8<ST> qf[QN][NS];
+#pragma unroll
+        for (int qs = 0; qs < QN; ++qs) {
+            const int r = min(wr0 + 16 * qs + c16, rn - 1);
+            const ST* qp = qrow_ptr<ST>(a, a.q, b, hk, r, a.gd.div(r));
+#pragma unroll
+            for (int st = 0; st < NS; ++st) qf[qs][st] = frag8_load<ST>(qp + 32 * st + 8 * g);
+        }
+        // Take the rows now: a first use inside the pipeline would wait there
+        // for every load in flight, the next tiles' included.
+#pragma unroll
+        for (int qs = 0; qs < QN; ++qs)
+#pragma unroll
+            for (int st = 0; st < NS; ++st) asm volatile("" : "+v"(qf[qs][st].v));
+
+        // 16-byte unit p = 64 (wave + 4 j) + lane of a tile is row p / U, stored
+        // unit p % U, which holds the row's unit (p % U) ^ swizzle(row)
+        const uint32_t lbase = __builtin_amdgcn_readfirstlane(lds_addr(smem)) +
+                               1024 * (uint32_t)__builtin_amdgcn_readfirstlane(wave);
+        int drow[LD], kcol[LD], vcol[LD];
+#pragma unroll
+        for (int j = 0; j < LD; ++j) {
+            const int p = 64 * (wave + 4 * j) + lane, r = p / U, u = p % U;
+            drow[j] = r;
+            kcol[j] = 8 * (u ^ wk_swz<DH>(r));
+            vcol[j] = 8 * (u ^ wv_swz<DH>(r));
+        }
+        const ST* kp = row_ptr<ST>(a.k, b, hk, 0);
+        const ST* vp = row_ptr<ST>(a.v, b, hk, 0);
+        const int64_t krow = a.k.row, vrow = a.v.row;
+        // tile t of this part (past the end: the last one again, into a buffer
+        // that nobody reads); entries past the list are its last one (masked)
+        auto issue = [&](int t, int buf) {
+            const int e0 = KB * (tbeg + min(t, ntile - 1));
+            const uint32_t base = lbase + buf * STAGE;
+#pragma unroll
+            for (int j = 0; j < LD; ++j) {
+                const int key = list.key(min(e0 + drow[j], list.count - 1));
+                lds_load16(kp + key * krow + kcol[j], base + 4096 * j);
+                lds_load16(vp + key * vrow + vcol[j], base + TILE + 4096 * j);
+            }
+        };
+        // byte offsets within a V tile of the transposed reads: keys
+        // 32 u + 4 g + c16 / 4 and 16 more, columns 16 db + 4 (c16 % 4); both
+        // swizzles depend on the row's low 4 bits only
+        int voff[ND];
+#pragma unroll
+        for (int db = 0; db < ND; ++db) {
+            const int kk = 4 * g + (c16 >> 2), col = 16 * db + 4 * (c16 & 3), un = col >> 3, half = (col >> 2) & 1;
+            voff[db] = (kk * U + (un ^ wv_swz<DH>(kk))) * 16 + 8 * half;
+        }
+        int koff[NS];
+#pragma unroll
+        for (int st = 0; st < NS; ++st) koff[st] = (c16 * U + ((4 * st + g) ^ wk_swz<DH>(c16))) * 16;
+
+        const float c2 = a.scale * kLog2e;  // scores in log2 units
+#pragma unroll
+        for (int s = 0; s < STG - 1; ++s) issue(s, s);
+        auto tile_step = [&](int it, auto bufc) {
+            constexpr int BUF = decltype(bufc)::value;
+            wait_vmcnt<(STG - 2) * 2 * LD>();  // tile it is in LDS
+            __syncthreads();                   // for every wave; the buffer of tile it - 1 is free
+            issue(it + STG - 1, (BUF + STG - 1) % STG);
+            const unsigned char* Kb = smem + BUF * STAGE;
+            const unsigned char* Vb = Kb + TILE;
+            const int e0 = KB * (tbeg + it);
+            // keys of the tile's window part: at least kmin, at most kmax
+            const int kmax = list.key(min(e0 + KB, list.count) - 1), kmin = e0 >= list.s ? list.key(e0) : list.lo;
+            if (e0 >= list.s && (kmin > pw1 || (a.W && kmax <= pw0 - a.W && kmin >= a.S))) return;  // nothing for this wave
+
+            f32x4 s[QN][4];
+#pragma unroll
+            for (int sb = 0; sb < 4; ++sb) {
+                Frag8<ST> kf[NS];
+#pragma unroll
+                for (int st = 0; st < NS; ++st)
+                    kf[st].v = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(Kb + koff[st] + 16 * U * 16 * sb));
+#pragma unroll
+                for (int qs = 0; qs < QN; ++qs) s[qs][sb] = zero4();
+#pragma unroll
+                for (int st = 0; st < NS; ++st)
+#pragma unroll
+                    for (int qs = 0; qs < QN; ++qs) mma8(s[qs][sb], kf[st], qf[qs][st]);
+            }
+            // per-element mask only where the tile is not seen whole by the wave's rows
+            if (e0 + KB > list.count || kmax > pw0 || (a.W && kmin <= pw1 - a.W)) {
+#pragma unroll
+                for (int sb = 0; sb < 4; ++sb)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int e = e0 + 16 * sb + 4 * g + i, key = list.key(e);
+                        const bool in = e < list.count;
+#pragma unroll
+                        for (int qs = 0; qs < QN; ++qs)
+                            s[qs][sb][i] = in && sees(a, pos[qs], key) ? s[qs][sb][i] : -__builtin_inff();
+                    }
+            }
+#pragma unroll
+            for (int qs = 0; qs < QN; ++qs) {
+                float mloc = -__builtin_inff();  // over the raw scores (the scale is positive)
+#pragma unroll
+                for (int sb = 0; sb < 4; ++sb)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) mloc = fmaxf(mloc, s[qs][sb][i]);
+                mloc = rows4_max(mloc) * c2;
+                // The reference maximum moves only when the tile's exceeds it by
+                // more than 8 (log2 units): weights stay below 2^8, and O and l
+                // are rescaled only in tiles where some row of the wave moved.
+                const float m_new = mloc > m_run[qs] + 8.f ? mloc : m_run[qs];
+                const float m_use = m_new == -__builtin_inff() ? 0.f : m_new;
+                if (__builtin_amdgcn_ballot_w64(m_new != m_run[qs])) {
+                    const float alpha = __builtin_amdgcn_exp2f(m_run[qs] - m_use);
+                    l_run[qs] *= alpha;
+#pragma unroll
+                    for (int db = 0; db < ND; ++db) o[qs][db] *= alpha;
+                    m_run[qs] = m_new;
+                }
+                float lsum = 0.f;
+#pragma unroll
+                for (int sb = 0; sb < 4; ++sb)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        s[qs][sb][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[qs][sb][i], c2, -m_use));
+                        lsum += s[qs][sb][i];
+                    }
+                l_run[qs] += lsum;  // this lane's keys; the 4 lanes of a row are added at the end
+            }
+            // O^T += V^T P^T, 32 keys per instruction: slots 0..3 are keys 4 g + i
+            // of block 2 u, slots 4..7 those of block 2 u + 1.  P is rounded to
+            // bf16 here, the type of the matrix operands (l sums it unrounded).
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                Frag8<ST> pf[QN];
+#pragma unroll
+                for (int qs = 0; qs < QN; ++qs) {
+                    const f32x4 &x = s[qs][2 * u], &y = s[qs][2 * u + 1];
+                    const float pv[8] = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+                    pf[qs] = frag8_from<ST>(pv);
+                }
+#pragma unroll
+                for (int db = 0; db < ND; ++db) {
+                    const u32x2 lo = lds_tr16(Vb + voff[db] + 32 * u * U * 16);
+                    const u32x2 hi = lds_tr16(Vb + voff[db] + (32 * u + 16) * U * 16);
+                    Frag8<ST> vf;
+                    vf.v = __builtin_bit_cast(bf16x8, u32x4{lo.x, lo.y, hi.x, hi.y});
+#pragma unroll
+                    for (int qs = 0; qs < QN; ++qs) mma8(o[qs][db], vf, pf[qs]);
+                }
+            }
+        };
+        for (int it0 = 0;; it0 += STG) {
+            bool last = false;
+            static_for<0, STG>([&](auto u) {
+                if (last) return;
+                const int it = it0 + decltype(u)::value;
+                tile_step(it, u);
+                last = it + 1 >= ntile;
+            });
+            if (last) break;
+        }
+        mfma_drain();     // the MFMA results are read below
+        wait_vmcnt<0>();  // the trailing loads still write into the ring
+    }
+    __syncthreads();
+#pragma unroll
+    for (int qs = 0; qs < QN; ++qs) l_run[qs] = rows4_sum(l_run[qs]);
+
+    // A weight of 0 times a value that is not finite is NaN: if some result of
+    // the wave is not finite, its rows are done again one by one, over the keys
+    // that each of them sees.
+    bool fine = true;
+#pragma unroll
+    for (int qs = 0; qs < QN; ++qs) {
+        float t = l_run[qs] * 0.f;
+#pragma unroll
+        for (int db = 0; db < ND; ++db)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) t = __builtin_fmaf(o[qs][db][i], 0.f, t);
+        fine &= t == 0.f;
+    }
+    const bool parts = G.parts > 1;
+    const int64_t rows = (int64_t)a.B * a.Hq * a.Tq;
+    if (__builtin_amdgcn_ballot_w64(!fine)) {
+#pragma unroll 1
+        for (int r = wr0; r < min(wr0 + 16 * QN, R); ++r) {
+            const int i = a.gd.div(r), h = hk * a.G + r - i * a.G;
+            const int64_t row = qrow_index(a, b, hk, r, i);
+            float q[RowLanes<DH>::N], x[RowLanes<DH>::N] = {}, m = -__builtin_inff(), l = 0.f;
+            if (r < rn) {
+                row_load<ST, DH>(row_ptr<ST>(a.q, b, h, i), lane, q);
+                row_attend<DH>(a, WideKeys<ST, DH>{a, b, hk}, [&](int e) { return list.key(e); }, KB * tbeg,
+                               min(KB * (tbeg + ntile), list.count), off + i, kn, q, lane, m, l, x);
+            }
+            row_finish<ST, DH>(a, b, h, i, row, lane, m, l, x, parts ? part.o + (pt * rows + row) * DH : nullptr,
+                               part.ml + (pt * rows + row) * 2);
+        }
+        return;
+    }
+    if (parts) {
+#pragma unroll
+        for (int qs = 0; qs < QN; ++qs) {
+            const int r = wr0 + 16 * qs + c16;
+            if (r >= R) continue;
+            const int64_t at = pt * rows + qrow_index(a, b, hk, r, qi[qs]);
+            const bool live = r < rn;
+#pragma unroll
+            for (int db = 0; db < ND; ++db)
+                *reinterpret_cast<float4*>(part.o + at * DH + 16 * db + 4 * g) =
+                    live ? make_float4(o[qs][db][0], o[qs][db][1], o[qs][db][2], o[qs][db][3]) : make_float4(0, 0, 0, 0);
+            if (g == 0) *reinterpret_cast<float2*>(part.ml + at * 2) = live ? make_float2(m_run[qs], l_run[qs]) : make_float2(-__builtin_inff(), 0.f);
+        }
+        return;
+    }
+    // out = O / l through LDS to 16-byte row stores, lse = m ln 2 + log l
+    constexpr int LDO = DH + 8;
+    ST* Os = reinterpret_cast<ST*>(smem) + wave * 16 * QN * LDO;
+#pragma unroll
+    for (int qs = 0; qs < QN; ++qs) {
+        const int r = wr0 + 16 * qs + c16;
+        const bool live = r < rn && l_run[qs] > 0.f;
+        const float inv = live ? 1.f / l_run[qs] : 0.f;
+#pragma unroll
+        for (int db = 0; db < ND; ++db)
+            *reinterpret_cast<uint2*>(Os + (16 * qs + c16) * LDO + 16 * db + 4 * g) =
+                make_uint2(pack_bf16x2(o[qs][db][0] * inv, o[qs][db][1] * inv),
+                           pack_bf16x2(o[qs][db][2] * inv, o[qs][db][3] * inv));
+        if (a.lse && g == 0 && r < R)
+            a.lse[qrow_index(a, b, hk, r, qi[qs])] = live ? m_run[qs] * kLn2 + logf(l_run[qs]) : -__builtin_inff();
+    }
+    __syncthreads();
+#pragma unroll
+    for (int e = lane; e < 16 * QN * U; e += 64) {
+        const int lr = e / U, dc = (e % U) * 8, r = wr0 + lr;
+        if (r < R)
+            *reinterpret_cast<uint4*>(qrow_ptr<ST>(a, a.out, b, hk, r, a.gd.div(r)) + dc) =
+                *reinterpret_cast<const uint4*>(Os + lr * LDO + dc);
+    }
+}
+
+// A row of the call: the parts in their order, M = max m_s, L = sum l_s 2^(m_s - M).
+template <typename ST, int DH>
+__global__ __launch_bounds__(256) void wattn_merge_kernel(AttnArgs a, int parts, Parts p, uint32_t first) {
+    const int lane = threadIdx.x & 63;
+    const int64_t rows = (int64_t)a.B * a.Hq * a.Tq, row = ((int64_t)first + blockIdx.x) * 4 + (threadIdx.x >> 6);
+    if (row >= rows) return;
+    float M = -__builtin_inff(), L = 0.f, o[RowLanes<DH>::N] = {};
+    for (int s = lane; s < parts; s += 64) M = fmaxf(M, p.ml[(s * rows + row) * 2]);
+#pragma unroll
+    for (int x = 32; x > 0; x >>= 1) M = fmaxf(M, __shfl_xor(M, x, 64));
+    const float mu = M == -__builtin_inff() ? 0.f : M;
+#pragma unroll 4
+    for (int s = 0; s < parts; ++s) {
+        const float2 ml = *reinterpret_cast<const float2*>(p.ml + (s * rows + row) * 2);
+        const float f = __builtin_amdgcn_exp2f(ml.x - mu);
+        L += ml.y * f;
+#pragma unroll
+        for (int n = 0; n < RowLanes<DH>::N; ++n)
+            if (RowLanes<DH>::has(lane)) {
+                const float x = p.o[(s * rows + row) * DH + lane + 64 * n];
+                o[n] += f == 0.f ? 0.f : x * f;
+            }
+    }
+    const int i = (int)(row % a.Tq), h = (int)(row / a.Tq % a.Hq), b = (int)(row / a.Tq / a.Hq);
+    row_finish<ST, DH>(a, b, h, i, row, lane, M, L, o, nullptr, nullptr);
+}
+
+// Blocks of 128 rows share K and V fragments over two matrix instructions each;
+// blocks of 64 where those of 128 leave CUs idle, and parts of a block's keys
+// where even they do.
+template <int DH>
+int blocks_of(const AttnArgs& a, int qn) { return (int)(((int64_t)a.Tq * a.G + 64 * qn - 1) / (64 * qn)); }
+
+template <int DH>
+int fwd_qn(const AttnArgs& a) { return (int64_t)blocks_of<DH>(a, 2) * a.B * a.Hkv >= 512 ? 2 : 1; }
+
+template <int DH>
+FwdGeom fwd_geom(const AttnArgs& a) {
+    FwdGeom G;
+    G.nb = blocks_of<DH>(a, fwd_qn<DH>(a));
+    const int64_t blocks = (int64_t)G.nb * a.B * a.Hkv;
+    // most keys of a block, in tiles; a part keeps at least 4 of them
+    const int64_t span = a.W ? (int64_t)a.W + a.S + 64 / a.G + 1 : a.N;
+    const int64_t tiles = ((span < a.N ? span : a.N) + kKB - 1) / kKB;
+    int64_t parts = blocks >= 256 ? 1 : (512 + blocks - 1) / blocks;
+    if (parts > tiles / 4) parts = tiles / 4;
+    G.parts = parts < 1 ? 1 : (int)parts;
+    return G;
+}
+
+template <int DH, int QN>
+int launch_fwd(const AttnArgs& a, const FwdGeom& G, float* buf, hipStream_t stream) {
+    const size_t ring = (size_t)stages<DH>() * 2 * kKB * DH * 2, outs = (size_t)64 * QN * (DH + 8) * 2;
+    const size_t lds = ring > outs ? ring : outs;
+    const Parts part = make_parts(buf, G.parts, (int64_t)a.B * a.Hq * a.Tq, DH);
+    auto kern = wattn_fwd_kernel<DH, QN>;
+    if (allow_lds((const void*)kern, lds)) return -1;
+    return launch_parts((uint64_t)a.B * a.Hkv * G.nb * G.parts, 256, [&](uint32_t first, uint32_t blocks) {
+        hipLaunchKernelGGL(kern, dim3(blocks), dim3(256), lds, stream, a, G, part, first);
+        return hipGetLastError() == hipSuccess ? 0 : -1;
+    });
+}
+
+}  // namespace
+
+int launch_merge_parts(int dtype, int dh, const AttnArgs& a, int parts, const Parts& p, hipStream_t stream) {
+    return heads_by_type(dtype, dh, [&](auto st, auto d) {
+        return launch_parts(((uint64_t)a.B * a.Hq * a.Tq + 3) / 4, 256, [&](uint32_t first, uint32_t blocks) {
+            hipLaunchKernelGGL((wattn_merge_kernel<decltype(st), decltype(d)::value>), dim3(blocks), dim3(256), 0,
+                               stream, a, parts, p, first);
+            return hipGetLastError() == hipSuccess ? 0 : -1;
+        });
+    });
+}
+
+size_t wattn_tiled_scratch(int dh, const AttnArgs& a) {
+    const FwdGeom G = dh == 128 ? fwd_geom<128>(a) : dh == 64 ? fwd_geom<64>(a) : fwd_geom<32>(a);
+    return parts_bytes(G.parts, (int64_t)a.B * a.Hq * a.Tq, dh);
+}
+
+int launch_wattn_tiled(int dh, const AttnArgs& a, float* buf, hipStream_t stream) {
+    auto run = [&](auto d) {
+        constexpr int DH = decltype(d)::value;
+        const FwdGeom G = fwd_geom<DH>(a);
+        const int e = fwd_qn<DH>(a) == 2 ? launch_fwd<DH, 2>(a, G, buf, stream) : launch_fwd<DH, 1>(a, G, buf, stream);
+        if (e || G.parts == 1) return e;
+        return launch_merge_parts(kBF16, DH, a, G.parts, make_parts(buf, G.parts, (int64_t)a.B * a.Hq * a.Tq, DH), stream);
+    };
+    if (dh == 128) return run(std::integral_constant<int, 128>{});
+    if (dh == 64) return run(std::integral_constant<int, 64>{});
+    return run(std::integral_constant<int, 32>{});
+}
+
+}  // namespace mosa
