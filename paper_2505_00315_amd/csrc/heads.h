@@ -79,7 +79,7 @@ struct AttnArgs {
     Rows q, k, v, out, dout, dq, dk, dv;
     const int32_t *ql, *kl;
     float* lse;  // [B, Hq, Tq] (forward: may be nullptr)
-    float* D;    // backward: sum(out dout) of every query row
+    float2* ld;  // backward: of every query row, lse in log2 units (+inf where it sees nothing) and sum(out dout)
 };
 
 // Lengths of sequence b, taken into the tensors.
@@ -135,9 +135,11 @@ int launch_wattn_tiled(int dh, const AttnArgs& a, float* part, hipStream_t strea
 int launch_merge_parts(int dtype, int dh, const AttnArgs& a, int parts, const Parts& p, hipStream_t stream);
 
 size_t attn_fwd_scratch(int dtype, int dh, const AttnArgs& a);
-size_t attn_bwd_scratch(const AttnArgs& a);
+size_t attn_bwd_scratch(int dtype, int dh, const AttnArgs& a);
 int launch_window_attn(int dtype, int dh, const AttnArgs& a, float* part, hipStream_t stream);
-int launch_window_attn_bwd(int dtype, int dh, const AttnArgs& a, hipStream_t stream);
+int launch_window_attn_bwd(int dtype, int dh, AttnArgs a, void* scratch, hipStream_t stream);
+int launch_wattn_bwd_tiled(int dh, const AttnArgs& a, float* sums, hipStream_t stream);  // bf16
+size_t wattn_bwd_sums(int dh, const AttnArgs& a);
 
 // ---------------------------------------------------------------------------
 // the 4-bit cache

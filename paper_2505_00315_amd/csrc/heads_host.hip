@@ -204,7 +204,7 @@ int mosa_attn_scratch_size(const mosa_attn_shape* s, size_t* forward_bytes, size
     const AttnArgs a = attn_args(s, nullptr, nullptr);
     const size_t rows = attn_fwd_scratch(s->dtype, s->d_head, a), cache = cache4_attn_scratch(s->dtype, s->d_head, a);
     *forward_bytes = rows > cache ? rows : cache;
-    *backward_bytes = attn_bwd_scratch(a);
+    *backward_bytes = attn_bwd_scratch(s->dtype, s->d_head, a);
     return MOSA_OK;
 }
 
@@ -234,9 +234,8 @@ int mosa_window_attention_backward(const mosa_attn_shape* s, const mosa_rows* q,
     if (const int e = take_rows(dq, a.B, a.Hq, a.Tq, s->d_head, s->dtype, true, &a.dq)) return e;
     if (const int e = take_rows(dk, a.B, a.Hkv, a.N, s->d_head, s->dtype, true, &a.dk)) return e;
     if (const int e = take_rows(dv, a.B, a.Hkv, a.N, s->d_head, s->dtype, true, &a.dv)) return e;
-    if (const int e = check_scratch(scratch, scratch_bytes, attn_bwd_scratch(a))) return e;
-    a.D = static_cast<float*>(scratch);
-    return done(launch_window_attn_bwd(s->dtype, s->d_head, a, static_cast<hipStream_t>(stream)));
+    if (const int e = check_scratch(scratch, scratch_bytes, attn_bwd_scratch(s->dtype, s->d_head, a))) return e;
+    return done(launch_window_attn_bwd(s->dtype, s->d_head, a, scratch, static_cast<hipStream_t>(stream)));
 }
 
 int mosa_cache4_size(const mosa_cache_shape* s, size_t* cache_bytes) {

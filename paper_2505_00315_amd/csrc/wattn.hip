@@ -32,117 +32,100 @@ __global__ __launch_bounds__(256) void wattn_rows_kernel(AttnArgs a, uint32_t fi
     row_finish<ST, DH>(a, b, h, i, row, lane, m, l, o, nullptr, nullptr);
 }
 
-// D = sum(out dout) of a query row (0 past the length).
+// (lse in log2 units, D = sum(out dout)) of every query row, 8 columns per lane:
+// what the backward's kernels read of a row beside q and dout.  Bound by the
+// rows of out and dout, which it reads once.
 template <typename ST, int DH>
-__global__ __launch_bounds__(256) void wattn_d_kernel(AttnArgs a, uint32_t first) {
-    const int lane = threadIdx.x & 63;
-    const int64_t row = ((int64_t)first + blockIdx.x) * 4 + (threadIdx.x >> 6);
+__global__ __launch_bounds__(256) void wattn_ld_kernel(AttnArgs a, uint32_t first) {
+    constexpr int L = DH / 8;
+    const int64_t row = ((int64_t)first + blockIdx.x) * (256 / L) + threadIdx.x / L;
     if (row >= (int64_t)a.B * a.Hq * a.Tq) return;
+    const int li = threadIdx.x % L;
     const int i = (int)(row % a.Tq), h = (int)(row / a.Tq % a.Hq), b = (int)(row / a.Tq / a.Hq);
-    float x[RowLanes<DH>::N], y[RowLanes<DH>::N], d = 0.f;
-    if (i < seq_len_of(a.ql, b, a.Tq)) {
-        row_load<ST, DH>(row_ptr<ST>(a.out, b, h, i), lane, x);
-        row_load<ST, DH>(row_ptr<ST>(a.dout, b, h, i), lane, y);
-        d = row_dot<DH>(x, y);
+    float d = 0.f;
+    const bool live = i < seq_len_of(a.ql, b, a.Tq);
+    if (live) {
+        float x[8], y[8];
+        frag8_to_f32<ST>(frag8_load<ST>(row_ptr<ST>(a.out, b, h, i) + 8 * li), x);
+        frag8_to_f32<ST>(frag8_load<ST>(row_ptr<ST>(a.dout, b, h, i) + 8 * li), y);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) d += x[e] * y[e];
     }
-    if (lane == 0) a.D[row] = d;
+#pragma unroll
+    for (int o = L / 2; o > 0; o >>= 1) d += __shfl_xor(d, o, 64);
+    if (li == 0) {
+        const float l = live ? a.lse[row] : -__builtin_inff();
+        a.ld[row] = make_float2(l == -__builtin_inff() ? __builtin_inff() : l * kLog2e, d);
+    }
 }
 
-// One wave per query row: dq = scale sum_j ds_j k_j, ds = p (dout v_j - D).
+// One wave per query row, and one per key row.
 template <typename ST, int DH>
 __global__ __launch_bounds__(256) void wattn_dq_rows_kernel(AttnArgs a, uint32_t first) {
-    constexpr int N = RowLanes<DH>::N;
     const int lane = threadIdx.x & 63;
     const int64_t row = ((int64_t)first + blockIdx.x) * 4 + (threadIdx.x >> 6);
     if (row >= (int64_t)a.B * a.Hq * a.Tq) return;
     const int i = (int)(row % a.Tq), h = (int)(row / a.Tq % a.Hq), b = (int)(row / a.Tq / a.Hq);
-    const int qn = seq_len_of(a.ql, b, a.Tq), kn = seq_len_of(a.kl, b, a.N), p = kn - qn + i;
-    float dq[N] = {};
-    if (i < qn) {
-        float q[N], g[N], k[N], v[N];
-        row_load<ST, DH>(row_ptr<ST>(a.q, b, h, i), lane, q);
-        row_load<ST, DH>(row_ptr<ST>(a.dout, b, h, i), lane, g);
-        const float lse = a.lse[row], D = a.D[row];
-        const KeyList list = keys_of(a, p, p, kn);
-        const WideKeys<ST, DH> keys{a, b, h / a.G};
-        for (int e = 0; e < list.count; ++e) {
-            keys.load(list.key(e), lane, k, v);
-            const float w = __builtin_amdgcn_exp2f((row_dot<DH>(q, k) * a.scale - lse) * kLog2e);
-            const float ds = w * (row_dot<DH>(g, v) - D) * a.scale;
-#pragma unroll
-            for (int n = 0; n < N; ++n) dq[n] += ds * k[n];
-        }
-    }
-    row_store<ST, DH>(row_ptr<ST>(a.dq, b, h, i), lane, dq, 1.f);
+    const int qn = seq_len_of(a.ql, b, a.Tq), kn = seq_len_of(a.kl, b, a.N);
+    const float zero[RowLanes<DH>::N] = {};
+    if (i < qn) row_dq<ST, DH>(a, b, h, i, kn - qn + i, kn, lane);
+    else row_store<ST, DH>(row_ptr<ST>(a.dq, b, h, i), lane, zero, 0.f);
 }
 
-// One wave per key row: dv = sum_i p_i dout_i, dk = scale sum_i ds_i q_i over
-// the queries that see it, of every query head of the group.
 template <typename ST, int DH>
 __global__ __launch_bounds__(256) void wattn_dkv_rows_kernel(AttnArgs a, uint32_t first) {
-    constexpr int N = RowLanes<DH>::N;
     const int lane = threadIdx.x & 63;
     const int64_t row = ((int64_t)first + blockIdx.x) * 4 + (threadIdx.x >> 6);
     if (row >= (int64_t)a.B * a.Hkv * a.N) return;
     const int j = (int)(row % a.N), hk = (int)(row / a.N % a.Hkv), b = (int)(row / a.N / a.Hkv);
     const int qn = seq_len_of(a.ql, b, a.Tq), kn = seq_len_of(a.kl, b, a.N), off = kn - qn;
-    float dk[N] = {}, dv[N] = {};
-    if (j < kn) {
-        float q[N], g[N], k[N], v[N];
-        const WideKeys<ST, DH> keys{a, b, hk};
-        keys.load(j, lane, k, v);
-        for (int h = hk * a.G; h < (hk + 1) * a.G; ++h)
-            for (int i = max(0, j - off); i < qn; ++i) {
-                if (!sees(a, off + i, j)) break;
-                const int64_t qr = ((int64_t)b * a.Hq + h) * a.Tq + i;
-                row_load<ST, DH>(row_ptr<ST>(a.q, b, h, i), lane, q);
-                row_load<ST, DH>(row_ptr<ST>(a.dout, b, h, i), lane, g);
-                const float w = __builtin_amdgcn_exp2f((row_dot<DH>(q, k) * a.scale - a.lse[qr]) * kLog2e);
-                const float ds = w * (row_dot<DH>(g, v) - a.D[qr]) * a.scale;
-#pragma unroll
-                for (int n = 0; n < N; ++n) {
-                    dk[n] += ds * q[n];
-                    dv[n] += w * g[n];
-                }
-            }
-    }
+    float dk[RowLanes<DH>::N] = {}, dv[RowLanes<DH>::N] = {};
+    if (j < kn)
+        row_dkv<ST, DH>(a, b, hk, j, off, min(max(0, j - off), qn) * a.G, qn * a.G, [&](int p) { return sees(a, p, j); }, lane, dk,
+                        dv);
     row_store<ST, DH>(row_ptr<ST>(a.dk, b, hk, j), lane, dk, 1.f);
     row_store<ST, DH>(row_ptr<ST>(a.dv, b, hk, j), lane, dv, 1.f);
 }
 
 template <class K>
-int launch_rows(K kern, int64_t rows, const AttnArgs& a, hipStream_t stream) {
-    return launch_parts((uint64_t)(rows + 3) / 4, 256, [&](uint32_t first, uint32_t blocks) {
+int launch_rows(K kern, int64_t rows, int per_block, const AttnArgs& a, hipStream_t stream) {
+    return launch_parts((uint64_t)(rows + per_block - 1) / per_block, 256, [&](uint32_t first, uint32_t blocks) {
         hipLaunchKernelGGL(kern, dim3(blocks), dim3(256), 0, stream, a, first);
         return hipGetLastError() == hipSuccess ? 0 : -1;
     });
 }
 
-template <typename ST, int DH>
-int bwd_t(const AttnArgs& a, hipStream_t stream) {
-    const int64_t qrows = (int64_t)a.B * a.Hq * a.Tq, krows = (int64_t)a.B * a.Hkv * a.N;
-    int e = launch_rows(wattn_d_kernel<ST, DH>, qrows, a, stream);
-    if (!e) e = launch_rows(wattn_dq_rows_kernel<ST, DH>, qrows, a, stream);
-    if (!e) e = launch_rows(wattn_dkv_rows_kernel<ST, DH>, krows, a, stream);
-    return e;
-}
+size_t ld_bytes(const AttnArgs& a) { return ((size_t)a.B * a.Hq * a.Tq * sizeof(float2) + 255) / 256 * 256; }
 
 }  // namespace
 
 size_t attn_fwd_scratch(int dtype, int dh, const AttnArgs& a) {
     return dtype == kBF16 ? wattn_tiled_scratch(dh, a) : 0;
 }
-size_t attn_bwd_scratch(const AttnArgs& a) { return (size_t)a.B * a.Hq * a.Tq * sizeof(float); }
+size_t attn_bwd_scratch(int dtype, int dh, const AttnArgs& a) {
+    return ld_bytes(a) + (dtype == kBF16 ? wattn_bwd_sums(dh, a) : 0);
+}
 
 int launch_window_attn(int dtype, int dh, const AttnArgs& a, float* part, hipStream_t stream) {
     if (dtype == kBF16) return launch_wattn_tiled(dh, a, part, stream);
     return heads_by_type(dtype, dh, [&](auto st, auto d) {
-        return launch_rows(wattn_rows_kernel<decltype(st), decltype(d)::value>, (int64_t)a.B * a.Hq * a.Tq, a, stream);
+        return launch_rows(wattn_rows_kernel<decltype(st), decltype(d)::value>, (int64_t)a.B * a.Hq * a.Tq, 4, a, stream);
     });
 }
 
-int launch_window_attn_bwd(int dtype, int dh, const AttnArgs& a, hipStream_t stream) {
-    return heads_by_type(dtype, dh, [&](auto st, auto d) { return bwd_t<decltype(st), decltype(d)::value>(a, stream); });
+int launch_window_attn_bwd(int dtype, int dh, AttnArgs a, void* scratch, hipStream_t stream) {
+    a.ld = static_cast<float2*>(scratch);
+    const int64_t qrows = (int64_t)a.B * a.Hq * a.Tq, krows = (int64_t)a.B * a.Hkv * a.N;
+    return heads_by_type(dtype, dh, [&](auto st, auto d) {
+        using ST = decltype(st);
+        constexpr int DH = decltype(d)::value;
+        int e = launch_rows(wattn_ld_kernel<ST, DH>, qrows, 256 / (DH / 8), a, stream);
+        if (e) return e;
+        if (dtype == kBF16)
+            return launch_wattn_bwd_tiled(dh, a, reinterpret_cast<float*>(static_cast<char*>(scratch) + ld_bytes(a)), stream);
+        e = launch_rows(wattn_dq_rows_kernel<ST, DH>, qrows, 4, a, stream);
+        return e ? e : launch_rows(wattn_dkv_rows_kernel<ST, DH>, krows, 4, a, stream);
+    });
 }
 
 }  // namespace mosa

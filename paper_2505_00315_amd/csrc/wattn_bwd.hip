@@ -1,0 +1,622 @@
+// Causal attention with a sliding window and first tokens that stay visible:
+// the backward over rows in bf16.
+//
+//   p = 2^(s c - lse'),  dp = dout v,  ds = p (dp - D)
+//   dv = sum p dout,  dk = scale sum ds q,  dq = scale sum ds k
+//
+// Two kinds of workgroups in one launch, neither with atomics: one owns 64 CB
+// keys of a key head and walks the rows that see them (the group's heads are
+// in the row list, so their sum is the loop's), one owns 64 QN rows and walks
+// the keys that they see.  Both form s and dp again from tiles of 64 that come
+// through an LDS ring: 7 products in place of the 5 that one pass with atomic
+// sums would take, for results that do not depend on the order of workgroups.
+// The other operand stays in registers, and p and ds are fed to the second
+// products as they lie in them, against tiles read transposed.
+//
+// Sinks are seen by every later row.  So that their keys' workgroups do not
+// walk the whole sequence while all others walk a window, the pairs beyond the
+// window are a third kind of work: up to kSinkKeys first keys, the rows cut
+// into chunks, fp32 sums of every chunk added in order by a last kernel.
+#include "attn_lds.h"
+#include "heads.h"
+#include "launch_parts.h"
+#include "rowattn.h"
+
+namespace mosa {
+
+namespace {
+
+constexpr int kTB = 64;          // rows or keys per tile
+constexpr int kSinkKeys = 256;   // most sinks whose far pairs go by chunks of rows
+constexpr int kSinkChunks = 32;  // most chunks of a key head's rows
+
+// Unit permutation of the tiles' rows, free of bank conflicts for 16-byte reads
+// of one unit of 16 rows and for transposed reads of unit pairs of 8 rows; it
+// depends on the row's low 4 bits.
+template <int DH>
+__device__ __forceinline__ int bswz(int r) {
+    constexpr int U = DH / 8, L = 16 / U;
+    return 2 * ((r / L) % (U / 2)) + ((r >> 3) & 1);
+}
+template <int DH>
+constexpr int bstages() { return DH == 128 ? 2 : 4; }
+
+// Launch geometry: nk blocks of 64 CB keys and nq blocks of 64 QN rows per (b,
+// key head); nc chunks for each of ns blocks of 64 sinks (0: far pairs are the
+// key blocks' own work).
+struct BwdGeom {
+    int nk, nq, ns, nc;
+};
+
+// Direct global -> LDS load of 4 bytes per lane (as lds_load16, 256 bytes per wave).
+__device__ __forceinline__ void lds_load4(const void* g, uint32_t base) {
+    asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dword %0, off" : : "v"(g), "s"(base) : "memory", "m0");
+}
+
+// DMA slots of a lane: unit p = 64 (wave + 4 j) + lane of a tile.
+template <int DH>
+struct Slots {
+    static constexpr int U = DH / 8, LD = kTB * DH * 2 / 4096;
+    int row[LD], col[LD];
+    __device__ __forceinline__ Slots(int wave, int lane) {
+#pragma unroll
+        for (int j = 0; j < LD; ++j) {
+            const int p = 64 * (wave + 4 * j) + lane;
+            row[j] = p / U;
+            col[j] = 8 * (p % U ^ bswz<DH>(p / U));
+        }
+    }
+};
+
+// Fragment reads of a tile: 16 rows by 32 columns (row-major) and, transposed,
+// 16 columns by 32 rows in the slot order of two 16-row result blocks.
+template <int DH>
+struct TileReads {
+    static constexpr int U = DH / 8, NS = DH / 32, ND = DH / 16;
+    int row[NS], tr[ND];
+    __device__ __forceinline__ TileReads(int g, int c16) {
+#pragma unroll
+        for (int st = 0; st < NS; ++st) row[st] = (c16 * U + ((4 * st + g) ^ bswz<DH>(c16))) * 16;
+        const int r = 4 * g + (c16 >> 2);
+#pragma unroll
+        for (int db = 0; db < ND; ++db) {
+            const int col = 16 * db + 4 * (c16 & 3);
+            tr[db] = (r * U + ((col >> 3) ^ bswz<DH>(r))) * 16 + 8 * ((col >> 2) & 1);
+        }
+    }
+    __device__ __forceinline__ Frag8<uint16_t> rows(const unsigned char* t, int sb, int st) const {
+        Frag8<uint16_t> f;
+        f.v = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(t + row[st] + 16 * U * 16 * sb));
+        return f;
+    }
+    __device__ __forceinline__ Frag8<uint16_t> cols(const unsigned char* t, int u, int db) const {
+        const u32x2 lo = lds_tr16(t + tr[db] + 32 * u * U * 16);
+        const u32x2 hi = lds_tr16(t + tr[db] + (32 * u + 16) * U * 16);
+        Frag8<uint16_t> f;
+        f.v = __builtin_bit_cast(bf16x8, u32x4{lo.x, lo.y, hi.x, hi.y});
+        return f;
+    }
+};
+
+__device__ __forceinline__ Frag8<uint16_t> pack_frag(const f32x4& x, const f32x4& y) {
+    const float v[8] = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+    return frag8_from<uint16_t>(v);
+}
+
+template <int N>
+__device__ __forceinline__ bool finite4(const f32x4 (&x)[N]) {
+    float t = 0.f;
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) t = __builtin_fmaf(x[n][i], 0.f, t);
+    return t == 0.f;
+}
+
+// LDS written by lanes of this wave is seen by its other lanes.
+__device__ __forceinline__ void wave_sync() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+// Rows of 16 N results (column c16 of block n, values 4 g + i of every 16)
+// through this wave's part of LDS to 16-byte stores: to(row) is the row's
+// address or nullptr.
+template <int DH, int N, class TO>
+__device__ __forceinline__ void store_rows(unsigned char* lds, const f32x4 (&x)[N][DH / 16], float f, int lane, const TO& to) {
+    using ST = uint16_t;
+    constexpr int LDO = DH + 8, U = DH / 8;
+    ST* o = reinterpret_cast<ST*>(lds);
+    const int g = lane >> 4, c16 = lane & 15;
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int db = 0; db < DH / 16; ++db)
+            *reinterpret_cast<uint2*>(o + (16 * n + c16) * LDO + 16 * db + 4 * g) =
+                make_uint2(pack_bf16x2(x[n][db][0] * f, x[n][db][1] * f), pack_bf16x2(x[n][db][2] * f, x[n][db][3] * f));
+    wave_sync();
+#pragma unroll
+    for (int e = lane; e < 16 * N * U; e += 64) {
+        const int r = e / U, dc = (e % U) * 8;
+        if (ST* p = to(r)) *reinterpret_cast<uint4*>(p + dc) = *reinterpret_cast<const uint4*>(o + r * LDO + dc);
+    }
+    wave_sync();
+}
+
+// Keys k0 .. of (b, hk), 16 CB per wave.  far (chunk >= 0): the pairs beyond the
+// window of sinks, rows of one chunk, sums to `sums`.
+template <int DH, int CB>
+__device__ __forceinline__ void dkv_body(unsigned char* smem, const AttnArgs& a, const BwdGeom& G, int b, int hk, int k0,
+                                         int chunk, float* sums) {
+    using ST = uint16_t;
+    constexpr int NS = DH / 32, ND = DH / 16, STG = bstages<DH>(), LD = Slots<DH>::LD;
+    constexpr int TILE = kTB * DH * 2, LDB = 4 * kTB * 8, STAGE = 2 * TILE + LDB;  // q, dout, a copy of (lse, D) per wave
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, c16 = lane & 15;
+    const bool far = chunk >= 0, apart = G.ns > 0;  // apart: far pairs are done by chunks
+    const int qn = seq_len_of(a.ql, b, a.Tq), kn = seq_len_of(a.kl, b, a.N), off = kn - qn;
+    const int kend = min(far ? min(a.S, k0 + 64) : k0 + 64 * CB, kn);  // past the block's last key
+    const int wk0 = k0 + 16 * CB * wave, wk1 = min(wk0 + 16 * CB, kend) - 1;  // this wave's keys (none: wk1 < wk0)
+
+    // rows that may see the block's keys
+    int i0 = 0, i1 = 0;
+    if (k0 < kend && qn > 0) {
+        i0 = max(0, (far ? k0 + a.W : k0) - off);
+        i1 = far || a.W == 0 || (!apart && k0 < a.S) ? qn : min(qn, kend - 1 + a.W - off);
+    }
+    const int rlo = i0 * a.G, rhi = max(i1, i0) * a.G;
+    const int all = (rhi - rlo + kTB - 1) / kTB, share = far ? (all + G.nc - 1) / G.nc : all;
+    const int tbeg = far ? min(chunk * share, all) : 0, ntile = min(all, tbeg + share) - tbeg;
+
+    f32x4 dk[CB][ND], dv[CB][ND];
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+        for (int db = 0; db < ND; ++db) dk[cb][db] = dv[cb][db] = zero4();
+
+    if (ntile > 0) {
+        int key[CB];
+        Frag8<ST> kf[CB][NS], vf[CB][NS];
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb) {
+            key[cb] = min(wk0 + 16 * cb + c16, kend - 1);  // (past the block: its last key again, not written)
+#pragma unroll
+            for (int st = 0; st < NS; ++st) {
+                kf[cb][st] = frag8_load<ST>(row_ptr<ST>(a.k, b, hk, key[cb]) + 32 * st + 8 * g);
+                vf[cb][st] = frag8_load<ST>(row_ptr<ST>(a.v, b, hk, key[cb]) + 32 * st + 8 * g);
+            }
+        }
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+            for (int st = 0; st < NS; ++st) asm volatile("" : "+v"(kf[cb][st].v), "+v"(vf[cb][st].v));
+
+        const Slots<DH> slots(wave, lane);
+        const TileReads<DH> rd(g, c16);
+        const uint32_t base = __builtin_amdgcn_readfirstlane(lds_addr(smem));
+        const uint32_t wv = (uint32_t)__builtin_amdgcn_readfirstlane(wave);
+        // tile t (past the end: the last one again, into a buffer that nobody
+        // reads); rows past the range are its last one (masked)
+        auto issue = [&](int t, int buf) {
+            const int r0 = rlo + kTB * (tbeg + min(t, ntile - 1));
+            const uint32_t at = base + buf * STAGE;
+#pragma unroll
+            for (int j = 0; j < LD; ++j) {
+                const int r = min(r0 + slots.row[j], rhi - 1), i = a.gd.div(r);
+                lds_load16(qrow_ptr<ST>(a, a.q, b, hk, r, i) + slots.col[j], at + 1024 * wv + 4096 * j);
+                lds_load16(qrow_ptr<ST>(a, a.dout, b, hk, r, i) + slots.col[j], at + TILE + 1024 * wv + 4096 * j);
+            }
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {  // 32 rows of (lse, D), a word per lane
+                const int r = min(r0 + 32 * j + (lane >> 1), rhi - 1), i = a.gd.div(r);
+                lds_load4(reinterpret_cast<const float*>(a.ld + qrow_index(a, b, hk, r, i)) + (lane & 1),
+                          at + 2 * TILE + 512 * wv + 256 * j);
+            }
+        };
+        const float c2 = a.scale * kLog2e;
+#pragma unroll
+        for (int s = 0; s < STG - 1; ++s) issue(s, s);
+        auto tile_step = [&](int it, auto bufc) {
+            constexpr int BUF = decltype(bufc)::value;
+            wait_vmcnt<(STG - 2) * (2 * LD + 2)>();
+            __syncthreads();
+            issue(it + STG - 1, (BUF + STG - 1) % STG);
+            const unsigned char* Qt = smem + BUF * STAGE;
+            const unsigned char* Gt = Qt + TILE;
+            const unsigned char* Lt = Gt + TILE + 512 * wave;
+            const int r0 = rlo + kTB * (tbeg + it);
+            const int pt0 = off + a.gd.div(r0), pt1 = off + a.gd.div(min(r0 + kTB, rhi) - 1);  // positions of the tile
+            // nothing for this wave: no keys, rows before the keys, or past their window
+            if (wk1 < wk0) return;
+            if (far ? wk0 >= a.S || pt1 - wk0 < a.W : pt1 < wk0 || (a.W && pt0 - wk1 >= a.W && (apart || wk0 >= a.S))) return;
+            const bool whole = r0 + kTB <= rhi &&
+                               (far ? pt0 - wk1 >= a.W : pt0 >= wk1 && (a.W == 0 || pt1 - wk0 < a.W));
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {  // 32 rows at a time
+                f32x4 s[CB][2], dp[CB][2];
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    const int sb = 2 * u + x;
+#pragma unroll
+                    for (int cb = 0; cb < CB; ++cb) s[cb][x] = dp[cb][x] = zero4();
+#pragma unroll
+                    for (int st = 0; st < NS; ++st) {
+                        const Frag8<ST> qa = rd.rows(Qt, sb, st), ga = rd.rows(Gt, sb, st);
+#pragma unroll
+                        for (int cb = 0; cb < CB; ++cb) {
+                            mma8(s[cb][x], qa, kf[cb][st]);
+                            mma8(dp[cb][x], ga, vf[cb][st]);
+                        }
+                    }
+                    const float4 l0 = *reinterpret_cast<const float4*>(Lt + 8 * (16 * sb + 4 * g));
+                    const float4 l1 = *reinterpret_cast<const float4*>(Lt + 8 * (16 * sb + 4 * g) + 16);
+                    const float lse[4] = {l0.x, l0.z, l1.x, l1.z}, D[4] = {l0.y, l0.w, l1.y, l1.w};
+#pragma unroll
+                    for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            s[cb][x][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[cb][x][i], c2, -lse[i]));
+                            dp[cb][x][i] = s[cb][x][i] * (dp[cb][x][i] - D[i]);
+                        }
+                    if (!whole) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const int r = r0 + 16 * sb + 4 * g + i, p = off + a.gd.div(min(r, rhi - 1));
+#pragma unroll
+                            for (int cb = 0; cb < CB; ++cb) {
+                                const int j = key[cb];
+                                const bool in = r < rhi && (far ? p - j >= a.W
+                                                                : j <= p && (a.W == 0 || p - j < a.W || (!apart && j < a.S)));
+                                s[cb][x][i] = in ? s[cb][x][i] : 0.f;
+                                dp[cb][x][i] = in ? dp[cb][x][i] : 0.f;
+                            }
+                        }
+                    }
+                }
+                // dv^T += dout^T p, dk^T += q^T ds: p and ds are rounded to bf16,
+                // the type of the matrix operands
+                Frag8<ST> pf[CB], df[CB];
+#pragma unroll
+                for (int cb = 0; cb < CB; ++cb) {
+                    pf[cb] = pack_frag(s[cb][0], s[cb][1]);
+                    df[cb] = pack_frag(dp[cb][0], dp[cb][1]);
+                }
+#pragma unroll
+                for (int db = 0; db < ND; ++db) {
+                    const Frag8<ST> gt = rd.cols(Gt, u, db), qt = rd.cols(Qt, u, db);
+#pragma unroll
+                    for (int cb = 0; cb < CB; ++cb) {
+                        mma8(dv[cb][db], gt, pf[cb]);
+                        mma8(dk[cb][db], qt, df[cb]);
+                    }
+                }
+            }
+        };
+        for (int it0 = 0;; it0 += STG) {
+            bool last = false;
+            static_for<0, STG>([&](auto u) {
+                if (last) return;
+                const int it = it0 + decltype(u)::value;
+                tile_step(it, u);
+                last = it + 1 >= ntile;
+            });
+            if (last) break;
+        }
+        mfma_drain();
+        wait_vmcnt<0>();
+    }
+    __syncthreads();
+
+    // slot 0 of the sums: the window's pairs, slot 1 + c: chunk c
+    const int64_t keys = (int64_t)a.B * a.Hkv * a.S;
+    float* sum = sums + ((far ? 1 + chunk : 0) * keys + ((int64_t)b * a.Hkv + hk) * a.S) * 2 * DH;
+    const int top = far ? a.S : a.N;  // keys of the output
+    bool fine = true;
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb) fine &= finite4(dk[cb]) && finite4(dv[cb]);
+    if (__builtin_amdgcn_ballot_w64(!fine)) {
+        // rows one by one (a pair outside the rule meets every value with a weight of 0)
+#pragma unroll 1
+        for (int j = wk0; j < min(wk0 + 16 * CB, top); ++j) {
+            float x[RowLanes<DH>::N] = {}, y[RowLanes<DH>::N] = {};
+            if (j <= wk1) {
+                const int ra = rlo + kTB * tbeg, rb = min(rhi, ra + kTB * ntile);
+                row_dkv<ST, DH>(a, b, hk, j, off, ra, rb, [&](int p) {
+                    return far ? p - j >= a.W : j <= p && (a.W == 0 || p - j < a.W || (!apart && j < a.S));
+                }, lane, x, y);
+            }
+            const bool part = far || (apart && j < a.S);
+#pragma unroll
+            for (int n = 0; n < RowLanes<DH>::N; ++n) {
+                if (!RowLanes<DH>::has(lane)) continue;
+                const int c = lane + 64 * n;
+                if (part) {
+                    sum[(int64_t)j * 2 * DH + c] = x[n];
+                    sum[(int64_t)j * 2 * DH + DH + c] = y[n];
+                } else {
+                    st1<ST>(row_ptr<ST>(a.dk, b, hk, j) + c, x[n]);
+                    st1<ST>(row_ptr<ST>(a.dv, b, hk, j) + c, y[n]);
+                }
+            }
+        }
+        return;
+    }
+    if (far || (apart && wk0 < a.S)) {
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb) {
+            const int j = wk0 + 16 * cb + c16;
+            if (j >= a.S) continue;
+            const float f = j <= wk1 ? 1.f : 0.f;
+#pragma unroll
+            for (int db = 0; db < ND; ++db) {
+                float* to = sum + (int64_t)j * 2 * DH + 16 * db + 4 * g;
+                const float fs = f * a.scale;
+                *reinterpret_cast<float4*>(to) = make_float4(dk[cb][db][0] * fs, dk[cb][db][1] * fs, dk[cb][db][2] * fs, dk[cb][db][3] * fs);
+                *reinterpret_cast<float4*>(to + DH) = make_float4(dv[cb][db][0] * f, dv[cb][db][1] * f, dv[cb][db][2] * f, dv[cb][db][3] * f);
+            }
+        }
+    }
+    if (far) return;
+    // keys past the sequence are zero (their lanes computed its last key again)
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb)
+        if (wk0 + 16 * cb + c16 > wk1)
+#pragma unroll
+            for (int db = 0; db < ND; ++db) dk[cb][db] = dv[cb][db] = zero4();
+    unsigned char* mine = smem + wave * 16 * CB * (DH + 8) * 2;
+    auto key_at = [&](const Rows& t, int r) {
+        const int j = wk0 + r;
+        return j < top && !(apart && j < a.S) ? row_ptr<ST>(t, b, hk, j) : nullptr;
+    };
+    store_rows<DH, CB>(mine, dk, a.scale, lane, [&](int r) { return key_at(a.dk, r); });
+    store_rows<DH, CB>(mine, dv, 1.f, lane, [&](int r) { return key_at(a.dv, r); });
+}
+
+// Rows r0 .. of (b, hk), 16 QN per wave.
+template <int DH, int QN>
+__device__ __forceinline__ void dq_body(unsigned char* smem, const AttnArgs& a, int b, int hk, int r0) {
+    using ST = uint16_t;
+    constexpr int NS = DH / 32, ND = DH / 16, STG = bstages<DH>(), LD = Slots<DH>::LD;
+    constexpr int TILE = kTB * DH * 2, STAGE = 2 * TILE;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, c16 = lane & 15;
+    const int qn = seq_len_of(a.ql, b, a.Tq), kn = seq_len_of(a.kl, b, a.N), off = kn - qn;
+    const int R = a.Tq * a.G, rn = qn * a.G, wr0 = r0 + 16 * QN * wave;
+    KeyList list{0, 0, 0};
+    if (r0 < rn) list = keys_of(a, off + a.gd.div(r0), off + a.gd.div(min(r0 + 64 * QN, rn) - 1), kn);
+    const int ntile = (list.count + kTB - 1) / kTB;
+
+    f32x4 dq[QN][ND];
+#pragma unroll
+    for (int qs = 0; qs < QN; ++qs)
+#pragma unroll
+        for (int db = 0; db < ND; ++db) dq[qs][db] = zero4();
+
+    if (ntile > 0) {
+        const int pw0 = off + a.gd.div(min(wr0, rn - 1)), pw1 = off + a.gd.div(min(wr0 + 16 * QN, rn) - 1);
+        int pos[QN];
+        float2 ld[QN];
+        Frag8<ST> qf[QN][NS], gf[QN][NS];
+#pragma unroll
+        for (int qs = 0; qs < QN; ++qs) {
+            const int r = min(wr0 + 16 * qs + c16, rn - 1), i = a.gd.div(r);
+            pos[qs] = off + i;
+            ld[qs] = a.ld[qrow_index(a, b, hk, r, i)];
+#pragma unroll
+            for (int st = 0; st < NS; ++st) {
+                qf[qs][st] = frag8_load<ST>(qrow_ptr<ST>(a, a.q, b, hk, r, i) + 32 * st + 8 * g);
+                gf[qs][st] = frag8_load<ST>(qrow_ptr<ST>(a, a.dout, b, hk, r, i) + 32 * st + 8 * g);
+            }
+        }
+#pragma unroll
+        for (int qs = 0; qs < QN; ++qs) {
+            asm volatile("" : "+v"(ld[qs].x), "+v"(ld[qs].y));
+#pragma unroll
+            for (int st = 0; st < NS; ++st) asm volatile("" : "+v"(qf[qs][st].v), "+v"(gf[qs][st].v));
+        }
+        const Slots<DH> slots(wave, lane);
+        const TileReads<DH> rd(g, c16);
+        const uint32_t lbase = __builtin_amdgcn_readfirstlane(lds_addr(smem)) +
+                               1024 * (uint32_t)__builtin_amdgcn_readfirstlane(wave);
+        const ST* kp = row_ptr<ST>(a.k, b, hk, 0);
+        const ST* vp = row_ptr<ST>(a.v, b, hk, 0);
+        auto issue = [&](int t, int buf) {
+            const int e0 = kTB * min(t, ntile - 1);
+            const uint32_t at = lbase + buf * STAGE;
+#pragma unroll
+            for (int j = 0; j < LD; ++j) {
+                const int64_t key = list.key(min(e0 + slots.row[j], list.count - 1));
+                lds_load16(kp + key * a.k.row + slots.col[j], at + 4096 * j);
+                lds_load16(vp + key * a.v.row + slots.col[j], at + TILE + 4096 * j);
+            }
+        };
+        const float c2 = a.scale * kLog2e;
+#pragma unroll
+        for (int s = 0; s < STG - 1; ++s) issue(s, s);
+        auto tile_step = [&](int it, auto bufc) {
+            constexpr int BUF = decltype(bufc)::value;
+            wait_vmcnt<(STG - 2) * 2 * LD>();
+            __syncthreads();
+            issue(it + STG - 1, (BUF + STG - 1) % STG);
+            const unsigned char* Kt = smem + BUF * STAGE;
+            const unsigned char* Vt = Kt + TILE;
+            const int e0 = kTB * it;
+            const int kmax = list.key(min(e0 + kTB, list.count) - 1), kmin = e0 >= list.s ? list.key(e0) : list.lo;
+            if (e0 >= list.s && (kmin > pw1 || (a.W && kmax <= pw0 - a.W && kmin >= a.S))) return;
+            const bool whole = e0 + kTB <= list.count && kmax <= pw0 && (a.W == 0 || kmin > pw1 - a.W);
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {  // 32 keys at a time
+                f32x4 s[QN][2], dp[QN][2];
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    const int sb = 2 * u + x;
+#pragma unroll
+                    for (int qs = 0; qs < QN; ++qs) s[qs][x] = dp[qs][x] = zero4();
+#pragma unroll
+                    for (int st = 0; st < NS; ++st) {
+                        const Frag8<ST> ka = rd.rows(Kt, sb, st), va = rd.rows(Vt, sb, st);
+#pragma unroll
+                        for (int qs = 0; qs < QN; ++qs) {
+                            mma8(s[qs][x], ka, qf[qs][st]);
+                            mma8(dp[qs][x], va, gf[qs][st]);
+                        }
+                    }
+#pragma unroll
+                    for (int qs = 0; qs < QN; ++qs)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            dp[qs][x][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[qs][x][i], c2, -ld[qs].x)) *
+                                           (dp[qs][x][i] - ld[qs].y);
+                    if (!whole) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const int e = e0 + 16 * sb + 4 * g + i, key = list.key(e);
+#pragma unroll
+                            for (int qs = 0; qs < QN; ++qs)
+                                dp[qs][x][i] = e < list.count && sees(a, pos[qs], key) ? dp[qs][x][i] : 0.f;
+                        }
+                    }
+                }
+                Frag8<ST> df[QN];
+#pragma unroll
+                for (int qs = 0; qs < QN; ++qs) df[qs] = pack_frag(dp[qs][0], dp[qs][1]);
+#pragma unroll
+                for (int db = 0; db < ND; ++db) {
+                    const Frag8<ST> kt = rd.cols(Kt, u, db);
+#pragma unroll
+                    for (int qs = 0; qs < QN; ++qs) mma8(dq[qs][db], kt, df[qs]);
+                }
+            }
+        };
+        for (int it0 = 0;; it0 += STG) {
+            bool last = false;
+            static_for<0, STG>([&](auto u) {
+                if (last) return;
+                const int it = it0 + decltype(u)::value;
+                tile_step(it, u);
+                last = it + 1 >= ntile;
+            });
+            if (last) break;
+        }
+        mfma_drain();
+        wait_vmcnt<0>();
+    }
+    __syncthreads();
+    bool fine = true;
+#pragma unroll
+    for (int qs = 0; qs < QN; ++qs) fine &= finite4(dq[qs]);
+    if (__builtin_amdgcn_ballot_w64(!fine)) {
+#pragma unroll 1
+        for (int r = wr0; r < min(wr0 + 16 * QN, rn); ++r) {
+            const int i = a.gd.div(r);
+            row_dq<ST, DH>(a, b, hk * a.G + r - i * a.G, i, off + i, kn, lane);
+        }
+    }
+    const bool redone = __builtin_amdgcn_ballot_w64(!fine) != 0;
+#pragma unroll
+    for (int qs = 0; qs < QN; ++qs)
+        if (wr0 + 16 * qs + c16 >= rn)
+#pragma unroll
+            for (int db = 0; db < ND; ++db) dq[qs][db] = zero4();
+    store_rows<DH, QN>(smem + wave * 16 * QN * (DH + 8) * 2, dq, a.scale, lane, [&](int lr) -> ST* {
+        const int r = wr0 + lr;
+        return r < R && !(redone && r < rn) ? qrow_ptr<ST>(a, a.dq, b, hk, r, a.gd.div(r)) : nullptr;
+    });
+}
+
+template <int DH, int CB, int QN>
+__global__ __launch_bounds__(256, 2) void wattn_bwd_kernel(AttnArgs a, BwdGeom G, float* __restrict__ sums, uint32_t first) {
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+    // key blocks, then chunks of far rows, then row blocks; each kind in
+    // neighbouring order on an XCD (a key head's workgroups share its rows and keys)
+    const uint32_t heads = (uint32_t)a.B * a.Hkv, n0 = heads * G.nk, n1 = heads * G.ns * G.nc, n2 = heads * G.nq;
+    uint32_t id = first + blockIdx.x;
+    const bool one = first == 0 && gridDim.x == n0 + n1 + n2;
+    if (id < n0) {
+        if (one) id = xcd_logical_id(id, n0);
+        const int bh = id / G.nk, kb = id % G.nk;
+        dkv_body<DH, CB>(smem, a, G, bh / a.Hkv, bh % a.Hkv, kb * 64 * CB, -1, sums);
+    } else if (id < n0 + n1) {
+        id -= n0;
+        const int per = G.ns * G.nc, bh = id / per, k = id % per;
+        dkv_body<DH, 1>(smem, a, G, bh / a.Hkv, bh % a.Hkv, k / G.nc * 64, k % G.nc, sums);
+    } else {
+        id -= n0 + n1;
+        if (one) id = xcd_logical_id(id, n2);
+        const int bh = id / G.nq, q = id % G.nq;
+        dq_body<DH, QN>(smem, a, bh / a.Hkv, bh % a.Hkv, (a.W ? q : G.nq - 1 - q) * 64 * QN);
+    }
+}
+
+// dk and dv of the sinks: the window's pairs, then the chunks in order.
+template <int DH>
+__global__ __launch_bounds__(256) void wattn_sinks_kernel(AttnArgs a, int slots, const float* __restrict__ sums) {
+    const int64_t keys = (int64_t)a.B * a.Hkv * a.S, all = keys * 2 * DH;
+    for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < all; e += (int64_t)gridDim.x * 256) {
+        const int c = (int)(e % DH), which = (int)(e / DH % 2);
+        const int64_t row = e / (2 * DH);
+        const int j = (int)(row % a.S), hk = (int)(row / a.S % a.Hkv), b = (int)(row / a.S / a.Hkv);
+        float s = 0.f;
+#pragma unroll 4
+        for (int k = 0; k < slots; ++k) s += sums[k * all + e];
+        if (j >= seq_len_of(a.kl, b, a.N)) s = 0.f;
+        st1<uint16_t>(row_ptr<uint16_t>(which ? a.dv : a.dk, b, hk, j) + c, s);
+    }
+}
+
+// Blocks of 128 keys and rows halve the reads of the tiles per product; blocks
+// of 64 where those leave CUs idle.
+template <int DH>
+bool wide_blocks(const AttnArgs& a) { return (int64_t)a.B * a.Hkv * ((a.N + 127) / 128) >= 512; }
+
+template <int DH>
+BwdGeom bwd_geom(const AttnArgs& a) {
+    BwdGeom G;
+    const int w = wide_blocks<DH>(a) ? 128 : 64;
+    const int64_t R = (int64_t)a.Tq * a.G;
+    G.nk = (a.N + w - 1) / w;
+    G.nq = (int)((R + w - 1) / w);
+    G.ns = a.W && a.S && a.S <= kSinkKeys ? (a.S + 63) / 64 : 0;
+    // a chunk walks about as many rows as a key block does
+    const int64_t c = (R + (int64_t)(a.W + w) * a.G - 1) / ((int64_t)(a.W + w) * a.G);
+    G.nc = G.ns ? (int)(c < kSinkChunks ? c : kSinkChunks) : 0;
+    return G;
+}
+
+template <int DH, int W>
+int launch_bwd(const AttnArgs& a, const BwdGeom& G, float* sums, hipStream_t stream) {
+    auto kern = wattn_bwd_kernel<DH, W, W>;
+    const size_t ring = (size_t)bstages<DH>() * (2 * kTB * DH * 2 + 4 * kTB * 8), outs = (size_t)64 * W * (DH + 8) * 2;
+    const size_t lds = ring > outs ? ring : outs;
+    if (allow_lds((const void*)kern, lds)) return -1;
+    const uint64_t blocks = (uint64_t)a.B * a.Hkv * ((uint64_t)G.nk + G.ns * G.nc + G.nq);
+    return launch_parts(blocks, 256, [&](uint32_t first, uint32_t n) {
+        hipLaunchKernelGGL(kern, dim3(n), dim3(256), lds, stream, a, G, sums, first);
+        return hipGetLastError() == hipSuccess ? 0 : -1;
+    });
+}
+
+template <int DH>
+int bwd_tiled(const AttnArgs& a, float* sums, hipStream_t stream) {
+    const BwdGeom G = bwd_geom<DH>(a);
+    const int e = wide_blocks<DH>(a) ? launch_bwd<DH, 2>(a, G, sums, stream) : launch_bwd<DH, 1>(a, G, sums, stream);
+    if (e || !G.ns) return e;
+    const int64_t all = (int64_t)a.B * a.Hkv * a.S * 2 * DH, blocks = (all + 255) / 256;
+    hipLaunchKernelGGL((wattn_sinks_kernel<DH>), dim3((unsigned)(blocks < 65536 ? blocks : 65536)), dim3(256), 0, stream, a,
+                       1 + G.nc, sums);
+    return hipGetLastError() == hipSuccess ? 0 : -1;
+}
+
+}  // namespace
+
+size_t wattn_bwd_sums(int dh, const AttnArgs& a) {
+    const BwdGeom G = dh == 128 ? bwd_geom<128>(a) : dh == 64 ? bwd_geom<64>(a) : bwd_geom<32>(a);
+    return G.ns ? (size_t)(1 + G.nc) * a.B * a.Hkv * a.S * 2 * dh * sizeof(float) : 0;
+}
+
+int launch_wattn_bwd_tiled(int dh, const AttnArgs& a, float* sums, hipStream_t stream) {
+    if (dh == 128) return bwd_tiled<128>(a, sums, stream);
+    if (dh == 64) return bwd_tiled<64>(a, sums, stream);
+    return bwd_tiled<32>(a, sums, stream);
+}
+
+}  // namespace mosa

@@ -77,6 +77,51 @@ def test_forward_and_backward(case, dtype):
         within(t, ref[n], bounds[n], f"{n} {case} {dtype}")
 
 
+# enough blocks of 128 rows and keys for every CU
+WIDE = [
+    (4, 16, 8, 128, 2077, 2077, 300, 5, "bthd", None),
+    (5, 8, 8, 64, 1733, 1733, 200, 4, "bhtd", ([1733, 1, 900, 0, 1600], [1733, 1, 900, 0, 1600])),
+    (4, 24, 8, 32, 2049, 2049, 77, 70, "packed", None),
+    (8, 8, 8, 128, 1100, 1100, 0, 0, "bthd", None),
+    (4, 8, 8, 64, 2050, 2100, 500, 300, "bthd", None),     # sinks that are key blocks' own work
+]
+
+
+@pytest.mark.parametrize("case", WIDE, ids=[f"dh{c[3]}w{c[6]}s{c[7]}" for c in WIDE])
+def test_wide_blocks(case):
+    shape, x, kw, dt = setup(case, "bf16", 11)
+    ref = reference(case, x, kw)
+    spoil_padding(x, kw)
+    out, lse = ops.window_attention(shape, x["q"], x["k"], x["v"], **kw)
+    dq, dk, dv = ops.window_attention_backward(shape, x["q"], x["k"], x["v"], out, lse, x["do"], **kw)
+    bounds = attention_bounds(ref, dt, case[3], max(case[5], case[4] * case[1] // case[2]))
+    for n, t in (("out", out), ("lse", lse), ("dq", dq), ("dk", dk), ("dv", dv)):
+        within(t, ref[n], bounds[n], f"{n} {case}")
+
+
+@pytest.mark.parametrize("dh", [64, 128])
+def test_unseen_keys_stay_out_of_wide_blocks(dh):
+    case = (4, 8, 8, dh, 2100, 2100, 300, 4, "bthd", None)
+    shape, x, _, _ = setup(case, "bf16", 12)
+    see = mask_of(2100, 2100, 2100, 2100, 300, 4).cuda()
+    clean = ops.window_attention(shape, x["q"], x["k"], x["v"])
+    cg = ops.window_attention_backward(shape, x["q"], x["k"], x["v"], *clean, x["do"])
+    for j in (1000, 2):
+        k, v = x["k"].clone(), x["v"].clone()
+        k[1, 3, j, 1], v[1, 3, j] = math.nan, math.inf
+        got = ops.window_attention(shape, x["q"], k, v)
+        grads = ops.window_attention_backward(shape, x["q"], k, v, *got, x["do"])
+        hit = torch.zeros(4, 8, 2100, dtype=torch.bool, device="cuda")
+        hit[1, 3] = see[:, j]
+        assert bool(torch.isnan(got[0][hit].float()).all())
+        torch.testing.assert_close(got[0][~hit].float(), clean[0][~hit].float(), rtol=2 ** -7, atol=2 ** -7)
+        torch.testing.assert_close(grads[0][~hit].float(), cg[0][~hit].float(), rtol=2 ** -7, atol=2 ** -5)
+        apart = torch.ones(4, 8, 2100, dtype=torch.bool, device="cuda")
+        apart[1, 3] = ~(see & see[:, j:j + 1]).any(0)
+        for t, c in zip(grads[1:], cg[1:]):
+            torch.testing.assert_close(t[apart].float(), c[apart].float(), rtol=2 ** -7, atol=2 ** -3)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("dh", [32, 64, 128])
 @pytest.mark.parametrize("Q,N,window,sinks", [(150, 150, 20, 3), (1, 150, 20, 3), (70, 300, 0, 0)])
