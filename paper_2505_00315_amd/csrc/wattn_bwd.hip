@@ -17,29 +17,20 @@
 // walk the whole sequence while all others walk a window, the pairs beyond the
 // window are a third kind of work: up to kSinkKeys first keys, the rows cut
 // into chunks, fp32 sums of every chunk added in order by a last kernel.
-#include "attn_lds.h"
-#include "heads.h"
 #include "launch_parts.h"
 #include "rowattn.h"
+#include "wattn_dma.h"
 
 namespace mosa {
 
 namespace {
 
-constexpr int kTB = 64;          // rows or keys per tile
 constexpr int kSinkKeys = 256;   // most sinks whose far pairs go by chunks of rows
 constexpr int kSinkChunks = 32;  // most chunks of a key head's rows
 
-// Unit permutation of the tiles' rows, free of bank conflicts for 16-byte reads
-// of one unit of 16 rows and for transposed reads of unit pairs of 8 rows; it
-// depends on the row's low 4 bits.
-template <int DH>
-__device__ __forceinline__ int bswz(int r) {
-    constexpr int U = DH / 8, L = 16 / U;
-    return 2 * ((r / L) % (U / 2)) + ((r >> 3) & 1);
-}
-template <int DH>
-constexpr int bstages() { return DH == 128 ? 2 : 4; }
+// Two: with 4 stages of the 64-wide heads' tiles a CU holds two workgroups in
+// place of four (8192 tokens, 4 heads, window 512, training step: 81 -> 65 us).
+constexpr int kStages = 2;
 
 // Launch geometry: nk blocks of 64 CB keys and nq blocks of 64 QN rows per (b,
 // key head); nc chunks for each of ns blocks of 64 sinks (0: far pairs are the
@@ -48,60 +39,66 @@ struct BwdGeom {
     int nk, nq, ns, nc;
 };
 
-// Direct global -> LDS load of 4 bytes per lane (as lds_load16, 256 bytes per wave).
-__device__ __forceinline__ void lds_load4(const void* g, uint32_t base) {
-    asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dword %0, off" : : "v"(g), "s"(base) : "memory", "m0");
-}
-
-// DMA slots of a lane: unit p = 64 (wave + 4 j) + lane of a tile.
+// Tiles of a key head's rows: q, dout and (lse, D).  A tile is 64 / G queries of
+// the group's G heads (its last 64 % G rows are none), or 64 rows where G is
+// larger, so that the lanes' offsets are the same for every tile.
 template <int DH>
-struct Slots {
-    static constexpr int U = DH / 8, LD = kTB * DH * 2 / 4096;
-    int row[LD], col[LD];
-    __device__ __forceinline__ Slots(int wave, int lane) {
+struct RowTiles {
+    using TL = TileLoad<DH>;
+    const AttnArgs& a;
+    int b, hk, nq, nr;  // queries and rows per tile (nq = 0: G > 64)
+    bool near;
+    uint32_t qoff[TL::LD], goff[TL::LD], loff[2];
+    __device__ __forceinline__ RowTiles(const AttnArgs& a, int b, int hk, const TL& tl, int lane) : a(a), b(b), hk(hk) {
+        nq = 64 / a.G;
+        nr = nq ? nq * a.G : kTB;
+        // 64 rows of G heads within 2^31 bytes
+        near = nq > 0 && fits(a.q) && fits(a.dout) && (int64_t)a.G * a.Tq < ((int64_t)1 << 27);
 #pragma unroll
-        for (int j = 0; j < LD; ++j) {
-            const int p = 64 * (wave + 4 * j) + lane;
-            row[j] = p / U;
-            col[j] = 8 * (p % U ^ bswz<DH>(p / U));
+        for (int j = 0; j < TL::LD; ++j) {
+            const int r = tl.row + TL::STEP * j, i = a.gd.div(r), g = r - i * a.G;
+            qoff[j] = (uint32_t)((g * a.q.head + i * a.q.row + tl.col) * 2);
+            goff[j] = (uint32_t)((g * a.dout.head + i * a.dout.row + tl.col) * 2);
+        }
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int r = 32 * j + (lane >> 1), i = a.gd.div(r), g = r - i * a.G;
+            loff[j] = (uint32_t)(((int64_t)g * a.Tq + i) * 8 + 4 * (lane & 1));
+        }
+    }
+    __device__ __forceinline__ bool fits(const Rows& t) const {
+        return a.G * t.head + kTB * t.row < ((int64_t)1 << 30);
+    }
+    // The tile from row r0 on (of rows below rhi; those past it are the last one), to LDS byte `at`:
+    // q, dout, and for this wave alone (lse, D) of every row.
+    __device__ __forceinline__ void issue(const TL& tl, int r0, int rhi, uint32_t at, uint32_t ld_at, int lane) const {
+        if (near && r0 + kTB <= rhi) {
+            const int i0 = a.gd.div(r0);
+            const char* q = uniform_ptr(reinterpret_cast<const char*>(row_ptr<uint16_t>(a.q, b, hk * a.G, i0)));
+            const char* g = uniform_ptr(reinterpret_cast<const char*>(row_ptr<uint16_t>(a.dout, b, hk * a.G, i0)));
+            const char* l = uniform_ptr(reinterpret_cast<const char*>(a.ld + ((int64_t)b * a.Hq + hk * a.G) * a.Tq + i0));
+#pragma unroll
+            for (int j = 0; j < TL::LD; ++j) {
+                lds_load16s(qoff[j], q, at + tl.lds + 4096 * j);
+                lds_load16s(goff[j], g, at + TL::BYTES + tl.lds + 4096 * j);
+            }
+#pragma unroll
+            for (int j = 0; j < 2; ++j) lds_load4s(loff[j], l, ld_at + 256 * j);
+            return;
+        }
+#pragma unroll
+        for (int j = 0; j < TL::LD; ++j) {
+            const int r = min(r0 + tl.row + TL::STEP * j, rhi - 1), i = a.gd.div(r);
+            lds_load16(qrow_ptr<uint16_t>(a, a.q, b, hk, r, i) + tl.col, at + tl.lds + 4096 * j);
+            lds_load16(qrow_ptr<uint16_t>(a, a.dout, b, hk, r, i) + tl.col, at + TL::BYTES + tl.lds + 4096 * j);
+        }
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int r = min(r0 + 32 * j + (lane >> 1), rhi - 1), i = a.gd.div(r);
+            lds_load4(reinterpret_cast<const float*>(a.ld + qrow_index(a, b, hk, r, i)) + (lane & 1), ld_at + 256 * j);
         }
     }
 };
-
-// Fragment reads of a tile: 16 rows by 32 columns (row-major) and, transposed,
-// 16 columns by 32 rows in the slot order of two 16-row result blocks.
-template <int DH>
-struct TileReads {
-    static constexpr int U = DH / 8, NS = DH / 32, ND = DH / 16;
-    int row[NS], tr[ND];
-    __device__ __forceinline__ TileReads(int g, int c16) {
-#pragma unroll
-        for (int st = 0; st < NS; ++st) row[st] = (c16 * U + ((4 * st + g) ^ bswz<DH>(c16))) * 16;
-        const int r = 4 * g + (c16 >> 2);
-#pragma unroll
-        for (int db = 0; db < ND; ++db) {
-            const int col = 16 * db + 4 * (c16 & 3);
-            tr[db] = (r * U + ((col >> 3) ^ bswz<DH>(r))) * 16 + 8 * ((col >> 2) & 1);
-        }
-    }
-    __device__ __forceinline__ Frag8<uint16_t> rows(const unsigned char* t, int sb, int st) const {
-        Frag8<uint16_t> f;
-        f.v = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(t + row[st] + 16 * U * 16 * sb));
-        return f;
-    }
-    __device__ __forceinline__ Frag8<uint16_t> cols(const unsigned char* t, int u, int db) const {
-        const u32x2 lo = lds_tr16(t + tr[db] + 32 * u * U * 16);
-        const u32x2 hi = lds_tr16(t + tr[db] + (32 * u + 16) * U * 16);
-        Frag8<uint16_t> f;
-        f.v = __builtin_bit_cast(bf16x8, u32x4{lo.x, lo.y, hi.x, hi.y});
-        return f;
-    }
-};
-
-__device__ __forceinline__ Frag8<uint16_t> pack_frag(const f32x4& x, const f32x4& y) {
-    const float v[8] = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
-    return frag8_from<uint16_t>(v);
-}
 
 template <int N>
 __device__ __forceinline__ bool finite4(const f32x4 (&x)[N]) {
@@ -150,8 +147,8 @@ template <int DH, int CB>
 __device__ __forceinline__ void dkv_body(unsigned char* smem, const AttnArgs& a, const BwdGeom& G, int b, int hk, int k0,
                                          int chunk, float* sums) {
     using ST = uint16_t;
-    constexpr int NS = DH / 32, ND = DH / 16, STG = bstages<DH>(), LD = Slots<DH>::LD;
-    constexpr int TILE = kTB * DH * 2, LDB = 4 * kTB * 8, STAGE = 2 * TILE + LDB;  // q, dout, a copy of (lse, D) per wave
+    constexpr int NS = DH / 32, ND = DH / 16, STG = kStages, LD = TileLoad<DH>::LD;
+    constexpr int TILE = TileLoad<DH>::BYTES, LDB = 4 * kTB * 8, STAGE = 2 * TILE + LDB;  // q, dout, a copy of (lse, D) per wave
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, c16 = lane & 15;
     const bool far = chunk >= 0, apart = G.ns > 0;  // apart: far pairs are done by chunks
     const int qn = seq_len_of(a.ql, b, a.Tq), kn = seq_len_of(a.kl, b, a.N), off = kn - qn;
@@ -165,7 +162,9 @@ __device__ __forceinline__ void dkv_body(unsigned char* smem, const AttnArgs& a,
         i1 = far || a.W == 0 || (!apart && k0 < a.S) ? qn : min(qn, kend - 1 + a.W - off);
     }
     const int rlo = i0 * a.G, rhi = max(i1, i0) * a.G;
-    const int all = (rhi - rlo + kTB - 1) / kTB, share = far ? (all + G.nc - 1) / G.nc : all;
+    const TileLoad<DH> tl(wave, lane);
+    const RowTiles<DH> rows(a, b, hk, tl, lane);
+    const int nr = rows.nr, all = (rhi - rlo + nr - 1) / nr, share = far ? (all + G.nc - 1) / G.nc : all;
     const int tbeg = far ? min(chunk * share, all) : 0, ntile = min(all, tbeg + share) - tbeg;
 
     f32x4 dk[CB][ND], dv[CB][ND];
@@ -191,27 +190,12 @@ __device__ __forceinline__ void dkv_body(unsigned char* smem, const AttnArgs& a,
 #pragma unroll
             for (int st = 0; st < NS; ++st) asm volatile("" : "+v"(kf[cb][st].v), "+v"(vf[cb][st].v));
 
-        const Slots<DH> slots(wave, lane);
         const TileReads<DH> rd(g, c16);
         const uint32_t base = __builtin_amdgcn_readfirstlane(lds_addr(smem));
-        const uint32_t wv = (uint32_t)__builtin_amdgcn_readfirstlane(wave);
-        // tile t (past the end: the last one again, into a buffer that nobody
-        // reads); rows past the range are its last one (masked)
+        // tile t (past the end: the last one again, into a buffer that nobody reads)
         auto issue = [&](int t, int buf) {
-            const int r0 = rlo + kTB * (tbeg + min(t, ntile - 1));
             const uint32_t at = base + buf * STAGE;
-#pragma unroll
-            for (int j = 0; j < LD; ++j) {
-                const int r = min(r0 + slots.row[j], rhi - 1), i = a.gd.div(r);
-                lds_load16(qrow_ptr<ST>(a, a.q, b, hk, r, i) + slots.col[j], at + 1024 * wv + 4096 * j);
-                lds_load16(qrow_ptr<ST>(a, a.dout, b, hk, r, i) + slots.col[j], at + TILE + 1024 * wv + 4096 * j);
-            }
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {  // 32 rows of (lse, D), a word per lane
-                const int r = min(r0 + 32 * j + (lane >> 1), rhi - 1), i = a.gd.div(r);
-                lds_load4(reinterpret_cast<const float*>(a.ld + qrow_index(a, b, hk, r, i)) + (lane & 1),
-                          at + 2 * TILE + 512 * wv + 256 * j);
-            }
+            rows.issue(tl, rlo + nr * (tbeg + min(t, ntile - 1)), rhi, at, at + 2 * TILE + tl.lds / 2, lane);
         };
         const float c2 = a.scale * kLog2e;
 #pragma unroll
@@ -224,12 +208,12 @@ __device__ __forceinline__ void dkv_body(unsigned char* smem, const AttnArgs& a,
             const unsigned char* Qt = smem + BUF * STAGE;
             const unsigned char* Gt = Qt + TILE;
             const unsigned char* Lt = Gt + TILE + 512 * wave;
-            const int r0 = rlo + kTB * (tbeg + it);
-            const int pt0 = off + a.gd.div(r0), pt1 = off + a.gd.div(min(r0 + kTB, rhi) - 1);  // positions of the tile
+            const int r0 = rlo + nr * (tbeg + it), rt = min(r0 + nr, rhi);  // the tile's rows
+            const int pt0 = off + a.gd.div(r0), pt1 = off + a.gd.div(rt - 1);  // and their positions
             // nothing for this wave: no keys, rows before the keys, or past their window
             if (wk1 < wk0) return;
             if (far ? wk0 >= a.S || pt1 - wk0 < a.W : pt1 < wk0 || (a.W && pt0 - wk1 >= a.W && (apart || wk0 >= a.S))) return;
-            const bool whole = r0 + kTB <= rhi &&
+            const bool whole = r0 + kTB == rt &&
                                (far ? pt0 - wk1 >= a.W : pt0 >= wk1 && (a.W == 0 || pt1 - wk0 < a.W));
 #pragma unroll
             for (int u = 0; u < 2; ++u) {  // 32 rows at a time
@@ -265,7 +249,7 @@ __device__ __forceinline__ void dkv_body(unsigned char* smem, const AttnArgs& a,
 #pragma unroll
                             for (int cb = 0; cb < CB; ++cb) {
                                 const int j = key[cb];
-                                const bool in = r < rhi && (far ? p - j >= a.W
+                                const bool in = r < rt && (far ? p - j >= a.W
                                                                 : j <= p && (a.W == 0 || p - j < a.W || (!apart && j < a.S)));
                                 s[cb][x][i] = in ? s[cb][x][i] : 0.f;
                                 dp[cb][x][i] = in ? dp[cb][x][i] : 0.f;
@@ -320,7 +304,7 @@ __device__ __forceinline__ void dkv_body(unsigned char* smem, const AttnArgs& a,
         for (int j = wk0; j < min(wk0 + 16 * CB, top); ++j) {
             float x[RowLanes<DH>::N] = {}, y[RowLanes<DH>::N] = {};
             if (j <= wk1) {
-                const int ra = rlo + kTB * tbeg, rb = min(rhi, ra + kTB * ntile);
+                const int ra = rlo + nr * tbeg, rb = min(rhi, ra + nr * ntile);
                 row_dkv<ST, DH>(a, b, hk, j, off, ra, rb, [&](int p) {
                     return far ? p - j >= a.W : j <= p && (a.W == 0 || p - j < a.W || (!apart && j < a.S));
                 }, lane, x, y);
@@ -376,8 +360,8 @@ __device__ __forceinline__ void dkv_body(unsigned char* smem, const AttnArgs& a,
 template <int DH, int QN>
 __device__ __forceinline__ void dq_body(unsigned char* smem, const AttnArgs& a, int b, int hk, int r0) {
     using ST = uint16_t;
-    constexpr int NS = DH / 32, ND = DH / 16, STG = bstages<DH>(), LD = Slots<DH>::LD;
-    constexpr int TILE = kTB * DH * 2, STAGE = 2 * TILE;
+    constexpr int NS = DH / 32, ND = DH / 16, STG = kStages, LD = TileLoad<DH>::LD;
+    constexpr int TILE = TileLoad<DH>::BYTES, STAGE = 2 * TILE;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, c16 = lane & 15;
     const int qn = seq_len_of(a.ql, b, a.Tq), kn = seq_len_of(a.kl, b, a.N), off = kn - qn;
     const int R = a.Tq * a.G, rn = qn * a.G, wr0 = r0 + 16 * QN * wave;
@@ -413,21 +397,14 @@ __device__ __forceinline__ void dq_body(unsigned char* smem, const AttnArgs& a, 
 #pragma unroll
             for (int st = 0; st < NS; ++st) asm volatile("" : "+v"(qf[qs][st].v), "+v"(gf[qs][st].v));
         }
-        const Slots<DH> slots(wave, lane);
+        const TileLoad<DH> tl(wave, lane);
         const TileReads<DH> rd(g, c16);
-        const uint32_t lbase = __builtin_amdgcn_readfirstlane(lds_addr(smem)) +
-                               1024 * (uint32_t)__builtin_amdgcn_readfirstlane(wave);
-        const ST* kp = row_ptr<ST>(a.k, b, hk, 0);
-        const ST* vp = row_ptr<ST>(a.v, b, hk, 0);
+        const KeyTiles<DH> kt(a.k, b, hk, tl), vt(a.v, b, hk, tl);
+        const uint32_t base = __builtin_amdgcn_readfirstlane(lds_addr(smem));
         auto issue = [&](int t, int buf) {
             const int e0 = kTB * min(t, ntile - 1);
-            const uint32_t at = lbase + buf * STAGE;
-#pragma unroll
-            for (int j = 0; j < LD; ++j) {
-                const int64_t key = list.key(min(e0 + slots.row[j], list.count - 1));
-                lds_load16(kp + key * a.k.row + slots.col[j], at + 4096 * j);
-                lds_load16(vp + key * a.v.row + slots.col[j], at + TILE + 4096 * j);
-            }
+            kt.issue(tl, list, e0, base + buf * STAGE);
+            vt.issue(tl, list, e0, base + buf * STAGE + TILE);
         };
         const float c2 = a.scale * kLog2e;
 #pragma unroll
@@ -481,9 +458,9 @@ __device__ __forceinline__ void dq_body(unsigned char* smem, const AttnArgs& a, 
                 for (int qs = 0; qs < QN; ++qs) df[qs] = pack_frag(dp[qs][0], dp[qs][1]);
 #pragma unroll
                 for (int db = 0; db < ND; ++db) {
-                    const Frag8<ST> kt = rd.cols(Kt, u, db);
+                    const Frag8<ST> kf = rd.cols(Kt, u, db);
 #pragma unroll
-                    for (int qs = 0; qs < QN; ++qs) mma8(dq[qs][db], kt, df[qs]);
+                    for (int qs = 0; qs < QN; ++qs) mma8(dq[qs][db], kf, df[qs]);
                 }
             }
         };
@@ -563,29 +540,34 @@ __global__ __launch_bounds__(256) void wattn_sinks_kernel(AttnArgs a, int slots,
     }
 }
 
-// Blocks of 128 keys and rows halve the reads of the tiles per product; blocks
-// of 64 where those leave CUs idle.
+// Keys and rows per block.  Blocks of 128 halve the reads of the tiles per
+// product; blocks of 64 where those leave CUs idle.  128-wide heads keep to 64
+// keys (16 per wave): the sums of 32 keys and their operands are 192 registers
+// of a lane, which leaves too few for the rest at 2 waves per SIMD.
 template <int DH>
 bool wide_blocks(const AttnArgs& a) { return (int64_t)a.B * a.Hkv * ((a.N + 127) / 128) >= 512; }
+template <int DH>
+constexpr int wide_keys() { return DH == 128 ? 1 : 2; }
 
 template <int DH>
 BwdGeom bwd_geom(const AttnArgs& a) {
     BwdGeom G;
-    const int w = wide_blocks<DH>(a) ? 128 : 64;
+    const bool wide = wide_blocks<DH>(a);
+    const int kw = wide ? 64 * wide_keys<DH>() : 64, qw = wide ? 128 : 64;
     const int64_t R = (int64_t)a.Tq * a.G;
-    G.nk = (a.N + w - 1) / w;
-    G.nq = (int)((R + w - 1) / w);
+    G.nk = (a.N + kw - 1) / kw;
+    G.nq = (int)((R + qw - 1) / qw);
     G.ns = a.W && a.S && a.S <= kSinkKeys ? (a.S + 63) / 64 : 0;
     // a chunk walks about as many rows as a key block does
-    const int64_t c = (R + (int64_t)(a.W + w) * a.G - 1) / ((int64_t)(a.W + w) * a.G);
+    const int64_t c = (R + (int64_t)(a.W + kw) * a.G - 1) / ((int64_t)(a.W + kw) * a.G);
     G.nc = G.ns ? (int)(c < kSinkChunks ? c : kSinkChunks) : 0;
     return G;
 }
 
-template <int DH, int W>
+template <int DH, int CB, int QN>
 int launch_bwd(const AttnArgs& a, const BwdGeom& G, float* sums, hipStream_t stream) {
-    auto kern = wattn_bwd_kernel<DH, W, W>;
-    const size_t ring = (size_t)bstages<DH>() * (2 * kTB * DH * 2 + 4 * kTB * 8), outs = (size_t)64 * W * (DH + 8) * 2;
+    auto kern = wattn_bwd_kernel<DH, CB, QN>;
+    const size_t ring = (size_t)kStages * (2 * kTB * DH * 2 + 4 * kTB * 8), outs = (size_t)64 * QN * (DH + 8) * 2;
     const size_t lds = ring > outs ? ring : outs;
     if (allow_lds((const void*)kern, lds)) return -1;
     const uint64_t blocks = (uint64_t)a.B * a.Hkv * ((uint64_t)G.nk + G.ns * G.nc + G.nq);
@@ -598,7 +580,8 @@ int launch_bwd(const AttnArgs& a, const BwdGeom& G, float* sums, hipStream_t str
 template <int DH>
 int bwd_tiled(const AttnArgs& a, float* sums, hipStream_t stream) {
     const BwdGeom G = bwd_geom<DH>(a);
-    const int e = wide_blocks<DH>(a) ? launch_bwd<DH, 2>(a, G, sums, stream) : launch_bwd<DH, 1>(a, G, sums, stream);
+    const int e = wide_blocks<DH>(a) ? launch_bwd<DH, wide_keys<DH>(), 2>(a, G, sums, stream)
+                                     : launch_bwd<DH, 1, 1>(a, G, sums, stream);
     if (e || !G.ns) return e;
     const int64_t all = (int64_t)a.B * a.Hkv * a.S * 2 * DH, blocks = (all + 255) / 256;
     hipLaunchKernelGGL((wattn_sinks_kernel<DH>), dim3((unsigned)(blocks < 65536 ? blocks : 65536)), dim3(256), 0, stream, a,

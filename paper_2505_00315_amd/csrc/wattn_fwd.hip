@@ -11,29 +11,15 @@
 // exponential about as much issue time as a quarter of them; a wave of 32 rows
 // reads each K and V fragment once per 2 matrix instructions, which is what the
 // LDS can deliver at their full rate.
-#include "attn_lds.h"
-#include "heads.h"
 #include "launch_parts.h"
 #include "rowattn.h"
+#include "wattn_dma.h"
 
 namespace mosa {
 
 namespace {
 
-constexpr int kKB = 64;  // keys per tile
-
-template <int DH>
-__device__ __forceinline__ int wk_swz(int r) {  // K tile: unit permutation of row r
-    if constexpr (DH == 128) return r & 15;
-    else return kswz(r, DH / 8);
-}
-template <int DH>
-__device__ __forceinline__ int wv_swz(int r) {  // V tile (even: transposed reads take unit pairs)
-    if constexpr (DH == 128) return 2 * (r & 7);
-    else return vt_swz<DH / 8>(r);
-}
-template <int DH>
-constexpr int stages() { return DH == 128 ? 2 : 4; }  // 64 KB of ring (32 KB for 32-wide heads): two workgroups per CU
+constexpr int kStages = 2;  // ring of at most 64 KB: two workgroups and more per CU (4 stages of the narrower heads: no faster)
 
 // Launch geometry: blocks of QB rows, nb per (b, key head), each cut into parts.
 struct FwdGeom {
@@ -43,8 +29,8 @@ struct FwdGeom {
 template <int DH, int QN>
 __global__ __launch_bounds__(256, 2) void wattn_fwd_kernel(AttnArgs a, FwdGeom G, Parts part, uint32_t first) {
     using ST = uint16_t;
-    constexpr int U = DH / 8, KB = kKB, QB = 64 * QN, STG = stages<DH>(), NS = DH / 32, ND = DH / 16;
-    constexpr int TILE = KB * DH * 2, STAGE = 2 * TILE, LD = TILE / 4096;  // LD: loads per wave and operand tile
+    constexpr int U = DH / 8, KB = kTB, QB = 64 * QN, STG = kStages, NS = DH / 32, ND = DH / 16;
+    constexpr int TILE = TileLoad<DH>::BYTES, STAGE = 2 * TILE, LD = TileLoad<DH>::LD;
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, c16 = lane & 15;
 
@@ -102,46 +88,17 @@ __global__ __launch_bounds__(256, 2) void wattn_fwd_kernel(AttnArgs a, FwdGeom G
 #pragma unroll
             for (int st = 0; st < NS; ++st) asm volatile("" : "+v"(qf[qs][st].v));
 
-        // 16-byte unit p = 64 (wave + 4 j) + lane of a tile is row p / U, stored
-        // unit p % U, which holds the row's unit (p % U) ^ swizzle(row)
-        const uint32_t lbase = __builtin_amdgcn_readfirstlane(lds_addr(smem)) +
-                               1024 * (uint32_t)__builtin_amdgcn_readfirstlane(wave);
-        int drow[LD], kcol[LD], vcol[LD];
-#pragma unroll
-        for (int j = 0; j < LD; ++j) {
-            const int p = 64 * (wave + 4 * j) + lane, r = p / U, u = p % U;
-            drow[j] = r;
-            kcol[j] = 8 * (u ^ wk_swz<DH>(r));
-            vcol[j] = 8 * (u ^ wv_swz<DH>(r));
-        }
-        const ST* kp = row_ptr<ST>(a.k, b, hk, 0);
-        const ST* vp = row_ptr<ST>(a.v, b, hk, 0);
-        const int64_t krow = a.k.row, vrow = a.v.row;
+        const TileLoad<DH> tl(wave, lane);
+        const TileReads<DH> rd(g, c16);
+        const KeyTiles<DH> kt(a.k, b, hk, tl), vt(a.v, b, hk, tl);
+        const uint32_t lbase = __builtin_amdgcn_readfirstlane(lds_addr(smem));
         // tile t of this part (past the end: the last one again, into a buffer
-        // that nobody reads); entries past the list are its last one (masked)
+        // that nobody reads); entries past the list are masked
         auto issue = [&](int t, int buf) {
             const int e0 = KB * (tbeg + min(t, ntile - 1));
-            const uint32_t base = lbase + buf * STAGE;
-#pragma unroll
-            for (int j = 0; j < LD; ++j) {
-                const int key = list.key(min(e0 + drow[j], list.count - 1));
-                lds_load16(kp + key * krow + kcol[j], base + 4096 * j);
-                lds_load16(vp + key * vrow + vcol[j], base + TILE + 4096 * j);
-            }
+            kt.issue(tl, list, e0, lbase + buf * STAGE);
+            vt.issue(tl, list, e0, lbase + buf * STAGE + TILE);
         };
-        // byte offsets within a V tile of the transposed reads: keys
-        // 32 u + 4 g + c16 / 4 and 16 more, columns 16 db + 4 (c16 % 4); both
-        // swizzles depend on the row's low 4 bits only
-        int voff[ND];
-#pragma unroll
-        for (int db = 0; db < ND; ++db) {
-            const int kk = 4 * g + (c16 >> 2), col = 16 * db + 4 * (c16 & 3), un = col >> 3, half = (col >> 2) & 1;
-            voff[db] = (kk * U + (un ^ wv_swz<DH>(kk))) * 16 + 8 * half;
-        }
-        int koff[NS];
-#pragma unroll
-        for (int st = 0; st < NS; ++st) koff[st] = (c16 * U + ((4 * st + g) ^ wk_swz<DH>(c16))) * 16;
-
         const float c2 = a.scale * kLog2e;  // scores in log2 units
 #pragma unroll
         for (int s = 0; s < STG - 1; ++s) issue(s, s);
@@ -162,8 +119,7 @@ __global__ __launch_bounds__(256, 2) void wattn_fwd_kernel(AttnArgs a, FwdGeom G
             for (int sb = 0; sb < 4; ++sb) {
                 Frag8<ST> kf[NS];
 #pragma unroll
-                for (int st = 0; st < NS; ++st)
-                    kf[st].v = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(Kb + koff[st] + 16 * U * 16 * sb));
+                for (int st = 0; st < NS; ++st) kf[st] = rd.rows(Kb, sb, st);
 #pragma unroll
                 for (int qs = 0; qs < QN; ++qs) s[qs][sb] = zero4();
 #pragma unroll
@@ -221,17 +177,10 @@ __global__ __launch_bounds__(256, 2) void wattn_fwd_kernel(AttnArgs a, FwdGeom G
             for (int u = 0; u < 2; ++u) {
                 Frag8<ST> pf[QN];
 #pragma unroll
-                for (int qs = 0; qs < QN; ++qs) {
-                    const f32x4 &x = s[qs][2 * u], &y = s[qs][2 * u + 1];
-                    const float pv[8] = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
-                    pf[qs] = frag8_from<ST>(pv);
-                }
+                for (int qs = 0; qs < QN; ++qs) pf[qs] = pack_frag(s[qs][2 * u], s[qs][2 * u + 1]);
 #pragma unroll
                 for (int db = 0; db < ND; ++db) {
-                    const u32x2 lo = lds_tr16(Vb + voff[db] + 32 * u * U * 16);
-                    const u32x2 hi = lds_tr16(Vb + voff[db] + (32 * u + 16) * U * 16);
-                    Frag8<ST> vf;
-                    vf.v = __builtin_bit_cast(bf16x8, u32x4{lo.x, lo.y, hi.x, hi.y});
+                    const Frag8<ST> vf = rd.cols(Vb, u, db);
 #pragma unroll
                     for (int qs = 0; qs < QN; ++qs) mma8(o[qs][db], vf, pf[qs]);
                 }
@@ -369,7 +318,7 @@ FwdGeom fwd_geom(const AttnArgs& a) {
     const int64_t blocks = (int64_t)G.nb * a.B * a.Hkv;
     // most keys of a block, in tiles; a part keeps at least 4 of them
     const int64_t span = a.W ? (int64_t)a.W + a.S + 64 / a.G + 1 : a.N;
-    const int64_t tiles = ((span < a.N ? span : a.N) + kKB - 1) / kKB;
+    const int64_t tiles = ((span < a.N ? span : a.N) + kTB - 1) / kTB;
     int64_t parts = blocks >= 256 ? 1 : (512 + blocks - 1) / blocks;
     if (parts > tiles / 4) parts = tiles / 4;
     G.parts = parts < 1 ? 1 : (int)parts;
@@ -378,7 +327,7 @@ FwdGeom fwd_geom(const AttnArgs& a) {
 
 template <int DH, int QN>
 int launch_fwd(const AttnArgs& a, const FwdGeom& G, float* buf, hipStream_t stream) {
-    const size_t ring = (size_t)stages<DH>() * 2 * kKB * DH * 2, outs = (size_t)64 * QN * (DH + 8) * 2;
+    const size_t ring = (size_t)kStages * 2 * kTB * DH * 2, outs = (size_t)64 * QN * (DH + 8) * 2;
     const size_t lds = ring > outs ? ring : outs;
     const Parts part = make_parts(buf, G.parts, (int64_t)a.B * a.Hq * a.Tq, DH);
     auto kern = wattn_fwd_kernel<DH, QN>;
