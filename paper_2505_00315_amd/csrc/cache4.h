@@ -9,9 +9,12 @@
 // column 2 i in nibble i and column 2 i + 1 in nibble i + 4: lane group kg of a
 // matrix instruction over the 32 columns of a group reads its words of all
 // groups with one load, and a shift and a mask give a pair of neighbours.
-// V is kept in 16-bit pieces of 4 columns of one position, the pieces of 4
-// neighbouring positions next to each other, so that a word holds the same
-// columns of two positions: there the matrix instruction runs over positions.
+// For V the instruction runs over positions, and its 16 columns have to be of one
+// group, whose scale goes with the weights: column 32 g + 2 c + e is number
+// c dh / 16 + 2 g + e of its row, so that the columns 2 c and 2 c + 1 of all
+// groups, lane c's share, lie together.  In that order a row is kept in 16-bit
+// pieces of 4 columns, the pieces of 4 neighbouring positions next to each other:
+// a word holds the same columns of two positions.
 #pragma once
 
 #include "heads.h"
@@ -57,8 +60,9 @@ __device__ __forceinline__ float cache_k(const CacheArgs& c, const CacheBlock& b
                        (w >> (4 * ((i >> 1) + 4 * (i & 1)))) & 15);
 }
 __device__ __forceinline__ float cache_v(const CacheArgs& c, const CacheBlock& blk, int tl, int d) {
-    const uint32_t w = *reinterpret_cast<const uint16_t*>(c.cache + blk.vpiece(tl, d >> 2));
-    return cache_value(*reinterpret_cast<const uint32_t*>(c.cache + blk.vmeta(tl, d >> 5)), (w >> (4 * (d & 3))) & 15);
+    const int n = ((d & 31) >> 1) * (c.dh / 16) + 2 * (d >> 5) + (d & 1);  // the column's number in the row
+    const uint32_t w = *reinterpret_cast<const uint16_t*>(c.cache + blk.vpiece(tl, n >> 2));
+    return cache_value(*reinterpret_cast<const uint32_t*>(c.cache + blk.vmeta(tl, d >> 5)), (w >> (4 * (n & 3))) & 15);
 }
 
 }  // namespace mosa

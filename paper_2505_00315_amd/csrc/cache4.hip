@@ -1,7 +1,5 @@
-// The 4-bit cache: rows written, rows read back, attention over it.
+// The 4-bit cache: rows written and read back (attention over it: cache4_attn.hip).
 #include "cache4.h"
-#include "launch_parts.h"
-#include "rowattn.h"
 
 namespace mosa {
 
@@ -69,6 +67,45 @@ __device__ __forceinline__ uint32_t quantise8(const float (&x)[8], uint32_t (&co
     return ok ? sb | (mb << 16) : 0x7fc00000u;
 }
 
+// V's column order: a lane's 8 columns 8 li .. + 7 are the pairs c = 4 (li % 4) +
+// 0 .. 3 of group g = li / 4, a byte each; the lanes of the other groups hold the
+// same pairs of theirs.  They trade bytes so that lane g ends with the bytes of
+// all groups of some of the pairs: the pieces `unit` (low half) and unit + 1 of
+// the row.  untrade undoes it.
+template <int DH>
+__device__ __forceinline__ int v_unit(int li) {
+    if constexpr (DH == 128) return 2 * (4 * (li & 3) + (li >> 2));
+    else if constexpr (DH == 64) return 4 * (li & 3) + 2 * (li >> 2);
+    else return 2 * li;
+}
+template <int DH>
+__device__ __forceinline__ uint32_t v_trade(uint32_t w, int li) {
+    const int lane = threadIdx.x & 63, g = li >> 2;
+    if constexpr (DH == 128) {  // byte k of the result: byte g of group k's lane
+        uint32_t r = 0;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) r |= (__shfl(w, lane + 4 * (k - g), 64) >> (8 * g) & 0xffu) << (8 * k);
+        return r;
+    } else if constexpr (DH == 64) {
+        const uint32_t o = __shfl_xor(w, 4, 64), a = g ? o : w, b = g ? w : o;  // groups 0 and 1
+        const uint32_t x = a >> (16 * g), y = b >> (16 * g);
+        return (x & 0xffu) | (y & 0xffu) << 8 | (x & 0xff00u) << 8 | (y & 0xff00u) << 16;
+    } else {
+        return w;
+    }
+}
+template <int DH>
+__device__ __forceinline__ uint32_t v_untrade(uint32_t w, int li) {
+    if constexpr (DH == 128) return v_trade<DH>(w, li);
+    else if constexpr (DH == 64) {
+        const int g = li >> 2;
+        const uint32_t o = __shfl_xor(w, 4, 64), a = (g ? o : w) >> (8 * g), b = (g ? w : o) >> (8 * g);
+        return (a & 0xffu) | (a >> 8 & 0xff00u) | (b & 0xffu) << 16 | (b >> 16 & 0xffu) << 24;
+    } else {
+        return w;
+    }
+}
+
 // Where a quad's lane works: its position, the row it comes from or goes to,
 // and its block of the cache.
 struct QuadSpot {
@@ -106,11 +143,16 @@ __global__ __launch_bounds__(256) void cache4_append_kernel(CacheArgs c, int qua
         }
         uint32_t kc[8], vc[8];
         const uint32_t km = quantise8(x, kc), vm = quantise8(y, vc);
-        // V: the pieces of columns 0..3 and 4..7; a word takes those of two
-        // neighbouring positions, the even one's lane the first piece, the odd one's the second
-        const uint32_t v0 = vc[0] | vc[1] << 4 | vc[2] << 8 | vc[3] << 12, v1 = vc[4] | vc[5] << 4 | vc[6] << 8 | vc[7] << 12;
+        // V: a word takes the pieces of two neighbouring positions, the even
+        // one's lane the first of its two pieces, the odd one's the second
+        uint32_t vw = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) vw |= vc[i] << (4 * i);
+        vw = v_trade<DH>(vw, li);
+        const uint32_t v0 = vw & 0xffffu, v1 = vw >> 16;
+        const int unit = v_unit<DH>(li);
         const int other = (threadIdx.x & 63) ^ Q::LPP;  // the neighbour's lane with the same columns
-        const uint32_t theirs = __shfl(v0 | v1 << 16, other, 64);
+        const uint32_t theirs = __shfl(vw, other, 64);
         const int both = __shfl((int)s.held, other, 64);
         if (!s.held) continue;
         uint32_t w = 0;
@@ -121,10 +163,10 @@ __global__ __launch_bounds__(256) void cache4_append_kernel(CacheArgs c, int qua
         if (both) {
             const bool odd = s.tl & 1;
             const uint32_t word = odd ? (theirs >> 16 | v1 << 16) : (v0 | theirs << 16);
-            *reinterpret_cast<uint32_t*>(c.cache + s.blk.vpiece(s.tl & ~1, 2 * li + odd)) = word;
+            *reinterpret_cast<uint32_t*>(c.cache + s.blk.vpiece(s.tl & ~1, unit + odd)) = word;
         } else {
-            *reinterpret_cast<uint16_t*>(c.cache + s.blk.vpiece(s.tl, 2 * li)) = (uint16_t)v0;
-            *reinterpret_cast<uint16_t*>(c.cache + s.blk.vpiece(s.tl, 2 * li + 1)) = (uint16_t)v1;
+            *reinterpret_cast<uint16_t*>(c.cache + s.blk.vpiece(s.tl, unit)) = (uint16_t)v0;
+            *reinterpret_cast<uint16_t*>(c.cache + s.blk.vpiece(s.tl, unit + 1)) = (uint16_t)v1;
         }
         if (kg == 0) {
             *reinterpret_cast<uint32_t*>(c.cache + s.blk.kmeta(s.tl, g)) = km;
@@ -140,15 +182,19 @@ __global__ __launch_bounds__(256) void cache4_read_kernel(CacheArgs c, int quads
     for (int64_t quad = (int64_t)blockIdx.x * Q::QPB + threadIdx.x / Q::LPQ;; quad += (int64_t)gridDim.x * Q::QPB) {
         QuadSpot s;
         if (!quad_spot<DH>(c, quad, quads, lane, s)) break;
-        if (!s.live) continue;
         float x[8] = {}, y[8] = {};
+        uint32_t w = 0, v = 0, km = 0, vm = 0;
         if (s.held) {
-            const uint32_t w = *reinterpret_cast<const uint32_t*>(c.cache + s.blk.kword(s.tl, kg * (DH / 32) + g));
-            const uint32_t v0 = *reinterpret_cast<const uint16_t*>(c.cache + s.blk.vpiece(s.tl, 2 * li));
-            const uint32_t v1 = *reinterpret_cast<const uint16_t*>(c.cache + s.blk.vpiece(s.tl, 2 * li + 1));
-            const uint32_t km = *reinterpret_cast<const uint32_t*>(c.cache + s.blk.kmeta(s.tl, g));
-            const uint32_t vm = *reinterpret_cast<const uint32_t*>(c.cache + s.blk.vmeta(s.tl, g));
-            const uint32_t v = v0 | v1 << 16;
+            const int unit = v_unit<DH>(li);
+            w = *reinterpret_cast<const uint32_t*>(c.cache + s.blk.kword(s.tl, kg * (DH / 32) + g));
+            v = *reinterpret_cast<const uint16_t*>(c.cache + s.blk.vpiece(s.tl, unit));
+            v |= (uint32_t)*reinterpret_cast<const uint16_t*>(c.cache + s.blk.vpiece(s.tl, unit + 1)) << 16;
+            km = *reinterpret_cast<const uint32_t*>(c.cache + s.blk.kmeta(s.tl, g));
+            vm = *reinterpret_cast<const uint32_t*>(c.cache + s.blk.vmeta(s.tl, g));
+        }
+        v = v_untrade<DH>(v, li);
+        if (!s.live) continue;
+        if (s.held) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 x[i] = cache_value(km, (w >> (4 * ((i >> 1) + 4 * (i & 1)))) & 15);
@@ -158,24 +204,6 @@ __global__ __launch_bounds__(256) void cache4_read_kernel(CacheArgs c, int quads
         store8(row_ptr<ST>(c.k, s.b, s.h, s.t) + 8 * li, x);
         store8(row_ptr<ST>(c.v, s.b, s.h, s.t) + 8 * li, y);
     }
-}
-
-// One wave per query row.
-template <typename ST, int DH>
-__global__ __launch_bounds__(256) void cache4_rows_kernel(AttnArgs a, CacheArgs c, uint32_t first) {
-    const int lane = threadIdx.x & 63;
-    const int64_t row = ((int64_t)first + blockIdx.x) * 4 + (threadIdx.x >> 6);
-    if (row >= (int64_t)a.B * a.Hq * a.Tq) return;
-    const int i = (int)(row % a.Tq), h = (int)(row / a.Tq % a.Hq), b = (int)(row / a.Tq / a.Hq);
-    const int qn = seq_len_of(a.ql, b, a.Tq), kn = seq_len_of(a.kl, b, a.N), p = kn - qn + i;
-    float q[RowLanes<DH>::N], o[RowLanes<DH>::N] = {}, m = -__builtin_inff(), l = 0.f;
-    if (i < qn) {
-        row_load<ST, DH>(row_ptr<ST>(a.q, b, h, i), lane, q);
-        const KeyList list = keys_of(a, p, p, kn);
-        row_attend<DH>(a, CacheKeys<DH>{c, b, h / a.G}, [&](int e) { return list.key(e); }, 0, list.count, p, kn, q, lane,
-                       m, l, o);
-    }
-    row_finish<ST, DH>(a, b, h, i, row, lane, m, l, o, nullptr, nullptr);
 }
 
 template <class K>
@@ -199,18 +227,6 @@ int launch_cache4_read(int dtype, const CacheArgs& c, hipStream_t stream) {
     return heads_by_type(dtype, c.dh, [&](auto st, auto d) {
         constexpr int DH = decltype(d)::value;
         return launch_quads(cache4_read_kernel<decltype(st), DH>, c, Quad<DH>::QPB, stream);
-    });
-}
-
-size_t cache4_attn_scratch(int, int, const AttnArgs&) { return 0; }
-
-int launch_cache4_attn(int dtype, const AttnArgs& a, const CacheArgs& c, float*, hipStream_t stream) {
-    return heads_by_type(dtype, c.dh, [&](auto st, auto d) {
-        return launch_parts(((uint64_t)a.B * a.Hq * a.Tq + 3) / 4, 256, [&](uint32_t first, uint32_t blocks) {
-            hipLaunchKernelGGL((cache4_rows_kernel<decltype(st), decltype(d)::value>), dim3(blocks), dim3(256), 0,
-                               stream, a, c, first);
-            return hipGetLastError() == hipSuccess ? 0 : -1;
-        });
     });
 }
 

@@ -1,0 +1,512 @@
+// Attention over the 4-bit cache: a few query rows of a key head against its
+// whole cache, so the cache's bytes bound it (dh + dh / 4 per position and head).
+//
+// What is read is multiplied as it is held.  A code n goes into a matrix
+// operand as the bf16 number 16 + n, which is a shift and a mask for two of
+// them, and the scales and minima come in around the products:
+//   q k = sum_g s_g (q (16 + n))_g + sum_g (m_g - 16 s_g) sum(q)_g
+// with one matrix instruction per group of 32 columns, and one for the whole
+// second sum: the words (s, m) of a position, as they are held, times
+// (-16 sum(q), sum(q)), split into three bf16 parts so that nothing is lost.
+//   out_g = sum_j (p_j s_jg) (16 + n_j) + sum_j p_j m_jg - 16 sum_j (p_j s_jg)
+// where the weights times the scales of a group are the matrix operand, rounded
+// to bf16 once, and the last sum is taken over the same rounded numbers (a
+// product with ones), so that the 16 cancels exactly.  fp32 storage takes q and
+// p s in three bf16 parts.
+//
+// Every wave walks its own tiles of 32 positions with its own running maximum
+// and sum, loads straight into registers one tile ahead and the page numbers
+// two ahead; the waves of a workgroup are joined in LDS, parts of the keys by
+// merge_parts.  Scores have the key in the lane, which so has the scales of its
+// key at hand for both products; the weights change lanes through LDS.
+#include "cache4.h"
+#include "launch_parts.h"
+#include "rowattn.h"
+
+namespace mosa {
+
+namespace {
+
+constexpr int kWaves = 4;
+
+// The keys that some row sees, in aligned octets: so octets of sinks, then
+// those from w0 on.
+struct OctetList {
+    int so, w0, count;
+    __device__ __forceinline__ int first_key(int e) const { return 8 * (e < so ? e : e - so + w0); }
+};
+__device__ __forceinline__ OctetList octets_of(const KeyList& l) {
+    OctetList o;
+    o.so = (l.s + 7) / 8;
+    o.w0 = max(l.lo / 8, o.so);
+    const int hi = l.lo + l.count - l.s;  // past the last key
+    o.count = l.count <= 0 ? 0 : o.so + max((hi + 7) / 8 - o.w0, 0);
+    return o;
+}
+
+template <int DH, int SPLIT>
+struct AttnLds {
+    static constexpr int NG = DH / 32;
+    static constexpr int PROW = 32 * 2 + 16;             // weights of a row: 32 positions, padded
+    static constexpr int PW = SPLIT * NG * 16 * PROW;    // of a wave and 16 rows
+};
+
+__device__ __forceinline__ uint32_t codes(uint32_t w, int nib) {  // nibbles nib and nib + 4 of w as bf16 16 + n
+    const int sh = 4 * nib - 3;
+    return ((sh < 0 ? w << 3 : w >> sh) & 0x00780078u) | 0x41804180u;
+}
+
+template <int N>
+__device__ __forceinline__ void load_words(const unsigned char* p, uint32_t (&w)[N]) {
+    if constexpr (N == 4) {
+        const uint4 u = *reinterpret_cast<const uint4*>(p);
+        w[0] = u.x, w[1] = u.y, w[2] = u.z, w[3] = u.w;
+    } else if constexpr (N == 2) {
+        const uint2 u = *reinterpret_cast<const uint2*>(p);
+        w[0] = u.x, w[1] = u.y;
+    } else {
+        w[0] = *reinterpret_cast<const uint32_t*>(p);
+    }
+}
+
+// A lane's words of a tile.
+template <int DH>
+struct Tile {
+    static constexpr int NG = DH / 32, NV = DH == 128 ? 4 : 2;
+    uint32_t kc[2][NG], km[2][NG], vm[2][NG], vc[2][NV];
+    int key;    // the lane's keys are key and key + 1 (negative: on no page)
+};
+
+__device__ __forceinline__ bf16x8 frag_of(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    return __builtin_bit_cast(bf16x8, u32x4_t{a, b, c, d});
+}
+
+// Row sums and maxima over the 16 lanes of a result's row.
+__device__ __forceinline__ float lanes16_max(float x) {
+    x = fmaxf(x, dpp_f32<0xB1, 0xf>(x));
+    x = fmaxf(x, dpp_f32<0x4E, 0xf>(x));
+    x = fmaxf(x, dpp_f32<0x141, 0xf>(x));
+    return fmaxf(x, dpp_f32<0x140, 0xf>(x));
+}
+__device__ __forceinline__ float lanes16_sum(float x) {
+    x += dpp_f32<0xB1, 0xf>(x);
+    x += dpp_f32<0x4E, 0xf>(x);
+    x += dpp_f32<0x141, 0xf>(x);
+    return x + dpp_f32<0x140, 0xf>(x);
+}
+
+struct CacheGeom {
+    int nb, parts;  // blocks of 16 NQ rows per (b, key head), parts of their keys
+    UDiv page;      // by the page size
+};
+
+// SPLIT: bf16 parts of q and of the weights (1 for bf16 storage, 3 for fp32).
+template <typename ST, int DH, int NQ>
+__global__ __launch_bounds__(64 * kWaves, 2) void cache4_attn_kernel(AttnArgs a, CacheArgs c, CacheGeom G, Parts part,
+                                                                    uint32_t first) {
+    constexpr int SPLIT = sizeof(ST) == 2 ? 1 : 3, NG = DH / 32, ND = DH / 16;
+    using L = AttnLds<DH, SPLIT>;
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, c16 = lane & 15;
+    uint32_t id = first + blockIdx.x;
+    const int pt = (int)(id % G.parts);
+    id /= G.parts;
+    const int blk = (int)(id % G.nb), bh = (int)(id / G.nb), b = bh / a.Hkv, hk = bh % a.Hkv;
+    const int R = a.Tq * a.G, r0 = blk * 16 * NQ;
+    const int qn = seq_len_of(a.ql, b, a.Tq), kn = seq_len_of(a.kl, b, a.N), off = kn - qn, rn = qn * a.G;
+
+    KeyList keys{0, 0, 0};
+    int p0 = 0, p1 = 0;  // positions of the block's first and last row
+    if (r0 < rn) {
+        p0 = off + a.gd.div(r0);
+        p1 = off + a.gd.div(min(r0 + 16 * NQ, rn) - 1);
+        keys = keys_of(a, p0, p1, kn);
+    }
+    const OctetList list = octets_of(keys);
+    const int all = (list.count + 3) / 4, share = (all + G.parts - 1) / G.parts;
+    const int tbeg = min(pt * share, all), tend = min(all, tbeg + share);  // this part's tiles; a wave takes every fourth
+
+    float m_run[NQ][4], l_run[NQ][4], pm[NQ][NG][4];
+    f32x4 o[NQ][ND], ones[NQ][NG];
+    int pos[NQ][4];
+#pragma unroll
+    for (int q = 0; q < NQ; ++q) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            m_run[q][i] = -__builtin_inff();
+            l_run[q][i] = 0.f;
+            pos[q][i] = off + a.gd.div(min(r0 + 16 * q + 4 * g + i, max(rn, 1) - 1));
+#pragma unroll
+            for (int gr = 0; gr < NG; ++gr) pm[q][gr][i] = 0.f;
+        }
+#pragma unroll
+        for (int d = 0; d < ND; ++d) o[q][d] = zero4();
+#pragma unroll
+        for (int gr = 0; gr < NG; ++gr) ones[q][gr] = zero4();
+    }
+
+    if (tbeg + wave < tend) {
+        // q as A operand: row c16, columns 32 gr + 8 g .. + 7, in SPLIT parts;
+        // its sums over a group, times (-16, 1), as the operand of the words (s, m):
+        // lane group 0 holds the upper bf16 part, 1 and 2 what that leaves
+        bf16x8 qf[NQ][SPLIT][NG], qs[NQ];
+#pragma unroll
+        for (int q = 0; q < NQ; ++q) {
+            const int r = min(r0 + 16 * q + c16, rn - 1);
+            const ST* qp = qrow_ptr<ST>(a, a.q, b, hk, r, a.gd.div(r));
+            uint32_t sums[4] = {0, 0, 0, 0};
+#pragma unroll
+            for (int gr = 0; gr < NG; ++gr) {
+                float x[8], s = 0.f;
+                frag8_to_f32<ST>(frag8_load<ST>(qp + 32 * gr + 8 * g), x);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) s += x[e];
+                s = rows4_sum(s);
+#pragma unroll
+                for (int sp = 0; sp < SPLIT; ++sp) {
+                    qf[q][sp][gr] = frag8_from<uint16_t>(x).v;
+                    float y[8];
+                    Frag8<uint16_t> f;
+                    f.v = qf[q][sp][gr];
+                    frag8_to_f32<uint16_t>(f, y);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) x[e] -= y[e];
+                }
+                const float hi = bf16_to_f32(f32_to_bf16(s)), mid = bf16_to_f32(f32_to_bf16(s - hi)), lo = s - hi - mid;
+                const float mine = g == 0 ? hi : g == 1 ? mid : g == 2 ? lo : 0.f;
+                sums[gr] = pack_bf16x2(-16.f * mine, mine);
+            }
+            qs[q] = frag_of(sums[0], sums[1], sums[2], sums[3]);
+        }
+
+        const size_t block = cache_block_bytes(c.ps, DH);
+        const int32_t* table = c.table + (size_t)b * c.per;
+        // pages of the octets of tile t: that of this lane's two keys, and that of its octet of V
+        struct Pages { int k, v; };
+        auto octet = [&](int t, int x) { return list.first_key(min(4 * t + x, list.count - 1)); };
+        auto pages = [&](int t) {
+            t = min(t, tend - 1);
+            return Pages{table[G.page.div(octet(t, c16 >> 2))], table[G.page.div(octet(t, g))]};
+        };
+        auto load = [&](int t, const Pages& pg, Tile<DH>& x) {
+            t = min(t, tend - 1);
+            const int ek = octet(t, c16 >> 2), ev = octet(t, g);
+            const bool kin = pg.k >= 0 && pg.k < c.pages && 4 * t + (c16 >> 2) < list.count;
+            const bool vin = pg.v >= 0 && pg.v < c.pages;
+            const int tk = ek - G.page.div(ek) * c.ps + 2 * (c16 & 3), tv = ev - G.page.div(ev) * c.ps;
+            x.key = kin ? ek + 2 * (c16 & 3) : -2;
+            // (a page that does not exist: page 0 is read and masked)
+            const unsigned char* kb = c.cache + ((size_t)(kin ? pg.k : 0) * c.H + hk) * block;
+            const unsigned char* vb = c.cache + ((size_t)(vin ? pg.v : 0) * c.H + hk) * block;
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+                load_words<NG>(kb + (tk + y) * (DH / 2) + g * (DH / 8), x.kc[y]);
+                load_words<NG>(kb + c.ps * DH + (tk + y) * (DH / 8), x.km[y]);
+                load_words<NG>(kb + c.ps * (DH + DH / 8) + (tk + y) * (DH / 8), x.vm[y]);
+                load_words<Tile<DH>::NV>(vb + c.ps * (DH / 2) + (tv / 4 + y) * (2 * DH) + (DH == 32 ? c16 / 2 * 8 : c16 * (DH / 8)),
+                                         x.vc[y]);
+            }
+        };
+        const float c2 = a.scale * kLog2e;
+        unsigned char* pw = smem + wave * NQ * L::PW;  // this wave's weights
+        const bf16x8 one8 = frag_of(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u);
+
+        Tile<DH> cur, nxt;
+        Pages pg = pages(tbeg + wave);
+        load(tbeg + wave, pg, nxt);
+        pg = pages(tbeg + wave + kWaves);
+#pragma unroll 1
+        for (int t = tbeg + wave; t < tend; t += kWaves) {
+            cur = nxt;
+            load(t + kWaves, pg, nxt);
+            pg = pages(t + 2 * kWaves);
+
+            // scores of rows 4 g + i and keys cur.key + y
+            f32x4 s[NQ][2];
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+                bf16x8 meta;
+                if constexpr (NG == 4) meta = frag_of(cur.km[y][0], cur.km[y][1], cur.km[y][2], cur.km[y][3]);
+                else if constexpr (NG == 2) meta = frag_of(cur.km[y][0], cur.km[y][1], 0, 0);
+                else meta = frag_of(cur.km[y][0], 0, 0, 0);
+#pragma unroll
+                for (int q = 0; q < NQ; ++q)
+                    s[q][y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(qs[q], meta, zero4(), 0, 0, 0);
+#pragma unroll
+                for (int gr = 0; gr < NG; ++gr) {
+                    const uint32_t w = cur.kc[y][gr];
+                    const bf16x8 kf = frag_of(codes(w, 0), codes(w, 1), codes(w, 2), codes(w, 3));
+                    const float sc = __uint_as_float(cur.km[y][gr] << 16);
+#pragma unroll
+                    for (int q = 0; q < NQ; ++q) {
+                        f32x4 x = zero4();
+#pragma unroll
+                        for (int sp = SPLIT - 1; sp >= 0; --sp)
+                            x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(qf[q][sp][gr], kf, x, 0, 0, 0);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) s[q][y][i] = __builtin_fmaf(x[i], sc, s[q][y][i]);
+                    }
+                }
+            }
+            // masks only where some row does not see some key of the tile
+            const int lastkey = octet(t, 3) + 7, firstkey = octet(t, 0);
+            const bool whole = 4 * t >= list.so && 4 * t + 4 <= list.count && lastkey <= p0 &&
+                               (a.W == 0 || firstkey > p1 - a.W) && __builtin_amdgcn_ballot_w64(cur.key < 0) == 0;
+            if (!whole) {
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {
+                    const int key = cur.key + y;
+                    const bool in = key >= 0 && key < kn;
+                    bool any = false;
+#pragma unroll
+                    for (int q = 0; q < NQ; ++q)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const bool ok = in && sees(a, pos[q][i], key);
+                            s[q][y][i] = ok ? s[q][y][i] : -__builtin_inff();
+                            any |= ok;
+                        }
+                    // what no row sees may be anything: its scale and minimum are taken as 0
+                    const uint64_t bal = __builtin_amdgcn_ballot_w64(any);
+                    const bool seen = (bal >> c16 | bal >> (c16 + 16) | bal >> (c16 + 32) | bal >> (c16 + 48)) & 1;
+#pragma unroll
+                    for (int gr = 0; gr < NG; ++gr) cur.vm[y][gr] = seen ? cur.vm[y][gr] : 0u;
+                }
+            }
+            // running maximum (moved only when exceeded by 8 in log2 units), weights
+            bool up = false;
+#pragma unroll
+            for (int q = 0; q < NQ; ++q)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) up |= fmaxf(s[q][0][i], s[q][1][i]) * c2 > m_run[q][i] + 8.f;
+            if (__builtin_amdgcn_ballot_w64(up)) {
+#pragma unroll
+                for (int q = 0; q < NQ; ++q)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float top = lanes16_max(fmaxf(s[q][0][i], s[q][1][i])) * c2;
+                        const float mn = fmaxf(m_run[q][i], top);
+                        const float al = mn == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f(m_run[q][i] - mn);
+                        m_run[q][i] = mn;
+                        l_run[q][i] *= al;
+#pragma unroll
+                        for (int d = 0; d < ND; ++d) o[q][d][i] *= al;
+#pragma unroll
+                        for (int gr = 0; gr < NG; ++gr) {
+                            pm[q][gr][i] *= al;
+                            ones[q][gr][i] *= al;
+                        }
+                    }
+            }
+#pragma unroll
+            for (int q = 0; q < NQ; ++q)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float mu = m_run[q][i] == -__builtin_inff() ? 0.f : m_run[q][i];
+                    const float w0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[q][0][i], c2, -mu));
+                    const float w1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[q][1][i], c2, -mu));
+                    l_run[q][i] += w0 + w1;
+#pragma unroll
+                    for (int gr = 0; gr < NG; ++gr) {
+                        pm[q][gr][i] = __builtin_fmaf(w0, __uint_as_float(cur.vm[0][gr] & 0xffff0000u), pm[q][gr][i]);
+                        pm[q][gr][i] = __builtin_fmaf(w1, __uint_as_float(cur.vm[1][gr] & 0xffff0000u), pm[q][gr][i]);
+                        float x0 = w0 * __uint_as_float(cur.vm[0][gr] << 16), x1 = w1 * __uint_as_float(cur.vm[1][gr] << 16);
+#pragma unroll
+                        for (int sp = 0; sp < SPLIT; ++sp) {
+                            const uint32_t u = pack_bf16x2(x0, x1);
+                            *reinterpret_cast<uint32_t*>(pw + ((((q * SPLIT + sp) * NG + gr) * 16) + 4 * g + i) * L::PROW + 4 * c16) = u;
+                            if constexpr (SPLIT > 1) {
+                                x0 -= __uint_as_float(u << 16);
+                                x1 -= __uint_as_float(u & 0xffff0000u);
+                            }
+                        }
+                    }
+                }
+            wave_sync();
+            // out += (p s) (16 + n): column c16 of result (gr, e) is 32 gr + 2 c16 + e
+#pragma unroll
+            for (int gr = 0; gr < NG; ++gr) {
+                bf16x8 wf[NQ][SPLIT];
+#pragma unroll
+                for (int q = 0; q < NQ; ++q)
+#pragma unroll
+                    for (int sp = 0; sp < SPLIT; ++sp) {
+                        wf[q][sp] = __builtin_bit_cast(
+                            bf16x8, *reinterpret_cast<const u32x4_t*>(pw + ((((q * SPLIT + sp) * NG + gr) * 16) + c16) * L::PROW + 16 * g));
+                        ones[q][gr] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf[q][sp], one8, ones[q][gr], 0, 0, 0);
+                    }
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    constexpr int H = DH == 128 ? 2 : 0;  // words of a second unit
+                    const int u = H * (gr / 2), nib = DH == 128 ? 2 * (gr % 2) + e : 2 * gr + e;
+                    uint32_t w[4] = {cur.vc[0][u], cur.vc[0][u + 1], cur.vc[1][u], cur.vc[1][u + 1]};
+                    if constexpr (DH == 32)
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) w[x] >>= 8 * (c16 & 1);
+                    const bf16x8 vf = frag_of(codes(w[0], nib), codes(w[1], nib), codes(w[2], nib), codes(w[3], nib));
+#pragma unroll
+                    for (int q = 0; q < NQ; ++q)
+#pragma unroll
+                        for (int sp = SPLIT - 1; sp >= 0; --sp)
+                            o[q][2 * gr + e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf[q][sp], vf, o[q][2 * gr + e], 0, 0, 0);
+                }
+            }
+            wave_sync();  // the weights' place is written again by the next tile
+        }
+        mfma_drain();
+    }
+
+    // This wave's rows to LDS: [16 NQ][DH] sums, then m and l of every row.
+    __syncthreads();
+    float* wo = reinterpret_cast<float*>(smem) + wave * 16 * NQ * (DH + 2);
+    float* wml = wo + 16 * NQ * DH;
+    bool fine = true;
+#pragma unroll
+    for (int q = 0; q < NQ; ++q)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            l_run[q][i] = lanes16_sum(l_run[q][i]);
+            float bad = l_run[q][i] * 0.f;
+#pragma unroll
+            for (int gr = 0; gr < NG; ++gr) {
+                const float add = lanes16_sum(pm[q][gr][i]) - 16.f * ones[q][gr][i];
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const float x = o[q][2 * gr + e][i] + add;
+                    bad = __builtin_fmaf(x, 0.f, bad);
+                    wo[(16 * q + 4 * g + i) * DH + 32 * gr + 2 * c16 + e] = x;
+                }
+            }
+            fine &= bad == 0.f;
+            if (c16 == 0) {
+                wml[2 * (16 * q + 4 * g + i)] = m_run[q][i];
+                wml[2 * (16 * q + 4 * g + i) + 1] = l_run[q][i];
+            }
+        }
+    if (__builtin_amdgcn_ballot_w64(!fine)) {
+        // a weight of 0 met a value that is not finite: this wave's rows again, one by one
+        wave_sync();
+#pragma unroll 1
+        for (int lr = 0; lr < 16 * NQ && r0 + lr < rn; ++lr) {
+            const int r = r0 + lr, i = a.gd.div(r);
+            float q[RowLanes<DH>::N], x[RowLanes<DH>::N], m, l;
+            row_load<ST, DH>(qrow_ptr<ST>(a, a.q, b, hk, r, i), lane, q);
+            const int mine = max(tend - tbeg - wave + kWaves - 1, 0) / kWaves;  // tiles of this wave
+            row_attend<DH>(a, CacheKeys<DH>{c, b, hk}, [&](int e) {
+                const int oc = 4 * (tbeg + wave + kWaves * (e / 32)) + e / 8 % 4;
+                return oc < list.count ? list.first_key(oc) + e % 8 : -1;
+            }, 0, 32 * mine, off + i, kn, q, lane, m, l, x);
+#pragma unroll
+            for (int n = 0; n < RowLanes<DH>::N; ++n)
+                if (RowLanes<DH>::has(lane)) wo[lr * DH + lane + 64 * n] = x[n];
+            if (lane == 0) wml[2 * lr] = m, wml[2 * lr + 1] = l;
+        }
+    }
+    __syncthreads();
+    // The waves in order: M = max m_w, L = sum l_w 2^(m_w - M); 8 columns per thread.
+    const float* base = reinterpret_cast<const float*>(smem);
+    const int64_t rows = (int64_t)a.B * a.Hq * a.Tq;
+    for (int e = tid; e < 16 * NQ * (DH / 8); e += 64 * kWaves) {
+        const int lr = e / (DH / 8), d0 = e % (DH / 8) * 8, r = r0 + lr;
+        if (r >= R) continue;
+        const int i = a.gd.div(r);
+        const int64_t row = qrow_index(a, b, hk, r, i);
+        float M = -__builtin_inff(), S = 0.f, x[8] = {};
+        if (r < rn) {
+            float ml[kWaves][2];
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) {
+                const float* p = base + w * 16 * NQ * (DH + 2) + 16 * NQ * DH + 2 * lr;
+                ml[w][0] = p[0], ml[w][1] = p[1];
+                M = fmaxf(M, ml[w][0]);
+            }
+            const float mu = M == -__builtin_inff() ? 0.f : M;
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) {
+                const float f = __builtin_amdgcn_exp2f(ml[w][0] - mu);
+                S += ml[w][1] * f;
+                const float* p = base + w * 16 * NQ * (DH + 2) + lr * DH + d0;
+#pragma unroll
+                for (int n = 0; n < 8; ++n) x[n] += f == 0.f ? 0.f : p[n] * f;
+            }
+        }
+        if (G.parts > 1) {
+            float* to = part.o + (pt * rows + row) * DH + d0;
+            reinterpret_cast<float4*>(to)[0] = make_float4(x[0], x[1], x[2], x[3]);
+            reinterpret_cast<float4*>(to)[1] = make_float4(x[4], x[5], x[6], x[7]);
+            if (d0 == 0) *reinterpret_cast<float2*>(part.ml + (pt * rows + row) * 2) = make_float2(M, S);
+        } else {
+            const float f = S > 0.f ? 1.f / S : S == 0.f ? 0.f : S;
+#pragma unroll
+            for (int n = 0; n < 8; ++n) x[n] *= f;
+            ST* to = qrow_ptr<ST>(a, a.out, b, hk, r, i) + d0;
+            if constexpr (SPLIT == 1) {
+                *reinterpret_cast<uint4*>(to) = __builtin_bit_cast(uint4, frag8_from<uint16_t>(x).v);
+            } else {
+                reinterpret_cast<float4*>(to)[0] = make_float4(x[0], x[1], x[2], x[3]);
+                reinterpret_cast<float4*>(to)[1] = make_float4(x[4], x[5], x[6], x[7]);
+            }
+            if (a.lse && d0 == 0) a.lse[row] = S == 0.f ? -__builtin_inff() : M * kLn2 + logf(S);
+        }
+    }
+}
+
+// 32 rows per block share what is expanded of a tile, where there are more than
+// 16 and the registers hold them (not with 128-wide heads or fp32's three parts).
+int rows_per_block(int dtype, int dh, const AttnArgs& a) {
+    return dtype == kBF16 && dh <= 64 && (int64_t)a.Tq * a.G > 16 ? 32 : 16;
+}
+
+CacheGeom cache_geom(int dtype, int dh, const AttnArgs& a) {
+    CacheGeom G{};
+    const int rb = rows_per_block(dtype, dh, a);
+    const int64_t R = (int64_t)a.Tq * a.G;
+    G.nb = (int)((R + rb - 1) / rb);
+    // Parts until there are about four workgroups for each that the chip holds,
+    // so that sequences of different lengths even out; a part keeps at least 512
+    // positions (4 tiles per wave), or 128 where even then CUs are left idle.
+    const int64_t blocks = (int64_t)G.nb * a.B * a.Hkv;
+    const int64_t span = a.W ? (int64_t)a.W + a.S + rb / a.G + 16 : a.N;
+    const int64_t tiles = ((span < a.N ? span : a.N) + 31) / 32;
+    int64_t parts = blocks >= 2048 ? 1 : (2048 + blocks - 1) / blocks;
+    const int64_t most = blocks * (tiles / 16) >= 512 ? tiles / 16 : tiles / 4;
+    if (parts > most) parts = most;
+    G.parts = parts < 1 ? 1 : (int)parts;
+    return G;
+}
+
+template <typename ST, int DH, int NQ>
+int launch_attn(const AttnArgs& a, const CacheArgs& c, const CacheGeom& G, float* buf, hipStream_t stream) {
+    constexpr int SPLIT = sizeof(ST) == 2 ? 1 : 3;
+    const size_t w = (size_t)kWaves * NQ * AttnLds<DH, SPLIT>::PW, o = (size_t)kWaves * 16 * NQ * (DH + 2) * 4;
+    const size_t lds = w > o ? w : o;
+    auto kern = cache4_attn_kernel<ST, DH, NQ>;
+    if (allow_lds((const void*)kern, lds)) return -1;
+    const Parts part = make_parts(buf, G.parts, (int64_t)a.B * a.Hq * a.Tq, DH);
+    return launch_parts((uint64_t)G.nb * a.B * a.Hkv * G.parts, 64 * kWaves, [&](uint32_t first, uint32_t blocks) {
+        hipLaunchKernelGGL(kern, dim3(blocks), dim3(64 * kWaves), lds, stream, a, c, G, part, first);
+        return hipGetLastError() == hipSuccess ? 0 : -1;
+    });
+}
+
+}  // namespace
+
+size_t cache4_attn_scratch(int dtype, int dh, const AttnArgs& a) {
+    return parts_bytes(cache_geom(dtype, dh, a).parts, (int64_t)a.B * a.Hq * a.Tq, dh);
+}
+
+int launch_cache4_attn(int dtype, const AttnArgs& a, const CacheArgs& c, float* buf, hipStream_t stream) {
+    CacheGeom G = cache_geom(dtype, c.dh, a);
+    G.page = make_udiv((uint32_t)c.ps);
+    const int e = heads_by_type(dtype, c.dh, [&](auto st, auto d) {
+        using ST = decltype(st);
+        constexpr int DH = decltype(d)::value;
+        if constexpr (sizeof(ST) == 2 && DH <= 64)
+            if (rows_per_block(dtype, DH, a) == 32) return launch_attn<ST, DH, 2>(a, c, G, buf, stream);
+        return launch_attn<ST, DH, 1>(a, c, G, buf, stream);
+    });
+    if (e || G.parts == 1) return e;
+    return launch_merge_parts(dtype, c.dh, a, G.parts, make_parts(buf, G.parts, (int64_t)a.B * a.Hq * a.Tq, c.dh), stream);
+}
+
+}  // namespace mosa

@@ -110,13 +110,6 @@ __device__ __forceinline__ bool finite4(const f32x4 (&x)[N]) {
     return t == 0.f;
 }
 
-// LDS written by lanes of this wave is seen by its other lanes.
-__device__ __forceinline__ void wave_sync() {
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-}
-
 // Rows of 16 N results (column c16 of block n, values 4 g + i of every 16)
 // through this wave's part of LDS to 16-byte stores: to(row) is the row's
 // address or nullptr.
