@@ -29,6 +29,7 @@ constexpr int kGroupTokens = 8;  // most tokens of a group (LDS: 8 * 64 pairs = 
 // Workgroups of the backward: each leaves one fp32 partial of dwq and dwk.
 // Four per CU keep 32 KB of loads per CU in flight.
 constexpr int kBwdBlocks = 1024;
+constexpr int kFwdBlocks = 2048;
 
 template <typename ST, int DH>
 struct NormGeom {
@@ -161,60 +162,61 @@ __device__ __forceinline__ void load_group(const NormArgs& a, GroupLds& g, int64
 }
 
 template <typename ST, int DH>
-__global__ __launch_bounds__(256) void qk_norm_kernel(NormArgs a, int TB, FastDiv heads) {
+__global__ __launch_bounds__(256) void qk_norm_kernel(NormArgs a, int TB, FastDiv hq, FastDiv hk) {
     using G = NormGeom<ST, DH>;
-    constexpr int E = G::E, U = 4;
+    constexpr int E = G::E, U = 2;
     __shared__ GroupLds lds;
     const int lane = threadIdx.x & 63, slot = threadIdx.x / G::LPR;
     const Turn<ST, DH> turn(a, lane);
-    float w[2][E], wp[2][E];  // weights of this lane's columns and of its partner's, q and k
-    const int cp = turn.c0 + (turn.partner - lane) * E;
-    load_weight<ST, E>(a.wq, turn.c0, w[0]);
-    load_weight<ST, E>(a.wk, turn.c0, w[1]);
-    load_weight<ST, E>(a.wq, cp, wp[0]);
-    load_weight<ST, E>(a.wk, cp, wp[1]);
+    const int cp = turn.c0 + (turn.partner - lane) * E;  // the partner's columns
     const int64_t total = (int64_t)a.B * a.T;
     for (int64_t tok0 = (int64_t)blockIdx.x * TB; tok0 < total; tok0 += (int64_t)gridDim.x * TB) {
-        const int nt = (int)min((int64_t)TB, total - tok0), R = nt * heads.n;
+        const int nt = (int)min((int64_t)TB, total - tok0);
         __syncthreads();
         load_group(a, lds, tok0, nt);
         __syncthreads();
-        for (int r0 = slot; r0 < R; r0 += U * G::RP) {
-            Chunk<ST> x[U];
-            ST* to[U];
-            int tl[U], isk[U];
+        static_for<0, 2>([&](auto kc) {
+            constexpr int K = decltype(kc)::value;
+            const Rows &in = K ? a.k : a.q, &out = K ? a.ko : a.qo;
+            const FastDiv& heads = K ? hk : hq;
+            const int R = nt * heads.n;
+            float w[E], wp[E];
+            load_weight<ST, E>(K ? a.wk : a.wq, turn.c0, w);
+            load_weight<ST, E>(K ? a.wk : a.wq, cp, wp);
+            for (int r0 = slot; r0 < R; r0 += U * G::RP) {
+                Chunk<ST> x[U];
+                ST* to[U];
+                int tl[U];
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                int h;
-                fast_divmod(heads, min(r0 + u * G::RP, R - 1), tl[u], h);
-                isk[u] = h >= a.Hq;
-                const Rows& in = isk[u] ? a.k : a.q;
-                const Rows& out = isk[u] ? a.ko : a.qo;
-                const int hh = isk[u] ? h - a.Hq : h, b = lds.b[tl[u]], t = lds.t[tl[u]];
-                x[u].u = *reinterpret_cast<const uint4*>(row_ptr<ST>(in, b, hh, t) + turn.c0);
-                to[u] = row_ptr<ST>(out, b, hh, t) + turn.c0;
-            }
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                float v[E], o[E];
-                x[u].get(v);
-                float ss = 0.f;
-#pragma unroll
-                for (int e = 0; e < E; ++e) ss += v[e] * v[e];
-                const float s = rsqrtf(lanes_sum<G::LPR>(ss) * (1.f / DH) + a.eps);
-#pragma unroll
-                for (int e = 0; e < E; ++e) v[e] = v[e] * s * (isk[u] ? w[1][e] : w[0][e]);
-                if (a.halves) {
-                    partner_chunk<ST, DH>(x[u], turn).get(o);
-#pragma unroll
-                    for (int e = 0; e < E; ++e) o[e] = o[e] * s * (isk[u] ? wp[1][e] : wp[0][e]);
+                for (int u = 0; u < U; ++u) {
+                    int h;
+                    fast_divmod(heads, min(r0 + u * G::RP, R - 1), tl[u], h);
+                    const int b = lds.b[tl[u]], t = lds.t[tl[u]];
+                    x[u].u = *reinterpret_cast<const uint4*>(row_ptr<ST>(in, b, h, t) + turn.c0);
+                    to[u] = row_ptr<ST>(out, b, h, t) + turn.c0;
                 }
-                turn_row<ST, DH>(a, turn, v, o, lds.cs + tl[u] * (a.rope / 2), 1.f);
-                Chunk<ST> y;
-                y.set(v);
-                if (r0 + u * G::RP < R) *reinterpret_cast<uint4*>(to[u]) = y.u;
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    float v[E], o[E];
+                    x[u].get(v);
+                    float ss = 0.f;
+#pragma unroll
+                    for (int e = 0; e < E; ++e) ss += v[e] * v[e];
+                    const float s = rsqrtf(lanes_sum<G::LPR>(ss) * (1.f / DH) + a.eps);
+#pragma unroll
+                    for (int e = 0; e < E; ++e) v[e] = v[e] * s * w[e];
+                    if (a.halves) {
+                        partner_chunk<ST, DH>(x[u], turn).get(o);
+#pragma unroll
+                        for (int e = 0; e < E; ++e) o[e] = o[e] * s * wp[e];
+                    }
+                    turn_row<ST, DH>(a, turn, v, o, lds.cs + tl[u] * (a.rope / 2), 1.f);
+                    Chunk<ST> y;
+                    y.set(v);
+                    if (r0 + u * G::RP < R) *reinterpret_cast<uint4*>(to[u]) = y.u;
+                }
             }
-        }
+        });
     }
 }
 
@@ -332,10 +334,10 @@ int group_tokens(int64_t total, int heads, int rows_per_pass, int unroll) {
 template <typename ST, int DH>
 int norm_t(const NormArgs& a, hipStream_t stream) {
     const int64_t total = (int64_t)a.B * a.T;
-    const int heads = a.Hq + a.Hkv, tb = group_tokens(total, heads, NormGeom<ST, DH>::RP, 4);
+    const int tb = group_tokens(total, a.Hkv, NormGeom<ST, DH>::RP, 2);
     const int64_t groups = (total + tb - 1) / tb;
-    hipLaunchKernelGGL((qk_norm_kernel<ST, DH>), dim3((unsigned)(groups < (1 << 20) ? groups : 1 << 20)), dim3(256), 0,
-                       stream, a, tb, make_fastdiv(heads));
+    hipLaunchKernelGGL((qk_norm_kernel<ST, DH>), dim3((unsigned)(groups < kFwdBlocks ? groups : kFwdBlocks)), dim3(256),
+                       0, stream, a, tb, make_fastdiv(a.Hq), make_fastdiv(a.Hkv));
     return hipGetLastError() == hipSuccess ? 0 : -1;
 }
 

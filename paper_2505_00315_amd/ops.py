@@ -14,6 +14,7 @@ current.
 """
 import contextlib
 import ctypes
+import functools
 import math
 
 import torch
@@ -70,6 +71,11 @@ def _lib():
             f.argtypes, f.restype = args, ctypes.c_int
         _fn = L
     return _fn
+
+
+@functools.lru_cache(maxsize=None)
+def _function(name):
+    return getattr(_lib(), name)
 
 
 _DTYPE = {"bf16": mosa.MOSA_BF16, "f32": mosa.MOSA_F32, torch.bfloat16: mosa.MOSA_BF16, torch.float32: mosa.MOSA_F32}
@@ -136,22 +142,23 @@ def _like(t, given, stream):
         return torch.empty_like(t)
 
 
-def _scratch(t, need, device, stream):
-    if need == 0:
-        return None, 0
+def _scratch(t, size, device, stream):
+    """(tensor, address, bytes) of a call's scratch: the given buffer, whose size the library checks, or a new one of
+    size() bytes."""
     if t is None:
+        need = size()
+        if need == 0:
+            return None, None, 0
         with _on(stream):
             t = torch.empty(need, dtype=torch.uint8, device=device)
-    if t.dtype != torch.uint8 or not t.is_contiguous() or t.device != device:
+    elif t.dtype != torch.uint8 or not t.is_contiguous() or t.device != device:
         raise ValueError(f"scratch: a contiguous uint8 tensor on {device} is required")
-    if t.numel() < need:
-        raise ValueError(f"scratch: {t.numel()} bytes, at least {need} required")
-    return t, t.numel()
+    return t, t.data_ptr(), t.numel()
 
 
 def _call(name, device, stream, *args):
     """Call a library function on ``device``, whichever is current; the stream is its last argument."""
-    f = getattr(_lib(), name)
+    f = _function(name)
     if stream is None:
         stream = torch.cuda.current_stream(device)
     elif stream.device != device:
@@ -161,7 +168,8 @@ def _call(name, device, stream, *args):
     else:
         with torch.cuda.device(device):
             status = f(*args, stream.cuda_stream)
-    mosa._check(status, name)
+    if status:
+        mosa._check(status, name)
 
 
 # ---------------------------------------------------------------------------
@@ -209,14 +217,14 @@ def qk_norm_rope_backward(shape, q, k, wq, wk, dq_out, dk_out, positions=None, d
     dk = _like(k, dk, stream)
     dwq = dwq if wq is None else _like(wq, dwq, stream)
     dwk = dwk if wk is None else _like(wk, dwk, stream)
-    need = norm_scratch_size(shape) if dwq is not None or dwk is not None else 0
-    buf, size = _scratch(scratch, need, dev, stream)
+    grads = dwq is not None or dwk is not None
+    buf, at, size = _scratch(scratch, lambda: norm_scratch_size(shape) if grads else 0, dev, stream)
     _call("mosa_qk_norm_rope_backward", dev, stream, shape, _rows(q, "q", qs, st, dev), _rows(k, "k", ks, st, dev),
           _array(wq, "wq", st, shape.d_head, dev), _array(wk, "wk", st, shape.d_head, dev),
           _array(positions, "positions", torch.int32, shape.batch * shape.seq_len, dev),
           _rows(dq_out, "dq_out", qs, st, dev), _rows(dk_out, "dk_out", ks, st, dev), _rows(dq, "dq", qs, st, dev),
           _rows(dk, "dk", ks, st, dev), _array(dwq, "dwq", st, shape.d_head, dev),
-          _array(dwk, "dwk", st, shape.d_head, dev), None if buf is None else buf.data_ptr(), size)
+          _array(dwk, "dwk", st, shape.d_head, dev), at, size)
     return dq, dk, dwq, dwk
 
 
@@ -251,11 +259,11 @@ def window_attention(shape, q, k, v, q_lens=None, kv_lens=None, out=None, lse=No
     if lse is None:
         with _on(stream):
             lse = torch.empty(qs[:3], dtype=torch.float32, device=dev)
-    buf, size = _scratch(scratch, attn_scratch_size(shape)[0], dev, stream)
+    buf, at, size = _scratch(scratch, lambda: attn_scratch_size(shape)[0], dev, stream)
     _call("mosa_window_attention", dev, stream, shape, _rows(q, "q", qs, st, dev), _rows(k, "k", ks, st, dev),
           _rows(v, "v", ks, st, dev), _array(q_lens, "q_lens", torch.int32, shape.batch, dev),
           _array(kv_lens, "kv_lens", torch.int32, shape.batch, dev), _rows(out, "out", qs, st, dev),
-          _array(lse, "lse", torch.float32, qs[0] * qs[1] * qs[2], dev), None if buf is None else buf.data_ptr(), size)
+          _array(lse, "lse", torch.float32, qs[0] * qs[1] * qs[2], dev), at, size)
     return out, lse
 
 
@@ -268,13 +276,13 @@ def window_attention_backward(shape, q, k, v, out, lse, d_out, q_lens=None, kv_l
     dq = _like(q, dq, stream)
     dk = _like(k, dk, stream)
     dv = _like(v, dv, stream)
-    buf, size = _scratch(scratch, attn_scratch_size(shape)[1], dev, stream)
+    buf, at, size = _scratch(scratch, lambda: attn_scratch_size(shape)[1], dev, stream)
     _call("mosa_window_attention_backward", dev, stream, shape, _rows(q, "q", qs, st, dev),
           _rows(k, "k", ks, st, dev), _rows(v, "v", ks, st, dev), _rows(out, "out", qs, st, dev),
           _array(lse, "lse", torch.float32, qs[0] * qs[1] * qs[2], dev, required=True),
           _rows(d_out, "d_out", qs, st, dev), _array(q_lens, "q_lens", torch.int32, shape.batch, dev),
           _array(kv_lens, "kv_lens", torch.int32, shape.batch, dev), _rows(dq, "dq", qs, st, dev),
-          _rows(dk, "dk", ks, st, dev), _rows(dv, "dv", ks, st, dev), None if buf is None else buf.data_ptr(), size)
+          _rows(dk, "dk", ks, st, dev), _rows(dv, "dv", ks, st, dev), at, size)
     return dq, dk, dv
 
 
@@ -287,13 +295,18 @@ def cache4_size(shape):
     return n.value
 
 
+@functools.lru_cache(maxsize=64)
+def _cache_bytes(fields):
+    return cache4_size(CacheShape.from_buffer_copy(fields))
+
+
 def alloc_cache4(shape, device="cuda"):
     """The cache's memory (uint8).  Positions that were never written hold zeros."""
     return torch.zeros(cache4_size(shape), dtype=torch.uint8, device=device)
 
 
 def _cache(shape, cache, table, device):
-    need = cache4_size(shape)
+    need = _cache_bytes(bytes(shape))
     if cache.dtype != torch.uint8 or not cache.is_contiguous() or cache.device != device or cache.numel() < need:
         raise ValueError(f"cache: a contiguous uint8 tensor on {device} of at least {need} bytes is required")
     return cache.data_ptr(), _array(table, "page_table", torch.int32, shape.batch * shape.max_pages, device, True)
@@ -340,9 +353,9 @@ def cache4_attention(shape, cache_shape, q, cache, page_table, kv_lens, q_lens=N
     dev = _device(q, "q")
     out = _like(q, out, stream)
     where, pages = _cache(cache_shape, cache, page_table, dev)
-    buf, size = _scratch(scratch, attn_scratch_size(shape)[0], dev, stream)
+    buf, at, size = _scratch(scratch, lambda: attn_scratch_size(shape)[0], dev, stream)
     _call("mosa_cache4_attention", dev, stream, shape, cache_shape, _rows(q, "q", qs, st, dev), where, pages,
           _array(q_lens, "q_lens", torch.int32, shape.batch, dev),
           _array(kv_lens, "kv_lens", torch.int32, shape.batch, dev, True), _rows(out, "out", qs, st, dev),
-          _array(lse, "lse", torch.float32, qs[0] * qs[1] * qs[2], dev), None if buf is None else buf.data_ptr(), size)
+          _array(lse, "lse", torch.float32, qs[0] * qs[1] * qs[2], dev), at, size)
     return out
