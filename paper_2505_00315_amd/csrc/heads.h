@@ -130,16 +130,12 @@ inline size_t parts_bytes(int parts, int64_t rows, int dh) {
 inline Parts make_parts(float* buf, int parts, int64_t rows, int dh) {
     return {buf, buf + (size_t)parts * (size_t)rows * (size_t)dh};
 }
-size_t wattn_tiled_scratch(int dh, const AttnArgs& a);  // bf16
-int launch_wattn_tiled(int dh, const AttnArgs& a, float* part, hipStream_t stream);
 int launch_merge_parts(int dtype, int dh, const AttnArgs& a, int parts, const Parts& p, hipStream_t stream);
 
 size_t attn_fwd_scratch(int dtype, int dh, const AttnArgs& a);
 size_t attn_bwd_scratch(int dtype, int dh, const AttnArgs& a);
 int launch_window_attn(int dtype, int dh, const AttnArgs& a, float* part, hipStream_t stream);
 int launch_window_attn_bwd(int dtype, int dh, AttnArgs a, void* scratch, hipStream_t stream);
-int launch_wattn_bwd_tiled(int dh, const AttnArgs& a, float* sums, hipStream_t stream);  // bf16
-size_t wattn_bwd_sums(int dh, const AttnArgs& a);
 
 // ---------------------------------------------------------------------------
 // the 4-bit cache

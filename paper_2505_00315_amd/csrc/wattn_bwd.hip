@@ -1,5 +1,5 @@
 // Causal attention with a sliding window and first tokens that stay visible:
-// the backward over rows in bf16.
+// the backward over rows.
 //
 //   p = 2^(s c - lse'),  dp = dout v,  ds = p (dp - D)
 //   dv = sum p dout,  dk = scale sum ds q,  dq = scale sum ds k
@@ -7,7 +7,7 @@
 // Two kinds of workgroups in one launch, neither with atomics: one owns 64 CB
 // keys of a key head and walks the rows that see them (the group's heads are
 // in the row list, so their sum is the loop's), one owns 64 QN rows and walks
-// the keys that they see.  Both form s and dp again from tiles of 64 that come
+// the keys that they see.  Both form s and dp again from tiles of 64 (fp32: 32) that come
 // through an LDS ring: 7 products in place of the 5 that one pass with atomic
 // sums would take, for results that do not depend on the order of workgroups.
 // The other operand stays in registers, and p and ds are fed to the second
@@ -42,40 +42,39 @@ struct BwdGeom {
 // Tiles of a key head's rows: q, dout and (lse, D).  A tile is 64 / G queries of
 // the group's G heads (its last 64 % G rows are none), or 64 rows where G is
 // larger, so that the lanes' offsets are the same for every tile.
-template <int DH>
+template <typename ST, int DH>
 struct RowTiles {
-    using TL = TileLoad<DH>;
+    using TL = TileLoad<ST, DH>;
+    static constexpr int TB = TL::TB, ES = (int)sizeof(ST), LL = TB / 32;  // loads of (lse, D), a word per lane
     const AttnArgs& a;
-    int b, hk, nq, nr;  // queries and rows per tile (nq = 0: G > 64)
+    int b, hk, nr;  // rows per tile
     bool near;
-    uint32_t qoff[TL::LD], goff[TL::LD], loff[2];
+    uint32_t qoff[TL::LD], goff[TL::LD], loff[LL];
     __device__ __forceinline__ RowTiles(const AttnArgs& a, int b, int hk, const TL& tl, int lane) : a(a), b(b), hk(hk) {
-        nq = 64 / a.G;
-        nr = nq ? nq * a.G : kTB;
-        // 64 rows of G heads within 2^31 bytes
+        const int nq = TB / a.G;  // queries per tile
+        nr = nq ? nq * a.G : TB;
+        // a tile's rows of G heads within 2^31 bytes
         near = nq > 0 && fits(a.q) && fits(a.dout) && (int64_t)a.G * a.Tq < ((int64_t)1 << 27);
 #pragma unroll
         for (int j = 0; j < TL::LD; ++j) {
             const int r = tl.row + TL::STEP * j, i = a.gd.div(r), g = r - i * a.G;
-            qoff[j] = (uint32_t)((g * a.q.head + i * a.q.row + tl.col) * 2);
-            goff[j] = (uint32_t)((g * a.dout.head + i * a.dout.row + tl.col) * 2);
+            qoff[j] = (uint32_t)((g * a.q.head + i * a.q.row + tl.col) * ES);
+            goff[j] = (uint32_t)((g * a.dout.head + i * a.dout.row + tl.col) * ES);
         }
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
+        for (int j = 0; j < LL; ++j) {
             const int r = 32 * j + (lane >> 1), i = a.gd.div(r), g = r - i * a.G;
             loff[j] = (uint32_t)(((int64_t)g * a.Tq + i) * 8 + 4 * (lane & 1));
         }
     }
-    __device__ __forceinline__ bool fits(const Rows& t) const {
-        return a.G * t.head + kTB * t.row < ((int64_t)1 << 30);
-    }
+    __device__ __forceinline__ bool fits(const Rows& t) const { return a.G * t.head + TB * t.row < ((int64_t)1 << 29); }
     // The tile from row r0 on (of rows below rhi; those past it are the last one), to LDS byte `at`:
     // q, dout, and for this wave alone (lse, D) of every row.
     __device__ __forceinline__ void issue(const TL& tl, int r0, int rhi, uint32_t at, uint32_t ld_at, int lane) const {
-        if (near && r0 + kTB <= rhi) {
+        if (near && r0 + TB <= rhi) {
             const int i0 = a.gd.div(r0);
-            const char* q = uniform_ptr(reinterpret_cast<const char*>(row_ptr<uint16_t>(a.q, b, hk * a.G, i0)));
-            const char* g = uniform_ptr(reinterpret_cast<const char*>(row_ptr<uint16_t>(a.dout, b, hk * a.G, i0)));
+            const char* q = uniform_ptr(reinterpret_cast<const char*>(row_ptr<ST>(a.q, b, hk * a.G, i0)));
+            const char* g = uniform_ptr(reinterpret_cast<const char*>(row_ptr<ST>(a.dout, b, hk * a.G, i0)));
             const char* l = uniform_ptr(reinterpret_cast<const char*>(a.ld + ((int64_t)b * a.Hq + hk * a.G) * a.Tq + i0));
 #pragma unroll
             for (int j = 0; j < TL::LD; ++j) {
@@ -83,17 +82,17 @@ struct RowTiles {
                 lds_load16s(goff[j], g, at + TL::BYTES + tl.lds + 4096 * j);
             }
 #pragma unroll
-            for (int j = 0; j < 2; ++j) lds_load4s(loff[j], l, ld_at + 256 * j);
+            for (int j = 0; j < LL; ++j) lds_load4s(loff[j], l, ld_at + 256 * j);
             return;
         }
 #pragma unroll
         for (int j = 0; j < TL::LD; ++j) {
             const int r = min(r0 + tl.row + TL::STEP * j, rhi - 1), i = a.gd.div(r);
-            lds_load16(qrow_ptr<uint16_t>(a, a.q, b, hk, r, i) + tl.col, at + tl.lds + 4096 * j);
-            lds_load16(qrow_ptr<uint16_t>(a, a.dout, b, hk, r, i) + tl.col, at + TL::BYTES + tl.lds + 4096 * j);
+            lds_load16(qrow_ptr<ST>(a, a.q, b, hk, r, i) + tl.col, at + tl.lds + 4096 * j);
+            lds_load16(qrow_ptr<ST>(a, a.dout, b, hk, r, i) + tl.col, at + TL::BYTES + tl.lds + 4096 * j);
         }
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
+        for (int j = 0; j < LL; ++j) {
             const int r = min(r0 + 32 * j + (lane >> 1), rhi - 1), i = a.gd.div(r);
             lds_load4(reinterpret_cast<const float*>(a.ld + qrow_index(a, b, hk, r, i)) + (lane & 1), ld_at + 256 * j);
         }
@@ -110,38 +109,14 @@ __device__ __forceinline__ bool finite4(const f32x4 (&x)[N]) {
     return t == 0.f;
 }
 
-// Rows of 16 N results (column c16 of block n, values 4 g + i of every 16)
-// through this wave's part of LDS to 16-byte stores: to(row) is the row's
-// address or nullptr.
-template <int DH, int N, class TO>
-__device__ __forceinline__ void store_rows(unsigned char* lds, const f32x4 (&x)[N][DH / 16], float f, int lane, const TO& to) {
-    using ST = uint16_t;
-    constexpr int LDO = DH + 8, U = DH / 8;
-    ST* o = reinterpret_cast<ST*>(lds);
-    const int g = lane >> 4, c16 = lane & 15;
-#pragma unroll
-    for (int n = 0; n < N; ++n)
-#pragma unroll
-        for (int db = 0; db < DH / 16; ++db)
-            *reinterpret_cast<uint2*>(o + (16 * n + c16) * LDO + 16 * db + 4 * g) =
-                make_uint2(pack_bf16x2(x[n][db][0] * f, x[n][db][1] * f), pack_bf16x2(x[n][db][2] * f, x[n][db][3] * f));
-    wave_sync();
-#pragma unroll
-    for (int e = lane; e < 16 * N * U; e += 64) {
-        const int r = e / U, dc = (e % U) * 8;
-        if (ST* p = to(r)) *reinterpret_cast<uint4*>(p + dc) = *reinterpret_cast<const uint4*>(o + r * LDO + dc);
-    }
-    wave_sync();
-}
-
 // Keys k0 .. of (b, hk), 16 CB per wave.  far (chunk >= 0): the pairs beyond the
 // window of sinks, rows of one chunk, sums to `sums`.
-template <int DH, int CB>
+template <typename ST, int DH, int CB>
 __device__ __forceinline__ void dkv_body(unsigned char* smem, const AttnArgs& a, const BwdGeom& G, int b, int hk, int k0,
                                          int chunk, float* sums) {
-    using ST = uint16_t;
-    constexpr int NS = DH / 32, ND = DH / 16, STG = kStages, LD = TileLoad<DH>::LD;
-    constexpr int TILE = TileLoad<DH>::BYTES, LDB = 4 * kTB * 8, STAGE = 2 * TILE + LDB;  // q, dout, a copy of (lse, D) per wave
+    using TL = TileLoad<ST, DH>;
+    constexpr int TB = TL::TB, NS = DH / 32, ND = DH / 16, STG = kStages, LD = TL::LD;
+    constexpr int TILE = TL::BYTES, LDB = 4 * TB * 8, STAGE = 2 * TILE + LDB;  // q, dout, a copy of (lse, D) per wave
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, c16 = lane & 15;
     const bool far = chunk >= 0, apart = G.ns > 0;  // apart: far pairs are done by chunks
     const int qn = seq_len_of(a.ql, b, a.Tq), kn = seq_len_of(a.kl, b, a.N), off = kn - qn;
@@ -155,8 +130,8 @@ __device__ __forceinline__ void dkv_body(unsigned char* smem, const AttnArgs& a,
         i1 = far || a.W == 0 || (!apart && k0 < a.S) ? qn : min(qn, kend - 1 + a.W - off);
     }
     const int rlo = i0 * a.G, rhi = max(i1, i0) * a.G;
-    const TileLoad<DH> tl(wave, lane);
-    const RowTiles<DH> rows(a, b, hk, tl, lane);
+    const TL tl(wave, lane);
+    const RowTiles<ST, DH> rows(a, b, hk, tl, lane);
     const int nr = rows.nr, all = (rhi - rlo + nr - 1) / nr, share = far ? (all + G.nc - 1) / G.nc : all;
     const int tbeg = far ? min(chunk * share, all) : 0, ntile = min(all, tbeg + share) - tbeg;
 
@@ -181,35 +156,35 @@ __device__ __forceinline__ void dkv_body(unsigned char* smem, const AttnArgs& a,
 #pragma unroll
         for (int cb = 0; cb < CB; ++cb)
 #pragma unroll
-            for (int st = 0; st < NS; ++st) asm volatile("" : "+v"(kf[cb][st].v), "+v"(vf[cb][st].v));
+            for (int st = 0; st < NS; ++st) take(kf[cb][st]), take(vf[cb][st]);
 
-        const TileReads<DH> rd(g, c16);
+        const TileReads<ST, DH> rd(g, c16);
         const uint32_t base = __builtin_amdgcn_readfirstlane(lds_addr(smem));
         // tile t (past the end: the last one again, into a buffer that nobody reads)
         auto issue = [&](int t, int buf) {
             const uint32_t at = base + buf * STAGE;
-            rows.issue(tl, rlo + nr * (tbeg + min(t, ntile - 1)), rhi, at, at + 2 * TILE + tl.lds / 2, lane);
+            rows.issue(tl, rlo + nr * (tbeg + min(t, ntile - 1)), rhi, at, at + 2 * TILE + 8 * TB * (tl.lds / 1024), lane);
         };
         const float c2 = a.scale * kLog2e;
 #pragma unroll
         for (int s = 0; s < STG - 1; ++s) issue(s, s);
         auto tile_step = [&](int it, auto bufc) {
             constexpr int BUF = decltype(bufc)::value;
-            wait_vmcnt<(STG - 2) * (2 * LD + 2)>();
+            wait_vmcnt<(STG - 2) * (2 * LD + RowTiles<ST, DH>::LL)>();
             __syncthreads();
             issue(it + STG - 1, (BUF + STG - 1) % STG);
             const unsigned char* Qt = smem + BUF * STAGE;
             const unsigned char* Gt = Qt + TILE;
-            const unsigned char* Lt = Gt + TILE + 512 * wave;
+            const unsigned char* Lt = Gt + TILE + 8 * TB * wave;
             const int r0 = rlo + nr * (tbeg + it), rt = min(r0 + nr, rhi);  // the tile's rows
             const int pt0 = off + a.gd.div(r0), pt1 = off + a.gd.div(rt - 1);  // and their positions
             // nothing for this wave: no keys, rows before the keys, or past their window
             if (wk1 < wk0) return;
             if (far ? wk0 >= a.S || pt1 - wk0 < a.W : pt1 < wk0 || (a.W && pt0 - wk1 >= a.W && (apart || wk0 >= a.S))) return;
-            const bool whole = r0 + kTB == rt &&
+            const bool whole = r0 + TB == rt &&
                                (far ? pt0 - wk1 >= a.W : pt0 >= wk1 && (a.W == 0 || pt1 - wk0 < a.W));
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {  // 32 rows at a time
+            for (int u = 0; u < TB / 32; ++u) {  // 32 rows at a time
                 f32x4 s[CB][2], dp[CB][2];
 #pragma unroll
                 for (int x = 0; x < 2; ++x) {
@@ -250,13 +225,13 @@ __device__ __forceinline__ void dkv_body(unsigned char* smem, const AttnArgs& a,
                         }
                     }
                 }
-                // dv^T += dout^T p, dk^T += q^T ds: p and ds are rounded to bf16,
-                // the type of the matrix operands
+                // dv^T += dout^T p, dk^T += q^T ds: with bf16 storage p and ds are
+                // rounded to it, the type of the matrix operands
                 Frag8<ST> pf[CB], df[CB];
 #pragma unroll
                 for (int cb = 0; cb < CB; ++cb) {
-                    pf[cb] = pack_frag(s[cb][0], s[cb][1]);
-                    df[cb] = pack_frag(dp[cb][0], dp[cb][1]);
+                    pf[cb] = pack_frag<ST>(s[cb][0], s[cb][1]);
+                    df[cb] = pack_frag<ST>(dp[cb][0], dp[cb][1]);
                 }
 #pragma unroll
                 for (int db = 0; db < ND; ++db) {
@@ -340,27 +315,30 @@ __device__ __forceinline__ void dkv_body(unsigned char* smem, const AttnArgs& a,
         if (wk0 + 16 * cb + c16 > wk1)
 #pragma unroll
             for (int db = 0; db < ND; ++db) dk[cb][db] = dv[cb][db] = zero4();
-    unsigned char* mine = smem + wave * 16 * CB * (DH + 8) * 2;
+    unsigned char* mine = smem + wave * store_rows_bytes<ST, DH>(CB);
+    float fk[CB], fv[CB];
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb) fk[cb] = a.scale, fv[cb] = 1.f;
     auto key_at = [&](const Rows& t, int r) {
         const int j = wk0 + r;
         return j < top && !(apart && j < a.S) ? row_ptr<ST>(t, b, hk, j) : nullptr;
     };
-    store_rows<DH, CB>(mine, dk, a.scale, lane, [&](int r) { return key_at(a.dk, r); });
-    store_rows<DH, CB>(mine, dv, 1.f, lane, [&](int r) { return key_at(a.dv, r); });
+    store_rows<ST, DH, CB>(mine, dk, fk, lane, [&](int r) { return key_at(a.dk, r); });
+    store_rows<ST, DH, CB>(mine, dv, fv, lane, [&](int r) { return key_at(a.dv, r); });
 }
 
 // Rows r0 .. of (b, hk), 16 QN per wave.
-template <int DH, int QN>
+template <typename ST, int DH, int QN>
 __device__ __forceinline__ void dq_body(unsigned char* smem, const AttnArgs& a, int b, int hk, int r0) {
-    using ST = uint16_t;
-    constexpr int NS = DH / 32, ND = DH / 16, STG = kStages, LD = TileLoad<DH>::LD;
-    constexpr int TILE = TileLoad<DH>::BYTES, STAGE = 2 * TILE;
+    using TL = TileLoad<ST, DH>;
+    constexpr int TB = TL::TB, NS = DH / 32, ND = DH / 16, STG = kStages, LD = TL::LD;
+    constexpr int TILE = TL::BYTES, STAGE = 2 * TILE;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, c16 = lane & 15;
     const int qn = seq_len_of(a.ql, b, a.Tq), kn = seq_len_of(a.kl, b, a.N), off = kn - qn;
     const int R = a.Tq * a.G, rn = qn * a.G, wr0 = r0 + 16 * QN * wave;
     KeyList list{0, 0, 0};
     if (r0 < rn) list = keys_of(a, off + a.gd.div(r0), off + a.gd.div(min(r0 + 64 * QN, rn) - 1), kn);
-    const int ntile = (list.count + kTB - 1) / kTB;
+    const int ntile = (list.count + TB - 1) / TB;
 
     f32x4 dq[QN][ND];
 #pragma unroll
@@ -388,14 +366,14 @@ __device__ __forceinline__ void dq_body(unsigned char* smem, const AttnArgs& a, 
         for (int qs = 0; qs < QN; ++qs) {
             asm volatile("" : "+v"(ld[qs].x), "+v"(ld[qs].y));
 #pragma unroll
-            for (int st = 0; st < NS; ++st) asm volatile("" : "+v"(qf[qs][st].v), "+v"(gf[qs][st].v));
+            for (int st = 0; st < NS; ++st) take(qf[qs][st]), take(gf[qs][st]);
         }
-        const TileLoad<DH> tl(wave, lane);
-        const TileReads<DH> rd(g, c16);
-        const KeyTiles<DH> kt(a.k, b, hk, tl), vt(a.v, b, hk, tl);
+        const TL tl(wave, lane);
+        const TileReads<ST, DH> rd(g, c16);
+        const KeyTiles<ST, DH> kt(a.k, b, hk, tl), vt(a.v, b, hk, tl);
         const uint32_t base = __builtin_amdgcn_readfirstlane(lds_addr(smem));
         auto issue = [&](int t, int buf) {
-            const int e0 = kTB * min(t, ntile - 1);
+            const int e0 = TB * min(t, ntile - 1);
             kt.issue(tl, list, e0, base + buf * STAGE);
             vt.issue(tl, list, e0, base + buf * STAGE + TILE);
         };
@@ -409,12 +387,12 @@ __device__ __forceinline__ void dq_body(unsigned char* smem, const AttnArgs& a, 
             issue(it + STG - 1, (BUF + STG - 1) % STG);
             const unsigned char* Kt = smem + BUF * STAGE;
             const unsigned char* Vt = Kt + TILE;
-            const int e0 = kTB * it;
-            const int kmax = list.key(min(e0 + kTB, list.count) - 1), kmin = e0 >= list.s ? list.key(e0) : list.lo;
+            const int e0 = TB * it;
+            const int kmax = list.key(min(e0 + TB, list.count) - 1), kmin = e0 >= list.s ? list.key(e0) : list.lo;
             if (e0 >= list.s && (kmin > pw1 || (a.W && kmax <= pw0 - a.W && kmin >= a.S))) return;
-            const bool whole = e0 + kTB <= list.count && kmax <= pw0 && (a.W == 0 || kmin > pw1 - a.W);
+            const bool whole = e0 + TB <= list.count && kmax <= pw0 && (a.W == 0 || kmin > pw1 - a.W);
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {  // 32 keys at a time
+            for (int u = 0; u < TB / 32; ++u) {  // 32 keys at a time
                 f32x4 s[QN][2], dp[QN][2];
 #pragma unroll
                 for (int x = 0; x < 2; ++x) {
@@ -448,7 +426,7 @@ __device__ __forceinline__ void dq_body(unsigned char* smem, const AttnArgs& a, 
                 }
                 Frag8<ST> df[QN];
 #pragma unroll
-                for (int qs = 0; qs < QN; ++qs) df[qs] = pack_frag(dp[qs][0], dp[qs][1]);
+                for (int qs = 0; qs < QN; ++qs) df[qs] = pack_frag<ST>(dp[qs][0], dp[qs][1]);
 #pragma unroll
                 for (int db = 0; db < ND; ++db) {
                     const Frag8<ST> kf = rd.cols(Kt, u, db);
@@ -487,13 +465,16 @@ __device__ __forceinline__ void dq_body(unsigned char* smem, const AttnArgs& a, 
         if (wr0 + 16 * qs + c16 >= rn)
 #pragma unroll
             for (int db = 0; db < ND; ++db) dq[qs][db] = zero4();
-    store_rows<DH, QN>(smem + wave * 16 * QN * (DH + 8) * 2, dq, a.scale, lane, [&](int lr) -> ST* {
+    float fq[QN];
+#pragma unroll
+    for (int qs = 0; qs < QN; ++qs) fq[qs] = a.scale;
+    store_rows<ST, DH, QN>(smem + wave * store_rows_bytes<ST, DH>(QN), dq, fq, lane, [&](int lr) -> ST* {
         const int r = wr0 + lr;
         return r < R && !(redone && r < rn) ? qrow_ptr<ST>(a, a.dq, b, hk, r, a.gd.div(r)) : nullptr;
     });
 }
 
-template <int DH, int CB, int QN>
+template <typename ST, int DH, int CB, int QN>
 __global__ __launch_bounds__(256, 2) void wattn_bwd_kernel(AttnArgs a, BwdGeom G, float* __restrict__ sums, uint32_t first) {
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     // key blocks, then chunks of far rows, then row blocks; each kind in
@@ -504,21 +485,48 @@ __global__ __launch_bounds__(256, 2) void wattn_bwd_kernel(AttnArgs a, BwdGeom G
     if (id < n0) {
         if (one) id = xcd_logical_id(id, n0);
         const int bh = id / G.nk, kb = id % G.nk;
-        dkv_body<DH, CB>(smem, a, G, bh / a.Hkv, bh % a.Hkv, kb * 64 * CB, -1, sums);
+        dkv_body<ST, DH, CB>(smem, a, G, bh / a.Hkv, bh % a.Hkv, kb * 64 * CB, -1, sums);
     } else if (id < n0 + n1) {
         id -= n0;
         const int per = G.ns * G.nc, bh = id / per, k = id % per;
-        dkv_body<DH, 1>(smem, a, G, bh / a.Hkv, bh % a.Hkv, k / G.nc * 64, k % G.nc, sums);
+        dkv_body<ST, DH, 1>(smem, a, G, bh / a.Hkv, bh % a.Hkv, k / G.nc * 64, k % G.nc, sums);
     } else {
         id -= n0 + n1;
         if (one) id = xcd_logical_id(id, n2);
         const int bh = id / G.nq, q = id % G.nq;
-        dq_body<DH, QN>(smem, a, bh / a.Hkv, bh % a.Hkv, (a.W ? q : G.nq - 1 - q) * 64 * QN);
+        dq_body<ST, DH, QN>(smem, a, bh / a.Hkv, bh % a.Hkv, (a.W ? q : G.nq - 1 - q) * 64 * QN);
+    }
+}
+
+// (lse in log2 units, D = sum(out dout)) of every query row, 8 columns per lane:
+// what the backward's kernels read of a row beside q and dout.  Bound by the
+// rows of out and dout, which it reads once.
+template <typename ST, int DH>
+__global__ __launch_bounds__(256) void wattn_ld_kernel(AttnArgs a, uint32_t first) {
+    constexpr int L = DH / 8;
+    const int64_t row = ((int64_t)first + blockIdx.x) * (256 / L) + threadIdx.x / L;
+    if (row >= (int64_t)a.B * a.Hq * a.Tq) return;
+    const int li = threadIdx.x % L;
+    const int i = (int)(row % a.Tq), h = (int)(row / a.Tq % a.Hq), b = (int)(row / a.Tq / a.Hq);
+    float d = 0.f;
+    const bool live = i < seq_len_of(a.ql, b, a.Tq);
+    if (live) {
+        float x[8], y[8];
+        frag8_to_f32<ST>(frag8_load<ST>(row_ptr<ST>(a.out, b, h, i) + 8 * li), x);
+        frag8_to_f32<ST>(frag8_load<ST>(row_ptr<ST>(a.dout, b, h, i) + 8 * li), y);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) d += x[e] * y[e];
+    }
+#pragma unroll
+    for (int o = L / 2; o > 0; o >>= 1) d += __shfl_xor(d, o, 64);
+    if (li == 0) {
+        const float l = live ? a.lse[row] : -__builtin_inff();
+        a.ld[row] = make_float2(l == -__builtin_inff() ? __builtin_inff() : l * kLog2e, d);
     }
 }
 
 // dk and dv of the sinks: the window's pairs, then the chunks in order.
-template <int DH>
+template <typename ST, int DH>
 __global__ __launch_bounds__(256) void wattn_sinks_kernel(AttnArgs a, int slots, const float* __restrict__ sums) {
     const int64_t keys = (int64_t)a.B * a.Hkv * a.S, all = keys * 2 * DH;
     for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < all; e += (int64_t)gridDim.x * 256) {
@@ -529,7 +537,7 @@ __global__ __launch_bounds__(256) void wattn_sinks_kernel(AttnArgs a, int slots,
 #pragma unroll 4
         for (int k = 0; k < slots; ++k) s += sums[k * all + e];
         if (j >= seq_len_of(a.kl, b, a.N)) s = 0.f;
-        st1<uint16_t>(row_ptr<uint16_t>(which ? a.dv : a.dk, b, hk, j) + c, s);
+        st1<ST>(row_ptr<ST>(which ? a.dv : a.dk, b, hk, j) + c, s);
     }
 }
 
@@ -537,16 +545,15 @@ __global__ __launch_bounds__(256) void wattn_sinks_kernel(AttnArgs a, int slots,
 // product; blocks of 64 where those leave CUs idle.  128-wide heads keep to 64
 // keys (16 per wave): the sums of 32 keys and their operands are 192 registers
 // of a lane, which leaves too few for the rest at 2 waves per SIMD.
-template <int DH>
-bool wide_blocks(const AttnArgs& a) { return (int64_t)a.B * a.Hkv * ((a.N + 127) / 128) >= 512; }
-template <int DH>
-constexpr int wide_keys() { return DH == 128 ? 1 : 2; }
+bool wide_blocks(int dtype, const AttnArgs& a) {
+    return dtype == kBF16 && (int64_t)a.B * a.Hkv * ((a.N + 127) / 128) >= 512;
+}
+constexpr int wide_keys(int dh) { return dh == 128 ? 1 : 2; }
 
-template <int DH>
-BwdGeom bwd_geom(const AttnArgs& a) {
+BwdGeom bwd_geom(int dtype, int dh, const AttnArgs& a) {
     BwdGeom G;
-    const bool wide = wide_blocks<DH>(a);
-    const int kw = wide ? 64 * wide_keys<DH>() : 64, qw = wide ? 128 : 64;
+    const bool wide = wide_blocks(dtype, a);
+    const int kw = wide ? 64 * wide_keys(dh) : 64, qw = wide ? 128 : 64;
     const int64_t R = (int64_t)a.Tq * a.G;
     G.nk = (a.N + kw - 1) / kw;
     G.nq = (int)((R + qw - 1) / qw);
@@ -557,42 +564,51 @@ BwdGeom bwd_geom(const AttnArgs& a) {
     return G;
 }
 
-template <int DH, int CB, int QN>
+template <typename ST, int DH, int CB, int QN>
 int launch_bwd(const AttnArgs& a, const BwdGeom& G, float* sums, hipStream_t stream) {
-    auto kern = wattn_bwd_kernel<DH, CB, QN>;
-    const size_t ring = (size_t)kStages * (2 * kTB * DH * 2 + 4 * kTB * 8), outs = (size_t)64 * QN * (DH + 8) * 2;
+    using TL = TileLoad<ST, DH>;
+    auto kern = wattn_bwd_kernel<ST, DH, CB, QN>;
+    const size_t ring = (size_t)kStages * (2 * TL::BYTES + 4 * TL::TB * 8);
+    const size_t outs = 4 * (size_t)store_rows_bytes<ST, DH>(CB > QN ? CB : QN);
     const size_t lds = ring > outs ? ring : outs;
     if (allow_lds((const void*)kern, lds)) return -1;
     const uint64_t blocks = (uint64_t)a.B * a.Hkv * ((uint64_t)G.nk + G.ns * G.nc + G.nq);
-    return launch_parts(blocks, 256, [&](uint32_t first, uint32_t n) {
+    const int e = launch_parts(blocks, 256, [&](uint32_t first, uint32_t n) {
         hipLaunchKernelGGL(kern, dim3(n), dim3(256), lds, stream, a, G, sums, first);
         return hipGetLastError() == hipSuccess ? 0 : -1;
     });
-}
-
-template <int DH>
-int bwd_tiled(const AttnArgs& a, float* sums, hipStream_t stream) {
-    const BwdGeom G = bwd_geom<DH>(a);
-    const int e = wide_blocks<DH>(a) ? launch_bwd<DH, wide_keys<DH>(), 2>(a, G, sums, stream)
-                                     : launch_bwd<DH, 1, 1>(a, G, sums, stream);
     if (e || !G.ns) return e;
-    const int64_t all = (int64_t)a.B * a.Hkv * a.S * 2 * DH, blocks = (all + 255) / 256;
-    hipLaunchKernelGGL((wattn_sinks_kernel<DH>), dim3((unsigned)(blocks < 65536 ? blocks : 65536)), dim3(256), 0, stream, a,
+    const int64_t all = (int64_t)a.B * a.Hkv * a.S * 2 * DH, n = (all + 255) / 256;
+    hipLaunchKernelGGL((wattn_sinks_kernel<ST, DH>), dim3((unsigned)(n < 65536 ? n : 65536)), dim3(256), 0, stream, a,
                        1 + G.nc, sums);
     return hipGetLastError() == hipSuccess ? 0 : -1;
 }
 
+size_t ld_bytes(const AttnArgs& a) { return ((size_t)a.B * a.Hq * a.Tq * sizeof(float2) + 255) / 256 * 256; }
+
 }  // namespace
 
-size_t wattn_bwd_sums(int dh, const AttnArgs& a) {
-    const BwdGeom G = dh == 128 ? bwd_geom<128>(a) : dh == 64 ? bwd_geom<64>(a) : bwd_geom<32>(a);
-    return G.ns ? (size_t)(1 + G.nc) * a.B * a.Hkv * a.S * 2 * dh * sizeof(float) : 0;
+size_t attn_bwd_scratch(int dtype, int dh, const AttnArgs& a) {
+    const BwdGeom G = bwd_geom(dtype, dh, a);
+    return ld_bytes(a) + (G.ns ? (size_t)(1 + G.nc) * a.B * a.Hkv * a.S * 2 * dh * sizeof(float) : 0);
 }
 
-int launch_wattn_bwd_tiled(int dh, const AttnArgs& a, float* sums, hipStream_t stream) {
-    if (dh == 128) return bwd_tiled<128>(a, sums, stream);
-    if (dh == 64) return bwd_tiled<64>(a, sums, stream);
-    return bwd_tiled<32>(a, sums, stream);
+int launch_window_attn_bwd(int dtype, int dh, AttnArgs a, void* scratch, hipStream_t stream) {
+    a.ld = static_cast<float2*>(scratch);
+    float* sums = reinterpret_cast<float*>(static_cast<char*>(scratch) + ld_bytes(a));
+    const BwdGeom G = bwd_geom(dtype, dh, a);
+    return heads_by_type(dtype, dh, [&](auto st, auto d) {
+        using ST = decltype(st);
+        constexpr int DH = decltype(d)::value, per = 256 / (DH / 8);
+        const int e = launch_parts(((uint64_t)a.B * a.Hq * a.Tq + per - 1) / per, 256, [&](uint32_t first, uint32_t n) {
+            hipLaunchKernelGGL((wattn_ld_kernel<ST, DH>), dim3(n), dim3(256), 0, stream, a, first);
+            return hipGetLastError() == hipSuccess ? 0 : -1;
+        });
+        if (e) return e;
+        if constexpr (sizeof(ST) == 2)
+            if (wide_blocks(dtype, a)) return launch_bwd<ST, DH, wide_keys(DH), 2>(a, G, sums, stream);
+        return launch_bwd<ST, DH, 1, 1>(a, G, sums, stream);
+    });
 }
 
 }  // namespace mosa

@@ -1,11 +1,11 @@
-// Tiles of 64 rows of bf16 copied from global memory straight into LDS by the 4
-// waves of a workgroup, for the windowed attention's kernels.
+// Tiles of 64 rows of bf16 or 32 rows of fp32 copied from global memory straight
+// into LDS by the 4 waves of a workgroup, for the windowed attention's kernels.
 //
 // One instruction of a wave fills 1 KB, lane l the bytes 16 l .. 16 l + 15: unit
 // p = 64 (wave + 4 j) + lane of a tile is row p / U, stored unit p % U (U units
 // of 16 bytes per row), and holds the row's unit (p % U) ^ swizzle(row).  The
-// swizzles depend on a row's low 4 bits, and the rows of a lane's loads are 16
-// or more apart, so all its loads take the same unit.
+// swizzles depend on a row's low 4 bits (3 for rows of 512 bytes), and the rows of
+// a lane's loads are 16 (8) or more apart, so all its loads take the same unit.
 //
 // A load's address is a uniform base in scalar registers and a lane offset of
 // 32 bits that does not change from tile to tile: the copies cost no vector
@@ -15,7 +15,7 @@
 #pragma once
 
 #include "attn_lds.h"
-#include "heads.h"
+#include "rowattn.h"
 
 namespace mosa {
 
@@ -35,49 +35,53 @@ __device__ __forceinline__ const char* uniform_ptr(const char* p) {
                          (uint32_t)__builtin_amdgcn_readfirstlane((int)u));
 }
 
-constexpr int kTB = 64;  // rows per tile
+template <typename ST>
+constexpr int kTileRows = sizeof(ST) == 2 ? 64 : 32;
 
-// Unit permutation of a tile's rows.  With 16-byte reads of one unit of 16 rows
-// and transposed 8-byte reads of unit pairs of 4 x 4 rows, both as fast as reads
-// of consecutive bytes (4.5 and 5.4 cycles of a CU's LDS per wave read; other
-// permutations of the 128-byte rows measured 8.2 and 5.4, none 16 and 8.3).
-template <int DH>
+// Unit permutation of a tile's rows.  bf16: with 16-byte reads of one unit of 16
+// rows and transposed 8-byte reads of unit pairs of 4 x 4 rows, both as fast as
+// reads of consecutive bytes (4.5 and 5.4 cycles of a CU's LDS per wave read;
+// other permutations of the 128-byte rows measured 8.2 and 5.4, none 16 and 8.3).
+// fp32: the columns' reads take 4 bytes of rows 4 apart.
+template <typename ST, int DH>
 __device__ __forceinline__ int tile_swz(int r) {
-    if constexpr (DH == 128) return r & 15;
+    if constexpr (sizeof(ST) == 4) return (r & 3) + 4 * ((r >> 2) & (DH == 64 ? 3 : 1));
+    else if constexpr (DH == 128) return r & 15;
     else if constexpr (DH == 64) return r & 7;
     else return (r >> 1) & 3;
 }
 
-template <int DH>
+template <typename ST, int DH>
 struct TileLoad {
-    static constexpr int U = DH / 8, LD = kTB * DH * 2 / 4096, STEP = 256 / U;  // loads per wave, rows between them
-    static constexpr int BYTES = kTB * DH * 2;
+    static constexpr int TB = kTileRows<ST>, E = 16 / (int)sizeof(ST), U = DH / E;  // values per unit, units per row
+    static constexpr int BYTES = TB * DH * (int)sizeof(ST), LD = BYTES / 4096, STEP = 256 / U;  // loads per wave, rows between them
     int row, col;     // this lane's row of load 0, and its first column
     uint32_t lds;     // byte offset of the wave's first block within a tile
     __device__ __forceinline__ TileLoad(int wave, int lane)
         : row((64 * wave + lane) / U), lds(1024 * (uint32_t)__builtin_amdgcn_readfirstlane(wave)) {
-        col = 8 * ((64 * wave + lane) % U ^ tile_swz<DH>(row));
+        col = E * ((64 * wave + lane) % U ^ tile_swz<ST, DH>(row));
     }
 };
 
-// Keys e0 .. e0 + 63 of a list.
-template <int DH>
+// Keys e0 .. e0 + TB - 1 of a list.
+template <typename ST, int DH>
 struct KeyTiles {
-    using TL = TileLoad<DH>;
-    const uint16_t* base;
+    using TL = TileLoad<ST, DH>;
+    const ST* base;
     int64_t stride;
     uint32_t off;
     bool near;
     __device__ __forceinline__ KeyTiles(const Rows& t, int b, int hk, const TL& tl)
-        : base(row_ptr<uint16_t>(t, b, hk, 0)), stride(t.row) {
-        near = stride < ((int64_t)1 << 24);  // 64 rows within 2^31 bytes
-        off = (uint32_t)(((int64_t)tl.row * stride + tl.col) * 2);
+        : base(row_ptr<ST>(t, b, hk, 0)), stride(t.row) {
+        near = stride < ((int64_t)1 << 24);  // a tile's rows within 2^31 bytes
+        off = (uint32_t)((tl.row * stride + tl.col) * (int)sizeof(ST));
     }
     __device__ __forceinline__ void issue(const TL& tl, const KeyList& l, int e0, uint32_t at) const {
-        if (near && e0 >= l.s && e0 + kTB <= l.count) {
+        if (near && e0 >= l.s && e0 + TL::TB <= l.count) {
             const char* p = uniform_ptr(reinterpret_cast<const char*>(base + (int64_t)(e0 - l.s + l.lo) * stride));
 #pragma unroll
-            for (int j = 0; j < TL::LD; ++j) lds_load16s(off, p + (int64_t)(2 * TL::STEP * j) * stride, at + tl.lds + 4096 * j);
+            for (int j = 0; j < TL::LD; ++j)
+                lds_load16s(off, p + (int64_t)((int)sizeof(ST) * TL::STEP * j) * stride, at + tl.lds + 4096 * j);
         } else {  // entries past the list are its last one
 #pragma unroll
             for (int j = 0; j < TL::LD; ++j)
@@ -90,18 +94,20 @@ struct KeyTiles {
 // Fragment reads of a tile: 16 rows by 32 columns as they lie, and, transposed,
 // 16 columns by 32 rows in the slot order of two 16-row result blocks (slots
 // 0 .. 3 rows 4 g + i of block 2 u, slots 4 .. 7 the same of block 2 u + 1).
+template <typename ST, int DH>
+struct TileReads;
 template <int DH>
-struct TileReads {
+struct TileReads<uint16_t, DH> {
     static constexpr int U = DH / 8, NS = DH / 32, ND = DH / 16;
     int row[NS], tr[ND];
     __device__ __forceinline__ TileReads(int g, int c16) {
 #pragma unroll
-        for (int st = 0; st < NS; ++st) row[st] = (c16 * U + ((4 * st + g) ^ tile_swz<DH>(c16))) * 16;
+        for (int st = 0; st < NS; ++st) row[st] = (c16 * U + ((4 * st + g) ^ tile_swz<uint16_t, DH>(c16))) * 16;
         const int r = 4 * g + (c16 >> 2);
 #pragma unroll
         for (int db = 0; db < ND; ++db) {
             const int col = 16 * db + 4 * (c16 & 3);
-            tr[db] = (r * U + ((col >> 3) ^ tile_swz<DH>(r))) * 16 + 8 * ((col >> 2) & 1);
+            tr[db] = (r * U + ((col >> 3) ^ tile_swz<uint16_t, DH>(r))) * 16 + 8 * ((col >> 2) & 1);
         }
     }
     __device__ __forceinline__ Frag8<uint16_t> rows(const unsigned char* t, int sb, int st) const {
@@ -117,10 +123,76 @@ struct TileReads {
         return f;
     }
 };
+template <int DH>
+struct TileReads<float, DH> {
+    static constexpr int U = DH / 4, NS = DH / 32, ND = DH / 16;
+    int g, c16;
+    __device__ __forceinline__ TileReads(int g, int c16) : g(g), c16(c16) {}
+    static __device__ __forceinline__ int at(int r, int unit) { return (r * U + (unit ^ tile_swz<float, DH>(r))) * 16; }
+    __device__ __forceinline__ Frag8<float> rows(const unsigned char* t, int sb, int st) const {
+        Frag8<float> f;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const float4 x = *reinterpret_cast<const float4*>(t + at(16 * sb + c16, 8 * st + 2 * g + h));
+            f.v[4 * h] = x.x, f.v[4 * h + 1] = x.y, f.v[4 * h + 2] = x.z, f.v[4 * h + 3] = x.w;
+        }
+        return f;
+    }
+    __device__ __forceinline__ Frag8<float> cols(const unsigned char* t, int u, int db) const {
+        Frag8<float> f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int r = 32 * u + 16 * (e >> 2) + 4 * g + (e & 3), col = 16 * db + c16;
+            f.v[e] = *reinterpret_cast<const float*>(t + at(r, col >> 2) + 4 * (col & 3));
+        }
+        return f;
+    }
+};
 
-__device__ __forceinline__ Frag8<uint16_t> pack_frag(const f32x4& x, const f32x4& y) {
+// A fragment's loads are waited for here: a first use inside a pipeline would
+// wait there for every load in flight, the next tiles' included.
+__device__ __forceinline__ void take(Frag8<uint16_t>& f) { asm volatile("" : "+v"(f.v)); }
+__device__ __forceinline__ void take(Frag8<float>& f) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) asm volatile("" : "+v"(f.v[e]));
+}
+
+// Two 16-row result blocks as an operand (bf16: rounded here).
+template <typename ST>
+__device__ __forceinline__ Frag8<ST> pack_frag(const f32x4& x, const f32x4& y) {
     const float v[8] = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
-    return frag8_from<uint16_t>(v);
+    return frag8_from<ST>(v);
+}
+
+// Rows of 16 N results (column c16 of block n, values 4 g + i of every 16, times
+// f[n]) through this wave's part of LDS to 16-byte stores: to(row) is the row's
+// address or nullptr.
+template <typename ST, int DH>
+constexpr int store_rows_bytes(int n) { return 16 * n * (DH * (int)sizeof(ST) + 16); }
+template <typename ST, int DH, int N, class TO>
+__device__ __forceinline__ void store_rows(unsigned char* lds, const f32x4 (&x)[N][DH / 16], const float (&f)[N], int lane,
+                                           const TO& to) {
+    constexpr int E = 16 / (int)sizeof(ST), LDO = DH + E, U = DH / E;
+    ST* o = reinterpret_cast<ST*>(lds);
+    const int g = lane >> 4, c16 = lane & 15;
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int db = 0; db < DH / 16; ++db) {
+            ST* p = o + (16 * n + c16) * LDO + 16 * db + 4 * g;
+            const f32x4 v = x[n][db] * f[n];
+            if constexpr (sizeof(ST) == 2)
+                *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+            else
+                *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
+        }
+    wave_sync();
+#pragma unroll
+    for (int e = lane; e < 16 * N * U; e += 64) {
+        const int r = e / U, dc = (e % U) * E;
+        if (ST* p = to(r)) *reinterpret_cast<uint4*>(p + dc) = *reinterpret_cast<const uint4*>(o + r * LDO + dc);
+    }
+    wave_sync();
 }
 
 }  // namespace mosa

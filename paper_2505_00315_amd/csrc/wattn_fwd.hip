@@ -1,10 +1,10 @@
 // Causal attention with a sliding window and first tokens that stay visible:
-// the forward over rows in bf16.
+// the forward over rows.
 //
 // One pass over the keys with the running maximum and sum of the softmax.  A
 // workgroup of 4 waves owns 64 QN rows of a key head's row list (16 QN per
 // wave) and walks the keys that some row of the block sees, sinks first, in
-// tiles of 64 through an LDS ring filled by direct global-to-LDS loads:
+// tiles of 64 (fp32: 32) through an LDS ring filled by direct global-to-LDS loads:
 //   S^T = K Q^T  (query in the lane),  p = 2^(s c - m),  O^T += V^T P^T
 // with P^T as it lies in the registers of S^T and V^T read transposed from the
 // row-major tile.  The products cost 4 d_head operations per pair and the
@@ -26,11 +26,11 @@ struct FwdGeom {
     int nb, parts;
 };
 
-template <int DH, int QN>
+template <typename ST, int DH, int QN>
 __global__ __launch_bounds__(256, 2) void wattn_fwd_kernel(AttnArgs a, FwdGeom G, Parts part, uint32_t first) {
-    using ST = uint16_t;
-    constexpr int U = DH / 8, KB = kTB, QB = 64 * QN, STG = kStages, NS = DH / 32, ND = DH / 16;
-    constexpr int TILE = TileLoad<DH>::BYTES, STAGE = 2 * TILE, LD = TileLoad<DH>::LD;
+    using TL = TileLoad<ST, DH>;
+    constexpr int KB = TL::TB, NB = KB / 16, QB = 64 * QN, STG = kStages, NS = DH / 32, ND = DH / 16;
+    constexpr int TILE = TL::BYTES, STAGE = 2 * TILE, LD = TL::LD;
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, c16 = lane & 15;
 
@@ -81,16 +81,14 @@ __global__ __launch_bounds__(256, 2) void wattn_fwd_kernel(AttnArgs a, FwdGeom G
 #pragma unroll
             for (int st = 0; st < NS; ++st) qf[qs][st] = frag8_load<ST>(qp + 32 * st + 8 * g);
         }
-        // Take the rows now: a first use inside the pipeline would wait there
-        // for every load in flight, the next tiles' included.
 #pragma unroll
         for (int qs = 0; qs < QN; ++qs)
 #pragma unroll
-            for (int st = 0; st < NS; ++st) asm volatile("" : "+v"(qf[qs][st].v));
+            for (int st = 0; st < NS; ++st) take(qf[qs][st]);
 
-        const TileLoad<DH> tl(wave, lane);
-        const TileReads<DH> rd(g, c16);
-        const KeyTiles<DH> kt(a.k, b, hk, tl), vt(a.v, b, hk, tl);
+        const TL tl(wave, lane);
+        const TileReads<ST, DH> rd(g, c16);
+        const KeyTiles<ST, DH> kt(a.k, b, hk, tl), vt(a.v, b, hk, tl);
         const uint32_t lbase = __builtin_amdgcn_readfirstlane(lds_addr(smem));
         // tile t of this part (past the end: the last one again, into a buffer
         // that nobody reads); entries past the list are masked
@@ -114,9 +112,9 @@ __global__ __launch_bounds__(256, 2) void wattn_fwd_kernel(AttnArgs a, FwdGeom G
             const int kmax = list.key(min(e0 + KB, list.count) - 1), kmin = e0 >= list.s ? list.key(e0) : list.lo;
             if (e0 >= list.s && (kmin > pw1 || (a.W && kmax <= pw0 - a.W && kmin >= a.S))) return;  // nothing for this wave
 
-            f32x4 s[QN][4];
+            f32x4 s[QN][NB];
 #pragma unroll
-            for (int sb = 0; sb < 4; ++sb) {
+            for (int sb = 0; sb < NB; ++sb) {
                 Frag8<ST> kf[NS];
 #pragma unroll
                 for (int st = 0; st < NS; ++st) kf[st] = rd.rows(Kb, sb, st);
@@ -130,7 +128,7 @@ __global__ __launch_bounds__(256, 2) void wattn_fwd_kernel(AttnArgs a, FwdGeom G
             // per-element mask only where the tile is not seen whole by the wave's rows
             if (e0 + KB > list.count || kmax > pw0 || (a.W && kmin <= pw1 - a.W)) {
 #pragma unroll
-                for (int sb = 0; sb < 4; ++sb)
+                for (int sb = 0; sb < NB; ++sb)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const int e = e0 + 16 * sb + 4 * g + i, key = list.key(e);
@@ -144,7 +142,7 @@ __global__ __launch_bounds__(256, 2) void wattn_fwd_kernel(AttnArgs a, FwdGeom G
             for (int qs = 0; qs < QN; ++qs) {
                 float mloc = -__builtin_inff();  // over the raw scores (the scale is positive)
 #pragma unroll
-                for (int sb = 0; sb < 4; ++sb)
+                for (int sb = 0; sb < NB; ++sb)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) mloc = fmaxf(mloc, s[qs][sb][i]);
                 mloc = rows4_max(mloc) * c2;
@@ -162,7 +160,7 @@ __global__ __launch_bounds__(256, 2) void wattn_fwd_kernel(AttnArgs a, FwdGeom G
                 }
                 float lsum = 0.f;
 #pragma unroll
-                for (int sb = 0; sb < 4; ++sb)
+                for (int sb = 0; sb < NB; ++sb)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         s[qs][sb][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[qs][sb][i], c2, -m_use));
@@ -170,14 +168,14 @@ __global__ __launch_bounds__(256, 2) void wattn_fwd_kernel(AttnArgs a, FwdGeom G
                     }
                 l_run[qs] += lsum;  // this lane's keys; the 4 lanes of a row are added at the end
             }
-            // O^T += V^T P^T, 32 keys per instruction: slots 0..3 are keys 4 g + i
-            // of block 2 u, slots 4..7 those of block 2 u + 1.  P is rounded to
-            // bf16 here, the type of the matrix operands (l sums it unrounded).
+            // O^T += V^T P^T, 32 keys at a time: slots 0..3 are keys 4 g + i of
+            // block 2 u, slots 4..7 those of block 2 u + 1.  With bf16 storage P is
+            // rounded to it here, the type of the matrix operands (l sums it unrounded).
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
+            for (int u = 0; u < NB / 2; ++u) {
                 Frag8<ST> pf[QN];
 #pragma unroll
-                for (int qs = 0; qs < QN; ++qs) pf[qs] = pack_frag(s[qs][2 * u], s[qs][2 * u + 1]);
+                for (int qs = 0; qs < QN; ++qs) pf[qs] = pack_frag<ST>(s[qs][2 * u], s[qs][2 * u + 1]);
 #pragma unroll
                 for (int db = 0; db < ND; ++db) {
                     const Frag8<ST> vf = rd.cols(Vb, u, db);
@@ -249,30 +247,20 @@ __global__ __launch_bounds__(256, 2) void wattn_fwd_kernel(AttnArgs a, FwdGeom G
         }
         return;
     }
-    // out = O / l through LDS to 16-byte row stores, lse = m ln 2 + log l
-    constexpr int LDO = DH + 8;
-    ST* Os = reinterpret_cast<ST*>(smem) + wave * 16 * QN * LDO;
+    // out = O / l, lse = m ln 2 + log l
+    float inv[QN];
 #pragma unroll
     for (int qs = 0; qs < QN; ++qs) {
         const int r = wr0 + 16 * qs + c16;
         const bool live = r < rn && l_run[qs] > 0.f;
-        const float inv = live ? 1.f / l_run[qs] : 0.f;
-#pragma unroll
-        for (int db = 0; db < ND; ++db)
-            *reinterpret_cast<uint2*>(Os + (16 * qs + c16) * LDO + 16 * db + 4 * g) =
-                make_uint2(pack_bf16x2(o[qs][db][0] * inv, o[qs][db][1] * inv),
-                           pack_bf16x2(o[qs][db][2] * inv, o[qs][db][3] * inv));
+        inv[qs] = live ? 1.f / l_run[qs] : 0.f;
         if (a.lse && g == 0 && r < R)
             a.lse[qrow_index(a, b, hk, r, qi[qs])] = live ? m_run[qs] * kLn2 + logf(l_run[qs]) : -__builtin_inff();
     }
-    __syncthreads();
-#pragma unroll
-    for (int e = lane; e < 16 * QN * U; e += 64) {
-        const int lr = e / U, dc = (e % U) * 8, r = wr0 + lr;
-        if (r < R)
-            *reinterpret_cast<uint4*>(qrow_ptr<ST>(a, a.out, b, hk, r, a.gd.div(r)) + dc) =
-                *reinterpret_cast<const uint4*>(Os + lr * LDO + dc);
-    }
+    store_rows<ST, DH, QN>(smem + wave * store_rows_bytes<ST, DH>(QN), o, inv, lane, [&](int lr) {
+        const int r = wr0 + lr;
+        return r < R ? qrow_ptr<ST>(a, a.out, b, hk, r, a.gd.div(r)) : nullptr;
+    });
 }
 
 // A row of the call: the parts in their order, M = max m_s, L = sum l_s 2^(m_s - M).
@@ -302,35 +290,34 @@ __global__ __launch_bounds__(256) void wattn_merge_kernel(AttnArgs a, int parts,
     row_finish<ST, DH>(a, b, h, i, row, lane, M, L, o, nullptr, nullptr);
 }
 
-// Blocks of 128 rows share K and V fragments over two matrix instructions each;
-// blocks of 64 where those of 128 leave CUs idle, and parts of a block's keys
-// where even they do.
-template <int DH>
+// Blocks of 128 rows share K and V fragments over two matrix instructions each
+// (bf16); blocks of 64 where those of 128 leave CUs idle, and parts of a block's
+// keys where even they do.
 int blocks_of(const AttnArgs& a, int qn) { return (int)(((int64_t)a.Tq * a.G + 64 * qn - 1) / (64 * qn)); }
 
-template <int DH>
-int fwd_qn(const AttnArgs& a) { return (int64_t)blocks_of<DH>(a, 2) * a.B * a.Hkv >= 512 ? 2 : 1; }
+int fwd_qn(int dtype, const AttnArgs& a) {
+    return dtype == kBF16 && (int64_t)blocks_of(a, 2) * a.B * a.Hkv >= 512 ? 2 : 1;
+}
 
-template <int DH>
-FwdGeom fwd_geom(const AttnArgs& a) {
+FwdGeom fwd_geom(int dtype, const AttnArgs& a) {
     FwdGeom G;
-    G.nb = blocks_of<DH>(a, fwd_qn<DH>(a));
-    const int64_t blocks = (int64_t)G.nb * a.B * a.Hkv;
+    G.nb = blocks_of(a, fwd_qn(dtype, a));
+    const int64_t blocks = (int64_t)G.nb * a.B * a.Hkv, tb = dtype == kBF16 ? 64 : 32;
     // most keys of a block, in tiles; a part keeps at least 4 of them
     const int64_t span = a.W ? (int64_t)a.W + a.S + 64 / a.G + 1 : a.N;
-    const int64_t tiles = ((span < a.N ? span : a.N) + kTB - 1) / kTB;
+    const int64_t tiles = ((span < a.N ? span : a.N) + tb - 1) / tb;
     int64_t parts = blocks >= 256 ? 1 : (512 + blocks - 1) / blocks;
     if (parts > tiles / 4) parts = tiles / 4;
     G.parts = parts < 1 ? 1 : (int)parts;
     return G;
 }
 
-template <int DH, int QN>
+template <typename ST, int DH, int QN>
 int launch_fwd(const AttnArgs& a, const FwdGeom& G, float* buf, hipStream_t stream) {
-    const size_t ring = (size_t)kStages * 2 * kTB * DH * 2, outs = (size_t)64 * QN * (DH + 8) * 2;
+    const size_t ring = (size_t)kStages * 2 * TileLoad<ST, DH>::BYTES, outs = 4 * (size_t)store_rows_bytes<ST, DH>(QN);
     const size_t lds = ring > outs ? ring : outs;
     const Parts part = make_parts(buf, G.parts, (int64_t)a.B * a.Hq * a.Tq, DH);
-    auto kern = wattn_fwd_kernel<DH, QN>;
+    auto kern = wattn_fwd_kernel<ST, DH, QN>;
     if (allow_lds((const void*)kern, lds)) return -1;
     return launch_parts((uint64_t)a.B * a.Hkv * G.nb * G.parts, 256, [&](uint32_t first, uint32_t blocks) {
         hipLaunchKernelGGL(kern, dim3(blocks), dim3(256), lds, stream, a, G, part, first);
@@ -350,22 +337,21 @@ int launch_merge_parts(int dtype, int dh, const AttnArgs& a, int parts, const Pa
     });
 }
 
-size_t wattn_tiled_scratch(int dh, const AttnArgs& a) {
-    const FwdGeom G = dh == 128 ? fwd_geom<128>(a) : dh == 64 ? fwd_geom<64>(a) : fwd_geom<32>(a);
-    return parts_bytes(G.parts, (int64_t)a.B * a.Hq * a.Tq, dh);
+size_t attn_fwd_scratch(int dtype, int dh, const AttnArgs& a) {
+    return parts_bytes(fwd_geom(dtype, a).parts, (int64_t)a.B * a.Hq * a.Tq, dh);
 }
 
-int launch_wattn_tiled(int dh, const AttnArgs& a, float* buf, hipStream_t stream) {
-    auto run = [&](auto d) {
+int launch_window_attn(int dtype, int dh, const AttnArgs& a, float* buf, hipStream_t stream) {
+    const FwdGeom G = fwd_geom(dtype, a);
+    const int e = heads_by_type(dtype, dh, [&](auto st, auto d) {
+        using ST = decltype(st);
         constexpr int DH = decltype(d)::value;
-        const FwdGeom G = fwd_geom<DH>(a);
-        const int e = fwd_qn<DH>(a) == 2 ? launch_fwd<DH, 2>(a, G, buf, stream) : launch_fwd<DH, 1>(a, G, buf, stream);
-        if (e || G.parts == 1) return e;
-        return launch_merge_parts(kBF16, DH, a, G.parts, make_parts(buf, G.parts, (int64_t)a.B * a.Hq * a.Tq, DH), stream);
-    };
-    if (dh == 128) return run(std::integral_constant<int, 128>{});
-    if (dh == 64) return run(std::integral_constant<int, 64>{});
-    return run(std::integral_constant<int, 32>{});
+        if constexpr (sizeof(ST) == 2)
+            if (fwd_qn(dtype, a) == 2) return launch_fwd<ST, DH, 2>(a, G, buf, stream);
+        return launch_fwd<ST, DH, 1>(a, G, buf, stream);
+    });
+    if (e || G.parts == 1) return e;
+    return launch_merge_parts(dtype, dh, a, G.parts, make_parts(buf, G.parts, (int64_t)a.B * a.Hq * a.Tq, dh), stream);
 }
 
 }  // namespace mosa
