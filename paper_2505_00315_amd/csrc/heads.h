@@ -79,7 +79,7 @@ struct AttnArgs {
     Rows q, k, v, out, dout, dq, dk, dv;
     const int32_t *ql, *kl;
     float* lse;  // [B, Hq, Tq] (forward: may be nullptr)
-    float2* ld;  // backward: of every query row, lse in log2 units (+inf where it sees nothing) and sum(out dout)
+    float2* ld;  // backward: of every query row, lse in log2 units (+inf where it sees nothing) and -sum(out dout)
 };
 
 // Lengths of sequence b, taken into the tensors.

@@ -118,7 +118,7 @@ __device__ __forceinline__ void row_dq(const AttnArgs& a, int b, int h, int i, i
     for (int e = 0; e < list.count; ++e) {
         keys.load(list.key(e), lane, k, v);
         const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(row_dot<DH>(q, k), c2, -ld.x));
-        const float ds = w * (row_dot<DH>(g, v) - ld.y);
+        const float ds = w * (row_dot<DH>(g, v) + ld.y);
 #pragma unroll
         for (int n = 0; n < N; ++n) dq[n] += ds * k[n];
     }
@@ -146,7 +146,7 @@ __device__ __forceinline__ void row_dkv(const AttnArgs& a, int b, int hk, int j,
         row_load<ST, DH>(row_ptr<ST>(a.dout, b, h, i), lane, g);
         const float2 ld = a.ld[((int64_t)b * a.Hq + h) * a.Tq + i];
         const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(row_dot<DH>(q, k), c2, -ld.x));
-        const float ds = w * (row_dot<DH>(g, v) - ld.y);
+        const float ds = w * (row_dot<DH>(g, v) + ld.y);
 #pragma unroll
         for (int n = 0; n < N; ++n) {
             dk[n] += ds * q[n];

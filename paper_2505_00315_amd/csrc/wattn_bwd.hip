@@ -39,22 +39,21 @@ struct BwdGeom {
     int nk, nq, ns, nc;
 };
 
-// Tiles of a key head's rows: q, dout and (lse, D).  A tile is 64 / G queries of
+// Tiles of a key head's rows: q, dout and (lse, -D).  A tile is 64 / G queries of
 // the group's G heads (its last 64 % G rows are none), or 64 rows where G is
 // larger, so that the lanes' offsets are the same for every tile.
 template <typename ST, int DH>
 struct RowTiles {
     using TL = TileLoad<ST, DH>;
-    static constexpr int TB = TL::TB, ES = (int)sizeof(ST), LL = TB / 32;  // loads of (lse, D), a word per lane
-    const AttnArgs& a;
-    int b, hk, nr;  // rows per tile
+    static constexpr int TB = TL::TB, ES = (int)sizeof(ST), LL = TB / 32;  // loads of (lse, -D), a word per lane
+    int b, hk, nr;  // nr: rows per tile
     bool near;
     uint32_t qoff[TL::LD], goff[TL::LD], loff[LL];
-    __device__ __forceinline__ RowTiles(const AttnArgs& a, int b, int hk, const TL& tl, int lane) : a(a), b(b), hk(hk) {
+    __device__ __forceinline__ RowTiles(const AttnArgs& a, int b, int hk, const TL& tl, int lane) : b(b), hk(hk) {
         const int nq = TB / a.G;  // queries per tile
         nr = nq ? nq * a.G : TB;
         // a tile's rows of G heads within 2^31 bytes
-        near = nq > 0 && fits(a.q) && fits(a.dout) && (int64_t)a.G * a.Tq < ((int64_t)1 << 27);
+        near = nq > 0 && fits(a, a.q) && fits(a, a.dout) && (int64_t)a.G * a.Tq < ((int64_t)1 << 27);
 #pragma unroll
         for (int j = 0; j < TL::LD; ++j) {
             const int r = tl.row + TL::STEP * j, i = a.gd.div(r), g = r - i * a.G;
@@ -67,10 +66,12 @@ struct RowTiles {
             loff[j] = (uint32_t)(((int64_t)g * a.Tq + i) * 8 + 4 * (lane & 1));
         }
     }
-    __device__ __forceinline__ bool fits(const Rows& t) const { return a.G * t.head + TB * t.row < ((int64_t)1 << 29); }
+    __device__ __forceinline__ bool fits(const AttnArgs& a, const Rows& t) const {
+        return a.G * t.head + TB * t.row < ((int64_t)1 << 29);
+    }
     // The tile from row r0 on (of rows below rhi; those past it are the last one), to LDS byte `at`:
-    // q, dout, and for this wave alone (lse, D) of every row.
-    __device__ __forceinline__ void issue(const TL& tl, int r0, int rhi, uint32_t at, uint32_t ld_at, int lane) const {
+    // q, dout, and for this wave alone (lse, -D) of every row.
+    __device__ __forceinline__ void issue(const AttnArgs& a, const TL& tl, int r0, int rhi, uint32_t at, uint32_t ld_at, int lane) const {
         if (near && r0 + TB <= rhi) {
             const int i0 = a.gd.div(r0);
             const char* q = uniform_ptr(reinterpret_cast<const char*>(row_ptr<ST>(a.q, b, hk * a.G, i0)));
@@ -109,16 +110,16 @@ __device__ __forceinline__ bool finite4(const f32x4 (&x)[N]) {
     return t == 0.f;
 }
 
-// Keys k0 .. of (b, hk), 16 CB per wave.  far (chunk >= 0): the pairs beyond the
-// window of sinks, rows of one chunk, sums to `sums`.
-template <typename ST, int DH, int CB>
-__device__ __forceinline__ void dkv_body(unsigned char* smem, const AttnArgs& a, const BwdGeom& G, int b, int hk, int k0,
+// Keys k0 .. of (b, hk), 16 CB per wave.  far: the pairs beyond the window of
+// sinks, rows of one chunk, sums to `sums`.
+template <typename ST, int DH, int CB, bool far>
+__device__ __forceinline__ void dkv_body(unsigned char* smem, const AttnArgs a, const BwdGeom G, int b, int hk, int k0,
                                          int chunk, float* sums) {
     using TL = TileLoad<ST, DH>;
     constexpr int TB = TL::TB, NS = DH / 32, ND = DH / 16, STG = kStages, LD = TL::LD;
-    constexpr int TILE = TL::BYTES, LDB = 4 * TB * 8, STAGE = 2 * TILE + LDB;  // q, dout, a copy of (lse, D) per wave
+    constexpr int TILE = TL::BYTES, LDB = 4 * TB * 8, STAGE = 2 * TILE + LDB;  // q, dout, a copy of (lse, -D) per wave
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, c16 = lane & 15;
-    const bool far = chunk >= 0, apart = G.ns > 0;  // apart: far pairs are done by chunks
+    const bool apart = G.ns > 0;  // apart: far pairs are done by chunks
     const int qn = seq_len_of(a.ql, b, a.Tq), kn = seq_len_of(a.kl, b, a.N), off = kn - qn;
     const int kend = min(far ? min(a.S, k0 + 64) : k0 + 64 * CB, kn);  // past the block's last key
     const int wk0 = k0 + 16 * CB * wave, wk1 = min(wk0 + 16 * CB, kend) - 1;  // this wave's keys (none: wk1 < wk0)
@@ -161,14 +162,14 @@ __device__ __forceinline__ void dkv_body(unsigned char* smem, const AttnArgs& a,
         const TileReads<ST, DH> rd(g, c16);
         const uint32_t base = __builtin_amdgcn_readfirstlane(lds_addr(smem));
         // tile t (past the end: the last one again, into a buffer that nobody reads)
-        auto issue = [&](int t, int buf) {
+        auto issue = [&](int t, int buf) __attribute__((always_inline)) {
             const uint32_t at = base + buf * STAGE;
-            rows.issue(tl, rlo + nr * (tbeg + min(t, ntile - 1)), rhi, at, at + 2 * TILE + 8 * TB * (tl.lds / 1024), lane);
+            rows.issue(a, tl, rlo + nr * (tbeg + min(t, ntile - 1)), rhi, at, at + 2 * TILE + 8 * TB * (tl.lds / 1024), lane);
         };
         const float c2 = a.scale * kLog2e;
 #pragma unroll
         for (int s = 0; s < STG - 1; ++s) issue(s, s);
-        auto tile_step = [&](int it, auto bufc) {
+        auto tile_step = [&](int it, auto bufc) __attribute__((always_inline)) {
             constexpr int BUF = decltype(bufc)::value;
             wait_vmcnt<(STG - 2) * (2 * LD + RowTiles<ST, DH>::LL)>();
             __syncthreads();
@@ -183,14 +184,34 @@ __device__ __forceinline__ void dkv_body(unsigned char* smem, const AttnArgs& a,
             if (far ? wk0 >= a.S || pt1 - wk0 < a.W : pt1 < wk0 || (a.W && pt0 - wk1 >= a.W && (apart || wk0 >= a.S))) return;
             const bool whole = r0 + TB == rt &&
                                (far ? pt0 - wk1 >= a.W : pt0 >= wk1 && (a.W == 0 || pt1 - wk0 < a.W));
+            // the tile's rows (less 4 g) that the lane's keys pair with: positions
+            // from the key on and within its window, or, far, from there on
+            Span run[CB];
+            if (!whole) {
+                const int skip = r0 - (pt0 - off) * a.G + 4 * g;  // rows of the first position before the tile
+#pragma unroll
+                for (int cb = 0; cb < CB; ++cb) {
+                    const int j = key[cb], n = rt - r0;
+                    const bool all_later = far || a.W == 0 || (!apart && j < a.S);
+                    const int from = min(max((far ? j + a.W : j) - pt0, -1), TB + 1);  // in positions of the tile's first
+                    const int to = min(max(j + a.W - pt0, 0), TB + 1);
+                    run[cb] = Span(from * a.G - skip, min(all_later ? n : to * a.G - (skip - 4 * g), n) - 1 - 4 * g);
+                }
+            }
 #pragma unroll
             for (int u = 0; u < TB / 32; ++u) {  // 32 rows at a time
                 f32x4 s[CB][2], dp[CB][2];
 #pragma unroll
                 for (int x = 0; x < 2; ++x) {
                     const int sb = 2 * u + x;
+                    const float4 l0 = *reinterpret_cast<const float4*>(Lt + 8 * (16 * sb + 4 * g));
+                    const float4 l1 = *reinterpret_cast<const float4*>(Lt + 8 * (16 * sb + 4 * g) + 16);
+                    const float lse[4] = {l0.x, l0.z, l1.x, l1.z};
 #pragma unroll
-                    for (int cb = 0; cb < CB; ++cb) s[cb][x] = dp[cb][x] = zero4();
+                    for (int cb = 0; cb < CB; ++cb) {
+                        s[cb][x] = zero4();
+                        dp[cb][x] = f32x4{l0.y, l0.w, l1.y, l1.w};  // the product adds to -D
+                    }
 #pragma unroll
                     for (int st = 0; st < NS; ++st) {
                         const Frag8<ST> qa = rd.rows(Qt, sb, st), ga = rd.rows(Gt, sb, st);
@@ -200,29 +221,22 @@ __device__ __forceinline__ void dkv_body(unsigned char* smem, const AttnArgs& a,
                             mma8(dp[cb][x], ga, vf[cb][st]);
                         }
                     }
-                    const float4 l0 = *reinterpret_cast<const float4*>(Lt + 8 * (16 * sb + 4 * g));
-                    const float4 l1 = *reinterpret_cast<const float4*>(Lt + 8 * (16 * sb + 4 * g) + 16);
-                    const float lse[4] = {l0.x, l0.z, l1.x, l1.z}, D[4] = {l0.y, l0.w, l1.y, l1.w};
 #pragma unroll
                     for (int cb = 0; cb < CB; ++cb)
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
                             s[cb][x][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[cb][x][i], c2, -lse[i]));
-                            dp[cb][x][i] = s[cb][x][i] * (dp[cb][x][i] - D[i]);
+                            dp[cb][x][i] *= s[cb][x][i];
                         }
                     if (!whole) {
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const int r = r0 + 16 * sb + 4 * g + i, p = off + a.gd.div(min(r, rhi - 1));
+                        for (int cb = 0; cb < CB; ++cb)
 #pragma unroll
-                            for (int cb = 0; cb < CB; ++cb) {
-                                const int j = key[cb];
-                                const bool in = r < rt && (far ? p - j >= a.W
-                                                                : j <= p && (a.W == 0 || p - j < a.W || (!apart && j < a.S)));
+                            for (int i = 0; i < 4; ++i) {
+                                const bool in = run[cb].has(16 * sb + i);
                                 s[cb][x][i] = in ? s[cb][x][i] : 0.f;
                                 dp[cb][x][i] = in ? dp[cb][x][i] : 0.f;
                             }
-                        }
                     }
                 }
                 // dv^T += dout^T p, dk^T += q^T ds: with bf16 storage p and ds are
@@ -308,7 +322,7 @@ __device__ __forceinline__ void dkv_body(unsigned char* smem, const AttnArgs& a,
             }
         }
     }
-    if (far) return;
+    if constexpr (far) return;
     // keys past the sequence are zero (their lanes computed its last key again)
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb)
@@ -316,20 +330,28 @@ __device__ __forceinline__ void dkv_body(unsigned char* smem, const AttnArgs& a,
 #pragma unroll
             for (int db = 0; db < ND; ++db) dk[cb][db] = dv[cb][db] = zero4();
     unsigned char* mine = smem + wave * store_rows_bytes<ST, DH>(CB);
+    const float scale = a.scale;
     float fk[CB], fv[CB];
 #pragma unroll
-    for (int cb = 0; cb < CB; ++cb) fk[cb] = a.scale, fv[cb] = 1.f;
-    auto key_at = [&](const Rows& t, int r) {
+    for (int cb = 0; cb < CB; ++cb) {
+        fk[cb] = scale;
+        fv[cb] = 1.f;
+    }
+    const int skip = apart ? a.S : 0;  // keys whose rows the last kernel writes
+    const Rows to_k = a.dk, to_v = a.dv;
+    store_rows<ST, DH, CB>(mine, dk, fk, lane, [&](int r) __attribute__((always_inline)) {
         const int j = wk0 + r;
-        return j < top && !(apart && j < a.S) ? row_ptr<ST>(t, b, hk, j) : nullptr;
-    };
-    store_rows<ST, DH, CB>(mine, dk, fk, lane, [&](int r) { return key_at(a.dk, r); });
-    store_rows<ST, DH, CB>(mine, dv, fv, lane, [&](int r) { return key_at(a.dv, r); });
+        return j < a.N && j >= skip ? row_ptr<ST>(to_k, b, hk, j) : nullptr;
+    });
+    store_rows<ST, DH, CB>(mine, dv, fv, lane, [&](int r) __attribute__((always_inline)) {
+        const int j = wk0 + r;
+        return j < a.N && j >= skip ? row_ptr<ST>(to_v, b, hk, j) : nullptr;
+    });
 }
 
 // Rows r0 .. of (b, hk), 16 QN per wave.
 template <typename ST, int DH, int QN>
-__device__ __forceinline__ void dq_body(unsigned char* smem, const AttnArgs& a, int b, int hk, int r0) {
+__device__ __forceinline__ void dq_body(unsigned char* smem, const AttnArgs a, int b, int hk, int r0) {
     using TL = TileLoad<ST, DH>;
     constexpr int TB = TL::TB, NS = DH / 32, ND = DH / 16, STG = kStages, LD = TL::LD;
     constexpr int TILE = TL::BYTES, STAGE = 2 * TILE;
@@ -372,7 +394,7 @@ __device__ __forceinline__ void dq_body(unsigned char* smem, const AttnArgs& a, 
         const TileReads<ST, DH> rd(g, c16);
         const KeyTiles<ST, DH> kt(a.k, b, hk, tl), vt(a.v, b, hk, tl);
         const uint32_t base = __builtin_amdgcn_readfirstlane(lds_addr(smem));
-        auto issue = [&](int t, int buf) {
+        auto issue = [&](int t, int buf) __attribute__((always_inline)) {
             const int e0 = TB * min(t, ntile - 1);
             kt.issue(tl, list, e0, base + buf * STAGE);
             vt.issue(tl, list, e0, base + buf * STAGE + TILE);
@@ -380,7 +402,7 @@ __device__ __forceinline__ void dq_body(unsigned char* smem, const AttnArgs& a, 
         const float c2 = a.scale * kLog2e;
 #pragma unroll
         for (int s = 0; s < STG - 1; ++s) issue(s, s);
-        auto tile_step = [&](int it, auto bufc) {
+        auto tile_step = [&](int it, auto bufc) __attribute__((always_inline)) {
             constexpr int BUF = decltype(bufc)::value;
             wait_vmcnt<(STG - 2) * 2 * LD>();
             __syncthreads();
@@ -391,6 +413,9 @@ __device__ __forceinline__ void dq_body(unsigned char* smem, const AttnArgs& a, 
             const int kmax = list.key(min(e0 + TB, list.count) - 1), kmin = e0 >= list.s ? list.key(e0) : list.lo;
             if (e0 >= list.s && (kmin > pw1 || (a.W && kmax <= pw0 - a.W && kmin >= a.S))) return;
             const bool whole = e0 + TB <= list.count && kmax <= pw0 && (a.W == 0 || kmin > pw1 - a.W);
+            // keys kmin + 0 .. TB - 1, no sinks: those of a row are a run (entries
+            // past the list lie behind every row)
+            const bool plain = e0 >= list.s && (a.W == 0 || kmin >= a.S);
 #pragma unroll
             for (int u = 0; u < TB / 32; ++u) {  // 32 keys at a time
                 f32x4 s[QN][2], dp[QN][2];
@@ -398,7 +423,10 @@ __device__ __forceinline__ void dq_body(unsigned char* smem, const AttnArgs& a, 
                 for (int x = 0; x < 2; ++x) {
                     const int sb = 2 * u + x;
 #pragma unroll
-                    for (int qs = 0; qs < QN; ++qs) s[qs][x] = dp[qs][x] = zero4();
+                    for (int qs = 0; qs < QN; ++qs) {
+                        s[qs][x] = zero4();
+                        dp[qs][x] = f32x4{ld[qs].y, ld[qs].y, ld[qs].y, ld[qs].y};  // the product adds to -D
+                    }
 #pragma unroll
                     for (int st = 0; st < NS; ++st) {
                         const Frag8<ST> ka = rd.rows(Kt, sb, st), va = rd.rows(Vt, sb, st);
@@ -412,9 +440,16 @@ __device__ __forceinline__ void dq_body(unsigned char* smem, const AttnArgs& a, 
                     for (int qs = 0; qs < QN; ++qs)
 #pragma unroll
                         for (int i = 0; i < 4; ++i)
-                            dp[qs][x][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[qs][x][i], c2, -ld[qs].x)) *
-                                           (dp[qs][x][i] - ld[qs].y);
-                    if (!whole) {
+                            dp[qs][x][i] *= __builtin_amdgcn_exp2f(__builtin_fmaf(s[qs][x][i], c2, -ld[qs].x));
+                    if (!whole && plain) {
+#pragma unroll
+                        for (int qs = 0; qs < QN; ++qs) {
+                            const int d = pos[qs] - kmin - 4 * g;
+                            const Span run(a.W ? d - a.W + 1 : -4 * TB, d);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) dp[qs][x][i] = run.has(16 * sb + i) ? dp[qs][x][i] : 0.f;
+                        }
+                    } else if (!whole) {
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
                             const int e = e0 + 16 * sb + 4 * g + i, key = list.key(e);
@@ -465,9 +500,10 @@ __device__ __forceinline__ void dq_body(unsigned char* smem, const AttnArgs& a, 
         if (wr0 + 16 * qs + c16 >= rn)
 #pragma unroll
             for (int db = 0; db < ND; ++db) dq[qs][db] = zero4();
+    const float scale = a.scale;
     float fq[QN];
 #pragma unroll
-    for (int qs = 0; qs < QN; ++qs) fq[qs] = a.scale;
+    for (int qs = 0; qs < QN; ++qs) fq[qs] = scale;
     store_rows<ST, DH, QN>(smem + wave * store_rows_bytes<ST, DH>(QN), dq, fq, lane, [&](int lr) -> ST* {
         const int r = wr0 + lr;
         return r < R && !(redone && r < rn) ? qrow_ptr<ST>(a, a.dq, b, hk, r, a.gd.div(r)) : nullptr;
@@ -485,11 +521,11 @@ __global__ __launch_bounds__(256, 2) void wattn_bwd_kernel(AttnArgs a, BwdGeom G
     if (id < n0) {
         if (one) id = xcd_logical_id(id, n0);
         const int bh = id / G.nk, kb = id % G.nk;
-        dkv_body<ST, DH, CB>(smem, a, G, bh / a.Hkv, bh % a.Hkv, kb * 64 * CB, -1, sums);
+        dkv_body<ST, DH, CB, false>(smem, a, G, bh / a.Hkv, bh % a.Hkv, kb * 64 * CB, 0, sums);
     } else if (id < n0 + n1) {
         id -= n0;
         const int per = G.ns * G.nc, bh = id / per, k = id % per;
-        dkv_body<ST, DH, 1>(smem, a, G, bh / a.Hkv, bh % a.Hkv, k / G.nc * 64, k % G.nc, sums);
+        dkv_body<ST, DH, 1, true>(smem, a, G, bh / a.Hkv, bh % a.Hkv, k / G.nc * 64, k % G.nc, sums);
     } else {
         id -= n0 + n1;
         if (one) id = xcd_logical_id(id, n2);
@@ -498,7 +534,7 @@ __global__ __launch_bounds__(256, 2) void wattn_bwd_kernel(AttnArgs a, BwdGeom G
     }
 }
 
-// (lse in log2 units, D = sum(out dout)) of every query row, 8 columns per lane:
+// (lse in log2 units, -D), D = sum(out dout), of every query row, 8 columns per lane:
 // what the backward's kernels read of a row beside q and dout.  Bound by the
 // rows of out and dout, which it reads once.
 template <typename ST, int DH>
@@ -521,7 +557,7 @@ __global__ __launch_bounds__(256) void wattn_ld_kernel(AttnArgs a, uint32_t firs
     for (int o = L / 2; o > 0; o >>= 1) d += __shfl_xor(d, o, 64);
     if (li == 0) {
         const float l = live ? a.lse[row] : -__builtin_inff();
-        a.ld[row] = make_float2(l == -__builtin_inff() ? __builtin_inff() : l * kLog2e, d);
+        a.ld[row] = make_float2(l == -__builtin_inff() ? __builtin_inff() : l * kLog2e, -d);
     }
 }
 

@@ -149,6 +149,15 @@ struct TileReads<float, DH> {
     }
 };
 
+// Numbers lo .. hi of a run: which rows (keys) of a tile a lane's key (row) pairs with.
+struct Span {
+    int lo = 1 << 30;  // (an empty run lies past every tile)
+    uint32_t n = 0;    // hi - lo
+    __device__ __forceinline__ Span() {}
+    __device__ __forceinline__ Span(int lo, int hi) : lo(hi < lo ? 1 << 30 : lo), n(hi < lo ? 0u : (uint32_t)(hi - lo)) {}
+    __device__ __forceinline__ bool has(int c) const { return (uint32_t)(c - lo) <= n; }
+};
+
 // A fragment's loads are waited for here: a first use inside a pipeline would
 // wait there for every load in flight, the next tiles' included.
 __device__ __forceinline__ void take(Frag8<uint16_t>& f) { asm volatile("" : "+v"(f.v)); }

@@ -92,7 +92,7 @@ __global__ __launch_bounds__(256, 2) void wattn_fwd_kernel(AttnArgs a, FwdGeom G
         const uint32_t lbase = __builtin_amdgcn_readfirstlane(lds_addr(smem));
         // tile t of this part (past the end: the last one again, into a buffer
         // that nobody reads); entries past the list are masked
-        auto issue = [&](int t, int buf) {
+        auto issue = [&](int t, int buf) __attribute__((always_inline)) {
             const int e0 = KB * (tbeg + min(t, ntile - 1));
             kt.issue(tl, list, e0, lbase + buf * STAGE);
             vt.issue(tl, list, e0, lbase + buf * STAGE + TILE);
@@ -100,7 +100,7 @@ __global__ __launch_bounds__(256, 2) void wattn_fwd_kernel(AttnArgs a, FwdGeom G
         const float c2 = a.scale * kLog2e;  // scores in log2 units
 #pragma unroll
         for (int s = 0; s < STG - 1; ++s) issue(s, s);
-        auto tile_step = [&](int it, auto bufc) {
+        auto tile_step = [&](int it, auto bufc) __attribute__((always_inline)) {
             constexpr int BUF = decltype(bufc)::value;
             wait_vmcnt<(STG - 2) * 2 * LD>();  // tile it is in LDS
             __syncthreads();                   // for every wave; the buffer of tile it - 1 is free
@@ -127,16 +127,31 @@ __global__ __launch_bounds__(256, 2) void wattn_fwd_kernel(AttnArgs a, FwdGeom G
             }
             // per-element mask only where the tile is not seen whole by the wave's rows
             if (e0 + KB > list.count || kmax > pw0 || (a.W && kmin <= pw1 - a.W)) {
+                if (e0 >= list.s && (a.W == 0 || kmin >= a.S)) {
+                    // keys kmin + 0 .. KB - 1, no sinks: those of the row are a run
+                    // (entries past the list lie behind every row)
 #pragma unroll
-                for (int sb = 0; sb < NB; ++sb)
+                    for (int qs = 0; qs < QN; ++qs) {
+                        const int d = pos[qs] - kmin - 4 * g;
+                        const Span run(a.W ? d - a.W + 1 : -4 * KB, d);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int e = e0 + 16 * sb + 4 * g + i, key = list.key(e);
-                        const bool in = e < list.count;
+                        for (int sb = 0; sb < NB; ++sb)
 #pragma unroll
-                        for (int qs = 0; qs < QN; ++qs)
-                            s[qs][sb][i] = in && sees(a, pos[qs], key) ? s[qs][sb][i] : -__builtin_inff();
+                            for (int i = 0; i < 4; ++i)
+                                s[qs][sb][i] = run.has(16 * sb + i) ? s[qs][sb][i] : -__builtin_inff();
                     }
+                } else {
+#pragma unroll
+                    for (int sb = 0; sb < NB; ++sb)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const int e = e0 + 16 * sb + 4 * g + i, key = list.key(e);
+                            const bool in = e < list.count;
+#pragma unroll
+                            for (int qs = 0; qs < QN; ++qs)
+                                s[qs][sb][i] = in && sees(a, pos[qs], key) ? s[qs][sb][i] : -__builtin_inff();
+                        }
+                }
             }
 #pragma unroll
             for (int qs = 0; qs < QN; ++qs) {
