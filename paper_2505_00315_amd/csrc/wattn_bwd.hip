@@ -16,7 +16,10 @@
 // Sinks are seen by every later row.  So that their keys' workgroups do not
 // walk the whole sequence while all others walk a window, the pairs beyond the
 // window are a third kind of work: up to kSinkKeys first keys, the rows cut
-// into chunks, fp32 sums of every chunk added in order by a last kernel.
+// into chunks, fp32 sums of every chunk added in order by a last kernel.  The
+// same kernel adds up the parts of all keys where there is no window and few key
+// blocks, whose rows are then cut into parts (the first keys are seen by every
+// row, the last by few).
 #include "launch_parts.h"
 #include "rowattn.h"
 #include "wattn_dma.h"
@@ -27,16 +30,18 @@ namespace {
 
 constexpr int kSinkKeys = 256;   // most sinks whose far pairs go by chunks of rows
 constexpr int kSinkChunks = 32;  // most chunks of a key head's rows
+constexpr int kMaxParts = 16;    // most parts of a key block's rows
 
 // Two: with 4 stages of the 64-wide heads' tiles a CU holds two workgroups in
 // place of four (8192 tokens, 4 heads, window 512, training step: 81 -> 65 us).
 constexpr int kStages = 2;
 
-// Launch geometry: nk blocks of 64 CB keys and nq blocks of 64 QN rows per (b,
-// key head); nc chunks for each of ns blocks of 64 sinks (0: far pairs are the
-// key blocks' own work).
+// Launch geometry: per (b, key head) nk blocks of keys, their rows cut into kp
+// parts, and nq blocks of rows; nc chunks for each of ns blocks of 64 sinks (ns =
+// 0: far pairs are the key blocks' own work).  Sums are kept of the first `keys`
+// keys of a head (all of them where kp > 1, the sinks where ns > 0).
 struct BwdGeom {
-    int nk, nq, ns, nc;
+    int nk, kp, nq, ns, nc, keys;
 };
 
 // Tiles of a key head's rows: q, dout and (lse, -D).  A tile is 64 / G queries of
@@ -110,8 +115,8 @@ __device__ __forceinline__ bool finite4(const f32x4 (&x)[N]) {
     return t == 0.f;
 }
 
-// Keys k0 .. of (b, hk), 16 CB per wave.  far: the pairs beyond the window of
-// sinks, rows of one chunk, sums to `sums`.
+// Keys k0 .. of (b, hk), 16 CB per wave: part `chunk` of the rows that see them
+// within the window, or, far, chunk `chunk` of those beyond the sinks' window.
 template <typename ST, int DH, int CB, bool far>
 __device__ __forceinline__ void dkv_body(unsigned char* smem, const AttnArgs a, const BwdGeom G, int b, int hk, int k0,
                                          int chunk, float* sums) {
@@ -133,8 +138,8 @@ __device__ __forceinline__ void dkv_body(unsigned char* smem, const AttnArgs a, 
     const int rlo = i0 * a.G, rhi = max(i1, i0) * a.G;
     const TL tl(wave, lane);
     const RowTiles<ST, DH> rows(a, b, hk, tl, lane);
-    const int nr = rows.nr, all = (rhi - rlo + nr - 1) / nr, share = far ? (all + G.nc - 1) / G.nc : all;
-    const int tbeg = far ? min(chunk * share, all) : 0, ntile = min(all, tbeg + share) - tbeg;
+    const int nr = rows.nr, all = (rhi - rlo + nr - 1) / nr, cuts = far ? G.nc : G.kp, share = (all + cuts - 1) / cuts;
+    const int tbeg = min(chunk * share, all), ntile = min(all, tbeg + share) - tbeg;
 
     f32x4 dk[CB][ND], dv[CB][ND];
 #pragma unroll
@@ -198,65 +203,73 @@ __device__ __forceinline__ void dkv_body(unsigned char* smem, const AttnArgs a, 
                     run[cb] = Span(from * a.G - skip, min(all_later ? n : to * a.G - (skip - 4 * g), n) - 1 - 4 * g);
                 }
             }
+            // the whole tile without a branch, so that its reads, products and
+            // exponentials overlap
+            auto products = [&](auto mc) __attribute__((always_inline)) {
+                constexpr bool masked = decltype(mc)::value;
 #pragma unroll
-            for (int u = 0; u < TB / 32; ++u) {  // 32 rows at a time
-                f32x4 s[CB][2], dp[CB][2];
+                for (int u = 0; u < TB / 32; ++u) {  // 32 rows at a time
+                    __builtin_amdgcn_sched_barrier(0);
+                    f32x4 s[CB][2], dp[CB][2];
 #pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    const int sb = 2 * u + x;
-                    const float4 l0 = *reinterpret_cast<const float4*>(Lt + 8 * (16 * sb + 4 * g));
-                    const float4 l1 = *reinterpret_cast<const float4*>(Lt + 8 * (16 * sb + 4 * g) + 16);
-                    const float lse[4] = {l0.x, l0.z, l1.x, l1.z};
-#pragma unroll
-                    for (int cb = 0; cb < CB; ++cb) {
-                        s[cb][x] = zero4();
-                        dp[cb][x] = f32x4{l0.y, l0.w, l1.y, l1.w};  // the product adds to -D
-                    }
-#pragma unroll
-                    for (int st = 0; st < NS; ++st) {
-                        const Frag8<ST> qa = rd.rows(Qt, sb, st), ga = rd.rows(Gt, sb, st);
+                    for (int x = 0; x < 2; ++x) {
+                        const int sb = 2 * u + x;
+                        const float4 l0 = *reinterpret_cast<const float4*>(Lt + 8 * (16 * sb + 4 * g));
+                        const float4 l1 = *reinterpret_cast<const float4*>(Lt + 8 * (16 * sb + 4 * g) + 16);
+                        const float lse[4] = {l0.x, l0.z, l1.x, l1.z};
 #pragma unroll
                         for (int cb = 0; cb < CB; ++cb) {
-                            mma8(s[cb][x], qa, kf[cb][st]);
-                            mma8(dp[cb][x], ga, vf[cb][st]);
+                            s[cb][x] = zero4();
+                            dp[cb][x] = f32x4{l0.y, l0.w, l1.y, l1.w};  // the product adds to -D
                         }
-                    }
 #pragma unroll
-                    for (int cb = 0; cb < CB; ++cb)
+                        for (int st = 0; st < NS; ++st) {
+                            const Frag8<ST> qa = rd.rows(Qt, sb, st), ga = rd.rows(Gt, sb, st);
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            s[cb][x][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[cb][x][i], c2, -lse[i]));
-                            dp[cb][x][i] *= s[cb][x][i];
+                            for (int cb = 0; cb < CB; ++cb) {
+                                mma8(s[cb][x], qa, kf[cb][st]);
+                                mma8(dp[cb][x], ga, vf[cb][st]);
+                            }
                         }
-                    if (!whole) {
 #pragma unroll
                         for (int cb = 0; cb < CB; ++cb)
 #pragma unroll
                             for (int i = 0; i < 4; ++i) {
-                                const bool in = run[cb].has(16 * sb + i);
-                                s[cb][x][i] = in ? s[cb][x][i] : 0.f;
-                                dp[cb][x][i] = in ? dp[cb][x][i] : 0.f;
+                                s[cb][x][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[cb][x][i], c2, -lse[i]));
+                                dp[cb][x][i] *= s[cb][x][i];
                             }
+                        if constexpr (masked) {
+#pragma unroll
+                            for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) {
+                                    const bool in = run[cb].has(16 * sb + i);
+                                    s[cb][x][i] = in ? s[cb][x][i] : 0.f;
+                                    dp[cb][x][i] = in ? dp[cb][x][i] : 0.f;
+                                }
+                        }
                     }
-                }
-                // dv^T += dout^T p, dk^T += q^T ds: with bf16 storage p and ds are
-                // rounded to it, the type of the matrix operands
-                Frag8<ST> pf[CB], df[CB];
-#pragma unroll
-                for (int cb = 0; cb < CB; ++cb) {
-                    pf[cb] = pack_frag<ST>(s[cb][0], s[cb][1]);
-                    df[cb] = pack_frag<ST>(dp[cb][0], dp[cb][1]);
-                }
-#pragma unroll
-                for (int db = 0; db < ND; ++db) {
-                    const Frag8<ST> gt = rd.cols(Gt, u, db), qt = rd.cols(Qt, u, db);
+                    // dv^T += dout^T p, dk^T += q^T ds: with bf16 storage p and ds are
+                    // rounded to it, the type of the matrix operands
+                    Frag8<ST> pf[CB], df[CB];
 #pragma unroll
                     for (int cb = 0; cb < CB; ++cb) {
-                        mma8(dv[cb][db], gt, pf[cb]);
-                        mma8(dk[cb][db], qt, df[cb]);
+                        pf[cb] = pack_frag<ST>(s[cb][0], s[cb][1]);
+                        df[cb] = pack_frag<ST>(dp[cb][0], dp[cb][1]);
+                    }
+#pragma unroll
+                    for (int db = 0; db < ND; ++db) {
+                        const Frag8<ST> gt = rd.cols(Gt, u, db), qt = rd.cols(Qt, u, db);
+#pragma unroll
+                        for (int cb = 0; cb < CB; ++cb) {
+                            mma8(dv[cb][db], gt, pf[cb]);
+                            mma8(dk[cb][db], qt, df[cb]);
+                        }
                     }
                 }
-            }
+            };
+            if (whole) products(std::false_type{});
+            else products(std::true_type{});
         };
         for (int it0 = 0;; it0 += STG) {
             bool last = false;
@@ -273,10 +286,11 @@ __device__ __forceinline__ void dkv_body(unsigned char* smem, const AttnArgs a, 
     }
     __syncthreads();
 
-    // slot 0 of the sums: the window's pairs, slot 1 + c: chunk c
-    const int64_t keys = (int64_t)a.B * a.Hkv * a.S;
-    float* sum = sums + ((far ? 1 + chunk : 0) * keys + ((int64_t)b * a.Hkv + hk) * a.S) * 2 * DH;
-    const int top = far ? a.S : a.N;  // keys of the output
+    // slots of the sums: the parts of the window's pairs, then the chunks (a
+    // block of keys whose sums are kept is one of both or of neither kind)
+    const int64_t slot = far ? G.kp + chunk : chunk;
+    float* sum = sums + (slot * a.B * a.Hkv + (int64_t)b * a.Hkv + hk) * G.keys * 2 * DH;
+    const int top = far ? a.S : a.N, summed = G.keys;  // keys of the output, those whose sums are kept
     bool fine = true;
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb) fine &= finite4(dk[cb]) && finite4(dv[cb]);
@@ -291,7 +305,7 @@ __device__ __forceinline__ void dkv_body(unsigned char* smem, const AttnArgs a, 
                     return far ? p - j >= a.W : j <= p && (a.W == 0 || p - j < a.W || (!apart && j < a.S));
                 }, lane, x, y);
             }
-            const bool part = far || (apart && j < a.S);
+            const bool part = j < summed;
 #pragma unroll
             for (int n = 0; n < RowLanes<DH>::N; ++n) {
                 if (!RowLanes<DH>::has(lane)) continue;
@@ -307,11 +321,11 @@ __device__ __forceinline__ void dkv_body(unsigned char* smem, const AttnArgs a, 
         }
         return;
     }
-    if (far || (apart && wk0 < a.S)) {
+    if (wk0 < summed) {
 #pragma unroll
         for (int cb = 0; cb < CB; ++cb) {
             const int j = wk0 + 16 * cb + c16;
-            if (j >= a.S) continue;
+            if (j >= (far ? a.S : min(summed, a.N))) continue;
             const float f = j <= wk1 ? 1.f : 0.f;
 #pragma unroll
             for (int db = 0; db < ND; ++db) {
@@ -337,15 +351,14 @@ __device__ __forceinline__ void dkv_body(unsigned char* smem, const AttnArgs a, 
         fk[cb] = scale;
         fv[cb] = 1.f;
     }
-    const int skip = apart ? a.S : 0;  // keys whose rows the last kernel writes
     const Rows to_k = a.dk, to_v = a.dv;
     store_rows<ST, DH, CB>(mine, dk, fk, lane, [&](int r) __attribute__((always_inline)) {
         const int j = wk0 + r;
-        return j < a.N && j >= skip ? row_ptr<ST>(to_k, b, hk, j) : nullptr;
+        return j < a.N && j >= summed ? row_ptr<ST>(to_k, b, hk, j) : nullptr;
     });
     store_rows<ST, DH, CB>(mine, dv, fv, lane, [&](int r) __attribute__((always_inline)) {
         const int j = wk0 + r;
-        return j < a.N && j >= skip ? row_ptr<ST>(to_v, b, hk, j) : nullptr;
+        return j < a.N && j >= summed ? row_ptr<ST>(to_v, b, hk, j) : nullptr;
     });
 }
 
@@ -416,59 +429,65 @@ __device__ __forceinline__ void dq_body(unsigned char* smem, const AttnArgs a, i
             // keys kmin + 0 .. TB - 1, no sinks: those of a row are a run (entries
             // past the list lie behind every row)
             const bool plain = e0 >= list.s && (a.W == 0 || kmin >= a.S);
+            auto products = [&](auto mc) __attribute__((always_inline)) {
+                constexpr bool masked = decltype(mc)::value;
 #pragma unroll
-            for (int u = 0; u < TB / 32; ++u) {  // 32 keys at a time
-                f32x4 s[QN][2], dp[QN][2];
+                for (int u = 0; u < TB / 32; ++u) {  // 32 keys at a time
+                    __builtin_amdgcn_sched_barrier(0);
+                    f32x4 s[QN][2], dp[QN][2];
 #pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    const int sb = 2 * u + x;
-#pragma unroll
-                    for (int qs = 0; qs < QN; ++qs) {
-                        s[qs][x] = zero4();
-                        dp[qs][x] = f32x4{ld[qs].y, ld[qs].y, ld[qs].y, ld[qs].y};  // the product adds to -D
-                    }
-#pragma unroll
-                    for (int st = 0; st < NS; ++st) {
-                        const Frag8<ST> ka = rd.rows(Kt, sb, st), va = rd.rows(Vt, sb, st);
+                    for (int x = 0; x < 2; ++x) {
+                        const int sb = 2 * u + x;
 #pragma unroll
                         for (int qs = 0; qs < QN; ++qs) {
-                            mma8(s[qs][x], ka, qf[qs][st]);
-                            mma8(dp[qs][x], va, gf[qs][st]);
+                            s[qs][x] = zero4();
+                            dp[qs][x] = f32x4{ld[qs].y, ld[qs].y, ld[qs].y, ld[qs].y};  // the product adds to -D
+                        }
+#pragma unroll
+                        for (int st = 0; st < NS; ++st) {
+                            const Frag8<ST> ka = rd.rows(Kt, sb, st), va = rd.rows(Vt, sb, st);
+#pragma unroll
+                            for (int qs = 0; qs < QN; ++qs) {
+                                mma8(s[qs][x], ka, qf[qs][st]);
+                                mma8(dp[qs][x], va, gf[qs][st]);
+                            }
+                        }
+#pragma unroll
+                        for (int qs = 0; qs < QN; ++qs)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i)
+                                dp[qs][x][i] *= __builtin_amdgcn_exp2f(__builtin_fmaf(s[qs][x][i], c2, -ld[qs].x));
+                        if (masked && plain) {
+#pragma unroll
+                            for (int qs = 0; qs < QN; ++qs) {
+                                const int d = pos[qs] - kmin - 4 * g;
+                                const Span run(a.W ? d - a.W + 1 : -4 * TB, d);
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) dp[qs][x][i] = run.has(16 * sb + i) ? dp[qs][x][i] : 0.f;
+                            }
+                        } else if (masked) {
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                const int e = e0 + 16 * sb + 4 * g + i, key = list.key(e);
+#pragma unroll
+                                for (int qs = 0; qs < QN; ++qs)
+                                    dp[qs][x][i] = e < list.count && sees(a, pos[qs], key) ? dp[qs][x][i] : 0.f;
+                            }
                         }
                     }
+                    Frag8<ST> df[QN];
 #pragma unroll
-                    for (int qs = 0; qs < QN; ++qs)
+                    for (int qs = 0; qs < QN; ++qs) df[qs] = pack_frag<ST>(dp[qs][0], dp[qs][1]);
 #pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            dp[qs][x][i] *= __builtin_amdgcn_exp2f(__builtin_fmaf(s[qs][x][i], c2, -ld[qs].x));
-                    if (!whole && plain) {
+                    for (int db = 0; db < ND; ++db) {
+                        const Frag8<ST> kf = rd.cols(Kt, u, db);
 #pragma unroll
-                        for (int qs = 0; qs < QN; ++qs) {
-                            const int d = pos[qs] - kmin - 4 * g;
-                            const Span run(a.W ? d - a.W + 1 : -4 * TB, d);
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) dp[qs][x][i] = run.has(16 * sb + i) ? dp[qs][x][i] : 0.f;
-                        }
-                    } else if (!whole) {
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const int e = e0 + 16 * sb + 4 * g + i, key = list.key(e);
-#pragma unroll
-                            for (int qs = 0; qs < QN; ++qs)
-                                dp[qs][x][i] = e < list.count && sees(a, pos[qs], key) ? dp[qs][x][i] : 0.f;
-                        }
+                        for (int qs = 0; qs < QN; ++qs) mma8(dq[qs][db], kf, df[qs]);
                     }
                 }
-                Frag8<ST> df[QN];
-#pragma unroll
-                for (int qs = 0; qs < QN; ++qs) df[qs] = pack_frag<ST>(dp[qs][0], dp[qs][1]);
-#pragma unroll
-                for (int db = 0; db < ND; ++db) {
-                    const Frag8<ST> kf = rd.cols(Kt, u, db);
-#pragma unroll
-                    for (int qs = 0; qs < QN; ++qs) mma8(dq[qs][db], kf, df[qs]);
-                }
-            }
+            };
+            if (whole) products(std::false_type{});
+            else products(std::true_type{});
         };
         for (int it0 = 0;; it0 += STG) {
             bool last = false;
@@ -515,13 +534,13 @@ __global__ __launch_bounds__(256, 2) void wattn_bwd_kernel(AttnArgs a, BwdGeom G
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     // key blocks, then chunks of far rows, then row blocks; each kind in
     // neighbouring order on an XCD (a key head's workgroups share its rows and keys)
-    const uint32_t heads = (uint32_t)a.B * a.Hkv, n0 = heads * G.nk, n1 = heads * G.ns * G.nc, n2 = heads * G.nq;
+    const uint32_t heads = (uint32_t)a.B * a.Hkv, n0 = heads * G.nk * G.kp, n1 = heads * G.ns * G.nc, n2 = heads * G.nq;
     uint32_t id = first + blockIdx.x;
     const bool one = first == 0 && gridDim.x == n0 + n1 + n2;
     if (id < n0) {
         if (one) id = xcd_logical_id(id, n0);
-        const int bh = id / G.nk, kb = id % G.nk;
-        dkv_body<ST, DH, CB, false>(smem, a, G, bh / a.Hkv, bh % a.Hkv, kb * 64 * CB, 0, sums);
+        const int per = G.nk * G.kp, bh = id / per, k = id % per;
+        dkv_body<ST, DH, CB, false>(smem, a, G, bh / a.Hkv, bh % a.Hkv, k / G.kp * 64 * CB, k % G.kp, sums);
     } else if (id < n0 + n1) {
         id -= n0;
         const int per = G.ns * G.nc, bh = id / per, k = id % per;
@@ -561,26 +580,36 @@ __global__ __launch_bounds__(256) void wattn_ld_kernel(AttnArgs a, uint32_t firs
     }
 }
 
-// dk and dv of the sinks: the window's pairs, then the chunks in order.
+// dk and dv of the keys whose sums are kept: the slots in order, 4 values per thread.
 template <typename ST, int DH>
-__global__ __launch_bounds__(256) void wattn_sinks_kernel(AttnArgs a, int slots, const float* __restrict__ sums) {
-    const int64_t keys = (int64_t)a.B * a.Hkv * a.S, all = keys * 2 * DH;
-    for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < all; e += (int64_t)gridDim.x * 256) {
+__global__ __launch_bounds__(256) void wattn_sums_kernel(AttnArgs a, BwdGeom G, const float* __restrict__ sums) {
+    const int slots = G.kp + G.nc;
+    const int64_t all = (int64_t)a.B * a.Hkv * G.keys * 2 * DH;
+    for (int64_t e = 4 * ((int64_t)blockIdx.x * 256 + threadIdx.x); e < all; e += 1024 * (int64_t)gridDim.x) {
         const int c = (int)(e % DH), which = (int)(e / DH % 2);
         const int64_t row = e / (2 * DH);
-        const int j = (int)(row % a.S), hk = (int)(row / a.S % a.Hkv), b = (int)(row / a.S / a.Hkv);
-        float s = 0.f;
+        const int j = (int)(row % G.keys), hk = (int)(row / G.keys % a.Hkv), b = (int)(row / G.keys / a.Hkv);
+        float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
-        for (int k = 0; k < slots; ++k) s += sums[k * all + e];
-        if (j >= seq_len_of(a.kl, b, a.N)) s = 0.f;
-        st1<ST>(row_ptr<ST>(which ? a.dv : a.dk, b, hk, j) + c, s);
+        for (int k = 0; k < slots; ++k) {
+            const float4 x = *reinterpret_cast<const float4*>(sums + k * all + e);
+            s.x += x.x, s.y += x.y, s.z += x.z, s.w += x.w;
+        }
+        if (j >= seq_len_of(a.kl, b, a.N)) s = make_float4(0.f, 0.f, 0.f, 0.f);
+        ST* to = row_ptr<ST>(which ? a.dv : a.dk, b, hk, j) + c;
+        if constexpr (sizeof(ST) == 2) *reinterpret_cast<uint2*>(to) = make_uint2(pack_bf16x2(s.x, s.y), pack_bf16x2(s.z, s.w));
+        else *reinterpret_cast<float4*>(to) = s;
     }
 }
 
 // Keys and rows per block.  Blocks of 128 halve the reads of the tiles per
 // product; blocks of 64 where those leave CUs idle.  128-wide heads keep to 64
 // keys (16 per wave): the sums of 32 keys and their operands are 192 registers
-// of a lane, which leaves too few for the rest at 2 waves per SIMD.
+// of a lane, which leaves too few for the rest at 2 waves per SIMD.  There the
+// transposed reads of the tiles take most of the LDS's time; workgroups of 8
+// waves, four for dv and four for dk of 32 keys each, halve them for one more
+// product, and measured slower (2 x 4096 tokens, 32 / 8 heads, window 1024,
+// training step: 787 against 687 us; 8 waves of 16 keys each: 722).
 bool wide_blocks(int dtype, const AttnArgs& a) {
     return dtype == kBF16 && (int64_t)a.B * a.Hkv * ((a.N + 127) / 128) >= 512;
 }
@@ -594,6 +623,16 @@ BwdGeom bwd_geom(int dtype, int dh, const AttnArgs& a) {
     G.nk = (a.N + kw - 1) / kw;
     G.nq = (int)((R + qw - 1) / qw);
     G.ns = a.W && a.S && a.S <= kSinkKeys ? (a.S + 63) / 64 : 0;
+    // Without a window the first keys' blocks are twice as long as the average.
+    // Where the key blocks are fewer than the workgroups that the chip holds, the
+    // longest alone would set the time: 2 x 2048 tokens, 16 / 4 heads of 128,
+    // training step: 325 us with whole blocks, 237 with parts.
+    const int64_t nk = (int64_t)a.B * a.Hkv * G.nk, tiles = R / 64;
+    int64_t kp = a.W == 0 && nk < 512 ? (1024 + nk - 1) / nk : 1;
+    if (kp > tiles / 8) kp = tiles / 8;
+    if (kp > kMaxParts) kp = kMaxParts;
+    G.kp = kp < 1 ? 1 : (int)kp;
+    G.keys = G.kp > 1 ? a.N : G.ns ? a.S : 0;
     // a chunk walks about as many rows as a key block does
     const int64_t c = (R + (int64_t)(a.W + kw) * a.G - 1) / ((int64_t)(a.W + kw) * a.G);
     G.nc = G.ns ? (int)(c < kSinkChunks ? c : kSinkChunks) : 0;
@@ -608,15 +647,14 @@ int launch_bwd(const AttnArgs& a, const BwdGeom& G, float* sums, hipStream_t str
     const size_t outs = 4 * (size_t)store_rows_bytes<ST, DH>(CB > QN ? CB : QN);
     const size_t lds = ring > outs ? ring : outs;
     if (allow_lds((const void*)kern, lds)) return -1;
-    const uint64_t blocks = (uint64_t)a.B * a.Hkv * ((uint64_t)G.nk + G.ns * G.nc + G.nq);
+    const uint64_t blocks = (uint64_t)a.B * a.Hkv * ((uint64_t)G.nk * G.kp + G.ns * G.nc + G.nq);
     const int e = launch_parts(blocks, 256, [&](uint32_t first, uint32_t n) {
         hipLaunchKernelGGL(kern, dim3(n), dim3(256), lds, stream, a, G, sums, first);
         return hipGetLastError() == hipSuccess ? 0 : -1;
     });
-    if (e || !G.ns) return e;
-    const int64_t all = (int64_t)a.B * a.Hkv * a.S * 2 * DH, n = (all + 255) / 256;
-    hipLaunchKernelGGL((wattn_sinks_kernel<ST, DH>), dim3((unsigned)(n < 65536 ? n : 65536)), dim3(256), 0, stream, a,
-                       1 + G.nc, sums);
+    if (e || !G.keys) return e;
+    const int64_t n = ((int64_t)a.B * a.Hkv * G.keys * 2 * DH + 1023) / 1024;
+    hipLaunchKernelGGL((wattn_sums_kernel<ST, DH>), dim3((unsigned)(n < 65536 ? n : 65536)), dim3(256), 0, stream, a, G, sums);
     return hipGetLastError() == hipSuccess ? 0 : -1;
 }
 
@@ -626,7 +664,7 @@ size_t ld_bytes(const AttnArgs& a) { return ((size_t)a.B * a.Hq * a.Tq * sizeof(
 
 size_t attn_bwd_scratch(int dtype, int dh, const AttnArgs& a) {
     const BwdGeom G = bwd_geom(dtype, dh, a);
-    return ld_bytes(a) + (G.ns ? (size_t)(1 + G.nc) * a.B * a.Hkv * a.S * 2 * dh * sizeof(float) : 0);
+    return ld_bytes(a) + (size_t)(G.kp + G.nc) * a.B * a.Hkv * G.keys * 2 * dh * sizeof(float);
 }
 
 int launch_window_attn_bwd(int dtype, int dh, AttnArgs a, void* scratch, hipStream_t stream) {

@@ -153,6 +153,11 @@ __global__ __launch_bounds__(256, 2) void wattn_fwd_kernel(AttnArgs a, FwdGeom G
                         }
                 }
             }
+            // The reference maximum moves only when the tile's exceeds it by more
+            // than 8 (log2 units): weights stay below 2^8, and O and l are rescaled
+            // only in tiles where some row of the wave moved.
+            float m_new[QN], m_use[QN];
+            bool moved = false;
 #pragma unroll
             for (int qs = 0; qs < QN; ++qs) {
                 float mloc = -__builtin_inff();  // over the raw scores (the scale is positive)
@@ -161,27 +166,31 @@ __global__ __launch_bounds__(256, 2) void wattn_fwd_kernel(AttnArgs a, FwdGeom G
 #pragma unroll
                     for (int i = 0; i < 4; ++i) mloc = fmaxf(mloc, s[qs][sb][i]);
                 mloc = rows4_max(mloc) * c2;
-                // The reference maximum moves only when the tile's exceeds it by
-                // more than 8 (log2 units): weights stay below 2^8, and O and l
-                // are rescaled only in tiles where some row of the wave moved.
-                const float m_new = mloc > m_run[qs] + 8.f ? mloc : m_run[qs];
-                const float m_use = m_new == -__builtin_inff() ? 0.f : m_new;
-                if (__builtin_amdgcn_ballot_w64(m_new != m_run[qs])) {
-                    const float alpha = __builtin_amdgcn_exp2f(m_run[qs] - m_use);
+                m_new[qs] = mloc > m_run[qs] + 8.f ? mloc : m_run[qs];
+                m_use[qs] = m_new[qs] == -__builtin_inff() ? 0.f : m_new[qs];
+                moved |= m_new[qs] != m_run[qs];
+            }
+            if (__builtin_amdgcn_ballot_w64(moved)) {
+#pragma unroll
+                for (int qs = 0; qs < QN; ++qs) {
+                    const float alpha = __builtin_amdgcn_exp2f(m_run[qs] - m_use[qs]);
                     l_run[qs] *= alpha;
 #pragma unroll
                     for (int db = 0; db < ND; ++db) o[qs][db] *= alpha;
-                    m_run[qs] = m_new;
+                    m_run[qs] = m_new[qs];
                 }
-                float lsum = 0.f;
+            }
+#pragma unroll
+            for (int qs = 0; qs < QN; ++qs) {
+                float lsum[2] = {0.f, 0.f};
 #pragma unroll
                 for (int sb = 0; sb < NB; ++sb)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        s[qs][sb][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[qs][sb][i], c2, -m_use));
-                        lsum += s[qs][sb][i];
+                        s[qs][sb][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[qs][sb][i], c2, -m_use[qs]));
+                        lsum[i & 1] += s[qs][sb][i];
                     }
-                l_run[qs] += lsum;  // this lane's keys; the 4 lanes of a row are added at the end
+                l_run[qs] += lsum[0] + lsum[1];  // this lane's keys; the 4 lanes of a row are added at the end
             }
             // O^T += V^T P^T, 32 keys at a time: slots 0..3 are keys 4 g + i of
             // block 2 u, slots 4..7 those of block 2 u + 1.  With bf16 storage P is

@@ -30,6 +30,13 @@ CASES = [
     (1, 2, 1, 128, 513, 513, 600, 9, "bhtd", None),        # a window of everything
     (1, 8, 1, 32, 5, 2050, 700, 3, "bthd", None),
     (2, 1, 1, 128, 3, 4100, 0, 0, "bhtd", ([3, 2], [4100, 1])),
+    # few key blocks with many rows: their rows in parts
+    (2, 8, 2, 64, 500, 700, 0, 0, "bthd", ([500, 77], [700, 300])),
+    (1, 12, 2, 128, 400, 400, 0, 3, "bhtd", None),
+    (1, 16, 4, 32, 333, 333, 0, 0, "packed", None),
+    # more heads to a key head than a tile has rows
+    (1, 70, 1, 32, 9, 40, 7, 2, "bthd", None),
+    (2, 130, 2, 64, 5, 70, 20, 1, "bhtd", ([5, 2], [70, 40])),
 ]
 IDS = [f"{c[0]}x{c[1]}/{c[2]}x{c[3]}-{c[4]}of{c[5]}-w{c[6]}s{c[7]}" for c in CASES]
 
