@@ -36,10 +36,12 @@ struct CacheBlock {
 __host__ __device__ inline size_t cache_block_bytes(int ps, int dh) { return (size_t)ps * (dh + dh / 32 * 8); }
 
 // The block and the place in it of position t of sequence b, head h; false
-// where the table ends or names no page.
-__device__ __forceinline__ bool cache_find(const CacheArgs& c, int b, int h, int t, CacheBlock& blk, int& tl) {
-    const int e = t / c.ps;
-    if (t < 0 || e >= c.per) return false;
+// where the table ends or names no page.  page_div: by the page size.
+__device__ __forceinline__ bool cache_find(const CacheArgs& c, const UDiv& page_div, int b, int h, int t, CacheBlock& blk,
+                                           int& tl) {
+    if (t < 0) return false;
+    const int e = page_div.div(t);
+    if (e >= c.per) return false;
     const int page = c.table[(size_t)b * c.per + e];
     if (page < 0 || page >= c.pages) return false;
     blk.at = ((size_t)page * c.H + h) * cache_block_bytes(c.ps, c.dh);

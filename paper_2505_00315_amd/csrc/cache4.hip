@@ -1,5 +1,6 @@
 // The 4-bit cache: rows written and read back (attention over it: cache4_attn.hip).
 #include "cache4.h"
+#include "launch_parts.h"
 
 namespace mosa {
 
@@ -27,44 +28,53 @@ __device__ __forceinline__ void store8(float* p, const float (&x)[8]) {
     reinterpret_cast<float4*>(p)[1] = make_float4(x[4], x[5], x[6], x[7]);
 }
 
-// Meta word and codes of a lane's 8 columns of a group of 32 (its 4 lanes).
+// Meta word and codes (a nibble each) of a lane's 8 columns of a group of 32 (its
+// 4 lanes).
 //
 // The code is the integer nearest to d / s, ties to even, for d = x - m in
-// fp32.  With n the integer part of d (1 / s), which may be off by one near an
-// integer, the sign of d - (n + 1/2) s decides between n and n + 1 exactly: the
-// product has 13 bits and the fused sum is rounded once, which keeps its sign.
-__device__ __forceinline__ uint32_t quantise8(const float (&x)[8], uint32_t (&code)[8]) {
-    float lo = x[0], hi = x[0], bad = 0.f;
+// fp32.  c, d (1 / s) rounded to an integer, may be off by one next to a
+// midpoint, and the remainder d - c s decides exactly: the product has 13 bits
+// and the fused sum is rounded once, which keeps its order against s / 2.  An odd
+// c is left at the midpoint too, an even one only past it.
+__device__ __forceinline__ uint32_t quantise8(const float (&x)[8], uint32_t& word) {
+    // (maximum and minimum hand on NaN)
+    float lo = x[0], hi = x[0];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        lo = fminf(lo, x[i]);
-        hi = fmaxf(hi, x[i]);
-        bad += x[i] * 0.f;  // NaN for infinities and NaN
+    for (int i = 1; i < 8; ++i) {
+        lo = __builtin_elementwise_minimum(lo, x[i]);
+        hi = __builtin_elementwise_maximum(hi, x[i]);
     }
-    lo = fminf(lo, dpp_f32<0xB1, 0xf>(lo));
-    hi = fmaxf(hi, dpp_f32<0xB1, 0xf>(hi));
-    bad += dpp_f32<0xB1, 0xf>(bad);
-    lo = fminf(lo, dpp_f32<0x4E, 0xf>(lo));
-    hi = fmaxf(hi, dpp_f32<0x4E, 0xf>(hi));
-    bad += dpp_f32<0x4E, 0xf>(bad);
+    lo = __builtin_elementwise_minimum(lo, dpp_f32<0xB1, 0xf>(lo));
+    hi = __builtin_elementwise_maximum(hi, dpp_f32<0xB1, 0xf>(hi));
+    lo = __builtin_elementwise_minimum(lo, dpp_f32<0x4E, 0xf>(lo));
+    hi = __builtin_elementwise_maximum(hi, dpp_f32<0x4E, 0xf>(hi));
     const uint32_t mb = f32_to_bf16(lo);
     const float m = __uint_as_float(mb << 16);
-    const float range = hi - m;
-    uint32_t sb = f32_to_bf16(range * (1.f / 15.f));
+    uint32_t sb = f32_to_bf16((hi - m) * (1.f / 15.f));
     float s = __uint_as_float(sb << 16);
+    // an infinity among the values makes m or s infinite or NaN, a NaN both
+    const bool ok = fabsf(m) < __builtin_inff() && fabsf(s) < __builtin_inff();
     if (!(s >= 1.17549435e-38f)) s = 0.f, sb = 0;
-    const bool ok = bad == 0.f && s < __builtin_inff() && fabsf(m) < __builtin_inff();
-    const float inv = s > 0.f && ok ? 1.f / s : 0.f;
+    const float inv = s > 0.f && ok ? 1.f / s : 0.f, half = 0.5f * s;
+    float c[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const float d = x[i] - m;
-        const float n = fminf(fmaxf(floorf(d * inv), 0.f), 15.f);
-        const float over = __builtin_fmaf(-(n + 0.5f), s, d);
-        const bool up = over > 0.f || (over == 0.f && ((int)n & 1));
-        const int c = min((int)n + (up ? 1 : 0), 15);
-        code[i] = inv > 0.f ? c : 0;
+        const float d = x[i] - m, n = __builtin_rintf(d * inv), r = __builtin_fmaf(-n, s, d);
+        const uint32_t odd = __float_as_uint(n + 8388608.f) & 1;
+        const float limit = __uint_as_float(__float_as_uint(half) - odd);  // the number next below half
+        c[i] = __builtin_amdgcn_fmed3f(n + (fabsf(r) > limit ? __builtin_copysignf(1.f, r) : 0.f), 0.f, 15.f);
     }
+    const float a = __builtin_fmaf(__builtin_fmaf(__builtin_fmaf(c[3], 16.f, c[2]), 16.f, c[1]), 16.f, c[0]);
+    const float b = __builtin_fmaf(__builtin_fmaf(__builtin_fmaf(c[7], 16.f, c[6]), 16.f, c[5]), 16.f, c[4]);
+    word = inv > 0.f ? (uint32_t)a | (uint32_t)b << 16 : 0u;
     return ok ? sb | (mb << 16) : 0x7fc00000u;
+}
+
+// The K word of 8 codes: column 2 i in nibble i, column 2 i + 1 in nibble i + 4.
+__device__ __forceinline__ uint32_t k_order(uint32_t w) {
+    uint32_t e = w & 0x0f0f0f0fu, o = w >> 4 & 0x0f0f0f0fu;  // the even columns' nibbles, the odd ones'
+    e = (e | e >> 4) & 0x00ff00ffu, o = (o | o >> 4) & 0x00ff00ffu;
+    return (e & 0xffu) | (e >> 8 & 0xff00u) | (o & 0xffu) << 16 | (o >> 16) << 24;
 }
 
 // V's column order: a lane's 8 columns 8 li .. + 7 are the pairs c = 4 (li % 4) +
@@ -106,48 +116,66 @@ __device__ __forceinline__ uint32_t v_untrade(uint32_t w, int li) {
     }
 }
 
-// Where a quad's lane works: its position, the row it comes from or goes to,
-// and its block of the cache.
+// Workgroups of a (sequence, head): each takes `span` quads of it, QPB at a time.
+struct QuadGeom {
+    UDiv per, heads, page;  // by the workgroups of a head, the heads, the page size
+    int span;
+};
+
+// What a workgroup's quads have in common.
+template <int DH>
+struct QuadRun {
+    int b, h, q0, len;
+    int64_t start;
+    __device__ __forceinline__ QuadRun(const CacheArgs& c, const QuadGeom& G, uint32_t id) {
+        const int bh = G.per.div((int)id);
+        q0 = ((int)id - bh * (int)G.per.n) * G.span;
+        b = G.heads.div(bh);
+        h = bh - b * (int)G.heads.n;
+        start = c.start ? c.start[b] : 0;
+        len = seq_len_of(c.lens, b, c.rows);
+    }
+};
+
+// Where a quad's lane works: the row t that it takes or fills, and its place in the cache.
 struct QuadSpot {
-    int b, h, t, pos, tl;
-    bool live, held;  // a row of the call; a position of the cache
+    int64_t t, pos;
+    int tl;
+    bool live, mine, held;  // a row of the call; within its length; on a page
     CacheBlock blk;
 };
 template <int DH>
-__device__ __forceinline__ bool quad_spot(const CacheArgs& c, int64_t quad, int quads, int lane, QuadSpot& s) {
-    if (quad >= (int64_t)c.B * c.H * quads) return false;
-    const int qi = (int)(quad % quads);
-    s.h = (int)(quad / quads % c.H);
-    s.b = (int)(quad / quads / c.H);
-    const int64_t start = c.start ? c.start[s.b] : 0;
-    // positions (start & ~3) + 4 qi + 0 .. 3
-    const int64_t pos = (start & ~(int64_t)3) + 4 * (int64_t)qi + lane / Quad<DH>::LPP, t = pos - start;
-    s.t = (int)t;
-    s.live = t >= 0 && t < c.rows;
-    s.pos = (int)pos;
-    s.held = s.live && t < seq_len_of(c.lens, s.b, c.rows) && pos <= 0x7fffffff && cache_find(c, s.b, s.h, s.pos, s.blk, s.tl);
-    return true;
+__device__ __forceinline__ QuadSpot quad_row(const CacheArgs& c, const QuadRun<DH>& r, int quad, int lane) {
+    QuadSpot s;
+    // positions (start & ~3) + 4 quad + 0 .. 3
+    s.pos = (r.start & ~(int64_t)3) + 4 * (int64_t)quad + lane / Quad<DH>::LPP;
+    s.t = s.pos - r.start;
+    s.live = s.t >= 0 && s.t < c.rows;
+    s.mine = s.t >= 0 && s.t < r.len && s.pos >= 0 && s.pos <= 0x7fffffff;
+    return s;
+}
+template <int DH>
+__device__ __forceinline__ void quad_place(const CacheArgs& c, const QuadGeom& G, const QuadRun<DH>& r, QuadSpot& s) {
+    s.held = s.mine && cache_find(c, G.page, r.b, r.h, (int)s.pos, s.blk, s.tl);
 }
 
 template <typename ST, int DH>
-__global__ __launch_bounds__(256) void cache4_append_kernel(CacheArgs c, int quads) {
+__global__ __launch_bounds__(256) void cache4_append_kernel(CacheArgs c, QuadGeom G, uint32_t first) {
     using Q = Quad<DH>;
     const int lane = threadIdx.x % Q::LPQ, li = lane % Q::LPP;
-    for (int64_t quad = (int64_t)blockIdx.x * Q::QPB + threadIdx.x / Q::LPQ;; quad += (int64_t)gridDim.x * Q::QPB) {
-        QuadSpot s;
-        if (!quad_spot<DH>(c, quad, quads, lane, s)) break;
+    const QuadRun<DH> run(c, G, first + blockIdx.x);
+    for (int quad = threadIdx.x / Q::LPQ; quad < G.span; quad += Q::QPB) {
+        QuadSpot s = quad_row<DH>(c, run, run.q0 + quad, lane);
         float x[8] = {}, y[8] = {};
-        if (s.held) {
-            load8<ST>(row_ptr<ST>(c.k, s.b, s.h, s.t) + 8 * li, x);
-            load8<ST>(row_ptr<ST>(c.v, s.b, s.h, s.t) + 8 * li, y);
+        if (s.mine) {
+            load8<ST>(row_ptr<ST>(c.k, run.b, run.h, s.t) + 8 * li, x);
+            load8<ST>(row_ptr<ST>(c.v, run.b, run.h, s.t) + 8 * li, y);
         }
-        uint32_t kc[8], vc[8];
-        const uint32_t km = quantise8(x, kc), vm = quantise8(y, vc);
+        quad_place<DH>(c, G, run, s);
+        uint32_t kw, vw;
+        const uint32_t km = quantise8(x, kw), vm = quantise8(y, vw);
         // V: a word takes the pieces of two neighbouring positions, the even
         // one's lane the first of its two pieces, the odd one's the second
-        uint32_t vw = 0;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) vw |= vc[i] << (4 * i);
         vw = v_trade<DH>(vw, li);
         const uint32_t v0 = vw & 0xffffu, v1 = vw >> 16;
         const int unit = v_unit<DH>(li);
@@ -155,11 +183,8 @@ __global__ __launch_bounds__(256) void cache4_append_kernel(CacheArgs c, int qua
         const uint32_t theirs = __shfl(vw, other, 64);
         const int both = __shfl((int)s.held, other, 64);
         if (!s.held) continue;
-        uint32_t w = 0;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) w |= kc[2 * i] << (4 * i) | kc[2 * i + 1] << (4 * i + 16);
         const int g = li >> 2, kg = li & 3;
-        *reinterpret_cast<uint32_t*>(c.cache + s.blk.kword(s.tl, kg * (DH / 32) + g)) = w;
+        *reinterpret_cast<uint32_t*>(c.cache + s.blk.kword(s.tl, kg * (DH / 32) + g)) = k_order(kw);
         if (both) {
             const bool odd = s.tl & 1;
             const uint32_t word = odd ? (theirs >> 16 | v1 << 16) : (v0 | theirs << 16);
@@ -176,12 +201,13 @@ __global__ __launch_bounds__(256) void cache4_append_kernel(CacheArgs c, int qua
 }
 
 template <typename ST, int DH>
-__global__ __launch_bounds__(256) void cache4_read_kernel(CacheArgs c, int quads) {
+__global__ __launch_bounds__(256) void cache4_read_kernel(CacheArgs c, QuadGeom G, uint32_t first) {
     using Q = Quad<DH>;
     const int lane = threadIdx.x % Q::LPQ, li = lane % Q::LPP, g = li >> 2, kg = li & 3;
-    for (int64_t quad = (int64_t)blockIdx.x * Q::QPB + threadIdx.x / Q::LPQ;; quad += (int64_t)gridDim.x * Q::QPB) {
-        QuadSpot s;
-        if (!quad_spot<DH>(c, quad, quads, lane, s)) break;
+    const QuadRun<DH> run(c, G, first + blockIdx.x);
+    for (int quad = threadIdx.x / Q::LPQ; quad < G.span; quad += Q::QPB) {
+        QuadSpot s = quad_row<DH>(c, run, run.q0 + quad, lane);
+        quad_place<DH>(c, G, run, s);
         float x[8] = {}, y[8] = {};
         uint32_t w = 0, v = 0, km = 0, vm = 0;
         if (s.held) {
@@ -201,17 +227,25 @@ __global__ __launch_bounds__(256) void cache4_read_kernel(CacheArgs c, int quads
                 y[i] = cache_value(vm, (v >> (4 * i)) & 15);
             }
         }
-        store8(row_ptr<ST>(c.k, s.b, s.h, s.t) + 8 * li, x);
-        store8(row_ptr<ST>(c.v, s.b, s.h, s.t) + 8 * li, y);
+        store8(row_ptr<ST>(c.k, run.b, run.h, s.t) + 8 * li, x);
+        store8(row_ptr<ST>(c.v, run.b, run.h, s.t) + 8 * li, y);
     }
 }
 
 template <class K>
-int launch_quads(K kern, const CacheArgs& c, int per_block, hipStream_t stream) {
+int launch_quads(K kern, const CacheArgs& c, int per_pass, hipStream_t stream) {
     const int quads = c.rows / 4 + 2;  // of a sequence and head: a start inside a quad adds one
-    const int64_t all = (int64_t)c.B * c.H * quads, blocks = (all + per_block - 1) / per_block;
-    hipLaunchKernelGGL(kern, dim3((unsigned)(blocks < (1 << 20) ? blocks : 1 << 20)), dim3(256), 0, stream, c, quads);
-    return hipGetLastError() == hipSuccess ? 0 : -1;
+    // up to 16 passes per workgroup, where that leaves 16 workgroups to a CU
+    const int64_t passes = (int64_t)c.B * c.H * ((quads + per_pass - 1) / per_pass);
+    const int64_t each = passes / 4096 < 1 ? 1 : passes / 4096 > 16 ? 16 : passes / 4096;
+    QuadGeom G;
+    G.span = (int)each * per_pass;
+    const int per = (quads + G.span - 1) / G.span;
+    G.per = make_udiv((uint32_t)per), G.heads = make_udiv((uint32_t)c.H), G.page = make_udiv((uint32_t)c.ps);
+    return launch_parts((uint64_t)c.B * c.H * per, 256, [&](uint32_t first, uint32_t blocks) {
+        hipLaunchKernelGGL(kern, dim3(blocks), dim3(256), 0, stream, c, G, first);
+        return hipGetLastError() == hipSuccess ? 0 : -1;
+    });
 }
 
 }  // namespace

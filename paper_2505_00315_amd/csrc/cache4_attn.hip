@@ -392,7 +392,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache4_attn_kernel(AttnArgs a,
             float q[RowLanes<DH>::N], x[RowLanes<DH>::N], m, l;
             row_load<ST, DH>(qrow_ptr<ST>(a, a.q, b, hk, r, i), lane, q);
             const int mine = max(tend - tbeg - wave + kWaves - 1, 0) / kWaves;  // tiles of this wave
-            row_attend<DH>(a, CacheKeys<DH>{c, b, hk}, [&](int e) {
+            row_attend<DH>(a, CacheKeys<DH>{c, G.page, b, hk}, [&](int e) {
                 const int oc = 4 * (tbeg + wave + kWaves * (e / 32)) + e / 8 % 4;
                 return oc < list.count ? list.first_key(oc) + e % 8 : -1;
             }, 0, 32 * mine, off + i, kn, q, lane, m, l, x);

@@ -60,11 +60,12 @@ struct WideKeys {
 template <int DH>
 struct CacheKeys {
     const CacheArgs& c;
+    UDiv page;
     int b, h;
     __device__ __forceinline__ bool load(int j, int lane, float (&k)[RowLanes<DH>::N], float (&v)[RowLanes<DH>::N]) const {
         CacheBlock blk;
         int tl;
-        if (!cache_find(c, b, h, j, blk, tl)) return false;
+        if (!cache_find(c, page, b, h, j, blk, tl)) return false;
 #pragma unroll
         for (int i = 0; i < RowLanes<DH>::N; ++i) {
             k[i] = RowLanes<DH>::has(lane) ? cache_k(c, blk, tl, lane + 64 * i) : 0.f;
