@@ -19,6 +19,12 @@
 // two ahead; the waves of a workgroup are joined in LDS, parts of the keys by
 // merge_parts.  Scores have the key in the lane, which so has the scales of its
 // key at hand for both products; the weights change lanes through LDS.
+//
+// Beside the bytes it is vector instructions that count: two for every pair of
+// codes, and, per tile and lane, those for RI score rows of two keys.  A lane of
+// the 16 x 16 result has rows 4 g .. 4 g + 3, so up to 4 query rows are put in rows
+// 0, 4, 8, 12 (RI = 1), up to 8 in rows 4 g and 4 g + 1, and no lane works on rows
+// that are none.
 #include "cache4.h"
 #include "launch_parts.h"
 #include "rowattn.h"
@@ -51,10 +57,18 @@ struct AttnLds {
     static constexpr int PW = SPLIT * NG * 16 * PROW;    // of a wave and 16 rows
 };
 
-__device__ __forceinline__ uint32_t codes(uint32_t w, int nib) {  // nibbles nib and nib + 4 of w as bf16 16 + n
-    const int sh = 4 * nib - 3;
-    return ((sh < 0 ? w << 3 : w >> sh) & 0x00780078u) | 0x41804180u;
-}
+// Nibbles nib and nib + 4 of w as bf16 16 + n.  The constants are registers, so
+// that the mask and the 16 are one instruction.
+struct CodeBits {
+    uint32_t mask, sixteen;
+    __device__ __forceinline__ CodeBits() : mask(0x00780078u), sixteen(0x41804180u) {
+        asm volatile("" : "+v"(mask), "+v"(sixteen));
+    }
+    __device__ __forceinline__ uint32_t operator()(uint32_t w, int nib) const {
+        const int sh = 4 * nib - 3;
+        return ((sh < 0 ? w << 3 : w >> sh) & mask) | sixteen;
+    }
+};
 
 template <int N>
 __device__ __forceinline__ void load_words(const unsigned char* p, uint32_t (&w)[N]) {
@@ -96,15 +110,16 @@ __device__ __forceinline__ float lanes16_sum(float x) {
 }
 
 struct CacheGeom {
-    int nb, parts;  // blocks of 16 NQ rows per (b, key head), parts of their keys
+    int nb, parts;  // blocks of rows per (b, key head), parts of their keys
     UDiv page;      // by the page size
 };
 
 // SPLIT: bf16 parts of q and of the weights (1 for bf16 storage, 3 for fp32).
-template <typename ST, int DH, int NQ>
+// A block has 4 RI NQ rows: row (4 q + g) RI + i is row 4 g + i of result q.
+template <typename ST, int DH, int NQ, int RI>
 __global__ __launch_bounds__(64 * kWaves, 2) void cache4_attn_kernel(AttnArgs a, CacheArgs c, CacheGeom G, Parts part,
                                                                     uint32_t first) {
-    constexpr int SPLIT = sizeof(ST) == 2 ? 1 : 3, NG = DH / 32, ND = DH / 16;
+    constexpr int SPLIT = sizeof(ST) == 2 ? 1 : 3, NG = DH / 32, ND = DH / 16, RB = 4 * RI * NQ;
     using L = AttnLds<DH, SPLIT>;
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, c16 = lane & 15;
@@ -112,30 +127,30 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache4_attn_kernel(AttnArgs a,
     const int pt = (int)(id % G.parts);
     id /= G.parts;
     const int blk = (int)(id % G.nb), bh = (int)(id / G.nb), b = bh / a.Hkv, hk = bh % a.Hkv;
-    const int R = a.Tq * a.G, r0 = blk * 16 * NQ;
+    const int R = a.Tq * a.G, r0 = blk * RB;
     const int qn = seq_len_of(a.ql, b, a.Tq), kn = seq_len_of(a.kl, b, a.N), off = kn - qn, rn = qn * a.G;
 
     KeyList keys{0, 0, 0};
     int p0 = 0, p1 = 0;  // positions of the block's first and last row
     if (r0 < rn) {
         p0 = off + a.gd.div(r0);
-        p1 = off + a.gd.div(min(r0 + 16 * NQ, rn) - 1);
+        p1 = off + a.gd.div(min(r0 + RB, rn) - 1);
         keys = keys_of(a, p0, p1, kn);
     }
     const OctetList list = octets_of(keys);
     const int all = (list.count + 3) / 4, share = (all + G.parts - 1) / G.parts;
     const int tbeg = min(pt * share, all), tend = min(all, tbeg + share);  // this part's tiles; a wave takes every fourth
 
-    float m_run[NQ][4], l_run[NQ][4], pm[NQ][NG][4];
+    float m_run[NQ][RI], l_run[NQ][RI], pm[NQ][NG][RI];
     f32x4 o[NQ][ND], ones[NQ][NG];
-    int pos[NQ][4];
+    int pos[NQ][RI];
 #pragma unroll
     for (int q = 0; q < NQ; ++q) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < RI; ++i) {
             m_run[q][i] = -__builtin_inff();
             l_run[q][i] = 0.f;
-            pos[q][i] = off + a.gd.div(min(r0 + 16 * q + 4 * g + i, max(rn, 1) - 1));
+            pos[q][i] = off + a.gd.div(min(r0 + (4 * q + g) * RI + i, max(rn, 1) - 1));
 #pragma unroll
             for (int gr = 0; gr < NG; ++gr) pm[q][gr][i] = 0.f;
         }
@@ -146,13 +161,49 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache4_attn_kernel(AttnArgs a,
     }
 
     if (tbeg + wave < tend) {
-        // q as A operand: row c16, columns 32 gr + 8 g .. + 7, in SPLIT parts;
+        const size_t block = cache_block_bytes(c.ps, DH);
+        const int32_t* table = c.table + (size_t)b * c.per;
+        // Where the octets of tile t are that this lane reads, that of its two
+        // keys and that of V: page, place in the page, and the keys.
+        struct Spots { int k, v, tk, tv, key; };
+        auto octet = [&](int t, int x) __attribute__((always_inline)) { return list.first_key(min(4 * t + x, list.count - 1)); };
+        auto spots = [&](int t) __attribute__((always_inline)) {
+            t = min(t, tend - 1);
+            const int ek = octet(t, c16 >> 2), ev = octet(t, g), pk = G.page.div(ek), pv = G.page.div(ev);
+            return Spots{table[pk], table[pv], ek - pk * c.ps + 2 * (c16 & 3), ev - pv * c.ps,
+                         4 * t + (c16 >> 2) < list.count ? ek + 2 * (c16 & 3) : -2};
+        };
+        auto load = [&](const Spots& sp, Tile<DH>& x) __attribute__((always_inline)) {
+            const bool kin = sp.k >= 0 && sp.k < c.pages, vin = sp.v >= 0 && sp.v < c.pages;
+            x.key = kin ? sp.key : -2;
+            // (a page that does not exist: page 0 is read and masked)
+            const unsigned char* kb = c.cache + ((size_t)(kin ? sp.k : 0) * c.H + hk) * block;
+            const unsigned char* vb = c.cache + ((size_t)(vin ? sp.v : 0) * c.H + hk) * block;
+            const unsigned char* kc = kb + sp.tk * (DH / 2) + g * (DH / 8);
+            const unsigned char* km = kb + c.ps * DH + sp.tk * (DH / 8);
+            const unsigned char* vm = km + c.ps * (DH / 8);
+            const unsigned char* vc = vb + c.ps * (DH / 2) + sp.tv * (DH / 2) + (DH == 32 ? c16 / 2 * 8 : c16 * (DH / 8));
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+                load_words<NG>(kc + y * (DH / 2), x.kc[y]);
+                load_words<NG>(km + y * (DH / 8), x.km[y]);
+                load_words<NG>(vm + y * (DH / 8), x.vm[y]);
+                load_words<Tile<DH>::NV>(vc + y * (2 * DH), x.vc[y]);
+            }
+        };
+        // the first tile is on its way while q is prepared
+        Tile<DH> even, odd;
+        Spots sp = spots(tbeg + wave);
+        load(sp, even);
+        sp = spots(tbeg + wave + kWaves);
+
+        // q as A operand: columns 32 gr + 8 g .. + 7 of the row, in SPLIT parts;
         // its sums over a group, times (-16, 1), as the operand of the words (s, m):
         // lane group 0 holds the upper bf16 part, 1 and 2 what that leaves
         bf16x8 qf[NQ][SPLIT][NG], qs[NQ];
 #pragma unroll
         for (int q = 0; q < NQ; ++q) {
-            const int r = min(r0 + 16 * q + c16, rn - 1);
+            const int r = min(r0 + (4 * q + (c16 >> 2)) * RI + min(c16 & 3, RI - 1), rn - 1);
             const ST* qp = qrow_ptr<ST>(a, a.q, b, hk, r, a.gd.div(r));
             uint32_t sums[4] = {0, 0, 0, 0};
 #pragma unroll
@@ -163,11 +214,11 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache4_attn_kernel(AttnArgs a,
                 for (int e = 0; e < 8; ++e) s += x[e];
                 s = rows4_sum(s);
 #pragma unroll
-                for (int sp = 0; sp < SPLIT; ++sp) {
-                    qf[q][sp][gr] = frag8_from<uint16_t>(x).v;
+                for (int sp2 = 0; sp2 < SPLIT; ++sp2) {
+                    qf[q][sp2][gr] = frag8_from<uint16_t>(x).v;
                     float y[8];
                     Frag8<uint16_t> f;
-                    f.v = qf[q][sp][gr];
+                    f.v = qf[q][sp2][gr];
                     frag8_to_f32<uint16_t>(f, y);
 #pragma unroll
                     for (int e = 0; e < 8; ++e) x[e] -= y[e];
@@ -178,51 +229,17 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache4_attn_kernel(AttnArgs a,
             }
             qs[q] = frag_of(sums[0], sums[1], sums[2], sums[3]);
         }
-
-        const size_t block = cache_block_bytes(c.ps, DH);
-        const int32_t* table = c.table + (size_t)b * c.per;
-        // pages of the octets of tile t: that of this lane's two keys, and that of its octet of V
-        struct Pages { int k, v; };
-        auto octet = [&](int t, int x) { return list.first_key(min(4 * t + x, list.count - 1)); };
-        auto pages = [&](int t) {
-            t = min(t, tend - 1);
-            return Pages{table[G.page.div(octet(t, c16 >> 2))], table[G.page.div(octet(t, g))]};
-        };
-        auto load = [&](int t, const Pages& pg, Tile<DH>& x) {
-            t = min(t, tend - 1);
-            const int ek = octet(t, c16 >> 2), ev = octet(t, g);
-            const bool kin = pg.k >= 0 && pg.k < c.pages && 4 * t + (c16 >> 2) < list.count;
-            const bool vin = pg.v >= 0 && pg.v < c.pages;
-            const int tk = ek - G.page.div(ek) * c.ps + 2 * (c16 & 3), tv = ev - G.page.div(ev) * c.ps;
-            x.key = kin ? ek + 2 * (c16 & 3) : -2;
-            // (a page that does not exist: page 0 is read and masked)
-            const unsigned char* kb = c.cache + ((size_t)(kin ? pg.k : 0) * c.H + hk) * block;
-            const unsigned char* vb = c.cache + ((size_t)(vin ? pg.v : 0) * c.H + hk) * block;
-#pragma unroll
-            for (int y = 0; y < 2; ++y) {
-                load_words<NG>(kb + (tk + y) * (DH / 2) + g * (DH / 8), x.kc[y]);
-                load_words<NG>(kb + c.ps * DH + (tk + y) * (DH / 8), x.km[y]);
-                load_words<NG>(kb + c.ps * (DH + DH / 8) + (tk + y) * (DH / 8), x.vm[y]);
-                load_words<Tile<DH>::NV>(vb + c.ps * (DH / 2) + (tv / 4 + y) * (2 * DH) + (DH == 32 ? c16 / 2 * 8 : c16 * (DH / 8)),
-                                         x.vc[y]);
-            }
-        };
         const float c2 = a.scale * kLog2e;
         unsigned char* pw = smem + wave * NQ * L::PW;  // this wave's weights
         const bf16x8 one8 = frag_of(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u);
+        const CodeBits codes;
 
-        Tile<DH> cur, nxt;
-        Pages pg = pages(tbeg + wave);
-        load(tbeg + wave, pg, nxt);
-        pg = pages(tbeg + wave + kWaves);
-#pragma unroll 1
-        for (int t = tbeg + wave; t < tend; t += kWaves) {
-            cur = nxt;
-            load(t + kWaves, pg, nxt);
-            pg = pages(t + 2 * kWaves);
+        auto tile_step = [&](int t, Tile<DH>& cur, Tile<DH>& nxt) __attribute__((always_inline)) {
+            load(sp, nxt);
+            sp = spots(t + 2 * kWaves);
 
             // scores of rows 4 g + i and keys cur.key + y
-            f32x4 s[NQ][2];
+            float s[NQ][2][RI];
 #pragma unroll
             for (int y = 0; y < 2; ++y) {
                 bf16x8 meta;
@@ -230,8 +247,11 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache4_attn_kernel(AttnArgs a,
                 else if constexpr (NG == 2) meta = frag_of(cur.km[y][0], cur.km[y][1], 0, 0);
                 else meta = frag_of(cur.km[y][0], 0, 0, 0);
 #pragma unroll
-                for (int q = 0; q < NQ; ++q)
-                    s[q][y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(qs[q], meta, zero4(), 0, 0, 0);
+                for (int q = 0; q < NQ; ++q) {
+                    const f32x4 x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(qs[q], meta, zero4(), 0, 0, 0);
+#pragma unroll
+                    for (int i = 0; i < RI; ++i) s[q][y][i] = x[i];
+                }
 #pragma unroll
                 for (int gr = 0; gr < NG; ++gr) {
                     const uint32_t w = cur.kc[y][gr];
@@ -241,10 +261,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache4_attn_kernel(AttnArgs a,
                     for (int q = 0; q < NQ; ++q) {
                         f32x4 x = zero4();
 #pragma unroll
-                        for (int sp = SPLIT - 1; sp >= 0; --sp)
-                            x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(qf[q][sp][gr], kf, x, 0, 0, 0);
+                        for (int p = SPLIT - 1; p >= 0; --p)
+                            x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(qf[q][p][gr], kf, x, 0, 0, 0);
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) s[q][y][i] = __builtin_fmaf(x[i], sc, s[q][y][i]);
+                        for (int i = 0; i < RI; ++i) s[q][y][i] = __builtin_fmaf(x[i], sc, s[q][y][i]);
                     }
                 }
             }
@@ -261,7 +281,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache4_attn_kernel(AttnArgs a,
 #pragma unroll
                     for (int q = 0; q < NQ; ++q)
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
+                        for (int i = 0; i < RI; ++i) {
                             const bool ok = in && sees(a, pos[q][i], key);
                             s[q][y][i] = ok ? s[q][y][i] : -__builtin_inff();
                             any |= ok;
@@ -278,12 +298,12 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache4_attn_kernel(AttnArgs a,
 #pragma unroll
             for (int q = 0; q < NQ; ++q)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) up |= fmaxf(s[q][0][i], s[q][1][i]) * c2 > m_run[q][i] + 8.f;
+                for (int i = 0; i < RI; ++i) up |= fmaxf(s[q][0][i], s[q][1][i]) * c2 > m_run[q][i] + 8.f;
             if (__builtin_amdgcn_ballot_w64(up)) {
 #pragma unroll
                 for (int q = 0; q < NQ; ++q)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
+                    for (int i = 0; i < RI; ++i) {
                         const float top = lanes16_max(fmaxf(s[q][0][i], s[q][1][i])) * c2;
                         const float mn = fmaxf(m_run[q][i], top);
                         const float al = mn == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f(m_run[q][i] - mn);
@@ -301,7 +321,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache4_attn_kernel(AttnArgs a,
 #pragma unroll
             for (int q = 0; q < NQ; ++q)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
+                for (int i = 0; i < RI; ++i) {
                     const float mu = m_run[q][i] == -__builtin_inff() ? 0.f : m_run[q][i];
                     const float w0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[q][0][i], c2, -mu));
                     const float w1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[q][1][i], c2, -mu));
@@ -312,9 +332,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache4_attn_kernel(AttnArgs a,
                         pm[q][gr][i] = __builtin_fmaf(w1, __uint_as_float(cur.vm[1][gr] & 0xffff0000u), pm[q][gr][i]);
                         float x0 = w0 * __uint_as_float(cur.vm[0][gr] << 16), x1 = w1 * __uint_as_float(cur.vm[1][gr] << 16);
 #pragma unroll
-                        for (int sp = 0; sp < SPLIT; ++sp) {
+                        for (int p = 0; p < SPLIT; ++p) {
                             const uint32_t u = pack_bf16x2(x0, x1);
-                            *reinterpret_cast<uint32_t*>(pw + ((((q * SPLIT + sp) * NG + gr) * 16) + 4 * g + i) * L::PROW + 4 * c16) = u;
+                            *reinterpret_cast<uint32_t*>(pw + ((((q * SPLIT + p) * NG + gr) * 16) + 4 * g + i) * L::PROW + 4 * c16) = u;
                             if constexpr (SPLIT > 1) {
                                 x0 -= __uint_as_float(u << 16);
                                 x1 -= __uint_as_float(u & 0xffff0000u);
@@ -324,16 +344,17 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache4_attn_kernel(AttnArgs a,
                 }
             wave_sync();
             // out += (p s) (16 + n): column c16 of result (gr, e) is 32 gr + 2 c16 + e
+            // (rows 4 g + RI .. hold what an earlier call left; nothing reads their results)
 #pragma unroll
             for (int gr = 0; gr < NG; ++gr) {
                 bf16x8 wf[NQ][SPLIT];
 #pragma unroll
                 for (int q = 0; q < NQ; ++q)
 #pragma unroll
-                    for (int sp = 0; sp < SPLIT; ++sp) {
-                        wf[q][sp] = __builtin_bit_cast(
-                            bf16x8, *reinterpret_cast<const u32x4_t*>(pw + ((((q * SPLIT + sp) * NG + gr) * 16) + c16) * L::PROW + 16 * g));
-                        ones[q][gr] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf[q][sp], one8, ones[q][gr], 0, 0, 0);
+                    for (int p = 0; p < SPLIT; ++p) {
+                        wf[q][p] = __builtin_bit_cast(
+                            bf16x8, *reinterpret_cast<const u32x4_t*>(pw + ((((q * SPLIT + p) * NG + gr) * 16) + c16) * L::PROW + 16 * g));
+                        ones[q][gr] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf[q][p], one8, ones[q][gr], 0, 0, 0);
                     }
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
@@ -347,47 +368,54 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache4_attn_kernel(AttnArgs a,
 #pragma unroll
                     for (int q = 0; q < NQ; ++q)
 #pragma unroll
-                        for (int sp = SPLIT - 1; sp >= 0; --sp)
-                            o[q][2 * gr + e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf[q][sp], vf, o[q][2 * gr + e], 0, 0, 0);
+                        for (int p = SPLIT - 1; p >= 0; --p)
+                            o[q][2 * gr + e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf[q][p], vf, o[q][2 * gr + e], 0, 0, 0);
                 }
             }
             wave_sync();  // the weights' place is written again by the next tile
+        };
+        // (by twos, so that the tile in hand and the next one keep their
+        // registers; the forms with the most sums have none left for that)
+        for (int t = tbeg + wave;;) {
+            tile_step(t, even, odd);
+            if ((t += kWaves) >= tend) break;
+            if constexpr (RI < 4) {
+                tile_step(t, odd, even);
+                if ((t += kWaves) >= tend) break;
+            } else {
+                even = odd;
+            }
         }
         mfma_drain();
     }
 
-    // This wave's rows to LDS: [16 NQ][DH] sums, then m and l of every row.
+    // This wave's rows to LDS: [RB][DH] sums, then m and l of every row.
     __syncthreads();
-    float* wo = reinterpret_cast<float*>(smem) + wave * 16 * NQ * (DH + 2);
-    float* wml = wo + 16 * NQ * DH;
+    float* wo = reinterpret_cast<float*>(smem) + wave * RB * (DH + 2);
+    float* wml = wo + RB * DH;
     bool fine = true;
 #pragma unroll
     for (int q = 0; q < NQ; ++q)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < RI; ++i) {
+            const int lr = (4 * q + g) * RI + i;
             l_run[q][i] = lanes16_sum(l_run[q][i]);
             float bad = l_run[q][i] * 0.f;
 #pragma unroll
             for (int gr = 0; gr < NG; ++gr) {
                 const float add = lanes16_sum(pm[q][gr][i]) - 16.f * ones[q][gr][i];
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const float x = o[q][2 * gr + e][i] + add;
-                    bad = __builtin_fmaf(x, 0.f, bad);
-                    wo[(16 * q + 4 * g + i) * DH + 32 * gr + 2 * c16 + e] = x;
-                }
+                const float x = o[q][2 * gr][i] + add, y = o[q][2 * gr + 1][i] + add;
+                bad = __builtin_fmaf(x, 0.f, __builtin_fmaf(y, 0.f, bad));
+                *reinterpret_cast<float2*>(wo + lr * DH + 32 * gr + 2 * c16) = make_float2(x, y);
             }
             fine &= bad == 0.f;
-            if (c16 == 0) {
-                wml[2 * (16 * q + 4 * g + i)] = m_run[q][i];
-                wml[2 * (16 * q + 4 * g + i) + 1] = l_run[q][i];
-            }
+            if (c16 == 0) *reinterpret_cast<float2*>(wml + 2 * lr) = make_float2(m_run[q][i], l_run[q][i]);
         }
     if (__builtin_amdgcn_ballot_w64(!fine)) {
         // a weight of 0 met a value that is not finite: this wave's rows again, one by one
         wave_sync();
 #pragma unroll 1
-        for (int lr = 0; lr < 16 * NQ && r0 + lr < rn; ++lr) {
+        for (int lr = 0; lr < RB && r0 + lr < rn; ++lr) {
             const int r = r0 + lr, i = a.gd.div(r);
             float q[RowLanes<DH>::N], x[RowLanes<DH>::N], m, l;
             row_load<ST, DH>(qrow_ptr<ST>(a, a.q, b, hk, r, i), lane, q);
@@ -406,7 +434,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache4_attn_kernel(AttnArgs a,
     // The waves in order: M = max m_w, L = sum l_w 2^(m_w - M); 8 columns per thread.
     const float* base = reinterpret_cast<const float*>(smem);
     const int64_t rows = (int64_t)a.B * a.Hq * a.Tq;
-    for (int e = tid; e < 16 * NQ * (DH / 8); e += 64 * kWaves) {
+    for (int e = tid; e < RB * (DH / 8); e += 64 * kWaves) {
         const int lr = e / (DH / 8), d0 = e % (DH / 8) * 8, r = r0 + lr;
         if (r >= R) continue;
         const int i = a.gd.div(r);
@@ -416,7 +444,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache4_attn_kernel(AttnArgs a,
             float ml[kWaves][2];
 #pragma unroll
             for (int w = 0; w < kWaves; ++w) {
-                const float* p = base + w * 16 * NQ * (DH + 2) + 16 * NQ * DH + 2 * lr;
+                const float* p = base + w * RB * (DH + 2) + RB * DH + 2 * lr;
                 ml[w][0] = p[0], ml[w][1] = p[1];
                 M = fmaxf(M, ml[w][0]);
             }
@@ -425,7 +453,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache4_attn_kernel(AttnArgs a,
             for (int w = 0; w < kWaves; ++w) {
                 const float f = __builtin_amdgcn_exp2f(ml[w][0] - mu);
                 S += ml[w][1] * f;
-                const float* p = base + w * 16 * NQ * (DH + 2) + lr * DH + d0;
+                const float* p = base + w * RB * (DH + 2) + lr * DH + d0;
 #pragma unroll
                 for (int n = 0; n < 8; ++n) x[n] += f == 0.f ? 0.f : p[n] * f;
             }
@@ -451,10 +479,12 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache4_attn_kernel(AttnArgs a,
     }
 }
 
-// 32 rows per block share what is expanded of a tile, where there are more than
-// 16 and the registers hold them (not with 128-wide heads or fp32's three parts).
+// Rows per block: 4, 8 or 16 by the rows there are; 32 share what is expanded of
+// a tile, where there are more than 16 and the registers hold them (bf16 heads of
+// 32 columns).
 int rows_per_block(int dtype, int dh, const AttnArgs& a) {
-    return dtype == kBF16 && dh <= 64 && (int64_t)a.Tq * a.G > 16 ? 32 : 16;
+    const int64_t R = (int64_t)a.Tq * a.G;
+    return R <= 4 ? 4 : R <= 8 ? 8 : R <= 16 || dtype != kBF16 || dh > 32 ? 16 : 32;
 }
 
 CacheGeom cache_geom(int dtype, int dh, const AttnArgs& a) {
@@ -475,12 +505,12 @@ CacheGeom cache_geom(int dtype, int dh, const AttnArgs& a) {
     return G;
 }
 
-template <typename ST, int DH, int NQ>
+template <typename ST, int DH, int NQ, int RI>
 int launch_attn(const AttnArgs& a, const CacheArgs& c, const CacheGeom& G, float* buf, hipStream_t stream) {
     constexpr int SPLIT = sizeof(ST) == 2 ? 1 : 3;
-    const size_t w = (size_t)kWaves * NQ * AttnLds<DH, SPLIT>::PW, o = (size_t)kWaves * 16 * NQ * (DH + 2) * 4;
+    const size_t w = (size_t)kWaves * NQ * AttnLds<DH, SPLIT>::PW, o = (size_t)kWaves * 4 * RI * NQ * (DH + 2) * 4;
     const size_t lds = w > o ? w : o;
-    auto kern = cache4_attn_kernel<ST, DH, NQ>;
+    auto kern = cache4_attn_kernel<ST, DH, NQ, RI>;
     if (allow_lds((const void*)kern, lds)) return -1;
     const Parts part = make_parts(buf, G.parts, (int64_t)a.B * a.Hq * a.Tq, DH);
     return launch_parts((uint64_t)G.nb * a.B * a.Hkv * G.parts, 64 * kWaves, [&](uint32_t first, uint32_t blocks) {
@@ -501,9 +531,12 @@ int launch_cache4_attn(int dtype, const AttnArgs& a, const CacheArgs& c, float* 
     const int e = heads_by_type(dtype, c.dh, [&](auto st, auto d) {
         using ST = decltype(st);
         constexpr int DH = decltype(d)::value;
-        if constexpr (sizeof(ST) == 2 && DH <= 64)
-            if (rows_per_block(dtype, DH, a) == 32) return launch_attn<ST, DH, 2>(a, c, G, buf, stream);
-        return launch_attn<ST, DH, 1>(a, c, G, buf, stream);
+        const int rb = rows_per_block(dtype, DH, a);
+        if constexpr (sizeof(ST) == 2 && DH == 32)
+            if (rb == 32) return launch_attn<ST, DH, 2, 4>(a, c, G, buf, stream);
+        if (rb == 4) return launch_attn<ST, DH, 1, 1>(a, c, G, buf, stream);
+        if (rb == 8) return launch_attn<ST, DH, 1, 2>(a, c, G, buf, stream);
+        return launch_attn<ST, DH, 1, 4>(a, c, G, buf, stream);
     });
     if (e || G.parts == 1) return e;
     return launch_merge_parts(dtype, c.dh, a, G.parts, make_parts(buf, G.parts, (int64_t)a.B * a.Hq * a.Tq, c.dh), stream);
