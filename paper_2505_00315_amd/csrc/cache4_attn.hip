@@ -8,11 +8,12 @@
 // with one matrix instruction per group of 32 columns, and one for the whole
 // second sum: the words (s, m) of a position, as they are held, times
 // (-16 sum(q), sum(q)), split into three bf16 parts so that nothing is lost.
-//   out_g = sum_j (p_j s_jg) (16 + n_j) + sum_j p_j m_jg - 16 sum_j (p_j s_jg)
+//   out_g = sum_j (p_j s_jg) (16 + n_j) - 24 sum_j (p_j s_jg) + sum_j p_j (m_jg + 8 s_jg)
 // where the weights times the scales of a group are the matrix operand, rounded
-// to bf16 once, and the last sum is taken over the same rounded numbers (a
-// product with ones), so that the 16 cancels exactly.  fp32 storage takes q and
-// p s in three bf16 parts.
+// to bf16 once, and the second sum is taken over the same rounded numbers (a
+// product with ones): the rounding meets n - 8, the distance from the middle of
+// the group, and not n, which would double its share.  fp32 storage takes q and
+// p s in three bf16 parts and the codes as n - 8, so that nothing large cancels.
 //
 // Every wave walks its own tiles of 32 positions with its own running maximum
 // and sum, loads straight into registers one tile ahead and the page numbers
@@ -57,14 +58,18 @@ struct AttnLds {
     static constexpr int PW = SPLIT * NG * 16 * PROW;    // of a wave and 16 rows
 };
 
-// Nibbles nib and nib + 4 of w as bf16 16 + n.  The constants are registers, so
-// that the mask and the 16 are one instruction.
+// Nibbles nib and nib + 4 of w as a pair of bf16: 16 + n (the constants are
+// registers, so that the mask and the 16 are one instruction), or n - 8.
+template <int SPLIT>
 struct CodeBits {
+    static constexpr float middle = SPLIT == 1 ? 24.f : 0.f, least = middle - 8.f;  // what 8 and 0 become
     uint32_t mask, sixteen;
     __device__ __forceinline__ CodeBits() : mask(0x00780078u), sixteen(0x41804180u) {
         asm volatile("" : "+v"(mask), "+v"(sixteen));
     }
     __device__ __forceinline__ uint32_t operator()(uint32_t w, int nib) const {
+        if constexpr (SPLIT > 1)
+            return pack_bf16x2((float)(w >> (4 * nib) & 15) - 8.f, (float)(w >> (4 * nib + 16) & 15) - 8.f);
         const int sh = 4 * nib - 3;
         return ((sh < 0 ? w << 3 : w >> sh) & mask) | sixteen;
     }
@@ -198,7 +203,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache4_attn_kernel(AttnArgs a,
         sp = spots(tbeg + wave + kWaves);
 
         // q as A operand: columns 32 gr + 8 g .. + 7 of the row, in SPLIT parts;
-        // its sums over a group, times (-16, 1), as the operand of the words (s, m):
+        // its sums over a group, times (-16, 1) (of codes n - 8: (8, 1)), as the operand of the words (s, m):
         // lane group 0 holds the upper bf16 part, 1 and 2 what that leaves
         bf16x8 qf[NQ][SPLIT][NG], qs[NQ];
 #pragma unroll
@@ -225,14 +230,14 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache4_attn_kernel(AttnArgs a,
                 }
                 const float hi = bf16_to_f32(f32_to_bf16(s)), mid = bf16_to_f32(f32_to_bf16(s - hi)), lo = s - hi - mid;
                 const float mine = g == 0 ? hi : g == 1 ? mid : g == 2 ? lo : 0.f;
-                sums[gr] = pack_bf16x2(-16.f * mine, mine);
+                sums[gr] = pack_bf16x2(-CodeBits<SPLIT>::least * mine, mine);
             }
             qs[q] = frag_of(sums[0], sums[1], sums[2], sums[3]);
         }
         const float c2 = a.scale * kLog2e;
         unsigned char* pw = smem + wave * NQ * L::PW;  // this wave's weights
         const bf16x8 one8 = frag_of(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u);
-        const CodeBits codes;
+        const CodeBits<SPLIT> codes;
 
         auto tile_step = [&](int t, Tile<DH>& cur, Tile<DH>& nxt) __attribute__((always_inline)) {
             load(sp, nxt);
@@ -328,9 +333,11 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache4_attn_kernel(AttnArgs a,
                     l_run[q][i] += w0 + w1;
 #pragma unroll
                     for (int gr = 0; gr < NG; ++gr) {
-                        pm[q][gr][i] = __builtin_fmaf(w0, __uint_as_float(cur.vm[0][gr] & 0xffff0000u), pm[q][gr][i]);
-                        pm[q][gr][i] = __builtin_fmaf(w1, __uint_as_float(cur.vm[1][gr] & 0xffff0000u), pm[q][gr][i]);
-                        float x0 = w0 * __uint_as_float(cur.vm[0][gr] << 16), x1 = w1 * __uint_as_float(cur.vm[1][gr] << 16);
+                        const float s0 = __uint_as_float(cur.vm[0][gr] << 16), s1 = __uint_as_float(cur.vm[1][gr] << 16);
+                        const float mid0 = __builtin_fmaf(8.f, s0, __uint_as_float(cur.vm[0][gr] & 0xffff0000u));
+                        const float mid1 = __builtin_fmaf(8.f, s1, __uint_as_float(cur.vm[1][gr] & 0xffff0000u));
+                        pm[q][gr][i] = __builtin_fmaf(w1, mid1, __builtin_fmaf(w0, mid0, pm[q][gr][i]));
+                        float x0 = w0 * s0, x1 = w1 * s1;
 #pragma unroll
                         for (int p = 0; p < SPLIT; ++p) {
                             const uint32_t u = pack_bf16x2(x0, x1);
@@ -343,7 +350,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache4_attn_kernel(AttnArgs a,
                     }
                 }
             wave_sync();
-            // out += (p s) (16 + n): column c16 of result (gr, e) is 32 gr + 2 c16 + e
+            // out += (p s) (16 + n), or (p s) (n - 8): column c16 of result (gr, e) is 32 gr + 2 c16 + e
             // (rows 4 g + RI .. hold what an earlier call left; nothing reads their results)
 #pragma unroll
             for (int gr = 0; gr < NG; ++gr) {
@@ -354,7 +361,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache4_attn_kernel(AttnArgs a,
                     for (int p = 0; p < SPLIT; ++p) {
                         wf[q][p] = __builtin_bit_cast(
                             bf16x8, *reinterpret_cast<const u32x4_t*>(pw + ((((q * SPLIT + p) * NG + gr) * 16) + c16) * L::PROW + 16 * g));
-                        ones[q][gr] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf[q][p], one8, ones[q][gr], 0, 0, 0);
+                        if constexpr (CodeBits<SPLIT>::middle != 0.f)
+                            ones[q][gr] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf[q][p], one8, ones[q][gr], 0, 0, 0);
                     }
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
@@ -403,7 +411,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache4_attn_kernel(AttnArgs a,
             float bad = l_run[q][i] * 0.f;
 #pragma unroll
             for (int gr = 0; gr < NG; ++gr) {
-                const float add = lanes16_sum(pm[q][gr][i]) - 16.f * ones[q][gr][i];
+                const float add = lanes16_sum(pm[q][gr][i]) - CodeBits<SPLIT>::middle * ones[q][gr][i];
                 const float x = o[q][2 * gr][i] + add, y = o[q][2 * gr + 1][i] + add;
                 bad = __builtin_fmaf(x, 0.f, __builtin_fmaf(y, 0.f, bad));
                 *reinterpret_cast<float2*>(wo + lr * DH + 32 * gr + 2 * c16) = make_float2(x, y);
