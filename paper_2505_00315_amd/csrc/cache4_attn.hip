@@ -500,15 +500,17 @@ CacheGeom cache_geom(int dtype, int dh, const AttnArgs& a) {
     const int rb = rows_per_block(dtype, dh, a);
     const int64_t R = (int64_t)a.Tq * a.G;
     G.nb = (int)((R + rb - 1) / rb);
-    // Parts until there are about four workgroups for each that the chip holds,
-    // so that sequences of different lengths even out; a part keeps at least 512
-    // positions (4 tiles per wave), or 128 where even then CUs are left idle.
+    // Parts as the chip's 512 places have room for (4 sequences of 16000, 8 key
+    // heads: 512 workgroups 27 us, 768 33, 1024 and 2048 34), and two where the
+    // blocks alone fill them, so that sequences of different lengths even out (64
+    // of 8k to 16k positions, 8 key heads: 512 workgroups 203 us, 1024 196, 2048
+    // 203); a part keeps at least 512 positions, 4 tiles per wave (8 sequences of
+    // 4000: parts of 128 positions 36 us, of 256 26, of 512 22, of 1024 22).
     const int64_t blocks = (int64_t)G.nb * a.B * a.Hkv;
     const int64_t span = a.W ? (int64_t)a.W + a.S + rb / a.G + 16 : a.N;
     const int64_t tiles = ((span < a.N ? span : a.N) + 31) / 32;
-    int64_t parts = blocks >= 2048 ? 1 : (2048 + blocks - 1) / blocks;
-    const int64_t most = blocks * (tiles / 16) >= 512 ? tiles / 16 : tiles / 4;
-    if (parts > most) parts = most;
+    int64_t parts = blocks >= 1024 ? 1 : blocks > 256 ? 2 : 512 / blocks;
+    if (parts > tiles / 16) parts = tiles / 16;
     G.parts = parts < 1 ? 1 : (int)parts;
     return G;
 }

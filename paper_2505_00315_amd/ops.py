@@ -117,7 +117,7 @@ def _rows(t, what, shape, dtype, device):
 
 
 def _device(t, what):
-    if t.device.type != "cuda":
+    if not t.is_cuda:
         raise ValueError(f"{what}: the operators run on the GPU only")
     return t.device
 
