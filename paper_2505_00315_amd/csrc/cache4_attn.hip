@@ -287,7 +287,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache4_attn_kernel(AttnArgs a,
                     for (int q = 0; q < NQ; ++q)
 #pragma unroll
                         for (int i = 0; i < RI; ++i) {
-                            const bool ok = in && sees(a, pos[q][i], key);
+                            const bool ok = in & sees(a, pos[q][i], key);
                             s[q][y][i] = ok ? s[q][y][i] : -__builtin_inff();
                             any |= ok;
                         }

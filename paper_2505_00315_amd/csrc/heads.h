@@ -89,7 +89,7 @@ __device__ __forceinline__ int seq_len_of(const int32_t* lens, int b, int most) 
 
 // The visibility rule (positions p, j of the query and the key).
 __device__ __forceinline__ bool sees(const AttnArgs& a, int p, int j) {
-    return j <= p && (a.W == 0 || p - j < a.W || j < a.S);
+    return (j <= p) & ((a.W == 0) | (p - j < a.W) | (j < a.S));  // (without branches)
 }
 
 // Keys that some query of positions p0 .. p1 sees: 0 .. s - 1 and lo .. hi - 1

@@ -148,6 +148,16 @@ __device__ __forceinline__ void dkv_body(unsigned char* smem, const AttnArgs a, 
         for (int db = 0; db < ND; ++db) dk[cb][db] = dv[cb][db] = zero4();
 
     if (ntile > 0) {
+        const TileReads<ST, DH> rd(g, c16);
+        const uint32_t base = __builtin_amdgcn_readfirstlane(lds_addr(smem));
+        // tile t (past the end: the last one again, into a buffer that nobody reads)
+        auto issue = [&](int t, int buf) __attribute__((always_inline)) {
+            const uint32_t at = base + buf * STAGE;
+            rows.issue(a, tl, rlo + nr * (tbeg + min(t, ntile - 1)), rhi, at, at + 2 * TILE + 8 * TB * (tl.lds / 1024), lane);
+        };
+        // (the first tiles are on their way while the keys are loaded)
+#pragma unroll
+        for (int s = 0; s < STG - 1; ++s) issue(s, s);
         int key[CB];
         Frag8<ST> kf[CB][NS], vf[CB][NS];
 #pragma unroll
@@ -164,16 +174,7 @@ __device__ __forceinline__ void dkv_body(unsigned char* smem, const AttnArgs a, 
 #pragma unroll
             for (int st = 0; st < NS; ++st) take(kf[cb][st]), take(vf[cb][st]);
 
-        const TileReads<ST, DH> rd(g, c16);
-        const uint32_t base = __builtin_amdgcn_readfirstlane(lds_addr(smem));
-        // tile t (past the end: the last one again, into a buffer that nobody reads)
-        auto issue = [&](int t, int buf) __attribute__((always_inline)) {
-            const uint32_t at = base + buf * STAGE;
-            rows.issue(a, tl, rlo + nr * (tbeg + min(t, ntile - 1)), rhi, at, at + 2 * TILE + 8 * TB * (tl.lds / 1024), lane);
-        };
         const float c2 = a.scale * kLog2e;
-#pragma unroll
-        for (int s = 0; s < STG - 1; ++s) issue(s, s);
         auto tile_step = [&](int it, auto bufc) __attribute__((always_inline)) {
             constexpr int BUF = decltype(bufc)::value;
             wait_vmcnt<(STG - 2) * (2 * LD + RowTiles<ST, DH>::LL)>();
@@ -383,6 +384,18 @@ __device__ __forceinline__ void dq_body(unsigned char* smem, const AttnArgs a, i
 
     if (ntile > 0) {
         const int pw0 = off + a.gd.div(min(wr0, rn - 1)), pw1 = off + a.gd.div(min(wr0 + 16 * QN, rn) - 1);
+        const TL tl(wave, lane);
+        const TileReads<ST, DH> rd(g, c16);
+        const KeyTiles<ST, DH> kt(a.k, b, hk, tl), vt(a.v, b, hk, tl);
+        const uint32_t base = __builtin_amdgcn_readfirstlane(lds_addr(smem));
+        auto issue = [&](int t, int buf) __attribute__((always_inline)) {
+            const int e0 = TB * min(t, ntile - 1);
+            kt.issue(tl, list, e0, base + buf * STAGE);
+            vt.issue(tl, list, e0, base + buf * STAGE + TILE);
+        };
+        // (the first tiles are on their way while the rows are loaded)
+#pragma unroll
+        for (int s = 0; s < STG - 1; ++s) issue(s, s);
         int pos[QN];
         float2 ld[QN];
         Frag8<ST> qf[QN][NS], gf[QN][NS];
@@ -403,18 +416,7 @@ __device__ __forceinline__ void dq_body(unsigned char* smem, const AttnArgs a, i
 #pragma unroll
             for (int st = 0; st < NS; ++st) take(qf[qs][st]), take(gf[qs][st]);
         }
-        const TL tl(wave, lane);
-        const TileReads<ST, DH> rd(g, c16);
-        const KeyTiles<ST, DH> kt(a.k, b, hk, tl), vt(a.v, b, hk, tl);
-        const uint32_t base = __builtin_amdgcn_readfirstlane(lds_addr(smem));
-        auto issue = [&](int t, int buf) __attribute__((always_inline)) {
-            const int e0 = TB * min(t, ntile - 1);
-            kt.issue(tl, list, e0, base + buf * STAGE);
-            vt.issue(tl, list, e0, base + buf * STAGE + TILE);
-        };
         const float c2 = a.scale * kLog2e;
-#pragma unroll
-        for (int s = 0; s < STG - 1; ++s) issue(s, s);
         auto tile_step = [&](int it, auto bufc) __attribute__((always_inline)) {
             constexpr int BUF = decltype(bufc)::value;
             wait_vmcnt<(STG - 2) * 2 * LD>();
@@ -471,7 +473,7 @@ __device__ __forceinline__ void dq_body(unsigned char* smem, const AttnArgs a, i
                                 const int e = e0 + 16 * sb + 4 * g + i, key = list.key(e);
 #pragma unroll
                                 for (int qs = 0; qs < QN; ++qs)
-                                    dp[qs][x][i] = e < list.count && sees(a, pos[qs], key) ? dp[qs][x][i] : 0.f;
+                                    dp[qs][x][i] = ((e < list.count) & sees(a, pos[qs], key)) ? dp[qs][x][i] : 0.f;
                             }
                         }
                     }

@@ -71,6 +71,20 @@ __global__ __launch_bounds__(256, 2) void wattn_fwd_kernel(AttnArgs a, FwdGeom G
     if (ntile > 0) {
         // positions of the wave's first and last row, for the tests of whole tiles
         const int pw0 = off + a.gd.div(min(wr0, rn - 1)), pw1 = off + a.gd.div(min(wr0 + 16 * QN, rn) - 1);
+        const TL tl(wave, lane);
+        const TileReads<ST, DH> rd(g, c16);
+        const KeyTiles<ST, DH> kt(a.k, b, hk, tl), vt(a.v, b, hk, tl);
+        const uint32_t lbase = __builtin_amdgcn_readfirstlane(lds_addr(smem));
+        // tile t of this part (past the end: the last one again, into a buffer
+        // that nobody reads); entries past the list are masked
+        auto issue = [&](int t, int buf) __attribute__((always_inline)) {
+            const int e0 = KB * (tbeg + min(t, ntile - 1));
+            kt.issue(tl, list, e0, lbase + buf * STAGE);
+            vt.issue(tl, list, e0, lbase + buf * STAGE + TILE);
+        };
+        // (the first tiles are on their way while the rows are loaded)
+#pragma unroll
+        for (int s = 0; s < STG - 1; ++s) issue(s, s);
         // query fragments (B operand): columns 32 st + 8 g .. + 7 (rows past the
         // sequence are clamped to its last one; they are not written)
         Frag8<ST> qf[QN][NS];
@@ -86,20 +100,7 @@ __global__ __launch_bounds__(256, 2) void wattn_fwd_kernel(AttnArgs a, FwdGeom G
 #pragma unroll
             for (int st = 0; st < NS; ++st) take(qf[qs][st]);
 
-        const TL tl(wave, lane);
-        const TileReads<ST, DH> rd(g, c16);
-        const KeyTiles<ST, DH> kt(a.k, b, hk, tl), vt(a.v, b, hk, tl);
-        const uint32_t lbase = __builtin_amdgcn_readfirstlane(lds_addr(smem));
-        // tile t of this part (past the end: the last one again, into a buffer
-        // that nobody reads); entries past the list are masked
-        auto issue = [&](int t, int buf) __attribute__((always_inline)) {
-            const int e0 = KB * (tbeg + min(t, ntile - 1));
-            kt.issue(tl, list, e0, lbase + buf * STAGE);
-            vt.issue(tl, list, e0, lbase + buf * STAGE + TILE);
-        };
         const float c2 = a.scale * kLog2e;  // scores in log2 units
-#pragma unroll
-        for (int s = 0; s < STG - 1; ++s) issue(s, s);
         auto tile_step = [&](int it, auto bufc) __attribute__((always_inline)) {
             constexpr int BUF = decltype(bufc)::value;
             wait_vmcnt<(STG - 2) * 2 * LD>();  // tile it is in LDS
@@ -149,7 +150,7 @@ __global__ __launch_bounds__(256, 2) void wattn_fwd_kernel(AttnArgs a, FwdGeom G
                             const bool in = e < list.count;
 #pragma unroll
                             for (int qs = 0; qs < QN; ++qs)
-                                s[qs][sb][i] = in && sees(a, pos[qs], key) ? s[qs][sb][i] : -__builtin_inff();
+                                s[qs][sb][i] = (in & sees(a, pos[qs], key)) ? s[qs][sb][i] : -__builtin_inff();
                         }
                 }
             }
