@@ -265,7 +265,8 @@ int mosa_forward_noalloc(const mosa_shape* s, const void* X, const mosa_weights*
  *     `data` is 16-byte aligned and every stride a multiple of 16 bytes and not
  *     negative; the stride of an axis of one entry is not read.  An input's
  *     strides may be 0 (a broadcast input); the rows of an output may not
- *     overlap (an output's strides are checked against that).
+ *     overlap (an output's strides are checked against that), and but for the
+ *     pairs named below an output shares no memory with another argument.
  *   - d_head is 32, 64 or 128; q_heads is a multiple of kv_heads, and query
  *     head h goes with key head h / (q_heads / kv_heads).
  *   - Arrays of int32 on the device (lengths, positions, page tables) cannot be
@@ -283,7 +284,7 @@ typedef struct mosa_rows {
 /* Norm and rotation of query and key rows.
  *   y = R(p) n,  n = w x / sqrt(mean(x^2) + eps)
  * for every row x of q (weights wq [d_head]) and k (wk), p the token's
- * position.  R(p) turns the first rope_dim columns in rope_dim / 2 pairs, pair j
+ * position; the mean of squares is taken in fp32.  R(p) turns the first rope_dim columns in rope_dim / 2 pairs, pair j
  * by the angle p rope_base^(-2 j / rope_dim): columns 2j and 2j + 1
  * (MOSA_PAIRS_ADJACENT, as in the layer), or j and j + rope_dim / 2
  * (MOSA_PAIRS_HALVES).  rope_dim 0 turns nothing; otherwise it is even, at most

@@ -17,17 +17,24 @@ bool d_head_ok(int dh) { return dh == 32 || dh == 64 || dh == 128; }
 // Rows counted in 32 bits by the kernels (offsets into tensors are 64-bit).
 bool rows_ok(int64_t a, int64_t b, int64_t c) { return (double)a * (double)b * (double)c <= 2147483647.0; }
 
+// Nothing on a device reaches over more; within it offsets and sizes, in bytes or
+// elements, stay far from 64 bits.
+constexpr double kMostBytes = 70368744177664.0;  // 2^46
+
 // One tensor of rows [B, H, T, dh]: address and strides checked and taken over.
 int take_rows(const mosa_rows* r, int B, int H, int T, int dh, int dtype, bool output, Rows* to) {
     if (!r || !r->data || !aligned(r->data, 16)) return MOSA_ERR_INVALID_ARG;
     const int64_t unit = 16 / elem_size(dtype);
     const int n[3] = {B, H, T};
     int64_t st[3] = {r->batch_stride, r->head_stride, r->row_stride};
+    double span = 0.0;  // from the first row to the last
     for (int i = 0; i < 3; ++i) {
         if (n[i] == 1) st[i] = 0;
         // (a stride beyond 2^40 elements is no tensor of this device)
         if (st[i] < 0 || st[i] % unit || st[i] > ((int64_t)1 << 40)) return MOSA_ERR_INVALID_ARG;
+        span += (double)(n[i] - 1) * (double)st[i];
     }
+    if (span > kMostBytes) return MOSA_ERR_INVALID_ARG;
     if (output) {  // nested axes: each stride at least the extent of those within
         int64_t extent = dh;
         bool used[3] = {false, false, false};
@@ -128,6 +135,7 @@ int check_cache(const mosa_cache_shape* s) {
     if (s->page_size < 16 || s->page_size > 1024 || s->page_size % 16) return MOSA_ERR_INVALID_ARG;
     if (!d_head_ok(s->d_head)) return MOSA_ERR_UNSUPPORTED;
     if ((double)s->max_pages * s->page_size > 536870912.0) return MOSA_ERR_UNSUPPORTED;  // positions, as above
+    if ((double)s->pages * s->kv_heads * s->page_size * 2.0 * s->d_head > kMostBytes) return MOSA_ERR_UNSUPPORTED;
     return MOSA_OK;
 }
 

@@ -304,3 +304,69 @@ def _plain(q, k, v, window, sinks):
     see = mask_of(q.shape[2], k.shape[2], q.shape[2], k.shape[2], window, sinks, q.device)
     s = (q @ k.transpose(-1, -2).contiguous()) / math.sqrt(q.shape[-1])
     return torch.softmax(s.masked_fill(~see, -math.inf), -1) @ v
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_more_sinks_than_go_by_chunks(dtype):
+    case = (2, 4, 2, 64, 420, 420, 40, 300, "bthd", ([420, 350], [420, 350]))
+    shape, x, kw, dt = setup(case, dtype, 40)
+    ref = reference(case, x, kw)
+    spoil_padding(x, kw)
+    out, lse = ops.window_attention(shape, x["q"], x["k"], x["v"], **kw)
+    dq, dk, dv = ops.window_attention_backward(shape, x["q"], x["k"], x["v"], out, lse, x["do"], **kw)
+    bounds = attention_bounds(ref, dt, case[3], max(case[5], case[4] * case[1] // case[2]))
+    for n, t in (("out", out), ("lse", lse), ("dq", dq), ("dk", dk), ("dv", dv)):
+        within(t, ref[n], bounds[n], f"{n} {case}")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rows_far_apart(dtype):
+    """Strides that pass 32 bits within a tile, of rows, heads and sequences."""
+    B, Hq, Hkv, dh, T = 2, 4, 2, 32, 70
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    shape = ops.make_attn_shape(B, Hq, Hkv, T, T, dh, dtype, window=30, sinks=3)
+    g = torch.Generator().manual_seed(41)
+    near = [rand_rows(g, B, H, T, dh, dt) for H in (Hq, Hkv, Hkv, Hq)]
+    want = ops.window_attention(shape, *near[:3])
+    wantg = ops.window_attention_backward(shape, *near[:3], *want, near[3])
+    row, head = 1 << 25, 1 << 28
+    room = torch.zeros(T * row, dtype=dt, device="cuda")  # holds B Hq heads as well
+    for by_rows in (True, False):
+        def place(i, H):  # the i-th tensor
+            if by_rows:  # rows apart, the heads beside each other
+                return torch.as_strided(room, (B, H, T, dh), (H * dh, dh, row, 1), i * B * Hq * dh)
+            return torch.as_strided(room, (B, H, T, dh), (H * head, head, dh, 1), i * T * dh)
+        heads = (Hq, Hkv, Hkv, Hq, Hq, Hq, Hkv, Hkv)
+        q, k, v, do, out, dq, dk, dv = (place(i, H) for i, H in enumerate(heads))
+        for t, x in zip((q, k, v, do), near):
+            t.copy_(x)
+        _, lse = ops.window_attention(shape, q, k, v, out=out)
+        assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
+        grads = ops.window_attention_backward(shape, q, k, v, out, lse, do, dq=dq, dk=dk, dv=dv)
+        for a, b in zip(grads, wantg):
+            assert torch.equal(a, b)
+
+
+def test_two_graphs_with_one_scratch():
+    """Replayed in turn, on one stream."""
+    case = (1, 8, 2, 64, 1, 2000, 0, 0, "bthd", None)
+    shape, x, _, _ = setup(case, "bf16", 42)
+    _, y, _, _ = setup(case, "bf16", 43)
+    scratch = ops.alloc_attn_scratch(shape)
+    outs, graphs = [], []
+    for z in (x, y):
+        outs.append(ops.window_attention(shape, z["q"], z["k"], z["v"], scratch=scratch))
+    want = [o[0].clone() for o in outs]
+    assert not torch.equal(*want)
+    torch.cuda.synchronize()
+    for z, o in zip((x, y), outs):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            ops.window_attention(shape, z["q"], z["k"], z["v"], out=o[0], lse=o[1], scratch=scratch)
+    for _ in range(3):
+        for o in outs:
+            o[0].fill_(5)
+        for graph in graphs:
+            graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(outs[0][0], want[0]) and torch.equal(outs[1][0], want[1])

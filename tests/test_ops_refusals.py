@@ -208,3 +208,20 @@ def test_structs_match_the_header():
     assert ctypes.sizeof(ops.NormShape) == 40
     assert ctypes.sizeof(ops.AttnShape) == 40
     assert ctypes.sizeof(ops.CacheShape) == 28
+
+
+def test_extents_past_any_memory():
+    """Sizes whose products pass 64 bits are refused, not taken modulo 2^64."""
+    far = 1 << 40
+    s = ops.make_norm_shape(2, 1 << 24, 1, 1, 64)
+    k = rows(2, 1, 1 << 24, 64)
+    assert status("mosa_qk_norm_rope", s, rows(2, 1, 1 << 24, 64, row_stride=far, batch_stride=64), k, None, None, None,
+                  k, k, None) == INV
+    assert status("mosa_qk_norm_rope", s, k, k, None, None, None, rows(2, 1, 1 << 24, 64, row_stride=far), k, None) == INV
+    for kw in (dict(pages=(1 << 31) - 1, kv_heads=(1 << 31) - 1), dict(pages=1 << 30, kv_heads=1 << 24, page_size=1024)):
+        with pytest.raises(mosa.MosaError) as e:
+            ops.cache4_size(ops.make_cache_shape(**{**dict(batch=1, kv_heads=1, d_head=64, pages=1, page_size=16,
+                                                           max_pages=1), **kw}))
+        assert e.value.status == UNS
+    # large ones that a device could hold are taken
+    assert ops.cache4_size(ops.make_cache_shape(1, 8, 128, 1 << 17, 1024, 1024)) == (1 << 17) * 8 * 1024 * 160
