@@ -39,7 +39,8 @@ constexpr int kStages = 2;
 // Launch geometry: per (b, key head) nk blocks of keys, their rows cut into kp
 // parts, and nq blocks of rows; nc chunks for each of ns blocks of 64 sinks (ns =
 // 0: far pairs are the key blocks' own work).  Sums are kept of the first `keys`
-// keys of a head (all of them where kp > 1, the sinks where ns > 0).
+// keys of a head (all of them where kp > 1, otherwise the sinks where ns > 0): of
+// every part, and of every chunk those of the sinks.
 struct BwdGeom {
     int nk, kp, nq, ns, nc, keys;
 };
@@ -287,11 +288,10 @@ __device__ __forceinline__ void dkv_body(unsigned char* smem, const AttnArgs a, 
     }
     __syncthreads();
 
-    // slots of the sums: the parts of the window's pairs, then the chunks (a
-    // block of keys whose sums are kept is one of both or of neither kind)
-    const int64_t slot = far ? G.kp + chunk : chunk;
-    float* sum = sums + (slot * a.B * a.Hkv + (int64_t)b * a.Hkv + hk) * G.keys * 2 * DH;
-    const int top = far ? a.S : a.N, summed = G.keys;  // keys of the output, those whose sums are kept
+    // sums: of every part the first G.keys keys, then of every chunk the sinks
+    const int top = far ? a.S : a.N, summed = far ? a.S : G.keys;  // keys of the output, those whose sums are kept
+    const int64_t heads = (int64_t)a.B * a.Hkv, bh = (int64_t)b * a.Hkv + hk;
+    float* sum = sums + ((far ? heads * G.kp * G.keys : 0) + (heads * chunk + bh) * summed) * 2 * DH;
     bool fine = true;
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb) fine &= finite4(dk[cb]) && finite4(dv[cb]);
@@ -326,7 +326,7 @@ __device__ __forceinline__ void dkv_body(unsigned char* smem, const AttnArgs a, 
 #pragma unroll
         for (int cb = 0; cb < CB; ++cb) {
             const int j = wk0 + 16 * cb + c16;
-            if (j >= (far ? a.S : min(summed, a.N))) continue;
+            if (j >= min(summed, top)) continue;
             const float f = j <= wk1 ? 1.f : 0.f;
 #pragma unroll
             for (int db = 0; db < ND; ++db) {
@@ -585,17 +585,22 @@ __global__ __launch_bounds__(256) void wattn_ld_kernel(AttnArgs a, uint32_t firs
 // dk and dv of the keys whose sums are kept: the slots in order, 4 values per thread.
 template <typename ST, int DH>
 __global__ __launch_bounds__(256) void wattn_sums_kernel(AttnArgs a, BwdGeom G, const float* __restrict__ sums) {
-    const int slots = G.kp + G.nc;
-    const int64_t all = (int64_t)a.B * a.Hkv * G.keys * 2 * DH;
+    const int64_t heads = (int64_t)a.B * a.Hkv, all = heads * G.keys * 2 * DH, chunk = heads * a.S * 2 * DH;
     for (int64_t e = 4 * ((int64_t)blockIdx.x * 256 + threadIdx.x); e < all; e += 1024 * (int64_t)gridDim.x) {
         const int c = (int)(e % DH), which = (int)(e / DH % 2);
-        const int64_t row = e / (2 * DH);
-        const int j = (int)(row % G.keys), hk = (int)(row / G.keys % a.Hkv), b = (int)(row / G.keys / a.Hkv);
+        const int64_t row = e / (2 * DH), bh = row / G.keys;
+        const int j = (int)(row % G.keys), hk = (int)(bh % a.Hkv), b = (int)(bh / a.Hkv);
         float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-        for (int k = 0; k < slots; ++k) {
-            const float4 x = *reinterpret_cast<const float4*>(sums + k * all + e);
+        auto add = [&](const float* p) {
+            const float4 x = *reinterpret_cast<const float4*>(p);
             s.x += x.x, s.y += x.y, s.z += x.z, s.w += x.w;
+        };
+#pragma unroll 4
+        for (int k = 0; k < G.kp; ++k) add(sums + k * all + e);
+        if (j < a.S) {
+            const float* far = sums + G.kp * all + (bh * a.S + j) * 2 * DH + which * DH + c;
+#pragma unroll 4
+            for (int k = 0; k < G.nc; ++k) add(far + k * chunk);
         }
         if (j >= seq_len_of(a.kl, b, a.N)) s = make_float4(0.f, 0.f, 0.f, 0.f);
         ST* to = row_ptr<ST>(which ? a.dv : a.dk, b, hk, j) + c;
@@ -625,13 +630,19 @@ BwdGeom bwd_geom(int dtype, int dh, const AttnArgs& a) {
     G.nk = (a.N + kw - 1) / kw;
     G.nq = (int)((R + qw - 1) / qw);
     G.ns = a.W && a.S && a.S <= kSinkKeys ? (a.S + 63) / 64 : 0;
-    // Without a window the first keys' blocks are twice as long as the average.
-    // Where the key blocks are fewer than the workgroups that the chip holds, the
-    // longest alone would set the time: 2 x 2048 tokens, 16 / 4 heads of 128,
-    // training step: 325 us with whole blocks, 237 with parts.
-    const int64_t nk = (int64_t)a.B * a.Hkv * G.nk, tiles = R / 64;
-    int64_t kp = a.W == 0 && nk < 512 ? (1024 + nk - 1) / nk : 1;
-    if (kp > tiles / 8) kp = tiles / 8;
+    // A key block walks more rows than a row block walks keys (G heads of a window
+    // of queries; without a window the first keys are seen by every row).  Where
+    // the key blocks are fewer than the chip's places their walks alone would set
+    // the time, so they are cut, into parts of at least 4 tiles: without a window
+    // up to the 512 places (2 x 2048 tokens, 16 / 4 heads of 128, training step: 325
+    // us with whole blocks, 232 with parts); with one up to half of them, as the
+    // row blocks fill the rest (2048 tokens, 16 / 4 heads of 128, window 1024: 184
+    // us whole, 165 with 512, 132 with 256; at 256 whole blocks parts lose, 199
+    // against 204).
+    const int64_t nk = (int64_t)a.B * a.Hkv * G.nk, walk = (int64_t)(a.W + kw) * a.G;
+    const int64_t tiles = (a.W && walk < R ? walk : R) / (dtype == kBF16 ? 64 : 32), places = a.W ? 256 : 512;
+    int64_t kp = nk < places ? (places + nk - 1) / nk : 1;
+    if (kp > tiles / 4) kp = tiles / 4;
     if (kp > kMaxParts) kp = kMaxParts;
     G.kp = kp < 1 ? 1 : (int)kp;
     G.keys = G.kp > 1 ? a.N : G.ns ? a.S : 0;
@@ -666,7 +677,7 @@ size_t ld_bytes(const AttnArgs& a) { return ((size_t)a.B * a.Hq * a.Tq * sizeof(
 
 size_t attn_bwd_scratch(int dtype, int dh, const AttnArgs& a) {
     const BwdGeom G = bwd_geom(dtype, dh, a);
-    return ld_bytes(a) + (size_t)(G.kp + G.nc) * a.B * a.Hkv * G.keys * 2 * dh * sizeof(float);
+    return ld_bytes(a) + ((size_t)G.kp * G.keys + (size_t)G.nc * a.S) * a.B * a.Hkv * 2 * dh * sizeof(float);
 }
 
 int launch_window_attn_bwd(int dtype, int dh, AttnArgs a, void* scratch, hipStream_t stream) {

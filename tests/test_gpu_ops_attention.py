@@ -306,6 +306,28 @@ def _plain(q, k, v, window, sinks):
     return torch.softmax(s.masked_fill(~see, -math.inf), -1) @ v
 
 
+# few key blocks whose windows span many rows: parts of them, beside chunks of the sinks' far rows or without
+PARTS = [
+    (2, 8, 2, 64, 500, 700, 200, 5, "bthd", ([500, 77], [700, 300])),
+    (1, 12, 2, 128, 400, 400, 190, 70, "bhtd", None),
+    (1, 16, 2, 32, 333, 420, 120, 0, "packed", None),
+    (2, 24, 2, 64, 350, 350, 90, 300, "bhtd", ([350, 10], [350, 200])),
+]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("case", PARTS, ids=[f"dh{c[3]}w{c[6]}s{c[7]}" for c in PARTS])
+def test_parts_of_windows(case, dtype):
+    shape, x, kw, dt = setup(case, dtype, 44)
+    ref = reference(case, x, kw)
+    spoil_padding(x, kw)
+    out, lse = ops.window_attention(shape, x["q"], x["k"], x["v"], **kw)
+    dq, dk, dv = ops.window_attention_backward(shape, x["q"], x["k"], x["v"], out, lse, x["do"], **kw)
+    bounds = attention_bounds(ref, dt, case[3], max(case[5], case[4] * case[1] // case[2]))
+    for n, t in (("out", out), ("lse", lse), ("dq", dq), ("dk", dk), ("dv", dv)):
+        within(t, ref[n], bounds[n], f"{n} {case}")
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_more_sinks_than_go_by_chunks(dtype):
     case = (2, 4, 2, 64, 420, 420, 40, 300, "bthd", ([420, 350], [420, 350]))
