@@ -106,6 +106,25 @@ struct RowTiles {
     }
 };
 
+// The order in which a key block takes its tiles of rows, so that the walks of
+// neighbouring blocks meet in L2: with a window each starts at the tile whose
+// number in the sequence its length divides, and goes round; without one from
+// the last tile down.  (2 x 4096 tokens, 32 / 8 heads of 128, window 1024: 0.54 GB
+// come from HBM in place of 2.0.)
+struct Walk {
+    int cut, early, late, step, last;
+    __device__ __forceinline__ Walk(int rlo, int nr, int tbeg, int n, bool down) {
+        const int r0 = rlo + nr * tbeg, far_end = down ? nr * (n - 1) : 0;
+        cut = down ? 0 : (rlo / nr + tbeg) % n;
+        early = r0 + nr * (n - cut);
+        late = r0 + far_end - nr * cut;
+        step = down ? -nr : nr;
+        last = n - 1;
+    }
+    // first row of tile t (past the end: the last one)
+    __device__ __forceinline__ int row(int t) const { return (t < cut ? early : late) + step * min(t, last); }
+};
+
 template <int N>
 __device__ __forceinline__ bool finite4(const f32x4 (&x)[N]) {
     float t = 0.f;
@@ -151,10 +170,11 @@ __device__ __forceinline__ void dkv_body(unsigned char* smem, const AttnArgs a, 
     if (ntile > 0) {
         const TileReads<ST, DH> rd(g, c16);
         const uint32_t base = __builtin_amdgcn_readfirstlane(lds_addr(smem));
+        const Walk walk(rlo, nr, tbeg, ntile, !far && a.W == 0);
         // tile t (past the end: the last one again, into a buffer that nobody reads)
         auto issue = [&](int t, int buf) __attribute__((always_inline)) {
             const uint32_t at = base + buf * STAGE;
-            rows.issue(a, tl, rlo + nr * (tbeg + min(t, ntile - 1)), rhi, at, at + 2 * TILE + 8 * TB * (tl.lds / 1024), lane);
+            rows.issue(a, tl, walk.row(t), rhi, at, at + 2 * TILE + 8 * TB * (tl.lds / 1024), lane);
         };
         // (the first tiles are on their way while the keys are loaded)
 #pragma unroll
@@ -184,7 +204,7 @@ __device__ __forceinline__ void dkv_body(unsigned char* smem, const AttnArgs a, 
             const unsigned char* Qt = smem + BUF * STAGE;
             const unsigned char* Gt = Qt + TILE;
             const unsigned char* Lt = Gt + TILE + 8 * TB * wave;
-            const int r0 = rlo + nr * (tbeg + it), rt = min(r0 + nr, rhi);  // the tile's rows
+            const int r0 = walk.row(it), rt = min(r0 + nr, rhi);  // the tile's rows
             const int pt0 = off + a.gd.div(r0), pt1 = off + a.gd.div(rt - 1);  // and their positions
             // nothing for this wave: no keys, rows before the keys, or past their window
             if (wk1 < wk0) return;
