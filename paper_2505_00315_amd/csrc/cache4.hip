@@ -63,8 +63,9 @@ __device__ __forceinline__ uint32_t quantise8(const float (&x)[8], uint32_t& wor
     float c[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const float d = x[i] - m, n = __builtin_rintf(d * inv), r = __builtin_fmaf(-n, s, d);
-        const uint32_t odd = __float_as_uint(n + 8388608.f) & 1;
+        // (a sum with 1.5 2^23 is rounded to an integer, its lowest bit in the last place)
+        const float d = x[i] - m, t = __builtin_fmaf(d, inv, 12582912.f), n = t - 12582912.f, r = __builtin_fmaf(-n, s, d);
+        const uint32_t odd = __float_as_uint(t) & 1;
         const float limit = __uint_as_float(__float_as_uint(half) - odd);  // the number next below half
         c[i] = __builtin_amdgcn_fmed3f(n + (fabsf(r) > limit ? __builtin_copysignf(1.f, r) : 0.f), 0.f, 15.f);
     }
