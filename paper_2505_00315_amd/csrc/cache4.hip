@@ -2,7 +2,7 @@
 //
 // Both copies move each byte once.  Measured (bf16, 4 x 4096 positions, 8 heads of
 // 128, 88 MB each): read 17 us, 5.2 TB/s, what memory gives; write 27 us, 3.3 TB/s,
-// bound by the vector instructions of the codes, about 23 per value.
+// bound by the vector instructions of the codes, more than 20 per value.
 #include "cache4.h"
 #include "launch_parts.h"
 
