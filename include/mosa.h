@@ -319,13 +319,17 @@ int mosa_qk_norm_rope_backward(const mosa_norm_shape* s, const mosa_rows* q, con
  * out = softmax(scale q k^T) v over the keys that it sees; a query that sees
  * none (Q > N) gives zeros.  lse: natural logarithm of the sum of exp(scale q k)
  * (-inf for such a query).  Keys that a query does not see do not reach its
- * output or gradient, whatever they hold. */
+ * output or gradient, whatever they hold.
+ * scale is positive; q_len and kv_len are at most 2^29, batch q_heads (q_len + 128)
+ * at most 2^31 - 1, and, where keys come as rows, batch kv_heads (kv_len + 128) too
+ * (kv_len of attention over the cache is only a bound of its lengths). */
 typedef struct mosa_attn_shape {
     int32_t batch, q_heads, kv_heads, q_len, kv_len, d_head, dtype, window, sinks;
     float scale;
 } mosa_attn_shape;
 
-/* Scratch of the forward (over rows or over the 4-bit cache) and of the backward. */
+/* Scratch of the forward (over rows or over the 4-bit cache) and of the backward
+ * (0 for a shape whose kv_len is only within the cache's limits). */
 int mosa_attn_scratch_size(const mosa_attn_shape* s, size_t* forward_bytes, size_t* backward_bytes);
 /* q_lens, kv_lens: int32 [batch], Q and N of every sequence (taken into
  * 0 .. q_len and 0 .. kv_len), or NULL for q_len and kv_len.  Rows past them are

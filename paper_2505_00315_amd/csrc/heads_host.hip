@@ -81,6 +81,9 @@ int norm_args(const mosa_norm_shape* s, const mosa_rows* q, const mosa_rows* k, 
     return take_rows(k, s->batch, s->kv_heads, s->seq_len, s->d_head, s->dtype, false, &a->k);
 }
 
+// Key rows that are passed as tensors (the cache has positions in their place).
+bool key_rows_ok(const mosa_attn_shape* s) { return rows_ok(s->batch, s->kv_heads, (int64_t)s->kv_len + 128); }
+
 int check_attn(const mosa_attn_shape* s) {
     if (!s || !dtype_ok(s->dtype)) return MOSA_ERR_INVALID_ARG;
     if (s->batch < 1 || s->q_heads < 1 || s->kv_heads < 1 || s->q_len < 1 || s->kv_len < 1) return MOSA_ERR_INVALID_ARG;
@@ -89,9 +92,7 @@ int check_attn(const mosa_attn_shape* s) {
     if (!d_head_ok(s->d_head)) return MOSA_ERR_UNSUPPORTED;
     // positions and their differences stay within 32 bits
     if (s->q_len > (1 << 29) || s->kv_len > (1 << 29)) return MOSA_ERR_UNSUPPORTED;
-    if (!rows_ok(s->batch, s->q_heads, (int64_t)s->q_len + 128) || !rows_ok(s->batch, s->kv_heads, (int64_t)s->kv_len + 128))
-        return MOSA_ERR_UNSUPPORTED;
-    return MOSA_OK;
+    return rows_ok(s->batch, s->q_heads, (int64_t)s->q_len + 128) ? MOSA_OK : MOSA_ERR_UNSUPPORTED;
 }
 
 AttnArgs attn_args(const mosa_attn_shape* s, const int32_t* q_lens, const int32_t* kv_lens) {
@@ -119,6 +120,7 @@ int take_queries(const mosa_attn_shape* s, const mosa_rows* q, const int32_t* q_
 }
 
 int take_keys(const mosa_attn_shape* s, const mosa_rows* k, const mosa_rows* v, AttnArgs* a) {
+    if (!key_rows_ok(s)) return MOSA_ERR_UNSUPPORTED;
     if (const int e = take_rows(k, a->B, a->Hkv, a->N, s->d_head, s->dtype, false, &a->k)) return e;
     return take_rows(v, a->B, a->Hkv, a->N, s->d_head, s->dtype, false, &a->v);
 }
@@ -210,9 +212,11 @@ int mosa_attn_scratch_size(const mosa_attn_shape* s, size_t* forward_bytes, size
     if (const int e = check_attn(s)) return e;
     if (!forward_bytes || !backward_bytes) return MOSA_ERR_INVALID_ARG;
     const AttnArgs a = attn_args(s, nullptr, nullptr);
-    const size_t rows = attn_fwd_scratch(s->dtype, s->d_head, a), cache = cache4_attn_scratch(s->dtype, s->d_head, a);
+    const bool over_rows = key_rows_ok(s);
+    const size_t rows = over_rows ? attn_fwd_scratch(s->dtype, s->d_head, a) : 0;
+    const size_t cache = cache4_attn_scratch(s->dtype, s->d_head, a);
     *forward_bytes = rows > cache ? rows : cache;
-    *backward_bytes = attn_bwd_scratch(s->dtype, s->d_head, a);
+    *backward_bytes = over_rows ? attn_bwd_scratch(s->dtype, s->d_head, a) : 0;
     return MOSA_OK;
 }
 
