@@ -251,8 +251,9 @@ const char* mosa_status_string(int status) {
     switch (status) {
         case MOSA_OK: return "ok";
         case MOSA_ERR_INVALID_ARG: return "invalid argument (size, null pointer or alignment)";
-        case MOSA_ERR_UNSUPPORTED: return "unsupported shape (d_head must be 32 or 64, d_model a multiple of 64, seq_len <= 16384)";
-        case MOSA_ERR_WORKSPACE: return "saved or scratch buffer smaller than mosa_workspace_size";
+        case MOSA_ERR_UNSUPPORTED: return "unsupported shape (layer: d_head 32 or 64, d_model a multiple of 64, seq_len <= 16384; "
+                                           "operators of the dense heads: d_head 32, 64 or 128, rows and lengths in the limits of mosa.h)";
+        case MOSA_ERR_WORKSPACE: return "saved, scratch or workspace buffer smaller than the shape's size function gives";
         case MOSA_ERR_HIP: return "HIP launch failure";
         default: return "unknown status";
     }
