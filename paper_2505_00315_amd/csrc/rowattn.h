@@ -158,21 +158,4 @@ __device__ __forceinline__ void row_dkv(const AttnArgs& a, int b, int hk, int j,
     for (int n = 0; n < N; ++n) dk[n] *= a.scale;
 }
 
-// A row's result: a part (part_o not NULL), or out and lse.
-template <typename ST, int DH>
-__device__ __forceinline__ void row_finish(const AttnArgs& a, int b, int h, int i, int64_t row, int lane, float m,
-                                           float l, const float (&o)[RowLanes<DH>::N], float* part_o, float* part_ml) {
-    // l is 0 for a row that sees nothing (its out is 0), and NaN stays NaN
-    const float f = part_o ? 1.f : l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;
-#pragma unroll
-    for (int n = 0; n < RowLanes<DH>::N; ++n) {
-        if (!RowLanes<DH>::has(lane)) continue;
-        if (part_o) part_o[lane + 64 * n] = o[n];
-        else st1<ST>(row_ptr<ST>(a.out, b, h, i) + lane + 64 * n, o[n] * f);
-    }
-    if (lane) return;
-    if (part_o) part_ml[0] = m, part_ml[1] = l;
-    else if (a.lse) a.lse[row] = l == 0.f ? -__builtin_inff() : m * kLn2 + logf(l);
-}
-
 }  // namespace mosa

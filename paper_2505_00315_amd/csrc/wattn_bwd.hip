@@ -133,16 +133,6 @@ struct Walk {
     __device__ __forceinline__ int row(int t) const { return (t < cut ? early : late) + step * min(t, last); }
 };
 
-template <int N>
-__device__ __forceinline__ bool finite4(const f32x4 (&x)[N]) {
-    float t = 0.f;
-#pragma unroll
-    for (int n = 0; n < N; ++n)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) t = __builtin_fmaf(x[n][i], 0.f, t);
-    return t == 0.f;
-}
-
 // Keys k0 .. of (b, hk), 16 CB per wave: part `chunk` of the rows that see them
 // within the window, or, far, chunk `chunk` of those beyond the sinks' window.
 template <typename ST, int DH, int CB, bool far>

@@ -35,6 +35,18 @@ __device__ __forceinline__ const char* uniform_ptr(const char* p) {
                          (uint32_t)__builtin_amdgcn_readfirstlane((int)u));
 }
 
+// A kernel's arguments by the address of their segment, in scalar registers.
+template <typename T>
+__device__ __forceinline__ T uniform_args(const void* segment) {
+    T t;
+    __builtin_memcpy(&t, (const __attribute__((address_space(4))) void*)(uintptr_t)uniform_ptr(static_cast<const char*>(segment)), sizeof(T));
+    return t;
+}
+// LDS by its byte address.
+__device__ __forceinline__ unsigned char* lds_at(uint32_t at) {
+    return (unsigned char*)(__attribute__((address_space(3))) unsigned char*)(uintptr_t)at;
+}
+
 template <typename ST>
 constexpr int kTileRows = sizeof(ST) == 2 ? 64 : 32;
 
@@ -171,6 +183,123 @@ template <typename ST>
 __device__ __forceinline__ Frag8<ST> pack_frag(const f32x4& x, const f32x4& y) {
     const float v[8] = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
     return frag8_from<ST>(v);
+}
+
+// What a row does not see has a weight of 0 in the products of a tile, which is
+// not enough where it holds infinities or NaN: 0 times those is NaN.  Only tiles
+// that some of the workgroup's rows (keys) pair with in part can do that harm.
+// A workgroup whose results are not finite walks its tiles a second time.  Before
+// such a tile is multiplied its infinities then become the largest numbers of
+// their sign, NaN too (keep_finite): scores keep their meaning, and a weight of 0
+// gives 0.  At the end these tiles are visited once more, and what was not finite
+// joins the results that it belongs to (add_not_finite).
+
+// One call by the whole workgroup; a barrier follows.
+template <typename ST, int DH>
+__device__ __forceinline__ void keep_finite(unsigned char* t, int tid) {
+    constexpr uint32_t body = sizeof(ST) == 2 ? 0x7fff7fffu : 0x7fffffffu, one = sizeof(ST) == 2 ? 0x00800080u : 0x00800000u;
+    constexpr uint32_t sign = ~body;  // where an exponent of all ones overflows to
+#pragma unroll 1
+    for (int i = 4 * tid; i < TileLoad<ST, DH>::BYTES; i += 1024) {
+        uint32_t* p = reinterpret_cast<uint32_t*>(t + i);
+        const uint32_t x = *p, bad = ((x & body) + one) & sign;
+        if constexpr (sizeof(ST) == 2) {
+            const uint32_t lo = bad & 0x8000u ? (x & 0x8000u) | 0x7f7fu : x & 0xffffu;
+            const uint32_t hi = bad >> 31 ? (x & 0x80000000u) | 0x7f7f0000u : x & 0xffff0000u;
+            *p = lo | hi;
+        } else {
+            *p = bad ? (x & sign) | 0x7f7fffffu : x;
+        }
+    }
+}
+
+// 1 where a value is infinite with this sign or NaN (any: not finite), otherwise 0.
+template <bool any>
+__device__ __forceinline__ Frag8<uint16_t> not_finite(const Frag8<uint16_t>& f, uint32_t sign) {
+    u32x4 w = __builtin_bit_cast(u32x4, f.v);
+    auto is = [&](uint32_t h) __attribute__((always_inline)) {
+        const uint32_t m = h & 0x7fffu;
+        return any ? m >= 0x7f80u : (m > 0x7f80u) | (h == (0x7f80u | sign << 15));
+    };
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        w[i] = (is(w[i] & 0xffffu) ? 0x3f80u : 0u) | (is(w[i] >> 16) ? 0x3f800000u : 0u);
+    Frag8<uint16_t> x;
+    x.v = __builtin_bit_cast(bf16x8, w);
+    return x;
+}
+template <bool any>
+__device__ __forceinline__ Frag8<float> not_finite(const Frag8<float>& f, uint32_t sign) {
+    const float inf = sign ? -__builtin_inff() : __builtin_inff();
+    Frag8<float> x;
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        x.v[e] = (any ? !(fabsf(f.v[e]) < __builtin_inff()) : (f.v[e] == inf) | (f.v[e] != f.v[e])) ? 1.f : 0.f;
+    return x;
+}
+
+// What is not finite in a tile joins the sums x (value i of x[n][db] is column
+// 16 db + 4 g + i of the lane's n-th row or key, which pairs with tile row r iff
+// in(r, n)): products of ones count it, by sign, as NaN where both signs count.
+// nan: NaN for either, for sums whose other factor may have any sign or be 0.
+template <typename ST, int DH, bool nan, int N, class IN>
+__device__ __forceinline__ void add_not_finite(const TileReads<ST, DH>& rd, const unsigned char* t, int g,
+                                               f32x4 (&x)[N][DH / 16], const IN& in) {
+    constexpr int M = kTileRows<ST> / 32;
+    Frag8<ST> pairs[N][M];
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int u = 0; u < M; ++u) {
+            float v[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = in(32 * u + 16 * (e >> 2) + 4 * g + (e & 3), n) ? 1.f : 0.f;
+            pairs[n][u] = frag8_from<ST>(v);
+        }
+#pragma unroll
+    for (int db = 0; db < DH / 16; ++db) {
+        __builtin_amdgcn_sched_barrier(0);  // (a rare path: few registers)
+        f32x4 up[N], down[N];
+#pragma unroll
+        for (int n = 0; n < N; ++n) up[n] = down[n] = zero4();
+#pragma unroll
+        for (int u = 0; u < M; ++u) {
+            const Frag8<ST> f = rd.cols(t, u, db), p = not_finite<nan>(f, 0), m = not_finite<nan>(f, 1);
+#pragma unroll
+            for (int n = 0; n < N; ++n) {
+                mma8(up[n], p, pairs[n][u]);
+                if constexpr (!nan) mma8(down[n], m, pairs[n][u]);
+            }
+        }
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                x[n][db][i] += up[n][i] > 0.f ? (nan ? __builtin_nanf("") : __builtin_inff()) : 0.f;
+                if constexpr (!nan) x[n][db][i] += down[n][i] > 0.f ? -__builtin_inff() : 0.f;
+            }
+    }
+}
+
+template <int N>
+__device__ __forceinline__ bool finite4(const f32x4 (&x)[N]) {
+    float t = 0.f;
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) t = __builtin_fmaf(x[n][i], 0.f, t);
+    return t == 0.f;
+}
+
+// Whether x holds in some lane of the workgroup's 4 waves (lds: 16 bytes that are free).
+__device__ __forceinline__ bool any_of_workgroup(unsigned char* lds, int wave, int lane, bool x) {
+    uint32_t* f = reinterpret_cast<uint32_t*>(lds);
+    const bool mine = __builtin_amdgcn_ballot_w64(x) != 0;
+    if (lane == 0) f[wave] = mine;
+    __syncthreads();
+    const uint32_t any = __builtin_amdgcn_readfirstlane((int)(f[0] | f[1] | f[2] | f[3]));
+    __syncthreads();
+    return any != 0;
 }
 
 // Rows of 16 N results (column c16 of block n, values 4 g + i of every 16, times

@@ -34,22 +34,27 @@ struct FwdGeom {
     int nb, parts;
 };
 
-template <typename ST, int DH, int QN>
-__global__ __launch_bounds__(256, 2) void wattn_fwd_kernel(AttnArgs a, FwdGeom G, Parts part, uint32_t first) {
-    using TL = TileLoad<ST, DH>;
-    constexpr int KB = TL::TB, NB = KB / 16, QB = 64 * QN, STG = kStages, NS = DH / 32, ND = DH / 16;
-    constexpr int TILE = TL::BYTES, STAGE = 2 * TILE, LD = TL::LD;
-    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, c16 = lane & 15;
+struct FwdCall {
+    AttnArgs a;
+    FwdGeom G;
+    Parts part;
+    uint32_t first;
+};
 
-    // Workgroups of one XCD take neighbouring blocks: the blocks of a key head
-    // share its keys.  Without a window later blocks are longer and go first.
+// A part of a block of QB rows, by its number: 64 QN of its rows, from row `from` on.
+// True (only without `again`): to be done again.
+template <typename ST, int DH, int QN, int QB, bool again>
+__device__ __forceinline__ bool fwd_body(unsigned char* smem, const AttnArgs& a, const FwdGeom& G, const Parts& part,
+                                         uint32_t id, int from, int tid) {
+    using TL = TileLoad<ST, DH>;
+    constexpr int KB = TL::TB, NB = KB / 16, STG = kStages, NS = DH / 32, ND = DH / 16;
+    constexpr int TILE = TL::BYTES, STAGE = 2 * TILE, LD = TL::LD;
+    const int lane = tid & 63, wave = tid >> 6, g = lane >> 4, c16 = lane & 15;
     const uint32_t per = (uint32_t)G.nb * G.parts;
-    uint32_t id = first ? first + blockIdx.x : (uint32_t)xcd_logical_id(blockIdx.x, gridDim.x);
     const int bh = (int)(id / per), b = bh / a.Hkv, hk = bh % a.Hkv;
     id %= per;
     const int pt = (int)(id % G.parts), blk = a.W ? (int)(id / G.parts) : G.nb - 1 - (int)(id / G.parts);
-    const int R = a.Tq * a.G, r0 = blk * QB, wr0 = r0 + 16 * QN * wave;
+    const int R = a.Tq * a.G, r0 = blk * QB, wr0 = r0 + from + 16 * QN * wave;
     const int qn = seq_len_of(a.ql, b, a.Tq), kn = seq_len_of(a.kl, b, a.N), off = kn - qn;
     const int rn = qn * a.G;  // rows of this sequence
 
@@ -109,6 +114,12 @@ __global__ __launch_bounds__(256, 2) void wattn_fwd_kernel(AttnArgs a, FwdGeom G
             for (int st = 0; st < NS; ++st) take(qf[qs][st]);
 
         const float c2 = a.scale * kLog2e;  // scores in log2 units
+        // whether the block's rows see tile e0 in part
+        const int pb0 = off + a.gd.div(r0), pb1 = off + a.gd.div(min(r0 + QB, rn) - 1);
+        auto in_part = [&](int e0) __attribute__((always_inline)) {
+            return e0 + KB > list.count || list.key(e0 + KB - 1) > pb0 ||
+                   (a.W && (e0 >= list.s ? list.key(e0) : list.lo) <= pb1 - a.W);
+        };
         auto tile_step = [&](int it, auto bufc) __attribute__((always_inline)) {
             constexpr int BUF = decltype(bufc)::value;
             wait_vmcnt<(STG - 2) * 2 * LD>();  // tile it is in LDS
@@ -119,6 +130,11 @@ __global__ __launch_bounds__(256, 2) void wattn_fwd_kernel(AttnArgs a, FwdGeom G
             const int e0 = KB * (tbeg + it);
             // keys of the tile's window part: at least kmin, at most kmax
             const int kmax = list.key(min(e0 + KB, list.count) - 1), kmin = e0 >= list.s ? list.key(e0) : list.lo;
+            if constexpr (again)
+                if (in_part(e0)) {
+                    keep_finite<ST, DH>(smem + BUF * STAGE + TILE, tid);
+                    __syncthreads();
+                }
             if (e0 >= list.s && (kmin > pw1 || (a.W && kmax <= pw0 - a.W && kmin >= a.S))) return;  // nothing for this wave
 
             f32x4 s[QN][NB];
@@ -175,7 +191,10 @@ __global__ __launch_bounds__(256, 2) void wattn_fwd_kernel(AttnArgs a, FwdGeom G
 #pragma unroll
                     for (int i = 0; i < 4; ++i) mloc = fmaxf(mloc, s[qs][sb][i]);
                 mloc = rows4_max(mloc) * c2;
-                m_new[qs] = mloc > m_run[qs] + 8.f ? mloc : m_run[qs];
+                // (again: 16 above the maximum, weights below 2^-8, so that sums over
+                // finite values of any size stay finite)
+                if constexpr (again) m_new[qs] = mloc > m_run[qs] - 8.f ? mloc + 16.f : m_run[qs];
+                else m_new[qs] = mloc > m_run[qs] + 8.f ? mloc : m_run[qs];
                 m_use[qs] = m_new[qs] == -__builtin_inff() ? 0.f : m_new[qs];
                 moved |= m_new[qs] != m_run[qs];
             }
@@ -229,43 +248,37 @@ __global__ __launch_bounds__(256, 2) void wattn_fwd_kernel(AttnArgs a, FwdGeom G
         }
         mfma_drain();     // the MFMA results are read below
         wait_vmcnt<0>();  // the trailing loads still write into the ring
-    }
-    __syncthreads();
+        __syncthreads();
 #pragma unroll
-    for (int qs = 0; qs < QN; ++qs) l_run[qs] = rows4_sum(l_run[qs]);
-
-    // A weight of 0 times a value that is not finite is NaN: if some result of
-    // the wave is not finite, its rows are done again one by one, over the keys
-    // that each of them sees.
-    bool fine = true;
-#pragma unroll
-    for (int qs = 0; qs < QN; ++qs) {
-        float t = l_run[qs] * 0.f;
-#pragma unroll
-        for (int db = 0; db < ND; ++db)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) t = __builtin_fmaf(o[qs][db][i], 0.f, t);
-        fine &= t == 0.f;
-    }
-    const bool parts = G.parts > 1;
-    const int64_t rows = (int64_t)a.B * a.Hq * a.Tq;
-    if (__builtin_amdgcn_ballot_w64(!fine)) {
+        for (int qs = 0; qs < QN; ++qs) l_run[qs] = rows4_sum(l_run[qs]);
+        if constexpr (again) {
+            TL ul = tl;  // (uniform, which the compiler does not see here)
+            ul.lds = __builtin_amdgcn_readfirstlane(ul.lds);
 #pragma unroll 1
-        for (int r = wr0; r < min(wr0 + 16 * QN, R); ++r) {
-            const int i = a.gd.div(r), h = hk * a.G + r - i * a.G;
-            const int64_t row = qrow_index(a, b, hk, r, i);
-            float q[RowLanes<DH>::N], x[RowLanes<DH>::N] = {}, m = -__builtin_inff(), l = 0.f;
-            if (r < rn) {
-                row_load<ST, DH>(row_ptr<ST>(a.q, b, h, i), lane, q);
-                row_attend<DH>(a, WideKeys<ST, DH>{a, b, hk}, [&](int e) { return list.key(e); }, KB * tbeg,
-                               min(KB * (tbeg + ntile), list.count), off + i, kn, q, lane, m, l, x);
+            for (int e0 = KB * tbeg; e0 < KB * (tbeg + ntile); e0 += KB) {
+                if (!in_part(e0)) continue;
+                vt.issue(ul, list, e0, __builtin_amdgcn_readfirstlane(lbase));
+                wait_vmcnt<0>();
+                __syncthreads();
+                add_not_finite<ST, DH, false>(rd, smem, g, o, [&](int r, int qs) __attribute__((always_inline)) {
+                    return (e0 + r < list.count) & sees(a, pos[qs], list.key(e0 + r));
+                });
+                __syncthreads();
             }
-            row_finish<ST, DH>(a, b, h, i, row, lane, m, l, x, parts ? part.o + (pt * rows + row) * DH : nullptr,
-                               part.ml + (pt * rows + row) * 2);
+        } else {
+            // A sum of weights that is not finite comes from the keys that the row
+            // sees (the others' scores are masked before), and is the result.  With
+            // finite weights a value of a key that the row does not see may have got in.
+            bool spoilt = false;
+#pragma unroll
+            for (int qs = 0; qs < QN; ++qs)
+                spoilt |= wr0 + 16 * qs + c16 < rn && fabsf(l_run[qs]) < __builtin_inff() && !finite4(o[qs]);
+            if (any_of_workgroup(smem, wave, lane, spoilt)) return true;
         }
-        return;
     }
-    if (parts) {
+
+    if (G.parts > 1) {
+        const int64_t rows = (int64_t)a.B * a.Hq * a.Tq;
 #pragma unroll
         for (int qs = 0; qs < QN; ++qs) {
             const int r = wr0 + 16 * qs + c16;
@@ -278,15 +291,18 @@ __global__ __launch_bounds__(256, 2) void wattn_fwd_kernel(AttnArgs a, FwdGeom G
                     live ? make_float4(o[qs][db][0], o[qs][db][1], o[qs][db][2], o[qs][db][3]) : make_float4(0, 0, 0, 0);
             if (g == 0) *reinterpret_cast<float2*>(part.ml + at * 2) = live ? make_float2(m_run[qs], l_run[qs]) : make_float2(-__builtin_inff(), 0.f);
         }
-        return;
+        return false;
     }
     // out = O / l, lse = m ln 2 + log l
     float inv[QN];
 #pragma unroll
     for (int qs = 0; qs < QN; ++qs) {
         const int r = wr0 + 16 * qs + c16;
-        const bool live = r < rn && l_run[qs] > 0.f;
+        const bool live = r < rn && l_run[qs] != 0.f;  // (a sum that is NaN is a result)
         inv[qs] = live ? 1.f / l_run[qs] : 0.f;
+        if (!live)
+#pragma unroll
+            for (int db = 0; db < ND; ++db) o[qs][db] = zero4();
         if (a.lse && g == 0 && r < R)
             a.lse[qrow_index(a, b, hk, r, qi[qs])] = live ? m_run[qs] * kLn2 + logf(l_run[qs]) : -__builtin_inff();
     }
@@ -294,6 +310,39 @@ __global__ __launch_bounds__(256, 2) void wattn_fwd_kernel(AttnArgs a, FwdGeom G
         const int r = wr0 + lr;
         return r < R ? qrow_ptr<ST>(a, a.out, b, hk, r, a.gd.div(r)) : nullptr;
     });
+    return false;
+}
+
+// The second time, as a function of its own: what it takes of registers, and how its
+// code is laid out, is no matter of the first walk.  c: the kernel's arguments, lds: its LDS.
+template <typename ST, int DH, int QB>
+__device__ __attribute__((noinline)) void fwd_again(const void* c, uint32_t lds, uint32_t id) {
+    const FwdCall call = uniform_args<FwdCall>(c);
+    unsigned char* smem = lds_at(__builtin_amdgcn_readfirstlane(lds));
+    id = __builtin_amdgcn_readfirstlane(id);
+#pragma unroll 1
+    for (int from = 0; from < QB; from += 64) {
+        __syncthreads();
+        fwd_body<ST, DH, 1, QB, true>(smem, call.a, call.G, call.part, id, from, threadIdx.x);
+    }
+}
+
+// Waves per SIMD that the first walk's registers allow.
+template <typename ST, int DH, int QN>
+constexpr int fwd_waves() {
+    if (DH == 128) return 2;
+    if (sizeof(ST) == 4) return DH == 64 ? 4 : 5;
+    return DH == 64 ? (QN == 2 ? 3 : 4) : QN == 2 ? 4 : 6;
+}
+
+template <typename ST, int DH, int QN>
+__global__ __launch_bounds__(256, (fwd_waves<ST, DH, QN>())) void wattn_fwd_kernel(FwdCall c) {
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+    // Workgroups of one XCD take neighbouring blocks: the blocks of a key head
+    // share its keys.  Without a window later blocks are longer and go first.
+    const uint32_t id = c.first ? c.first + blockIdx.x : (uint32_t)xcd_logical_id(blockIdx.x, gridDim.x);
+    if (fwd_body<ST, DH, QN, 64 * QN, false>(smem, c.a, c.G, c.part, id, 0, threadIdx.x))
+        fwd_again<ST, DH, 64 * QN>((const void*)__builtin_amdgcn_kernarg_segment_ptr(), lds_addr(smem), id);
 }
 
 // A row of the call: the parts in their order, M = max m_s, L = sum l_s 2^(m_s - M).
@@ -320,7 +369,12 @@ __global__ __launch_bounds__(256) void wattn_merge_kernel(AttnArgs a, int parts,
             }
     }
     const int i = (int)(row % a.Tq), h = (int)(row / a.Tq % a.Hq), b = (int)(row / a.Tq / a.Hq);
-    row_finish<ST, DH>(a, b, h, i, row, lane, M, L, o, nullptr, nullptr);
+    // L is 0 for a row that sees nothing (its out is 0), and NaN stays NaN
+    const float f = L == 0.f ? 0.f : 1.f / L;
+#pragma unroll
+    for (int n = 0; n < RowLanes<DH>::N; ++n)
+        if (RowLanes<DH>::has(lane)) st1<ST>(row_ptr<ST>(a.out, b, h, i) + lane + 64 * n, o[n] * f);
+    if (lane == 0 && a.lse) a.lse[row] = L == 0.f ? -__builtin_inff() : M * kLn2 + logf(L);
 }
 
 // Blocks of 128 rows share K and V fragments over two matrix instructions each
@@ -353,7 +407,7 @@ int launch_fwd(const AttnArgs& a, const FwdGeom& G, float* buf, hipStream_t stre
     auto kern = wattn_fwd_kernel<ST, DH, QN>;
     if (allow_lds((const void*)kern, lds)) return -1;
     return launch_parts((uint64_t)a.B * a.Hkv * G.nb * G.parts, 256, [&](uint32_t first, uint32_t blocks) {
-        hipLaunchKernelGGL(kern, dim3(blocks), dim3(256), lds, stream, a, G, part, first);
+        hipLaunchKernelGGL(kern, dim3(blocks), dim3(256), lds, stream, FwdCall{a, G, part, first});
         return hipGetLastError() == hipSuccess ? 0 : -1;
     });
 }

@@ -1,0 +1,186 @@
+"""Keys, values and queries that hold infinities or NaN: they reach what sees them, nothing else, and in about the
+time of any other call, also where a row's keys or a key's rows are worked on in parts."""
+import math
+
+import pytest
+import torch
+
+from ops_util import HALF, U32, mask_of, rand_rows
+from paper_2505_00315_amd import ops
+
+pytestmark = pytest.mark.gpu
+
+# B, Hq, Hkv, dh, Q, N, window, sinks
+CASES = [
+    (1, 2, 1, 64, 1, 3000, 0, 0),       # one token, its keys in parts
+    (2, 4, 2, 128, 5, 2500, 700, 3),    # a few tokens, their keys in parts
+    (1, 4, 2, 64, 300, 300, 40, 70),
+    (2, 8, 2, 64, 250, 350, 100, 5),    # few key blocks: their rows in parts
+    (1, 12, 2, 128, 200, 200, 0, 0),    # the same without a window
+    (1, 6, 2, 32, 150, 260, 60, 2),     # a group that does not divide a tile
+    (1, 70, 1, 32, 9, 40, 7, 2),        # more heads to a key head than a tile has rows
+]
+IDS = [f"{c[0]}x{c[1]}/{c[2]}x{c[3]}-{c[4]}of{c[5]}-w{c[6]}s{c[7]}" for c in CASES]
+WIDE = (5, 16, 8, 64, 1700, 1700, 200, 4)  # enough blocks of 128 rows and of 128 keys for every CU
+
+
+def setup(case, dtype, seed):
+    B, Hq, Hkv, dh, Q, N, window, sinks = case
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    g = torch.Generator().manual_seed(seed)
+    x = {n: rand_rows(g, B, H, T, dh, dt, "bthd") for n, H, T in (("q", Hq, Q), ("k", Hkv, N), ("v", Hkv, N), ("do", Hq, Q))}
+    x["q"] = torch.where(x["q"] == 0, 1.0, x["q"])  # (0 times infinity would be another case)
+    return ops.make_attn_shape(B, Hq, Hkv, Q, N, dh, dtype, window=window, sinks=sinks), x, dt
+
+
+def sums(see, w, y):
+    """sum over the pairs that see names of w [i, j] y [j, :], in 64 bits; other pairs take no part, whatever y holds."""
+    out = [torch.where(see[i:i + 64, :, None], w[i:i + 64, :, None] * y, 0.0).sum(1) for i in range(0, see.shape[0], 64)]
+    return torch.cat(out)
+
+
+def formula(x, b, h, G, see, grad=False):
+    """One query head by the definition.  A row whose scores are all minus infinity counts as one that sees nothing."""
+    Q, K, V = x["q"][b, h].double(), x["k"][b, h // G].double(), x["v"][b, h // G].double()
+    scale = 1 / math.sqrt(Q.shape[1])
+    S = torch.where(see, Q @ K.T * scale, -math.inf)
+    top = S.amax(1, keepdim=True)
+    E = torch.where(see, torch.exp(S - torch.where(top == -math.inf, 0.0, top)), 0.0)
+    total = E.sum(1, keepdim=True)
+    P = E / torch.where(total == 0, 1.0, total)
+    O = sums(see, P, V)
+    res = {"out": O, "lse": (top + torch.log(total)).squeeze(1), "mag": P.abs() @ torch.nan_to_num(V, 0.0, 0.0, 0.0).abs()}
+    return res
+
+
+def agree(got, ref, bound, what):
+    """Not finite in the same places, and within the bound elsewhere."""
+    g, r = got.double(), ref
+    assert torch.equal(torch.isfinite(g), torch.isfinite(r)), (what, int((torch.isfinite(g) != torch.isfinite(r)).sum()))
+    err = torch.where(torch.isfinite(r), (g - r).abs(), 0.0)
+    bad = ~(err <= bound) & torch.isfinite(r)
+    assert not bool(bad.any()), (what, float(err.max()))
+
+
+def bound(ref, dt, dh, n):
+    """As in attention_bounds: weights rounded to the storage type (bf16), the result once, and fp32 sums; scores of
+    standard normal rows are below 16 in magnitude here."""
+    e = U32 * ((dh + 4) * 16 + n + dh + 16)
+    return HALF[dt] * (ref["out"].abs() + (ref["mag"] if dt == torch.bfloat16 else 0)) + e * ref["mag"]
+
+
+def spoil_values(v, b, h, N, first, row):
+    """An infinity of either sign, NaN, and both infinities in one column, at keys spread from ``first`` on; a row of NaN."""
+    at = [first + (N - first) * i // 6 for i in range(6)]
+    v[b, h, at[0], 1], v[b, h, at[1], 2], v[b, h, at[2], 3] = math.inf, -math.inf, math.nan
+    v[b, h, at[3], 4], v[b, h, at[4], 4] = math.inf, -math.inf
+    if row:
+        v[b, h, at[5]] = math.nan
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("case", [*CASES, WIDE], ids=[*IDS, "wide"])
+def test_values_reach_the_rows_that_see_them(case, dtype):
+    B, Hq, Hkv, dh, Q, N, window, sinks = case
+    shape, x, dt = setup(case, dtype, 1)
+    G, b, hk = Hq // Hkv, B - 1, Hkv - 1
+    clean = ops.window_attention(shape, x["q"], x["k"], x["v"])
+    see = mask_of(Q, N, Q, N, window, sinks, "cuda")
+    for first, row in ((0, True), (N // 2, True), (0, False), (N // 2, False)):
+        y = {**x, "v": x["v"].clone()}
+        spoil_values(y["v"], b, hk, N, first, row)
+        out, lse = ops.window_attention(shape, y["q"], y["k"], y["v"])
+        # m ln 2 + log l, in the second walk with another m, up to 24 away in log2 units.  Either has 6 roundings of
+        # terms of at most |lse| + 24, and those of the exponentials' arguments, half a step of numbers below 64
+        assert bool(((lse - clean[1]).abs() <= 2 * U32 * (6 * (clean[1].abs() + 24) + 64 * math.log(2))).all())
+        for h in range(hk * G, (hk + 1) * G):
+            ref = formula(y, b, h, G, see)
+            agree(out[b, h], ref["out"], bound(ref, dt, dh, N), (case, h))
+            for s in (math.inf, -math.inf):
+                assert torch.equal(out[b, h].double() == s, ref["out"] == s)
+        rest = torch.ones(B, Hq, dtype=torch.bool, device="cuda")
+        rest[b, hk * G:(hk + 1) * G] = False
+        assert torch.equal(out[rest], clean[0][rest])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("case", CASES, ids=IDS)
+def test_keys_and_queries_reach_the_rows_that_see_them(case, dtype):
+    """NaN in a key; an infinity in one, which takes the weight of rows that it is against; NaN in a query."""
+    B, Hq, Hkv, dh, Q, N, window, sinks = case
+    shape, x, dt = setup(case, dtype, 2)
+    G, b, hk = Hq // Hkv, B - 1, Hkv - 1
+    see = mask_of(Q, N, Q, N, window, sinks, "cuda")
+    for j, what in ((N - 1 - N // 5, math.nan), (N // 3, math.inf), (N - 1, -math.inf), (0, math.inf)):
+        y = {**x, "k": x["k"].clone(), "q": x["q"].clone()}
+        y["k"][b, hk, j, 5] = what
+        y["q"][b, hk * G, Q // 2, 6] = math.nan
+        out, lse = ops.window_attention(shape, y["q"], y["k"], y["v"])
+        for h in range(hk * G, (hk + 1) * G):
+            ref = formula(y, b, h, G, see)
+            agree(out[b, h], ref["out"], bound(ref, dt, dh, N), (case, h, j))
+            assert torch.equal(torch.isnan(lse[b, h]), torch.isnan(ref["lse"]))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("case", CASES, ids=IDS)
+def test_sums_of_the_largest_values_are_finite(case, dtype):
+    """Values of up to 3e38: weights that reach 2^8 within the walk would take their sums past the type's range."""
+    B, Hq, Hkv, dh, Q, N, window, sinks = case
+    shape, x, dt = setup(case, dtype, 6)
+    x["v"] = (x["v"].sign() * 3e38 * torch.linspace(0.1, 1.0, dh, device="cuda")).to(dt)
+    out, _ = ops.window_attention(shape, x["q"], x["k"], x["v"])
+    see = mask_of(Q, N, Q, N, window, sinks, "cuda")
+    for h in range(Hq):
+        ref = formula(x, 0, h, Hq // Hkv, see)
+        agree(out[0, h], ref["out"], bound(ref, dt, dh, N), (case, h))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rows_past_the_lengths_are_zero_whatever_the_others_hold(dtype):
+    case = (2, 4, 2, 64, 200, 200, 30, 3)
+    shape, x, _ = setup(case, dtype, 3)
+    lens = torch.tensor([200, 77], dtype=torch.int32, device="cuda")
+    x["v"][:, :, 5::9] = math.inf
+    x["v"][1, :, 77:] = math.nan
+    out, lse = ops.window_attention(shape, x["q"], x["k"], x["v"], q_lens=lens, kv_lens=lens)
+    assert not bool(out[1, :, 77:].any()) and bool((lse[1, :, 77:] == -math.inf).all())
+
+
+def best_time(f, n=5):
+    f()
+    torch.cuda.synchronize()
+    times = []
+    for _ in range(n):
+        a, b = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+        a.record()
+        f()
+        b.record()
+        b.synchronize()
+        times.append(a.elapsed_time(b))
+    return min(times)
+
+
+# calls of some tenths of a millisecond
+TIMED = [(1, 16, 4, 128, 4096, 4096, 0, 0), (2, 8, 8, 64, 8192, 8192, 1000, 4), (16, 32, 8, 128, 1, 16384, 0, 0)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("case", TIMED, ids=[f"{c[3]}x{c[4]}of{c[5]}w{c[6]}" for c in TIMED])
+def test_a_diverged_call_takes_no_longer_than_a_few_others(case, dtype):
+    """All of a tensor NaN, or one early value that every later row sees: the tiles that are seen in part (2 or 3 of a
+    row block's) are visited twice, nothing is done key by key."""
+    shape, x, _ = setup(case, dtype, 4)
+    scratch = ops.alloc_attn_scratch(shape)
+    out, lse = ops.window_attention(shape, x["q"], x["k"], x["v"], scratch=scratch)
+
+    def call(y):
+        return lambda: ops.window_attention(shape, y["q"], y["k"], y["v"], out=out, lse=lse, scratch=scratch)
+    base = best_time(call(x))
+    for names in (("q", "k", "v"), ("v",), ("k",)):
+        y = {**x, **{n: torch.full_like(x[n], math.nan) for n in names}}
+        assert best_time(call(y)) <= 4 * base, names
+        assert bool(torch.isnan(out).all())
+    y = {**x, "v": x["v"].clone()}
+    y["v"][:, :, 0, 3] = math.inf
+    assert best_time(call(y)) <= 4 * base
