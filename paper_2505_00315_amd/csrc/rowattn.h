@@ -46,17 +46,7 @@ __device__ __forceinline__ float row_dot(const float (&x)[RowLanes<DH>::N], cons
     return wave_sum_f32(s);
 }
 
-// Sources of the keys and values of one sequence and key head.
-template <typename ST, int DH>
-struct WideKeys {
-    const AttnArgs& a;
-    int b, h;
-    __device__ __forceinline__ bool load(int j, int lane, float (&k)[RowLanes<DH>::N], float (&v)[RowLanes<DH>::N]) const {
-        row_load<ST, DH>(row_ptr<ST>(a.k, b, h, j), lane, k);
-        row_load<ST, DH>(row_ptr<ST>(a.v, b, h, j), lane, v);
-        return true;
-    }
-};
+// The keys and values of one sequence and key head.
 template <int DH>
 struct CacheKeys {
     const CacheArgs& c;
@@ -101,61 +91,6 @@ __device__ __forceinline__ void row_attend(const AttnArgs& a, const KEYS& keys, 
 #pragma unroll
         for (int i = 0; i < N; ++i) o[i] = o[i] * al + w * v[i];
     }
-}
-
-// Gradient of one query row: dq = scale sum_j ds_j k_j, ds = p (dout v_j - D)
-// over the keys that it sees.
-template <typename ST, int DH>
-__device__ __forceinline__ void row_dq(const AttnArgs& a, int b, int h, int i, int p, int kn, int lane) {
-    constexpr int N = RowLanes<DH>::N;
-    const float c2 = a.scale * kLog2e;
-    float q[N], g[N], k[N], v[N], dq[N] = {};
-    row_load<ST, DH>(row_ptr<ST>(a.q, b, h, i), lane, q);
-    row_load<ST, DH>(row_ptr<ST>(a.dout, b, h, i), lane, g);
-    const float2 ld = a.ld[((int64_t)b * a.Hq + h) * a.Tq + i];
-    const KeyList list = keys_of(a, p, p, kn);
-    const WideKeys<ST, DH> keys{a, b, h / a.G};
-#pragma unroll 1
-    for (int e = 0; e < list.count; ++e) {
-        keys.load(list.key(e), lane, k, v);
-        const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(row_dot<DH>(q, k), c2, -ld.x));
-        const float ds = w * (row_dot<DH>(g, v) + ld.y);
-#pragma unroll
-        for (int n = 0; n < N; ++n) dq[n] += ds * k[n];
-    }
-#pragma unroll
-    for (int n = 0; n < N; ++n)
-        if (RowLanes<DH>::has(lane)) st1<ST>(row_ptr<ST>(a.dq, b, h, i) + lane + 64 * n, dq[n] * a.scale);
-}
-
-// Gradients of one key row over the rows ra .. rb - 1 of the group's list for
-// which ok(position) holds: dv = sum_i p_i dout_i, dk = scale sum_i ds_i q_i.
-template <typename ST, int DH, class OK>
-__device__ __forceinline__ void row_dkv(const AttnArgs& a, int b, int hk, int j, int off, int ra, int rb, const OK& ok,
-                                        int lane, float (&dk)[RowLanes<DH>::N], float (&dv)[RowLanes<DH>::N]) {
-    constexpr int N = RowLanes<DH>::N;
-    const float c2 = a.scale * kLog2e;
-    float q[N], g[N], k[N], v[N];
-    WideKeys<ST, DH>{a, b, hk}.load(j, lane, k, v);
-#pragma unroll
-    for (int n = 0; n < N; ++n) dk[n] = dv[n] = 0.f;
-#pragma unroll 1
-    for (int r = ra; r < rb; ++r) {
-        const int i = a.gd.div(r), h = hk * a.G + r - i * a.G;
-        if (!ok(off + i)) continue;
-        row_load<ST, DH>(row_ptr<ST>(a.q, b, h, i), lane, q);
-        row_load<ST, DH>(row_ptr<ST>(a.dout, b, h, i), lane, g);
-        const float2 ld = a.ld[((int64_t)b * a.Hq + h) * a.Tq + i];
-        const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(row_dot<DH>(q, k), c2, -ld.x));
-        const float ds = w * (row_dot<DH>(g, v) + ld.y);
-#pragma unroll
-        for (int n = 0; n < N; ++n) {
-            dk[n] += ds * q[n];
-            dv[n] += w * g[n];
-        }
-    }
-#pragma unroll
-    for (int n = 0; n < N; ++n) dk[n] *= a.scale;
 }
 
 }  // namespace mosa

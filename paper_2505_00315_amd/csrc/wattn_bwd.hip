@@ -133,19 +133,21 @@ struct Walk {
     __device__ __forceinline__ int row(int t) const { return (t < cut ? early : late) + step * min(t, last); }
 };
 
-// Keys k0 .. of (b, hk), 16 CB per wave: part `chunk` of the rows that see them
+// Keys k0 .. k0 + KEYS - 1 of (b, hk): part `chunk` of the rows that see them
 // within the window, or, far, chunk `chunk` of those beyond the sinks' window.
-template <typename ST, int DH, int CB, bool far>
-__device__ __forceinline__ void dkv_body(unsigned char* smem, const AttnArgs a, const BwdGeom G, int b, int hk, int k0,
-                                         int chunk, float* sums) {
+// This call does 64 CB of the keys, from k0 + from on.  True (only without
+// `again`): to be done again.
+template <typename ST, int DH, int CB, int KEYS, bool far, bool again>
+__device__ __forceinline__ bool dkv_body(unsigned char* smem, const AttnArgs a, const BwdGeom G, int b, int hk, int k0,
+                                         int from, int chunk, float* sums) {
     using TL = TileLoad<ST, DH>;
     constexpr int TB = TL::TB, NS = DH / 32, ND = DH / 16, STG = kStages, LD = TL::LD;
     constexpr int TILE = TL::BYTES, LDB = 4 * TB * 8, STAGE = 2 * TILE + LDB;  // q, dout, a copy of (lse, -D) per wave
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, c16 = lane & 15;
     const bool apart = G.ns > 0;  // apart: far pairs are done by chunks
     const int qn = seq_len_of(a.ql, b, a.Tq), kn = seq_len_of(a.kl, b, a.N), off = kn - qn;
-    const int kend = min(far ? min(a.S, k0 + 64) : k0 + 64 * CB, kn);  // past the block's last key
-    const int wk0 = k0 + 16 * CB * wave, wk1 = min(wk0 + 16 * CB, kend) - 1;  // this wave's keys (none: wk1 < wk0)
+    const int kend = min(far ? min(a.S, k0 + KEYS) : k0 + KEYS, kn);  // past the block's last key
+    const int wk0 = k0 + from + 16 * CB * wave, wk1 = min(wk0 + 16 * CB, kend) - 1;  // this wave's keys (none: wk1 < wk0)
 
     // rows that may see the block's keys
     int i0 = 0, i1 = 0;
@@ -193,6 +195,25 @@ __device__ __forceinline__ void dkv_body(unsigned char* smem, const AttnArgs a, 
 #pragma unroll
             for (int st = 0; st < NS; ++st) take(kf[cb][st]), take(vf[cb][st]);
 
+        // Of the tile from row r0 on, the rows (less 4 g) that the lane's keys pair with:
+        // positions from the key on and within its window, or, far, from there on.
+        auto pairs = [&](int r0, Span (&run)[CB]) __attribute__((always_inline)) {
+            const int n = min(r0 + nr, rhi) - r0, i = a.gd.div(r0), p = off + i;
+            const int skip = r0 - i * a.G + 4 * g;  // rows of the first position before the tile
+#pragma unroll
+            for (int cb = 0; cb < CB; ++cb) {
+                const int j = key[cb];
+                const bool all_later = far || a.W == 0 || (!apart && j < a.S);
+                const int lo = min(max((far ? j + a.W : j) - p, -1), TB + 1);  // in positions of the tile's first
+                const int hi = min(max(j + a.W - p, 0), TB + 1);
+                run[cb] = Span(lo * a.G - skip, min(all_later ? n : hi * a.G - (skip - 4 * g), n) - 1 - 4 * g);
+            }
+        };
+        // whether the block's keys pair with the rows of the tile from r0 on in part
+        auto in_part = [&](int r0) __attribute__((always_inline)) {
+            const int rt = min(r0 + nr, rhi), p0 = off + a.gd.div(r0), p1 = off + a.gd.div(rt - 1);
+            return !(r0 + TB == rt && (far ? p0 - (kend - 1) >= a.W : p0 >= kend - 1 && (a.W == 0 || p1 - k0 < a.W)));
+        };
         const float c2 = a.scale * kLog2e;
         auto tile_step = [&](int it, auto bufc) __attribute__((always_inline)) {
             constexpr int BUF = decltype(bufc)::value;
@@ -204,25 +225,19 @@ __device__ __forceinline__ void dkv_body(unsigned char* smem, const AttnArgs a, 
             const unsigned char* Lt = Gt + TILE + 8 * TB * wave;
             const int r0 = walk.row(it), rt = min(r0 + nr, rhi);  // the tile's rows
             const int pt0 = off + a.gd.div(r0), pt1 = off + a.gd.div(rt - 1);  // and their positions
+            if constexpr (again)
+                if (in_part(r0)) {
+                    keep_finite<ST, DH>(smem + BUF * STAGE, tid);
+                    keep_finite<ST, DH>(smem + BUF * STAGE + TILE, tid);
+                    __syncthreads();
+                }
             // nothing for this wave: no keys, rows before the keys, or past their window
             if (wk1 < wk0) return;
             if (far ? wk0 >= a.S || pt1 - wk0 < a.W : pt1 < wk0 || (a.W && pt0 - wk1 >= a.W && (apart || wk0 >= a.S))) return;
             const bool whole = r0 + TB == rt &&
                                (far ? pt0 - wk1 >= a.W : pt0 >= wk1 && (a.W == 0 || pt1 - wk0 < a.W));
-            // the tile's rows (less 4 g) that the lane's keys pair with: positions
-            // from the key on and within its window, or, far, from there on
             Span run[CB];
-            if (!whole) {
-                const int skip = r0 - (pt0 - off) * a.G + 4 * g;  // rows of the first position before the tile
-#pragma unroll
-                for (int cb = 0; cb < CB; ++cb) {
-                    const int j = key[cb], n = rt - r0;
-                    const bool all_later = far || a.W == 0 || (!apart && j < a.S);
-                    const int from = min(max((far ? j + a.W : j) - pt0, -1), TB + 1);  // in positions of the tile's first
-                    const int to = min(max(j + a.W - pt0, 0), TB + 1);
-                    run[cb] = Span(from * a.G - skip, min(all_later ? n : to * a.G - (skip - 4 * g), n) - 1 - 4 * g);
-                }
-            }
+            if (!whole) pairs(r0, run);
             // the whole tile without a branch, so that its reads, products and
             // exponentials overlap
             auto products = [&](auto mc) __attribute__((always_inline)) {
@@ -303,67 +318,61 @@ __device__ __forceinline__ void dkv_body(unsigned char* smem, const AttnArgs a, 
         }
         mfma_drain();
         wait_vmcnt<0>();
-    }
-    __syncthreads();
-
-    // sums: of every part the first G.keys keys, then of every chunk the sinks
-    const int top = far ? a.S : a.N, summed = far ? a.S : G.keys;  // keys of the output, those whose sums are kept
-    const int64_t heads = (int64_t)a.B * a.Hkv, bh = (int64_t)b * a.Hkv + hk;
-    float* sum = sums + ((far ? heads * G.kp * G.keys : 0) + (heads * chunk + bh) * summed) * 2 * DH;
-    bool fine = true;
-#pragma unroll
-    for (int cb = 0; cb < CB; ++cb) fine &= finite4(dk[cb]) && finite4(dv[cb]);
-    if (__builtin_amdgcn_ballot_w64(!fine)) {
-        // rows one by one (a pair outside the rule meets every value with a weight of 0)
+        __syncthreads();
+        if constexpr (again) {
+            const uint32_t at = __builtin_amdgcn_readfirstlane(base);
+            TL ul = tl;  // (uniform, which the compiler does not see here)
+            ul.lds = __builtin_amdgcn_readfirstlane(ul.lds);
 #pragma unroll 1
-        for (int j = wk0; j < min(wk0 + 16 * CB, top); ++j) {
-            float x[RowLanes<DH>::N] = {}, y[RowLanes<DH>::N] = {};
-            if (j <= wk1) {
-                const int ra = rlo + nr * tbeg, rb = min(rhi, ra + nr * ntile);
-                row_dkv<ST, DH>(a, b, hk, j, off, ra, rb, [&](int p) {
-                    return far ? p - j >= a.W : j <= p && (a.W == 0 || p - j < a.W || (!apart && j < a.S));
-                }, lane, x, y);
+            for (int t = 0; t < ntile; ++t) {
+                const int r0 = walk.row(t);
+                if (!in_part(r0)) continue;
+                rows.issue(a, ul, r0, rhi, at, at + 2 * TILE + 8 * TB * (ul.lds / 1024), lane);
+                Span run[CB];
+                pairs(r0, run);
+                wait_vmcnt<0>();
+                __syncthreads();
+                auto in = [&](int r, int cb) __attribute__((always_inline)) { return run[cb].has(r - 4 * g); };
+                add_not_finite<ST, DH, true>(rd, smem, g, dk, in);
+                add_not_finite<ST, DH, false>(rd, smem + TILE, g, dv, in);
+                __syncthreads();
             }
-            const bool part = j < summed;
+        } else {
+            bool spoilt = false;
 #pragma unroll
-            for (int n = 0; n < RowLanes<DH>::N; ++n) {
-                if (!RowLanes<DH>::has(lane)) continue;
-                const int c = lane + 64 * n;
-                if (part) {
-                    sum[(int64_t)j * 2 * DH + c] = x[n];
-                    sum[(int64_t)j * 2 * DH + DH + c] = y[n];
-                } else {
-                    st1<ST>(row_ptr<ST>(a.dk, b, hk, j) + c, x[n]);
-                    st1<ST>(row_ptr<ST>(a.dv, b, hk, j) + c, y[n]);
-                }
-            }
-        }
-        return;
-    }
-    if (wk0 < summed) {
-#pragma unroll
-        for (int cb = 0; cb < CB; ++cb) {
-            const int j = wk0 + 16 * cb + c16;
-            if (j >= min(summed, top)) continue;
-            const float f = j <= wk1 ? 1.f : 0.f;
-#pragma unroll
-            for (int db = 0; db < ND; ++db) {
-                float* to = sum + (int64_t)j * 2 * DH + 16 * db + 4 * g;
-                const float fs = f * a.scale;
-                *reinterpret_cast<float4*>(to) = make_float4(dk[cb][db][0] * fs, dk[cb][db][1] * fs, dk[cb][db][2] * fs, dk[cb][db][3] * fs);
-                *reinterpret_cast<float4*>(to + DH) = make_float4(dv[cb][db][0] * f, dv[cb][db][1] * f, dv[cb][db][2] * f, dv[cb][db][3] * f);
-            }
+            for (int cb = 0; cb < CB; ++cb)
+                spoilt |= wk0 + 16 * cb + c16 <= wk1 && !(finite4(dk[cb]) && finite4(dv[cb]));
+            if (any_of_workgroup(smem, wave, lane, spoilt)) return true;
         }
     }
-    if constexpr (far) return;
+
     // keys past the sequence are zero (their lanes computed its last key again)
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb)
         if (wk0 + 16 * cb + c16 > wk1)
 #pragma unroll
             for (int db = 0; db < ND; ++db) dk[cb][db] = dv[cb][db] = zero4();
-    unsigned char* mine = smem + wave * store_rows_bytes<ST, DH>(CB);
+    // sums: of every part the first G.keys keys, then of every chunk the sinks
+    const int top = far ? a.S : a.N, summed = far ? a.S : G.keys;  // keys of the output, those whose sums are kept
+    const int64_t heads = (int64_t)a.B * a.Hkv, bh = (int64_t)b * a.Hkv + hk;
+    float* sum = sums + ((far ? heads * G.kp * G.keys : 0) + (heads * chunk + bh) * summed) * 2 * DH;
     const float scale = a.scale;
+    if (wk0 < summed) {
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb) {
+            const int j = wk0 + 16 * cb + c16;
+            if (j >= min(summed, top)) continue;
+#pragma unroll
+            for (int db = 0; db < ND; ++db) {
+                float* to = sum + (int64_t)j * 2 * DH + 16 * db + 4 * g;
+                const f32x4 x = dk[cb][db] * scale, y = dv[cb][db];
+                *reinterpret_cast<float4*>(to) = make_float4(x[0], x[1], x[2], x[3]);
+                *reinterpret_cast<float4*>(to + DH) = make_float4(y[0], y[1], y[2], y[3]);
+            }
+        }
+    }
+    if constexpr (far) return false;
+    unsigned char* mine = smem + wave * store_rows_bytes<ST, DH>(CB);
     float fk[CB], fv[CB];
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb) {
@@ -379,19 +388,21 @@ __device__ __forceinline__ void dkv_body(unsigned char* smem, const AttnArgs a, 
         const int j = wk0 + r;
         return j < a.N && j >= summed ? row_ptr<ST>(to_v, b, hk, j) : nullptr;
     });
+    return false;
 }
 
-// Rows r0 .. of (b, hk), 16 QN per wave.
-template <typename ST, int DH, int QN>
-__device__ __forceinline__ void dq_body(unsigned char* smem, const AttnArgs a, int b, int hk, int r0) {
+// Rows r0 .. r0 + ROWS - 1 of (b, hk); this call does 64 QN of them, from r0 + from on.
+// True (only without `again`): to be done again.
+template <typename ST, int DH, int QN, int ROWS, bool again>
+__device__ __forceinline__ bool dq_body(unsigned char* smem, const AttnArgs a, int b, int hk, int r0, int from) {
     using TL = TileLoad<ST, DH>;
     constexpr int TB = TL::TB, NS = DH / 32, ND = DH / 16, STG = kStages, LD = TL::LD;
     constexpr int TILE = TL::BYTES, STAGE = 2 * TILE;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, c16 = lane & 15;
     const int qn = seq_len_of(a.ql, b, a.Tq), kn = seq_len_of(a.kl, b, a.N), off = kn - qn;
-    const int R = a.Tq * a.G, rn = qn * a.G, wr0 = r0 + 16 * QN * wave;
+    const int R = a.Tq * a.G, rn = qn * a.G, wr0 = r0 + from + 16 * QN * wave;
     KeyList list{0, 0, 0};
-    if (r0 < rn) list = keys_of(a, off + a.gd.div(r0), off + a.gd.div(min(r0 + 64 * QN, rn) - 1), kn);
+    if (r0 < rn) list = keys_of(a, off + a.gd.div(r0), off + a.gd.div(min(r0 + ROWS, rn) - 1), kn);
     const int ntile = (list.count + TB - 1) / TB;
 
     f32x4 dq[QN][ND];
@@ -435,6 +446,12 @@ __device__ __forceinline__ void dq_body(unsigned char* smem, const AttnArgs a, i
             for (int st = 0; st < NS; ++st) take(qf[qs][st]), take(gf[qs][st]);
         }
         const float c2 = a.scale * kLog2e;
+        // whether the block's rows see tile e0 in part
+        const int pb0 = off + a.gd.div(r0), pb1 = off + a.gd.div(min(r0 + ROWS, rn) - 1);
+        auto in_part = [&](int e0) __attribute__((always_inline)) {
+            return e0 + TB > list.count || list.key(e0 + TB - 1) > pb0 ||
+                   (a.W && (e0 >= list.s ? list.key(e0) : list.lo) <= pb1 - a.W);
+        };
         auto tile_step = [&](int it, auto bufc) __attribute__((always_inline)) {
             constexpr int BUF = decltype(bufc)::value;
             wait_vmcnt<(STG - 2) * 2 * LD>();
@@ -444,6 +461,11 @@ __device__ __forceinline__ void dq_body(unsigned char* smem, const AttnArgs a, i
             const unsigned char* Vt = Kt + TILE;
             const int e0 = TB * it;
             const int kmax = list.key(min(e0 + TB, list.count) - 1), kmin = e0 >= list.s ? list.key(e0) : list.lo;
+            if constexpr (again)
+                if (in_part(e0)) {
+                    keep_finite<ST, DH>(smem + BUF * STAGE, tid);
+                    __syncthreads();
+                }
             if (e0 >= list.s && (kmin > pw1 || (a.W && kmax <= pw0 - a.W && kmin >= a.S))) return;
             const bool whole = e0 + TB <= list.count && kmax <= pw0 && (a.W == 0 || kmin > pw1 - a.W);
             // keys kmin + 0 .. TB - 1, no sinks: those of a row are a run (entries
@@ -521,19 +543,29 @@ __device__ __forceinline__ void dq_body(unsigned char* smem, const AttnArgs a, i
         }
         mfma_drain();
         wait_vmcnt<0>();
-    }
-    __syncthreads();
-    bool fine = true;
-#pragma unroll
-    for (int qs = 0; qs < QN; ++qs) fine &= finite4(dq[qs]);
-    if (__builtin_amdgcn_ballot_w64(!fine)) {
+        __syncthreads();
+        if constexpr (again) {
+            const uint32_t at = __builtin_amdgcn_readfirstlane(base);
+            TL ul = tl;  // (uniform, which the compiler does not see here)
+            ul.lds = __builtin_amdgcn_readfirstlane(ul.lds);
 #pragma unroll 1
-        for (int r = wr0; r < min(wr0 + 16 * QN, rn); ++r) {
-            const int i = a.gd.div(r);
-            row_dq<ST, DH>(a, b, hk * a.G + r - i * a.G, i, off + i, kn, lane);
+            for (int e0 = 0; e0 < list.count; e0 += TB) {
+                if (!in_part(e0)) continue;
+                kt.issue(ul, list, e0, at);
+                wait_vmcnt<0>();
+                __syncthreads();
+                add_not_finite<ST, DH, true>(rd, smem, g, dq, [&](int r, int qs) __attribute__((always_inline)) {
+                    return (e0 + r < list.count) & sees(a, pos[qs], list.key(e0 + r));
+                });
+                __syncthreads();
+            }
+        } else {
+            bool spoilt = false;
+#pragma unroll
+            for (int qs = 0; qs < QN; ++qs) spoilt |= wr0 + 16 * qs + c16 < rn && !finite4(dq[qs]);
+            if (any_of_workgroup(smem, wave, lane, spoilt)) return true;
         }
     }
-    const bool redone = __builtin_amdgcn_ballot_w64(!fine) != 0;
 #pragma unroll
     for (int qs = 0; qs < QN; ++qs)
         if (wr0 + 16 * qs + c16 >= rn)
@@ -545,32 +577,97 @@ __device__ __forceinline__ void dq_body(unsigned char* smem, const AttnArgs a, i
     for (int qs = 0; qs < QN; ++qs) fq[qs] = scale;
     store_rows<ST, DH, QN>(smem + wave * store_rows_bytes<ST, DH>(QN), dq, fq, lane, [&](int lr) -> ST* {
         const int r = wr0 + lr;
-        return r < R && !(redone && r < rn) ? qrow_ptr<ST>(a, a.dq, b, hk, r, a.gd.div(r)) : nullptr;
+        return r < R ? qrow_ptr<ST>(a, a.dq, b, hk, r, a.gd.div(r)) : nullptr;
     });
+    return false;
+}
+
+// Waves per SIMD that the first walk's registers allow.
+template <typename ST, int DH, int CB>
+constexpr int bwd_waves() {
+    return DH == 128 || (DH == 64 && (CB == 2 || sizeof(ST) == 4)) ? 2 : DH == 32 && CB == 1 && sizeof(ST) == 2 ? 5 : 3;
+}
+
+// A workgroup's work: key blocks, then chunks of far rows, then row blocks; each kind in
+// neighbouring order on an XCD (a key head's workgroups share its rows and keys).
+struct BwdWork {
+    int kind, bh, at, part;  // keys (0) or rows (2) from `at` on, part or chunk (1) of their rows
+    __device__ __forceinline__ BwdWork(const AttnArgs& a, const BwdGeom& G, uint32_t first, uint32_t block, uint32_t blocks,
+                                       int keys, int rows) {
+        const uint32_t heads = (uint32_t)a.B * a.Hkv, n0 = heads * G.nk * G.kp, n1 = heads * G.ns * G.nc, n2 = heads * G.nq;
+        uint32_t id = first + block;
+        const bool one = first == 0 && blocks == n0 + n1 + n2;
+        if (id < n0) {
+            if (one) id = xcd_logical_id(id, n0);
+            const int per = G.nk * G.kp, k = id % per;
+            kind = 0, bh = id / per, at = k / G.kp * keys, part = k % G.kp;
+        } else if (id < n0 + n1) {
+            id -= n0;
+            const int per = G.ns * G.nc, k = id % per;
+            kind = 1, bh = id / per, at = k / G.nc * 64, part = k % G.nc;
+        } else {
+            id -= n0 + n1;
+            if (one) id = xcd_logical_id(id, n2);
+            const int q = id % G.nq;
+            kind = 2, bh = id / G.nq, at = (a.W ? q : G.nq - 1 - q) * rows, part = 0;
+        }
+    }
+};
+
+struct BwdCall {
+    AttnArgs a;
+    BwdGeom G;
+    float* sums;
+    uint32_t first;
+};
+
+// The second time, as functions of their own: what they take of registers, and how their code
+// is laid out, is no matter of the first walk.  c: the kernel's arguments, lds: its LDS.
+template <typename ST, int DH, int KEYS, bool far>
+__device__ __attribute__((noinline)) void dkv_again(const void* c, uint32_t lds, int bh, int k0, int chunk) {
+    const BwdCall call = uniform_args<BwdCall>(c);
+    unsigned char* smem = lds_at(__builtin_amdgcn_readfirstlane(lds));
+    bh = __builtin_amdgcn_readfirstlane(bh), k0 = __builtin_amdgcn_readfirstlane(k0);
+    chunk = __builtin_amdgcn_readfirstlane(chunk);
+#pragma unroll 1
+    for (int from = 0; from < KEYS; from += 64) {
+        __syncthreads();
+        dkv_body<ST, DH, 1, KEYS, far, true>(smem, call.a, call.G, bh / call.a.Hkv, bh % call.a.Hkv, k0, from, chunk, call.sums);
+    }
+}
+template <typename ST, int DH, int ROWS>
+__device__ __attribute__((noinline)) void dq_again(const void* c, uint32_t lds, int bh, int r0) {
+    const BwdCall call = uniform_args<BwdCall>(c);
+    unsigned char* smem = lds_at(__builtin_amdgcn_readfirstlane(lds));
+    bh = __builtin_amdgcn_readfirstlane(bh), r0 = __builtin_amdgcn_readfirstlane(r0);
+#pragma unroll 1
+    for (int from = 0; from < ROWS; from += 64) {
+        __syncthreads();
+        dq_body<ST, DH, 1, ROWS, true>(smem, call.a, bh / call.a.Hkv, bh % call.a.Hkv, r0, from);
+    }
+}
+// (one call at the kernel's end: what lives across a call would take registers)
+template <typename ST, int DH, int CB, int QN>
+__device__ __attribute__((noinline)) void bwd_again(const void* c, uint32_t lds, uint32_t block, uint32_t blocks) {
+    const BwdCall call = uniform_args<BwdCall>(c);
+    const BwdWork w(call.a, call.G, call.first, __builtin_amdgcn_readfirstlane(block), __builtin_amdgcn_readfirstlane(blocks),
+                    64 * CB, 64 * QN);
+    if (w.kind == 0) dkv_again<ST, DH, 64 * CB, false>(c, lds, w.bh, w.at, w.part);
+    else if (w.kind == 1) dkv_again<ST, DH, 64, true>(c, lds, w.bh, w.at, w.part);
+    else dq_again<ST, DH, 64 * QN>(c, lds, w.bh, w.at);
 }
 
 template <typename ST, int DH, int CB, int QN>
-__global__ __launch_bounds__(256, 2) void wattn_bwd_kernel(AttnArgs a, BwdGeom G, float* __restrict__ sums, uint32_t first) {
+__global__ __launch_bounds__(256, (bwd_waves<ST, DH, CB>())) void wattn_bwd_kernel(BwdCall c) {
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-    // key blocks, then chunks of far rows, then row blocks; each kind in
-    // neighbouring order on an XCD (a key head's workgroups share its rows and keys)
-    const uint32_t heads = (uint32_t)a.B * a.Hkv, n0 = heads * G.nk * G.kp, n1 = heads * G.ns * G.nc, n2 = heads * G.nq;
-    uint32_t id = first + blockIdx.x;
-    const bool one = first == 0 && gridDim.x == n0 + n1 + n2;
-    if (id < n0) {
-        if (one) id = xcd_logical_id(id, n0);
-        const int per = G.nk * G.kp, bh = id / per, k = id % per;
-        dkv_body<ST, DH, CB, false>(smem, a, G, bh / a.Hkv, bh % a.Hkv, k / G.kp * 64 * CB, k % G.kp, sums);
-    } else if (id < n0 + n1) {
-        id -= n0;
-        const int per = G.ns * G.nc, bh = id / per, k = id % per;
-        dkv_body<ST, DH, 1, true>(smem, a, G, bh / a.Hkv, bh % a.Hkv, k / G.nc * 64, k % G.nc, sums);
-    } else {
-        id -= n0 + n1;
-        if (one) id = xcd_logical_id(id, n2);
-        const int bh = id / G.nq, q = id % G.nq;
-        dq_body<ST, DH, QN>(smem, a, bh / a.Hkv, bh % a.Hkv, (a.W ? q : G.nq - 1 - q) * 64 * QN);
-    }
+    const BwdWork w(c.a, c.G, c.first, blockIdx.x, gridDim.x, 64 * CB, 64 * QN);
+    const int b = w.bh / c.a.Hkv, hk = w.bh % c.a.Hkv;
+    bool redo;
+    if (w.kind == 0) redo = dkv_body<ST, DH, CB, 64 * CB, false, false>(smem, c.a, c.G, b, hk, w.at, 0, w.part, c.sums);
+    else if (w.kind == 1) redo = dkv_body<ST, DH, 1, 64, true, false>(smem, c.a, c.G, b, hk, w.at, 0, w.part, c.sums);
+    else redo = dq_body<ST, DH, QN, 64 * QN, false>(smem, c.a, b, hk, w.at, 0);
+    if (redo)
+        bwd_again<ST, DH, CB, QN>((const void*)__builtin_amdgcn_kernarg_segment_ptr(), lds_addr(smem), blockIdx.x, gridDim.x);
 }
 
 // (lse in log2 units, -D), D = sum(out dout), of every query row, 8 columns per lane:
@@ -680,7 +777,7 @@ int launch_bwd(const AttnArgs& a, const BwdGeom& G, float* sums, hipStream_t str
     if (allow_lds((const void*)kern, lds)) return -1;
     const uint64_t blocks = (uint64_t)a.B * a.Hkv * ((uint64_t)G.nk * G.kp + G.ns * G.nc + G.nq);
     const int e = launch_parts(blocks, 256, [&](uint32_t first, uint32_t n) {
-        hipLaunchKernelGGL(kern, dim3(n), dim3(256), lds, stream, a, G, sums, first);
+        hipLaunchKernelGGL(kern, dim3(n), dim3(256), lds, stream, BwdCall{a, G, sums, first});
         return hipGetLastError() == hipSuccess ? 0 : -1;
     });
     if (e || !G.keys) return e;

@@ -39,7 +39,7 @@ def sums(see, w, y):
     return torch.cat(out)
 
 
-def formula(x, b, h, G, see, grad=False):
+def formula(x, b, h, G, see):
     """One query head by the definition.  A row whose scores are all minus infinity counts as one that sees nothing."""
     Q, K, V = x["q"][b, h].double(), x["k"][b, h // G].double(), x["v"][b, h // G].double()
     scale = 1 / math.sqrt(Q.shape[1])
@@ -49,7 +49,28 @@ def formula(x, b, h, G, see, grad=False):
     total = E.sum(1, keepdim=True)
     P = E / torch.where(total == 0, 1.0, total)
     O = sums(see, P, V)
-    res = {"out": O, "lse": (top + torch.log(total)).squeeze(1), "mag": P.abs() @ torch.nan_to_num(V, 0.0, 0.0, 0.0).abs()}
+    return {"out": O, "lse": (top + torch.log(total)).squeeze(1), "mag": sums(see, P, V.abs()), "P": P}
+
+
+def gradients(x, b, hk, G, see, dt):
+    """Gradients of a key head and of its query heads, and the terms of their bounds, as in attention64; a pair that see
+    does not name takes no part."""
+    K, V = x["k"][b, hk].double(), x["v"][b, hk].double()
+    scale, half, back = 1 / math.sqrt(K.shape[1]), HALF[dt], see.T.contiguous()
+    res = {n: 0.0 for n in ("dk", "dk_mag", "dk_d", "dv", "dv_mag")}
+    for h in range(hk * G, (hk + 1) * G):
+        f = formula(x, b, h, G, see)
+        P, O, Q, D = f["P"], f["out"], x["q"][b, h].double(), x["do"][b, h].double()
+        dS = torch.where(see, P * (D @ V.T - (D * O).sum(1, keepdim=True)), 0.0)
+        eD = half * (D.abs() * (f["mag"] + O.abs())).sum(1, keepdim=True)
+        mag = torch.where(see, P * (D.abs() @ V.abs().T + (D * O).abs().sum(1, keepdim=True)), 0.0)
+        off = torch.where(see, P * eD + half * dS.abs(), 0.0)
+        for n, w, y in (("", dS, K), ("_mag", mag, K.abs()), ("_d", off, K.abs())):
+            res["dq" + n, h] = sums(see, w, y) * scale
+        for n, w, y in (("", dS, Q), ("_mag", mag, Q.abs()), ("_d", off, Q.abs())):
+            res["dk" + n] = res["dk" + n] + sums(back, w.T, y) * scale
+        for n, w, y in (("", P, D), ("_mag", P, D.abs())):
+            res["dv" + n] = res["dv" + n] + sums(back, w.T, y)
     return res
 
 
@@ -62,10 +83,14 @@ def agree(got, ref, bound, what):
     assert not bool(bad.any()), (what, float(err.max()))
 
 
+def rounding(dh, n):
+    return U32 * ((dh + 4) * 16 + n + dh + 16)
+
+
 def bound(ref, dt, dh, n):
     """As in attention_bounds: weights rounded to the storage type (bf16), the result once, and fp32 sums; scores of
     standard normal rows are below 16 in magnitude here."""
-    e = U32 * ((dh + 4) * 16 + n + dh + 16)
+    e = rounding(dh, n)
     return HALF[dt] * (ref["out"].abs() + (ref["mag"] if dt == torch.bfloat16 else 0)) + e * ref["mag"]
 
 
@@ -147,6 +172,60 @@ def test_rows_past_the_lengths_are_zero_whatever_the_others_hold(dtype):
     assert not bool(out[1, :, 77:].any()) and bool((lse[1, :, 77:] == -math.inf).all())
 
 
+def check_gradients(case, y, got, dt, b, hk):
+    B, Hq, Hkv, dh, Q, N, window, sinks = case
+    G, e = Hq // Hkv, rounding(dh, max(N, Q * Hq // Hkv))
+    ref = gradients(y, b, hk, G, mask_of(Q, N, Q, N, window, sinks, "cuda"), dt)
+    for n, t in (("dk", got[1]), ("dv", got[2])):
+        off = ref["dk_d"] if n == "dk" else HALF[dt] * ref["dv_mag"] * (dt == torch.bfloat16)
+        agree(t[b, hk], ref[n], HALF[dt] * ref[n].abs() + off + 3 * e * ref[n + "_mag"], (n, case))
+    for h in range(hk * G, (hk + 1) * G):
+        r = ref["dq", h]
+        agree(got[0][b, h], r, HALF[dt] * r.abs() + ref["dq_d", h] + 3 * e * ref["dq_mag", h], ("dq", h, case))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("case", [*CASES, WIDE], ids=[*IDS, "wide"])
+@pytest.mark.parametrize("what", ["v", "k", "k_inf", "q", "do", "do_inf"])
+def test_gradients_of_what_pairs_with_them(case, dtype, what):
+    """A value that is not finite reaches the gradients of its row, of what pairs with that, and of no others."""
+    B, Hq, Hkv, dh, Q, N, window, sinks = case
+    shape, x, dt = setup(case, dtype, 5)
+    G, b, hk = Hq // Hkv, B - 1, Hkv - 1
+    clean = ops.window_attention(shape, x["q"], x["k"], x["v"])
+    cg = ops.window_attention_backward(shape, x["q"], x["k"], x["v"], *clean, x["do"])
+    name = what.split("_")[0]
+    value = math.inf if what.endswith("inf") else math.nan
+    T = N if name in ("k", "v") else Q
+    for j in sorted({0, T // 3, T - 1}):
+        y = {**x, name: x[name].clone()}
+        y[name][b, hk if name in ("k", "v") else hk * G, j, 5] = value
+        if name == "v":
+            y[name][b, hk, j, 6] = -math.inf
+        out, lse = ops.window_attention(shape, y["q"], y["k"], y["v"])
+        got = ops.window_attention_backward(shape, y["q"], y["k"], y["v"], out, lse, y["do"])
+        check_gradients(case, y, got, dt, b, hk)
+        for t, c, H, n in ((got[0], cg[0], Hq, G), (got[1], cg[1], Hkv, 1), (got[2], cg[2], Hkv, 1)):
+            rest = torch.ones(B, H, dtype=torch.bool, device="cuda")
+            rest[b, hk * n:(hk + 1) * n] = False
+            assert torch.equal(t[rest], c[rest])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("window,sinks", [(30, 3), (0, 0), (20, 70)])
+def test_gradients_past_the_lengths_are_zero_whatever_the_others_hold(dtype, window, sinks):
+    case = (2, 8, 2, 64, 200, 200, window, sinks)
+    shape, x, _ = setup(case, dtype, 3)
+    lens = torch.tensor([200, 77], dtype=torch.int32, device="cuda")
+    for n in ("q", "k", "v", "do"):
+        y = {**x, n: x[n].clone()}
+        y[n][:, :, 5::9] = math.inf
+        y[n][1, :, 77:] = math.nan
+        out, lse = ops.window_attention(shape, y["q"], y["k"], y["v"], q_lens=lens, kv_lens=lens)
+        for t in ops.window_attention_backward(shape, y["q"], y["k"], y["v"], out, lse, y["do"], q_lens=lens, kv_lens=lens):
+            assert not bool(t[1, :, 77:].any())
+
+
 def best_time(f, n=5):
     f()
     torch.cuda.synchronize()
@@ -184,3 +263,30 @@ def test_a_diverged_call_takes_no_longer_than_a_few_others(case, dtype):
     y = {**x, "v": x["v"].clone()}
     y["v"][:, :, 0, 3] = math.inf
     assert best_time(call(y)) <= 4 * base
+
+
+TIMED_BACK = [(1, 16, 4, 128, 4096, 4096, 0, 0), (2, 8, 8, 64, 8192, 8192, 1000, 4), (1, 24, 8, 64, 4096, 4096, 0, 0)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("case", TIMED_BACK, ids=[f"{c[3]}x{c[4]}of{c[5]}w{c[6]}g{c[1] // c[2]}" for c in TIMED_BACK])
+def test_a_diverged_backward_takes_no_longer_than_a_few_others(case, dtype):
+    """Two walks, and in the second two barriers and two visits more of tiles that pair in part (all of them where a
+    group does not divide a tile)."""
+    shape, x, _ = setup(case, dtype, 7)
+    scratch = ops.alloc_attn_scratch(shape)
+    d = [torch.empty_like(x[n]) for n in ("q", "k", "v")]
+
+    def call(y):
+        out, lse = ops.window_attention(shape, y["q"], y["k"], y["v"], scratch=scratch)
+        return lambda: ops.window_attention_backward(shape, y["q"], y["k"], y["v"], out, lse, y["do"], dq=d[0], dk=d[1],
+                                                     dv=d[2], scratch=scratch)
+    base = best_time(call(x))
+    for names in (("q", "k", "v", "do"), ("do",), ("v",)):
+        y = {**x, **{n: torch.full_like(x[n], math.nan) for n in names}}
+        assert best_time(call(y)) <= 6 * base, names
+        assert bool(torch.isnan(d[0]).all()) and bool(torch.isnan(d[1]).all())
+    for n in ("v", "k", "do", "q"):
+        y = {**x, n: x[n].clone()}
+        y[n][:, :, -1 if n in ("do", "q") else 0, 3] = math.inf
+        assert best_time(call(y)) <= 6 * base, n
