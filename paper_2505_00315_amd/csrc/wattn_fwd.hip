@@ -181,6 +181,9 @@ __device__ __forceinline__ bool fwd_body(unsigned char* smem, const AttnArgs& a,
             // The reference maximum moves only when the tile's exceeds it by more
             // than 8 (log2 units): weights stay below 2^8, and O and l are rescaled
             // only in tiles where some row of the wave moved.
+            // Again: it is a score, not in log2 units, so that differences are not
+            // rounded at its size, and weights are 2^-16 of that, so that sums over
+            // values of any size stay finite.
             float m_new[QN], m_use[QN];
             bool moved = false;
 #pragma unroll
@@ -190,18 +193,15 @@ __device__ __forceinline__ bool fwd_body(unsigned char* smem, const AttnArgs& a,
                 for (int sb = 0; sb < NB; ++sb)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) mloc = fmaxf(mloc, s[qs][sb][i]);
-                mloc = rows4_max(mloc) * c2;
-                // (again: 16 above the maximum, weights below 2^-8, so that sums over
-                // finite values of any size stay finite)
-                if constexpr (again) m_new[qs] = mloc > m_run[qs] - 8.f ? mloc + 16.f : m_run[qs];
-                else m_new[qs] = mloc > m_run[qs] + 8.f ? mloc : m_run[qs];
+                mloc = rows4_max(mloc) * (again ? 1.f : c2);
+                m_new[qs] = mloc > m_run[qs] + (again ? 8.f / c2 : 8.f) ? mloc : m_run[qs];
                 m_use[qs] = m_new[qs] == -__builtin_inff() ? 0.f : m_new[qs];
                 moved |= m_new[qs] != m_run[qs];
             }
             if (__builtin_amdgcn_ballot_w64(moved)) {
 #pragma unroll
                 for (int qs = 0; qs < QN; ++qs) {
-                    const float alpha = __builtin_amdgcn_exp2f(m_run[qs] - m_use[qs]);
+                    const float alpha = __builtin_amdgcn_exp2f((m_run[qs] - m_use[qs]) * (again ? c2 : 1.f));
                     l_run[qs] *= alpha;
 #pragma unroll
                     for (int db = 0; db < ND; ++db) o[qs][db] *= alpha;
@@ -215,7 +215,8 @@ __device__ __forceinline__ bool fwd_body(unsigned char* smem, const AttnArgs& a,
                 for (int sb = 0; sb < NB; ++sb)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        s[qs][sb][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[qs][sb][i], c2, -m_use[qs]));
+                        if constexpr (again) s[qs][sb][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[qs][sb][i] - m_use[qs], c2, -16.f));
+                        else s[qs][sb][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[qs][sb][i], c2, -m_use[qs]));
                         lsum[i & 1] += s[qs][sb][i];
                     }
                 l_run[qs] += lsum[0] + lsum[1];  // this lane's keys; the 4 lanes of a row are added at the end
@@ -265,14 +266,18 @@ __device__ __forceinline__ bool fwd_body(unsigned char* smem, const AttnArgs& a,
                 });
                 __syncthreads();
             }
+#pragma unroll
+            for (int qs = 0; qs < QN; ++qs) m_run[qs] = __builtin_fmaf(m_run[qs], c2, 16.f);
         } else {
-            // A sum of weights that is not finite comes from the keys that the row
-            // sees (the others' scores are masked before), and is the result.  With
-            // finite weights a value of a key that the row does not see may have got in.
+            // A value of a key that the row does not see may have got in; or scores have
+            // passed 2^30, where a product with the scale is rounded by more than 2^5 and
+            // all weights of a row with it, out of the type's range at last.
             bool spoilt = false;
 #pragma unroll
-            for (int qs = 0; qs < QN; ++qs)
-                spoilt |= wr0 + 16 * qs + c16 < rn && fabsf(l_run[qs]) < __builtin_inff() && !finite4(o[qs]);
+            for (int qs = 0; qs < QN; ++qs) {
+                const bool sum = m_run[qs] == -__builtin_inff() || (l_run[qs] > 0x1p-32f && l_run[qs] < __builtin_inff());
+                spoilt |= wr0 + 16 * qs + c16 < rn && !(sum && finite4(o[qs]));
+            }
             if (any_of_workgroup(smem, wave, lane, spoilt)) return true;
         }
     }

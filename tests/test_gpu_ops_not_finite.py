@@ -162,6 +162,27 @@ def test_sums_of_the_largest_values_are_finite(case, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("case", CASES, ids=IDS)
+@pytest.mark.parametrize("size", [1e4, 1e6, 1e15])
+def test_the_largest_score_takes_the_row(case, dtype, size):
+    """Scores of 1e9 to 1e31, whose products with the scale are rounded by far more than an exponential may be off: a row
+    is the value of its largest score (the next is further away than the roundings of a score, 2^-17 of its size)."""
+    B, Hq, Hkv, dh, Q, N, window, sinks = case
+    shape, x, dt = setup(case, dtype, 11)
+    q, k = (x["q"].float() * size).to(dt), (x["k"].float() * size).to(dt)
+    out, lse = ops.window_attention(shape, q, k, x["v"])
+    see = mask_of(Q, N, Q, N, window, sinks, "cuda")
+    for h in range(Hq):
+        s = (q[0, h].double() @ k[0, h // (Hq // Hkv)].double().T / math.sqrt(dh)).masked_fill(~see, -math.inf)
+        top = s.topk(min(2, N), 1)
+        clear = see.any(1) & ((top.values[:, 0] - top.values[:, -1]) > 2.0 ** -17 * top.values[:, 0].abs())
+        assert int(clear.sum()) >= int(see.any(1).sum()) * 0.9
+        r = x["v"][0, h // (Hq // Hkv)].double()[top.indices[:, 0]]
+        assert bool(((out[0, h].double() - r).abs() <= 2 * HALF[dt] * r.abs())[clear].all())
+        assert bool(((lse[0, h].double() - top.values[:, 0]).abs() <= 2.0 ** -17 * top.values[:, 0].abs())[clear].all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_rows_past_the_lengths_are_zero_whatever_the_others_hold(dtype):
     case = (2, 4, 2, 64, 200, 200, 30, 3)
     shape, x, _ = setup(case, dtype, 3)
@@ -247,8 +268,8 @@ TIMED = [(1, 16, 4, 128, 4096, 4096, 0, 0), (2, 8, 8, 64, 8192, 8192, 1000, 4), 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("case", TIMED, ids=[f"{c[3]}x{c[4]}of{c[5]}w{c[6]}" for c in TIMED])
 def test_a_diverged_call_takes_no_longer_than_a_few_others(case, dtype):
-    """All of a tensor NaN, or one early value that every later row sees: the tiles that are seen in part (2 or 3 of a
-    row block's) are visited twice, nothing is done key by key."""
+    """All of a tensor NaN, or one early value that every later row sees: two walks, in the second of which the tiles that
+    are seen in part (2 or 3 of a row block's) are visited twice; nothing is done key by key."""
     shape, x, _ = setup(case, dtype, 4)
     scratch = ops.alloc_attn_scratch(shape)
     out, lse = ops.window_attention(shape, x["q"], x["k"], x["v"], scratch=scratch)
