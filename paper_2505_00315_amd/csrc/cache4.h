@@ -1,4 +1,4 @@
-// Layout of the 4-bit cache and access to single values of it.
+// Layout of the 4-bit cache.
 //
 // A page holds, for every key head, a block of page_size positions:
 //   codes of K   page_size rows of dh / 2 bytes
@@ -55,16 +55,4 @@ __device__ __forceinline__ bool cache_find(const CacheArgs& c, const UDiv& page_
 __device__ __forceinline__ float cache_value(uint32_t meta, uint32_t code) {
     return __builtin_fmaf((float)code, __uint_as_float(meta << 16), __uint_as_float(meta & 0xffff0000u));
 }
-__device__ __forceinline__ float cache_k(const CacheArgs& c, const CacheBlock& blk, int tl, int d) {
-    const int g = d >> 5, kg = (d >> 3) & 3, i = d & 7;
-    const uint32_t w = *reinterpret_cast<const uint32_t*>(c.cache + blk.kword(tl, kg * (c.dh / 32) + g));
-    return cache_value(*reinterpret_cast<const uint32_t*>(c.cache + blk.kmeta(tl, g)),
-                       (w >> (4 * ((i >> 1) + 4 * (i & 1)))) & 15);
-}
-__device__ __forceinline__ float cache_v(const CacheArgs& c, const CacheBlock& blk, int tl, int d) {
-    const int n = ((d & 31) >> 1) * (c.dh / 16) + 2 * (d >> 5) + (d & 1);  // the column's number in the row
-    const uint32_t w = *reinterpret_cast<const uint16_t*>(c.cache + blk.vpiece(tl, n >> 2));
-    return cache_value(*reinterpret_cast<const uint32_t*>(c.cache + blk.vmeta(tl, d >> 5)), (w >> (4 * (n & 3))) & 15);
-}
-
 }  // namespace mosa

@@ -33,13 +33,13 @@
 // and a chain of a table read, a tile's loads and four tiles.
 #include "cache4.h"
 #include "launch_parts.h"
-#include "rowattn.h"
 
 namespace mosa {
 
 namespace {
 
 constexpr int kWaves = 4;
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 
 // The keys that some row sees, in aligned octets: so octets of sinks, then
 // those from w0 on.
@@ -207,7 +207,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache4_attn_kernel(AttnArgs a,
         load(sp, even);
         sp = spots(tbeg + wave + kWaves);
 
-        // q as A operand: columns 32 gr + 8 g .. + 7 of the row, in SPLIT parts;
+        // q / 8 (16 + n and the minima make terms of up to 8 times a score, which is to
+        // stay finite where the score is) as A operand: columns 32 gr + 8 g .. + 7 of the
+        // row, in SPLIT parts;
         // its sums over a group, times (-16, 1) (of codes n - 8: (8, 1)), as the operand of the words (s, m):
         // lane group 0 holds the upper bf16 part, 1 and 2 what that leaves
         bf16x8 qf[NQ][SPLIT][NG], qs[NQ];
@@ -221,7 +223,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache4_attn_kernel(AttnArgs a,
                 float x[8], s = 0.f;
                 frag8_to_f32<ST>(frag8_load<ST>(qp + 32 * gr + 8 * g), x);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) s += x[e];
+                for (int e = 0; e < 8; ++e) {
+                    x[e] *= 0.125f;
+                    s += x[e];
+                }
                 s = rows4_sum(s);
 #pragma unroll
                 for (int sp2 = 0; sp2 < SPLIT; ++sp2) {
@@ -239,7 +244,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache4_attn_kernel(AttnArgs a,
             }
             qs[q] = frag_of(sums[0], sums[1], sums[2], sums[3]);
         }
-        const float c2 = a.scale * kLog2e;
+        const float c2 = a.scale * (8.f * kLog2e), step = 8.f / c2;
         unsigned char* pw = smem + wave * NQ * L::PW;  // this wave's weights
         const bf16x8 one8 = frag_of(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u);
         const CodeBits<SPLIT> codes;
@@ -287,36 +292,41 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache4_attn_kernel(AttnArgs a,
                 for (int y = 0; y < 2; ++y) {
                     const int key = cur.key + y;
                     const bool in = key >= 0 && key < kn;
-                    bool any = false;
 #pragma unroll
                     for (int q = 0; q < NQ; ++q)
 #pragma unroll
-                        for (int i = 0; i < RI; ++i) {
-                            const bool ok = in & sees(a, pos[q][i], key);
-                            s[q][y][i] = ok ? s[q][y][i] : -__builtin_inff();
-                            any |= ok;
-                        }
-                    // what no row sees may be anything: its scale and minimum are taken as 0
-                    const uint64_t bal = __builtin_amdgcn_ballot_w64(any);
-                    const bool seen = (bal >> c16 | bal >> (c16 + 16) | bal >> (c16 + 32) | bal >> (c16 + 48)) & 1;
+                        for (int i = 0; i < RI; ++i)
+                            s[q][y][i] = (in & sees(a, pos[q][i], key)) ? s[q][y][i] : -__builtin_inff();
+                    // What is not finite (what no row sees may hold anything) leaves the
+                    // products, and joins the sums of the rows that see it here.
 #pragma unroll
-                    for (int gr = 0; gr < NG; ++gr) cur.vm[y][gr] = seen ? cur.vm[y][gr] : 0u;
+                    for (int gr = 0; gr < NG; ++gr) {
+                        const bool bad = ((cur.vm[y][gr] & 0x7fff7fffu) + 0x00800080u) & 0x80008000u;
+                        cur.vm[y][gr] = bad ? 0u : cur.vm[y][gr];
+#pragma unroll
+                        for (int q = 0; q < NQ; ++q)
+#pragma unroll
+                            for (int i = 0; i < RI; ++i)
+                                pm[q][gr][i] += (bad & (s[q][y][i] != -__builtin_inff())) ? __builtin_nanf("") : 0.f;
+                    }
                 }
             }
-            // running maximum (moved only when exceeded by 8 in log2 units), weights
+            // Weights are 2^((s - m) c - 16): differences of scores, which are not rounded
+            // at the scores' size; below 2^-8, so that their products with the largest
+            // scales are finite.  m, a score, moves only when exceeded by 8 in log2 units.
             bool up = false;
 #pragma unroll
             for (int q = 0; q < NQ; ++q)
 #pragma unroll
-                for (int i = 0; i < RI; ++i) up |= fmaxf(s[q][0][i], s[q][1][i]) * c2 > m_run[q][i] + 8.f;
+                for (int i = 0; i < RI; ++i) up |= fmaxf(s[q][0][i], s[q][1][i]) > m_run[q][i] + step;
             if (__builtin_amdgcn_ballot_w64(up)) {
 #pragma unroll
                 for (int q = 0; q < NQ; ++q)
 #pragma unroll
                     for (int i = 0; i < RI; ++i) {
-                        const float top = lanes16_max(fmaxf(s[q][0][i], s[q][1][i])) * c2;
+                        const float top = lanes16_max(fmaxf(s[q][0][i], s[q][1][i]));
                         const float mn = fmaxf(m_run[q][i], top);
-                        const float al = mn == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f(m_run[q][i] - mn);
+                        const float al = mn == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f((m_run[q][i] - mn) * c2);
                         m_run[q][i] = mn;
                         l_run[q][i] *= al;
 #pragma unroll
@@ -333,8 +343,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache4_attn_kernel(AttnArgs a,
 #pragma unroll
                 for (int i = 0; i < RI; ++i) {
                     const float mu = m_run[q][i] == -__builtin_inff() ? 0.f : m_run[q][i];
-                    const float w0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[q][0][i], c2, -mu));
-                    const float w1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[q][1][i], c2, -mu));
+                    const float w0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[q][0][i] - mu, c2, -16.f));
+                    const float w1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[q][1][i] - mu, c2, -16.f));
                     l_run[q][i] += w0 + w1;
 #pragma unroll
                     for (int gr = 0; gr < NG; ++gr) {
@@ -406,43 +416,21 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache4_attn_kernel(AttnArgs a,
     __syncthreads();
     float* wo = reinterpret_cast<float*>(smem) + wave * RB * (DH + 2);
     float* wml = wo + RB * DH;
-    bool fine = true;
 #pragma unroll
     for (int q = 0; q < NQ; ++q)
 #pragma unroll
         for (int i = 0; i < RI; ++i) {
             const int lr = (4 * q + g) * RI + i;
             l_run[q][i] = lanes16_sum(l_run[q][i]);
-            float bad = l_run[q][i] * 0.f;
+            m_run[q][i] = __builtin_fmaf(m_run[q][i], a.scale * (8.f * kLog2e), 16.f);  // in log2 units, with the weights' 2^-16
 #pragma unroll
             for (int gr = 0; gr < NG; ++gr) {
                 const float add = lanes16_sum(pm[q][gr][i]) - CodeBits<SPLIT>::middle * ones[q][gr][i];
                 const float x = o[q][2 * gr][i] + add, y = o[q][2 * gr + 1][i] + add;
-                bad = __builtin_fmaf(x, 0.f, __builtin_fmaf(y, 0.f, bad));
                 *reinterpret_cast<float2*>(wo + lr * DH + 32 * gr + 2 * c16) = make_float2(x, y);
             }
-            fine &= bad == 0.f;
             if (c16 == 0) *reinterpret_cast<float2*>(wml + 2 * lr) = make_float2(m_run[q][i], l_run[q][i]);
         }
-    if (__builtin_amdgcn_ballot_w64(!fine)) {
-        // a weight of 0 met a value that is not finite: this wave's rows again, one by one
-        wave_sync();
-#pragma unroll 1
-        for (int lr = 0; lr < RB && r0 + lr < rn; ++lr) {
-            const int r = r0 + lr, i = a.gd.div(r);
-            float q[RowLanes<DH>::N], x[RowLanes<DH>::N], m, l;
-            row_load<ST, DH>(qrow_ptr<ST>(a, a.q, b, hk, r, i), lane, q);
-            const int mine = max(tend - tbeg - wave + kWaves - 1, 0) / kWaves;  // tiles of this wave
-            row_attend<DH>(a, CacheKeys<DH>{c, G.page, b, hk}, [&](int e) {
-                const int oc = 4 * (tbeg + wave + kWaves * (e / 32)) + e / 8 % 4;
-                return oc < list.count ? list.first_key(oc) + e % 8 : -1;
-            }, 0, 32 * mine, off + i, kn, q, lane, m, l, x);
-#pragma unroll
-            for (int n = 0; n < RowLanes<DH>::N; ++n)
-                if (RowLanes<DH>::has(lane)) wo[lr * DH + lane + 64 * n] = x[n];
-            if (lane == 0) wml[2 * lr] = m, wml[2 * lr + 1] = l;
-        }
-    }
     __syncthreads();
     // The waves in order: M = max m_w, L = sum l_w 2^(m_w - M); 8 columns per thread.
     const float* base = reinterpret_cast<const float*>(smem);

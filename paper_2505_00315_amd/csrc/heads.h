@@ -22,6 +22,15 @@ __device__ __forceinline__ ST* row_ptr(const Rows& r, int b, int h, int64_t t) {
     return reinterpret_cast<ST*>(r.p) + b * r.batch + h * r.head + t * r.row;
 }
 
+constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.69314718055994531f;
+
+// LDS written by lanes of this wave is seen by its other lanes.
+__device__ __forceinline__ void wave_sync() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 // f(storage value, integral constant d_head) for the type and head size of a call.
 template <typename F>
 inline int heads_by_type(int dtype, int dh, F f) {

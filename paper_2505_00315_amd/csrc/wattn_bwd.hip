@@ -29,7 +29,6 @@
 // blocks, whose rows are then cut into parts (the first keys are seen by every
 // row, the last by few).
 #include "launch_parts.h"
-#include "rowattn.h"
 #include "wattn_dma.h"
 
 namespace mosa {

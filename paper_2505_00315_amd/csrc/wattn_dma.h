@@ -15,7 +15,7 @@
 #pragma once
 
 #include "attn_lds.h"
-#include "rowattn.h"
+#include "heads.h"
 
 namespace mosa {
 

@@ -20,7 +20,6 @@
 // exponentials wait for each other.  fp32, at the fp32 matrix instructions' rate:
 // 67 to 82 TFLOP/s with the backward.
 #include "launch_parts.h"
-#include "rowattn.h"
 #include "wattn_dma.h"
 
 namespace mosa {
@@ -349,6 +348,13 @@ __global__ __launch_bounds__(256, (fwd_waves<ST, DH, QN>())) void wattn_fwd_kern
     if (fwd_body<ST, DH, QN, 64 * QN, false>(smem, c.a, c.G, c.part, id, 0, threadIdx.x))
         fwd_again<ST, DH, 64 * QN>((const void*)__builtin_amdgcn_kernarg_segment_ptr(), lds_addr(smem), id);
 }
+
+// Columns of a row of DH held by a lane: lane, lane + 64 (none past DH).
+template <int DH>
+struct RowLanes {
+    static constexpr int N = DH > 64 ? DH / 64 : 1;
+    static __device__ __forceinline__ bool has(int lane) { return DH >= 64 || lane < DH; }
+};
 
 // A row of the call: the parts in their order, M = max m_s, L = sum l_s 2^(m_s - M).
 template <typename ST, int DH>

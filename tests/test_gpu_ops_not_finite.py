@@ -5,7 +5,7 @@ import math
 import pytest
 import torch
 
-from ops_util import HALF, U32, mask_of, rand_rows
+from ops_util import HALF, U32, cache64, mask_of, rand_rows
 from paper_2505_00315_amd import ops
 
 pytestmark = pytest.mark.gpu
@@ -311,3 +311,115 @@ def test_a_diverged_backward_takes_no_longer_than_a_few_others(case, dtype):
         y = {**x, n: x[n].clone()}
         y[n][:, :, -1 if n in ("do", "q") else 0, 3] = math.inf
         assert best_time(call(y)) <= 6 * base, n
+
+
+# ---------------------------------------------------------------------------
+# attention over the 4-bit cache
+# ---------------------------------------------------------------------------
+# B, Hq, Hkv, dh, Q, N, page, window, sinks
+CACHED = [
+    (1, 4, 2, 64, 1, 2500, 16, 0, 0),      # one token, its positions in parts
+    (2, 8, 2, 128, 5, 2300, 64, 0, 0),     # 20 rows to a key head
+    (1, 12, 1, 32, 3, 2100, 48, 0, 0),     # 36
+    (1, 8, 1, 32, 1, 2100, 16, 1500, 4),
+    (1, 6, 2, 64, 17, 300, 16, 40, 3),
+    (2, 4, 4, 128, 40, 200, 16, 24, 70),
+]
+CIDS = [f"{c[0]}x{c[1]}/{c[2]}x{c[3]}-{c[4]}of{c[5]}-w{c[7]}s{c[8]}" for c in CACHED]
+
+
+def cached(case, dtype, seed):
+    """Shapes, a cache of random rows with pages in any order, what it holds, and the call."""
+    B, Hq, Hkv, dh, Q, N, ps, window, sinks = case
+    shape, x, dt = setup((B, Hq, Hkv, dh, Q, N, window, sinks), dtype, seed)
+    per = -(-N // ps)
+    cs = ops.make_cache_shape(B, Hkv, dh, B * per, ps, per, dtype)
+    g = torch.Generator().manual_seed(seed)
+    table = torch.randperm(B * per, generator=g).view(B, per).to(torch.int32).cuda()
+    cache = ops.alloc_cache4(cs)
+    lens = torch.full((B,), N, dtype=torch.int32, device="cuda")
+
+    def call(k, v, q=x["q"]):
+        cache.fill_(0xff)  # what was there before means nothing
+        ops.cache4_append(cs, cache, table, None, k, v)
+        lse = torch.empty(B, Hq, Q, dtype=torch.float32, device="cuda")
+        return ops.cache4_attention(shape, cs, q, cache, table, lens, lse=lse), lse
+    return x, dt, call, (shape, cs, cache, table, lens)
+
+
+def check_cached(case, y, out, lse, dt, b):
+    B, Hq, Hkv, dh, Q, N, ps, window, sinks = case
+    see = mask_of(Q, N, Q, N, window, sinks, "cuda")
+    (kh, ks), (vh, vs) = cache64(y["k"]), cache64(y["v"])
+    held = {"q": y["q"], "k": kh, "v": vh}
+    # a score adds up q times m and s code apart
+    smag = float((y["q"].double().abs().amax((0, 1, 2)) * ks.nan_to_num(0).amax((0, 1, 2))).sum()) / math.sqrt(dh)
+    e = U32 * ((dh + 4) * smag + N + dh + 16)
+    for h in range(Hq):
+        ref = formula(held, b, h, Hq // Hkv, see)
+        mag = sums(see, ref["P"], vs[b, h // (Hq // Hkv)])
+        off = HALF[dt] * (ref["out"].abs() + (mag if dt == torch.bfloat16 else 0)) + e * mag
+        agree(out[b, h], ref["out"], off, (case, h))
+        some = torch.isfinite(ref["lse"])
+        assert torch.equal(torch.isnan(lse[b, h]), torch.isnan(ref["lse"]))
+        assert bool(((lse[b, h].double() - ref["lse"]).abs() <= e * (1 + ref["lse"].abs()))[some].all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("case", CACHED, ids=CIDS)
+def test_cached_rows_reach_the_queries_that_see_them(case, dtype):
+    """A group of values that is not finite stands for NaN throughout, in K for every column of the rows that see it."""
+    B, Hq, Hkv, dh, Q, N = case[:6]
+    x, dt, call, _ = cached(case, dtype, 8)
+    for at in ((0, N // 3), (N // 2, N - 1), (N - 2,)):
+        y = {**x, "k": x["k"].clone(), "v": x["v"].clone()}
+        for n, j in enumerate(at):
+            y["v"][:, :, j, (7 + 40 * n) % dh] = math.inf if n else math.nan
+        out, lse = call(y["k"], y["v"])
+        check_cached(case, y, out, lse, dt, B - 1)
+        y["k"][B - 1, 0, at[-1], 3] = math.nan
+        out, lse = call(y["k"], y["v"])
+        check_cached(case, y, out, lse, dt, B - 1)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("case", CACHED, ids=CIDS)
+def test_cached_rows_of_the_largest_values(case, dtype):
+    """Values of up to 3e38, whose scales meet the weights before the codes do; and keys whose scores are about 1e37, of
+    which the largest takes the row (its distance to the next is far above a rounding, 1e30)."""
+    B, Hq, Hkv, dh, Q, N, ps, window, sinks = case
+    x, dt, call, _ = cached(case, dtype, 9)
+    v = (x["v"][..., :1].sign() * 3e38 * torch.linspace(0.1, 1.0, dh, device="cuda")).to(dt)
+    out, lse = call(x["k"], v)
+    check_cached(case, {**x, "v": v}, out, lse, dt, B - 1)
+    k = (x["k"].float() * 5e36).to(dt)
+    out, lse = call(k, x["v"])
+    see = mask_of(Q, N, Q, N, window, sinks, "cuda")
+    kh, (vh, vs) = cache64(k)[0], cache64(x["v"])
+    G = Hq // Hkv
+    for h in range(Hq):
+        s = (x["q"][B - 1, h].double() @ kh[B - 1, h // G].T).masked_fill(~see, -math.inf)
+        best = s.argmax(1)
+        r = vh[B - 1, h // G][best]
+        assert bool(((out[B - 1, h].double() - r).abs() <= 2 * HALF[dt] * (r.abs() + vs[B - 1, h // G][best])).all())
+
+
+TIMED_CACHE = [(4, 32, 8, 128, 1, 16000, 64, 0, 0), (2, 16, 4, 64, 64, 8000, 64, 0, 0), (4, 12, 4, 32, 8, 8000, 16, 4000, 4)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("case", TIMED_CACHE, ids=[f"{c[3]}x{c[4]}of{c[5]}w{c[7]}" for c in TIMED_CACHE])
+def test_a_diverged_cache_takes_no_longer(case, dtype):
+    """One walk, whatever the cache holds."""
+    x, _, call, (shape, cs, cache, table, lens) = cached(case, dtype, 10)
+    scratch, out = ops.alloc_attn_scratch(shape), torch.empty_like(x["q"])
+
+    def attend():
+        ops.cache4_attention(shape, cs, x["q"], cache, table, lens, out=out, scratch=scratch)
+    call(x["k"], x["v"])
+    base = best_time(attend)
+    for names in (("v",), ("k", "v")):
+        y = {**x, **{n: torch.full_like(x[n], math.nan) for n in names}}
+        call(y["k"], y["v"])
+        assert best_time(attend) <= 2 * base, names
+        assert bool(torch.isnan(out).all())
