@@ -32,10 +32,17 @@ namespace mosa {
 namespace {
 
 constexpr int kGroupTokens = 8;  // most tokens of a group (LDS: 8 * 64 pairs = 4 KB)
-// Workgroups of the backward: each leaves one fp32 partial of dwq and dwk.
+// Workgroups of the backward: each leaves one partial of dwq and dwk.
 // Four per CU keep 64 KB of loads per CU in flight (256 lanes, x and dy of 2 rows).
 constexpr int kBwdBlocks = 1024;
 constexpr int kFwdBlocks = 2048;
+
+// Sums of dwq and dwk.  With fp32 storage they are taken in 64 bits, so that the
+// result is rounded once, whatever the number of rows (in 32 bits the error was
+// three times that).  bf16 storage rounds the result to 2^-9, far above the
+// error of a lane's few dozen terms in fp32; only the partials' sum is in 64 bits.
+template <typename ST>
+using DwSum = std::conditional_t<sizeof(ST) == 4, double, float>;
 
 template <typename ST, int DH>
 struct NormGeom {
@@ -228,16 +235,16 @@ __global__ __launch_bounds__(256) void qk_norm_kernel(NormArgs a, int TB, FastDi
 
 template <typename ST, int DH, bool DW>
 __global__ __launch_bounds__(256) void qk_norm_bwd_kernel(NormArgs a, int TB, FastDiv hq, FastDiv hk,
-                                                          float* __restrict__ partial) {
+                                                          DwSum<ST>* __restrict__ partial) {
     using G = NormGeom<ST, DH>;
     constexpr int E = G::E, U = 2;
     __shared__ GroupLds lds;
-    __shared__ float red[DW ? 256 * E : 1];
+    __shared__ DwSum<ST> red[DW ? 256 * E : 1];
     const int lane = threadIdx.x & 63, slot = threadIdx.x / G::LPR;
     const Turn<ST, DH> turn(a, lane);
-    float acc[2][E];
+    DwSum<ST> acc[2][E];
 #pragma unroll
-    for (int e = 0; e < E; ++e) acc[0][e] = acc[1][e] = 0.f;
+    for (int e = 0; e < E; ++e) acc[0][e] = acc[1][e] = 0;
     const int64_t total = (int64_t)a.B * a.T;
     for (int64_t tok0 = (int64_t)blockIdx.x * TB; tok0 < total; tok0 += (int64_t)gridDim.x * TB) {
         const int nt = (int)min((int64_t)TB, total - tok0);
@@ -302,7 +309,7 @@ __global__ __launch_bounds__(256) void qk_norm_bwd_kernel(NormArgs a, int TB, Fa
             for (int e = 0; e < E; ++e) red[slot * DH + turn.c0 + e] = acc[K][e];
             __syncthreads();
             for (int d = threadIdx.x; d < DH; d += 256) {
-                float s = 0.f;
+                DwSum<ST> s = 0;
                 for (int r = 0; r < G::RP; ++r) s += red[r * DH + d];
                 partial[((size_t)blockIdx.x * 2 + K) * DH + d] = s;
             }
@@ -313,20 +320,20 @@ __global__ __launch_bounds__(256) void qk_norm_bwd_kernel(NormArgs a, int TB, Fa
 // dw = sum of the partials, 16 columns per workgroup: 64 strands of rows, then
 // the strands in order.
 template <typename ST>
-__global__ __launch_bounds__(1024) void qk_norm_dw_kernel(const float* __restrict__ partial, int blocks, int dh,
+__global__ __launch_bounds__(1024) void qk_norm_dw_kernel(const DwSum<ST>* __restrict__ partial, int blocks, int dh,
                                                           ST* __restrict__ dwq, ST* __restrict__ dwk) {
-    __shared__ float red[64][17];
+    __shared__ double red[64][17];
     const int c = threadIdx.x & 15, strand = threadIdx.x >> 4, col = blockIdx.x * 16 + c;
-    float s = 0.f;
+    double s = 0.0;
 #pragma unroll 4
     for (int i = strand; i < blocks; i += 64) s += partial[(size_t)i * 2 * dh + col];
     red[strand][c] = s;
     __syncthreads();
     if (threadIdx.x < 16) {
-        float t = 0.f;
+        double t = 0.0;
         for (int i = 0; i < 64; ++i) t += red[i][c];
         ST* to = col < dh ? dwq : dwk;
-        if (to) st1<ST>(to + (col < dh ? col : col - dh), t);
+        if (to) st1<ST>(to + (col < dh ? col : col - dh), (float)t);
     }
 }
 
@@ -348,7 +355,8 @@ int norm_t(const NormArgs& a, hipStream_t stream) {
 }
 
 template <typename ST, int DH>
-int norm_bwd_t(const NormArgs& a, void* dwq, void* dwk, float* partial, hipStream_t stream) {
+int norm_bwd_t(const NormArgs& a, void* dwq, void* dwk, void* scratch, hipStream_t stream) {
+    DwSum<ST>* partial = static_cast<DwSum<ST>*>(scratch);
     const int64_t total = (int64_t)a.B * a.T;
     const int tb = group_tokens(total, a.Hkv, NormGeom<ST, DH>::RP, 2);
     const int64_t groups = (total + tb - 1) / tb;
@@ -367,17 +375,17 @@ int norm_bwd_t(const NormArgs& a, void* dwq, void* dwk, float* partial, hipStrea
 
 }  // namespace
 
-size_t norm_partial_bytes(int64_t tokens, int dh) {
-    return (size_t)(tokens < kBwdBlocks ? tokens : kBwdBlocks) * 2 * dh * sizeof(float);
+size_t norm_partial_bytes(int dtype, int64_t tokens, int dh) {
+    return (size_t)(tokens < kBwdBlocks ? tokens : kBwdBlocks) * 2 * dh * (dtype == kBF16 ? sizeof(float) : sizeof(double));
 }
 
 int launch_qk_norm(int dtype, const NormArgs& a, hipStream_t stream) {
     return heads_by_type(dtype, a.dh, [&](auto st, auto dh) { return norm_t<decltype(st), decltype(dh)::value>(a, stream); });
 }
 
-int launch_qk_norm_bwd(int dtype, const NormArgs& a, void* dwq, void* dwk, float* partial, hipStream_t stream) {
+int launch_qk_norm_bwd(int dtype, const NormArgs& a, void* dwq, void* dwk, void* scratch, hipStream_t stream) {
     return heads_by_type(dtype, a.dh, [&](auto st, auto dh) {
-        return norm_bwd_t<decltype(st), decltype(dh)::value>(a, dwq, dwk, partial, stream);
+        return norm_bwd_t<decltype(st), decltype(dh)::value>(a, dwq, dwk, scratch, stream);
     });
 }
 

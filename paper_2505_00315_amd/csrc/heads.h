@@ -59,9 +59,9 @@ struct NormArgs {
     const int32_t* pos;
     Turns turns;
 };
-size_t norm_partial_bytes(int64_t tokens, int dh);
+size_t norm_partial_bytes(int dtype, int64_t tokens, int dh);
 int launch_qk_norm(int dtype, const NormArgs& a, hipStream_t stream);
-int launch_qk_norm_bwd(int dtype, const NormArgs& a, void* dwq, void* dwk, float* partial, hipStream_t stream);
+int launch_qk_norm_bwd(int dtype, const NormArgs& a, void* dwq, void* dwk, void* scratch, hipStream_t stream);
 
 // ---------------------------------------------------------------------------
 // windowed attention

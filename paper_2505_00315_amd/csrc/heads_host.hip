@@ -175,7 +175,7 @@ extern "C" {
 int mosa_norm_scratch_size(const mosa_norm_shape* s, size_t* scratch_bytes) {
     if (const int e = check_norm(s)) return e;
     if (!scratch_bytes) return MOSA_ERR_INVALID_ARG;
-    *scratch_bytes = norm_partial_bytes((int64_t)s->batch * s->seq_len, s->d_head);
+    *scratch_bytes = norm_partial_bytes(s->dtype, (int64_t)s->batch * s->seq_len, s->d_head);
     return MOSA_OK;
 }
 
@@ -202,10 +202,9 @@ int mosa_qk_norm_rope_backward(const mosa_norm_shape* s, const mosa_rows* q, con
     if (const int e = take_rows(dq, a.B, a.Hq, a.T, a.dh, s->dtype, true, &a.dq)) return e;
     if (const int e = take_rows(dk, a.B, a.Hkv, a.T, a.dh, s->dtype, true, &a.dk)) return e;
     if ((dwq && !aligned(dwq, 16)) || (dwk && !aligned(dwk, 16))) return MOSA_ERR_INVALID_ARG;
-    const size_t need = dwq || dwk ? norm_partial_bytes((int64_t)a.B * a.T, a.dh) : 0;
+    const size_t need = dwq || dwk ? norm_partial_bytes(s->dtype, (int64_t)a.B * a.T, a.dh) : 0;
     if (const int e = check_scratch(scratch, scratch_bytes, need)) return e;
-    return done(launch_qk_norm_bwd(s->dtype, a, dwq, dwk, static_cast<float*>(scratch),
-                                   static_cast<hipStream_t>(stream)));
+    return done(launch_qk_norm_bwd(s->dtype, a, dwq, dwk, scratch, static_cast<hipStream_t>(stream)));
 }
 
 int mosa_attn_scratch_size(const mosa_attn_shape* s, size_t* forward_bytes, size_t* backward_bytes) {
