@@ -17,8 +17,8 @@ bool d_head_ok(int dh) { return dh == 32 || dh == 64 || dh == 128; }
 // Rows counted in 32 bits by the kernels (offsets into tensors are 64-bit).
 bool rows_ok(int64_t a, int64_t b, int64_t c) { return (double)a * (double)b * (double)c <= 2147483647.0; }
 
-// Nothing on a device reaches over more; within it offsets and sizes, in bytes or
-// elements, stay far from 64 bits.
+// Nothing on a device reaches over more; within it offsets and sizes in bytes stay far
+// from 64 bits.
 constexpr double kMostBytes = 70368744177664.0;  // 2^46
 
 // One tensor of rows [B, H, T, dh]: address and strides checked and taken over.
@@ -34,7 +34,7 @@ int take_rows(const mosa_rows* r, int B, int H, int T, int dh, int dtype, bool o
         if (st[i] < 0 || st[i] % unit || st[i] > ((int64_t)1 << 40)) return MOSA_ERR_INVALID_ARG;
         span += (double)(n[i] - 1) * (double)st[i];
     }
-    if (span > kMostBytes) return MOSA_ERR_INVALID_ARG;
+    if (span * elem_size(dtype) > kMostBytes) return MOSA_ERR_INVALID_ARG;
     if (output) {  // nested axes: each stride at least the extent of those within
         int64_t extent = dh;
         bool used[3] = {false, false, false};
