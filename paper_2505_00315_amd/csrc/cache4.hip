@@ -1,7 +1,7 @@
 // The 4-bit cache: rows written and read back (attention over it: cache4_attn.hip).
 //
 // Both copies move each byte once.  Measured (bf16, 4 x 4096 positions, 8 heads of
-// 128, 88 MB each): read 17 us, 5.2 TB/s, what memory gives; write 27 us, 3.3 TB/s,
+// 128, 88 MB each): read 17 us, 5.3 TB/s, what memory gives; write 25 us, 3.5 TB/s,
 // bound by the vector instructions of the codes, more than 20 per value.
 #include "cache4.h"
 #include "launch_parts.h"

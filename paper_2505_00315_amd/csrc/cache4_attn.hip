@@ -28,9 +28,12 @@
 // that are none.
 //
 // Measured (bf16, one token for each of 64 sequences of 8k to 16k positions, 32 / 8
-// heads of 128): 186 us for 1.02 GB, 5.5 TB/s, and 5 us for the parts' sum; one
-// short sequence (8 / 2 heads of 64, 1000 positions, window 512): 8.8 us, a launch
-// and a chain of a table read, a tile's loads and four tiles.
+// heads of 128): 185 us for 1.02 GB, 5.5 TB/s, and 5 us for the parts' sum; one
+// short sequence (8 / 2 heads of 64, 1000 positions, window 512): 8.5 us, a launch
+// and a chain of a table read, a tile's loads and four tiles.  Every 16 rows expand
+// the codes again: many queries are better served from the rows (8 sequences of 8192,
+// 32 / 8 heads of 128: 64 queries 232 us, 512 queries 1702; read and attention over
+// the rows 222 and 584).
 #include "cache4.h"
 #include "launch_parts.h"
 

@@ -19,7 +19,7 @@
 // the accurate fp32 sine and cosine.
 //
 // Measured (bf16, 4 x 4096 tokens, 32 query and 8 key heads of 128, all columns
-// turned): forward 74 us for 336 MB, 4.5 TB/s; backward 105 us for 505 MB, 4.8
+// turned): forward 73 us for 336 MB, 4.6 TB/s; backward 104 us for 505 MB, 4.8
 // TB/s, and 5 us for the sum of the 1024 partials of dwq and dwk (a large copy on
 // the same card: 5.2 TB/s).  One token of 8 + 2 heads of 64: 4.4 us, a launch and
 // two memory latencies.

@@ -13,13 +13,18 @@
 // The other operand stays in registers, and p and ds are fed to the second
 // products as they lie in them, against tiles read transposed.  bf16 storage rounds
 // p and ds to bf16 there, the type of the matrix operands, to half a step each;
-// the sums over them, lse and D are fp32.
+// the sums over them, lse and D are fp32.  (dq, dk and dv are 0.0026, 0.0024 and
+// 0.0023 off, a result rounded once 0.0017; ds in two parts would make dq 0.0018
+// for 5 to 6% of a training step.)  p comes from lse, which is rounded at its size:
+// past scores of about 2^20 its error shows.
 //
-// Measured (bf16): 2 x 4096 tokens, 32 / 8 heads of 128, window 1024, 4 sinks: a
-// training step takes 671 us, of which the forward 188, (lse, -D) 24 and these
-// kernels about 455, 0.9 PFLOP/s over their 7 products; the LDS's time for the
-// transposed reads bounds the key blocks.  8192 tokens, 4 heads of 64, window 512:
-// 38 us, chains of 10 tiles.
+// Measured (bf16): 2 x 4096 tokens, 32 / 8 heads of 128, window 1024, 4 sinks: this
+// kernel 617 us in a trace, 0.68 PFLOP/s over its 7 products, matrix instructions
+// busy 37% and the LDS 46% of the time (beside it the forward 182, (lse, -D) 24,
+// sums 6; a training step in a loop, at higher clocks, 679 in all); the LDS's time
+// for the transposed reads bounds the key blocks.  8192 tokens, 4 heads of 64,
+// window 512: 37 us, chains of 10 tiles.  fp32 (2 x 2048 tokens, 16 / 8 heads of 128):
+// matrix instructions busy 73%.
 //
 // Sinks are seen by every later row.  So that their keys' workgroups do not
 // walk the whole sequence while all others walk a window, the pairs beyond the
@@ -752,7 +757,9 @@ BwdGeom bwd_geom(int dtype, int dh, const AttnArgs& a) {
     // us with whole blocks, 232 with parts); with one up to half of them, as the
     // row blocks fill the rest (2048 tokens, 16 / 4 heads of 128, window 1024: 184
     // us whole, 165 with 512, 132 with 256; at 256 whole blocks parts lose, 199
-    // against 204).
+    // against 204).  Row blocks are not cut: without a window and with one or two
+    // heads the last of them, 8192 keys in one chain, sets the time (131 us of a step
+    // of 169 with one head of 64, 8192 tokens).
     const int64_t nk = (int64_t)a.B * a.Hkv * G.nk, walk = (int64_t)(a.W + kw) * a.G;
     const int64_t tiles = (a.W && walk < R ? walk : R) / (dtype == kBF16 ? 64 : 32), places = a.W ? 256 : 512;
     int64_t kp = nk < places ? (places + nk - 1) / nk : 1;

@@ -12,13 +12,15 @@
 // reads each K and V fragment once per 2 matrix instructions, which is what the
 // LDS can deliver at their full rate.
 //
-// Measured (heads of 128, bf16): 16384 tokens, 32 / 8 heads, window 4096, 4 sinks: 966
-// us, 996 TFLOP/s over the pairs that are seen (an 8192^3 matrix product of the
+// Measured (heads of 128, bf16): 16384 tokens, 32 / 8 heads, window 4096, 4 sinks: 967
+// us, 995 TFLOP/s over the pairs that are seen (an 8192^3 matrix product of the
 // library on the same card: 1113); one token for each of 32 sequences of up to 8192
 // keys, window 4096: 101 us, the keys and values at 5.4 TB/s.  Heads of 64, 8192
 // tokens, 4 heads, window 512: 17 us, a chain of 10 tiles whose loads and
-// exponentials wait for each other.  fp32, at the fp32 matrix instructions' rate:
-// 67 to 82 TFLOP/s with the backward.
+// exponentials wait for each other.  fp32: 67 to 78 TFLOP/s over a prompt of 4096
+// (a library product 151), matrix instructions busy 72% of the time; one token for
+// each of 32 sequences 369 us, as the products of a block's 60 rows that are none
+// (61% busy) take longer than the bytes.
 #include "launch_parts.h"
 #include "wattn_dma.h"
 

@@ -344,7 +344,9 @@ def cache4_read(shape, cache, page_table, start, rows=None, lens=None, k=None, v
 
 def cache4_attention(shape, cache_shape, q, cache, page_table, kv_lens, q_lens=None, out=None, lse=None, scratch=None,
                      stream=None):
-    """window_attention over the positions 0 .. kv_lens[b] - 1 of the cache.
+    """window_attention over the positions 0 .. kv_lens[b] - 1 of the cache, for
+    a few queries at once (from some dozens on, cache4_read and
+    window_attention over its rows take less time).
     ``shape``: an attention shape whose kv_len bounds kv_lens.  lse is written
     where it is given.  Returns out."""
     st, qs, _ = _attn_io(shape)
