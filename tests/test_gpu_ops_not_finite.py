@@ -423,3 +423,40 @@ def test_a_diverged_cache_takes_no_longer(case, dtype):
         call(y["k"], y["v"])
         assert best_time(attend) <= 2 * base, names
         assert bool(torch.isnan(out).all())
+
+
+def test_second_walks_beside_other_calls_and_in_graphs():
+    """Calls that walk twice on one stream, ordinary ones on another, and both captured: the bits of a call alone."""
+    case = (2, 8, 2, 64, 400, 400, 90, 5)
+    shape, x, _ = setup(case, "bf16", 12)
+    y = {**x, "v": x["v"].clone(), "do": x["do"].clone()}
+    spoil_values(y["v"], 1, 1, 400, 10, False)
+    y["do"][0, 3, 50, 7] = math.inf
+
+    def call(z, stream=None):
+        o = ops.window_attention(shape, z["q"], z["k"], z["v"], stream=stream)
+        return (*o, *ops.window_attention_backward(shape, z["q"], z["k"], z["v"], *o, z["do"], stream=stream))
+
+    def same(a, b):
+        return all(torch.equal(s.nan_to_num(7.0, 8.0, 9.0), t.nan_to_num(7.0, 8.0, 9.0)) for s, t in zip(a, b))
+    want = [call(x), call(y)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(3):
+        got = [[], []]
+        for _ in range(4):
+            for i, z in enumerate((x, y)):
+                got[i].append(call(z, streams[i]))
+        torch.cuda.synchronize()
+        for i in range(2):
+            assert all(same(g, want[i]) for g in got[i])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = [call(x), call(y)]
+    for _ in range(3):
+        for t in (*held[0], *held[1]):
+            t.fill_(5)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert same(held[0], want[0]) and same(held[1], want[1])
+        assert same(call(y), want[1])
