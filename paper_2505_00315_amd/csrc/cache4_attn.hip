@@ -295,17 +295,24 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache4_attn_kernel(AttnArgs a,
                 for (int y = 0; y < 2; ++y) {
                     const int key = cur.key + y;
                     const bool in = key >= 0 && key < kn;
+                    bool any = false;
 #pragma unroll
                     for (int q = 0; q < NQ; ++q)
 #pragma unroll
-                        for (int i = 0; i < RI; ++i)
-                            s[q][y][i] = (in & sees(a, pos[q][i], key)) ? s[q][y][i] : -__builtin_inff();
-                    // What is not finite (what no row sees may hold anything) leaves the
-                    // products, and joins the sums of the rows that see it here.
+                        for (int i = 0; i < RI; ++i) {
+                            const bool ok = in & sees(a, pos[q][i], key);
+                            s[q][y][i] = ok ? s[q][y][i] : -__builtin_inff();
+                            any |= ok;
+                        }
+                    // what no row sees may be anything: its scale and minimum are taken as 0;
+                    // what is not finite leaves the products, and joins the sums of the rows
+                    // that see it here
+                    const uint64_t bal = __builtin_amdgcn_ballot_w64(any);
+                    const bool seen = (bal >> c16 | bal >> (c16 + 16) | bal >> (c16 + 32) | bal >> (c16 + 48)) & 1;
 #pragma unroll
                     for (int gr = 0; gr < NG; ++gr) {
                         const bool bad = ((cur.vm[y][gr] & 0x7fff7fffu) + 0x00800080u) & 0x80008000u;
-                        cur.vm[y][gr] = bad ? 0u : cur.vm[y][gr];
+                        cur.vm[y][gr] = (seen & !bad) ? cur.vm[y][gr] : 0u;
 #pragma unroll
                         for (int q = 0; q < NQ; ++q)
 #pragma unroll

@@ -460,3 +460,26 @@ def test_second_walks_beside_other_calls_and_in_graphs():
         torch.cuda.synchronize()
         assert same(held[0], want[0]) and same(held[1], want[1])
         assert same(call(y), want[1])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("Q,lens", [(1, (50, 1, 100)), (6, (50, 6, 100)), (40, (50, 41, 100))])
+@pytest.mark.parametrize("bits", [0x7e, 0x7f, 0xff, 0x80])
+def test_what_the_cache_never_held_may_be_any_bits(dtype, Q, lens, bits):
+    """Positions past the lengths that were never written: numbers near the type's end, NaN, and a page that no table names."""
+    B, Hq, Hkv, dh, N, ps = 3, 4, 2, 64, 112, 16
+    shape, x, dt = setup((B, Hq, Hkv, dh, Q, N, 20, 2), dtype, 13)
+    per = N // ps
+    cs = ops.make_cache_shape(B, Hkv, dh, B * per + 1, ps, per, dtype)
+    table = (1 + torch.arange(B * per, dtype=torch.int32, device="cuda")).view(B, per)
+    kl = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    table[0, 2] = -1
+    got = []
+    for fill in (0, bits):
+        cache = ops.alloc_cache4(cs)
+        cache.fill_(fill)
+        ops.cache4_append(cs, cache, table, None, x["k"], x["v"], lens=kl)
+        lse = torch.empty(B, Hq, Q, dtype=torch.float32, device="cuda")
+        got.append((ops.cache4_attention(shape, cs, x["q"], cache, table, kl, q_lens=kl.clamp(max=Q), lse=lse), lse))
+    assert bool(torch.isfinite(got[0][0].float()).all())
+    assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
