@@ -64,8 +64,8 @@ extern "C" {
 enum {
     MOSA_OK = 0,
     MOSA_ERR_INVALID_ARG = -1, /* bad size, null required pointer, misalignment */
-    MOSA_ERR_UNSUPPORTED = -2, /* valid but not implemented (d_head, d_model, T range) */
-    MOSA_ERR_WORKSPACE = -3,   /* saved or scratch smaller than mosa_workspace_size */
+    MOSA_ERR_UNSUPPORTED = -2, /* valid but not implemented (d_head, d_model, T range, rows) */
+    MOSA_ERR_WORKSPACE = -3,   /* saved or scratch smaller than the shape's size function gives */
     MOSA_ERR_HIP = -4          /* a HIP launch or query failed */
 };
 

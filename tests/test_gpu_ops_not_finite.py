@@ -247,7 +247,7 @@ def test_gradients_past_the_lengths_are_zero_whatever_the_others_hold(dtype, win
             assert not bool(t[1, :, 77:].any())
 
 
-def best_time(f, n=5):
+def best_time(f, n=9):
     f()
     torch.cuda.synchronize()
     times = []
