@@ -245,7 +245,7 @@ def prepare(c, seed):
     def new(*shape, dtype=torch.float32):
         return torch.empty(shape, dtype=dtype, device=DEVICE)
 
-    st["logp"], st["lse"] = new(c["rows"]), new(c["rows"])
+    st["logp"], st["lse"], st["stats"] = new(c["rows"]), new(c["rows"]), new(c["rows"], 2)
     st["entropy"] = new(c["rows"]) if c["entropy"] else None
     if c["top"]:
         st["top_logp"], st["top_index"] = new(c["rows"], c["top"]), new(c["rows"], c["top"], dtype=torch.int32)
@@ -287,11 +287,12 @@ def _run_own(st, c):
                                 dx=st["d_x"], dw=st["d_w"], db=get("d_b"), scratch=st["scratch"])
             out.update({n: st[n] for n in ("d_x", "d_w", "d_b") if n in st})
         return out
-    ops.token_logprobs(sh, st["logits"], st["targets"], logp=st["logp"], lse=st["lse"], entropy=st["entropy"],
-                       top_logp=get("top_logp"), top_index=get("top_index"), scratch=st["scratch"])
+    ops.token_logprobs(sh, st["logits"], st["targets"], logp=st["logp"], lse=st["lse"], stats=st["stats"],
+                       entropy=st["entropy"], top_logp=get("top_logp"), top_index=get("top_index"),
+                       scratch=st["scratch"])
     out = {n: st[n] for n in ("logp", "lse", "entropy", "top_logp", "top_index") if get(n) is not None}
     if train:
-        ops.token_logprobs_backward(sh, st["logits"], st["targets"], st["lse"], entropy=st["entropy"],
+        ops.token_logprobs_backward(sh, st["logits"], st["targets"], st["stats"], entropy=st["entropy"],
                                     d_logp=st["d_logp"], d_entropy=get("d_entropy"), d_logits=st["d_logits"])
         out["d_logits"] = st["d_logits"]
     return out
