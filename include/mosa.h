@@ -380,6 +380,122 @@ int mosa_cache4_attention(const mosa_attn_shape* s, const mosa_cache_shape* c, c
                           const int32_t* kv_lens, const mosa_rows* out, float* lse, void* scratch,
                           size_t scratch_bytes, void* stream);
 
+/* ---------------------------------------------------------------------------
+ * Operators around a block: what a model runs between two attention layers and
+ * behind the last one -- the residual stream with its norms, products with weight
+ * matrices, log probabilities of tokens.
+ *
+ * The conventions are those of the operators above: inputs may be broadcast
+ * (strides of 0), outputs do not overlap themselves nor, but for the pairs named
+ * below, another argument; sums, norms and softmax statistics are fp32 or wider;
+ * results are reproducible; a captured call records kernels only; calls that may
+ * overlap in time need scratch buffers of their own.
+ * ------------------------------------------------------------------------- */
+
+/* Rows of a matrix: `row_stride` elements from one to the next (not read where
+ * there is one row). */
+typedef struct mosa_matrix {
+    void* data;
+    int64_t row_stride;
+} mosa_matrix;
+
+/* The residual stream x and a block's output y, for every token
+ *   h = residual_scale x + branch_scale gate u,   u = w_post y / sqrt(mean(y^2) + eps)
+ *   n = w_pre h / sqrt(mean(h^2) + eps)
+ * h is the stream behind the block and n what the next block reads.  post_norm 0:
+ * u = y.  pre_norm 0: no n.  gate: none, one vector, one per sequence, or one per
+ * token.  n is taken from h before h is rounded to its storage type.
+ * d_model is a multiple of 8, at most 8192; batch seq_len is at most 2^31 - 1. */
+#define MOSA_GATE_NONE 0
+#define MOSA_GATE_VECTOR 1
+#define MOSA_GATE_SEQUENCE 2
+#define MOSA_GATE_TOKEN 3
+typedef struct mosa_residual_shape {
+    int32_t batch, seq_len, d_model, dtype, post_norm, pre_norm, gate;
+    float residual_scale, branch_scale, eps;
+} mosa_residual_shape;
+
+/* Scratch of mosa_residual_norm_backward. */
+int mosa_residual_scratch_size(const mosa_residual_shape* s, size_t* scratch_bytes);
+/* Tensors are rows [batch, 1, seq_len, d_model]: head strides are not read, nor are
+ * the batch and row strides of a gate that has no such axis.  y NULL: h is x (first
+ * block of a model; needs pre_norm 1, post_norm 0 and no gate) and h_out is not
+ * written.  gate and n_out are NULL where the shape has none; a NULL weight stands
+ * for ones.  h_out may be x or y, and n_out y (same address and strides); they
+ * are not each other. */
+int mosa_residual_norm(const mosa_residual_shape* s, const mosa_rows* x, const mosa_rows* y, const void* w_post,
+                       const mosa_rows* gate, const void* w_pre, const mosa_rows* h_out, const mosa_rows* n_out,
+                       void* stream);
+/* From x, y as they went in and the gradients dh of h (NULL: 0) and dn of n: dx
+ * (written, not added to), dy, and dw_post, dw_pre [d_model] and dgate (rows as
+ * the gate's), each of these NULL where it is not needed.  dx may be dh or dn and
+ * dy dn or dh, dx and dy not the same. */
+int mosa_residual_norm_backward(const mosa_residual_shape* s, const mosa_rows* x, const mosa_rows* y,
+                                const void* w_post, const mosa_rows* gate, const void* w_pre, const mosa_rows* dh,
+                                const mosa_rows* dn, const mosa_rows* dx, const mosa_rows* dy, void* dw_post,
+                                const mosa_rows* dgate, void* dw_pre, void* scratch, size_t scratch_bytes,
+                                void* stream);
+
+/* Product with a weight matrix:  y = act(x w + b) + r  for x [rows, d_in], w
+ * [d_in, d_out] (MOSA_W_IN_OUT, as the layer's weights) or [d_out, d_in]
+ * (MOSA_W_OUT_IN, as an embedding of tokens), b [d_out], r and y [rows, d_out].
+ * act: none, relu, gelu(z) = z Phi(z), silu(z) = z / (1 + exp(-z)).
+ * d_in and d_out are multiples of 8, at most 2^20; strides are multiples of 16
+ * bytes, below 2^22 elements; rows is at most 2^24. */
+#define MOSA_ACT_NONE 0
+#define MOSA_ACT_RELU 1
+#define MOSA_ACT_GELU 2
+#define MOSA_ACT_SILU 3
+#define MOSA_W_IN_OUT 0
+#define MOSA_W_OUT_IN 1
+typedef struct mosa_linear_shape {
+    int32_t rows, d_in, d_out, dtype, act, w_order;
+} mosa_linear_shape;
+
+int mosa_linear_scratch_size(const mosa_linear_shape* s, size_t* forward_bytes, size_t* backward_bytes);
+/* b and r may be NULL.  z: x w + b as well, in storage type, where it is not NULL
+ * (the backward of an activation reads it).  y may be r (same address and
+ * stride). */
+int mosa_linear(const mosa_linear_shape* s, const mosa_matrix* x, const mosa_matrix* w, const void* b,
+                const mosa_matrix* r, const mosa_matrix* y, const mosa_matrix* z, void* scratch,
+                size_t scratch_bytes, void* stream);
+/* From x, w, z (NULL with MOSA_ACT_NONE) and the gradient dy: dx, dw (rows as w's)
+ * and db [d_out], each NULL where it is not needed.  The gradient of r is dy.
+ * bf16 storage rounds dy act'(z) to bf16 where it enters the products. */
+int mosa_linear_backward(const mosa_linear_shape* s, const mosa_matrix* x, const mosa_matrix* w,
+                         const mosa_matrix* z, const mosa_matrix* dy, const mosa_matrix* dx, const mosa_matrix* dw,
+                         void* db, void* scratch, size_t scratch_bytes, void* stream);
+
+/* Log probabilities of tokens: for every row of logits x [rows, vocab], z = scale x,
+ *   lse = log sum_j exp(z_j),  log p_j = z_j - lse,
+ *   logp = log p_target,  entropy = -sum_j p_j log p_j,
+ * and the `top` largest log p_j with their indices, largest first, equal ones by
+ * index.  targets: int32 [rows]; a value that is not in 0 .. vocab - 1 is no target:
+ * logp is 0 there.  Logits of -inf are tokens that cannot come (p = 0).  A row of
+ * -inf alone has lse and every log p -inf, entropy 0 and gradients 0; a row with
+ * +inf or NaN has NaN in all of them (its alternatives are in order, NaN as -inf).
+ * vocab is at most 2^30; top is at most 32 and at most vocab; scale is positive.
+ * Logits and their gradient need the alignment of one value only, and their rows
+ * may lie any number of elements apart (at least vocab; logits also 0). */
+typedef struct mosa_logprob_shape {
+    int32_t rows, vocab, dtype, top;
+    float scale;
+} mosa_logprob_shape;
+
+int mosa_logprob_scratch_size(const mosa_logprob_shape* s, size_t* forward_bytes);
+/* All outputs are fp32 (top_index int32) and contiguous; each may be NULL (logp
+ * where targets are).  stats [rows, 2]: the row's largest logit and log sum_j
+ * exp(scale (x_j - largest)), which the backward reads. */
+int mosa_token_logprobs(const mosa_logprob_shape* s, const mosa_matrix* logits, const int32_t* targets, float* logp,
+                        float* lse, float* stats, float* entropy, float* top_logp, int32_t* top_index, void* scratch,
+                        size_t scratch_bytes, void* stream);
+/* Gradient of the logits from those of logp, lse and entropy [rows] (each NULL: 0;
+ * d_logp needs targets, d_entropy the forward's entropy).  d_logits may be logits
+ * (same address and stride). */
+int mosa_token_logprobs_backward(const mosa_logprob_shape* s, const mosa_matrix* logits, const int32_t* targets,
+                                 const float* stats, const float* entropy, const float* d_logp, const float* d_lse,
+                                 const float* d_entropy, const mosa_matrix* d_logits, void* stream);
+
 /* Static text for a status code (never NULL). */
 const char* mosa_status_string(int status);
 

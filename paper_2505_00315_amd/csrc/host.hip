@@ -252,7 +252,8 @@ const char* mosa_status_string(int status) {
         case MOSA_OK: return "ok";
         case MOSA_ERR_INVALID_ARG: return "invalid argument (size, null pointer or alignment)";
         case MOSA_ERR_UNSUPPORTED: return "unsupported shape (layer: d_head 32 or 64, d_model a multiple of 64, seq_len <= 16384; "
-                                           "operators of the dense heads: d_head 32, 64 or 128, rows and lengths in the limits of mosa.h)";
+                                           "operators of the dense heads: d_head 32, 64 or 128, rows and lengths in the limits of mosa.h; "
+                                           "operators around a block: widths multiples of 8, sizes in the limits of mosa.h)";
         case MOSA_ERR_WORKSPACE: return "saved, scratch or workspace buffer smaller than the shape's size function gives";
         case MOSA_ERR_HIP: return "HIP launch failure";
         default: return "unknown status";

@@ -1,0 +1,412 @@
+// Log probabilities of tokens out of rows of logits, forward and backward.
+//
+//   M = max_j x_j,  L = log sum_j exp(scale (x_j - M)),  lse = scale M + L,
+//   logp = scale (x_t - M) - L,
+//   entropy = L - sum_j e_j scale (x_j - M) / sum_j e_j,  e_j = exp(scale (x_j - M))
+//   dx_j = scale [ dlogp (1[j = t] - p_j) + dlse p_j - dentropy p_j (log p_j + entropy) ]
+//
+// The forward reads the logits once, the backward reads and writes them once:
+// memory bounds both where rows are many.  M and L are kept apart: differences
+// to M are exact where their sum lse would have rounded them away (rows far from
+// 0, rows of the type's lowest value alone).
+//
+// Forward: a workgroup takes a row or a part of one; every lane keeps a running
+// maximum and sum over its units of 16 bytes and they are joined at the end, the
+// parts of a row by a second kernel.
+//
+// Alternatives (the `top` largest, equal ones by index): every lane also keeps the
+// first of its units that holds its maximum.  The top-th of the lanes' (maximum,
+// unit) in order is a threshold: at least `top` values are at or above it, all of
+// them in the units of the `top` lanes that reach it, which are read once more
+// (from L2).  What is at or above the threshold is ranked by counting.  Where that
+// is more than the list in LDS holds (rows of equal values), the values are taken
+// one by one instead.
+#include <math.h>
+
+#include "block.h"
+
+namespace mosa {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kList = 1024;  // values that are ranked at once
+
+// Order of two values as unsigned numbers: larger first counts as larger; NaN as
+// -inf, -0 as 0.
+__device__ __forceinline__ uint32_t order_of(float x) {
+    if (x != x) x = -INFINITY;
+    const uint32_t u = __float_as_uint(x + 0.f);
+    return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+__device__ __forceinline__ float value_of(uint32_t o) { return __uint_as_float(o & 0x80000000u ? o & 0x7fffffffu : ~o); }
+__device__ __forceinline__ uint64_t key_of(float x, int index) { return (uint64_t)order_of(x) << 32 | (uint32_t)~index; }
+
+// A row in units of 16 bytes, counted from the aligned address at or before its
+// first value: the first and the last unit may hold fewer of its values.
+template <typename ST>
+struct Row {
+    static constexpr int E = Unit<ST>::E;
+    const ST* p;  // aligned
+    int lead, V, units;
+    __device__ __forceinline__ Row(const char* base, int64_t stride, int64_t r, int V) : V(V) {
+        const ST* at = reinterpret_cast<const ST*>(base) + r * stride;
+        lead = (int)(((uintptr_t)at & 15) / sizeof(ST));
+        p = at - lead;
+        units = (int)(((int64_t)lead + V + E - 1) / E);
+    }
+    __device__ __forceinline__ int first(int u) const { return u * E - lead; }  // index of a unit's first value
+    __device__ __forceinline__ bool whole(int u) const { return first(u) >= 0 && (int64_t)first(u) + E <= V; }
+    // values of unit u, -inf in the place of those that are not the row's
+    __device__ __forceinline__ void get(int u, float (&x)[E]) const {
+        if (whole(u)) {
+            Unit<ST> v;
+            v.load(p + (int64_t)u * E);
+            v.get(x);
+        } else {
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                const int64_t j = (int64_t)first(u) + e;
+                x[e] = j >= 0 && j < V ? ld1<ST>(p + (int64_t)u * E + e) : -INFINITY;
+            }
+        }
+    }
+};
+
+// Running maximum m, sum l of exp(scale (x - m)) and s of the same times the
+// exponent (in log2 units).
+struct Run {
+    float m, l, s;
+};
+template <bool ENT>
+__device__ __forceinline__ void rebase(Run& r, float m, float c) {  // to a maximum m >= r.m
+    const float d = r.m == m ? 0.f : fmaxf((r.m - m) * c, -1000.f);  // (no sum yet: r.m = -inf)
+    const float f = __builtin_amdgcn_exp2f(d);
+    if constexpr (ENT) r.s = f * (r.s + d * r.l);
+    r.l *= f;
+    r.m = m;
+}
+template <bool ENT, int N>
+__device__ __forceinline__ void add_values(Run& r, const float (&x)[N], float c) {
+    const float m = r.m == -INFINITY ? 0.f : r.m;
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+        const float d = (x[e] - m) * c, w = __builtin_amdgcn_exp2f(d);
+        r.l += w;
+        if constexpr (ENT) r.s += w * fmaxf(d, -1000.f);
+    }
+}
+template <bool ENT>
+__device__ __forceinline__ Run join(Run a, Run b, float c) {
+    const float m = fmaxf(a.m, b.m);
+    rebase<ENT>(a, m, c);
+    rebase<ENT>(b, m, c);
+    return {m, a.l + b.l, a.s + b.s};
+}
+template <bool ENT>
+__device__ __forceinline__ Run wave_join(Run r, float c) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+        Run q;
+        q.m = __shfl_xor(r.m, o, 64), q.l = __shfl_xor(r.l, o, 64), q.s = ENT ? __shfl_xor(r.s, o, 64) : 0.f;
+        // (the same order of the operands in both lanes)
+        const bool low = (threadIdx.x & o) == 0;
+        r = low ? join<ENT>(r, q, c) : join<ENT>(q, r, c);
+    }
+    return r;
+}
+
+// Scratch of a row's parts: their Runs, then their lists of keys.
+struct PartBuf {
+    Run* run;        // [R][P]
+    uint64_t* keys;  // [R][P][top]
+};
+
+// The outputs of a row, by one lane.  x_t: the target's logit.
+template <typename ST>
+__device__ __forceinline__ void write_row(const LogprobArgs& a, int r, const Run& t) {
+    // nothing but -inf: every weight is 0
+    const bool none = t.m == -INFINITY && t.l == 0.f;
+    const float L = none ? -INFINITY : logf(t.l);
+    if (a.stats) a.stats[2 * (int64_t)r] = t.m, a.stats[2 * (int64_t)r + 1] = L;
+    if (a.lse) a.lse[r] = none ? -INFINITY : a.scale * t.m + L;
+    if (a.entropy) a.entropy[r] = none ? 0.f : L - kLn2 * t.s / t.l;
+    if (a.logp) {
+        const int j = a.target[r];
+        float v = 0.f;
+        if (j >= 0 && j < a.V) {
+            const float x = ld1<ST>(reinterpret_cast<const ST*>(a.x) + (int64_t)r * a.row + j);
+            v = none ? -INFINITY : a.scale * (x - t.m) - L;
+        }
+        a.logp[r] = v;
+    }
+}
+__device__ __forceinline__ void write_top(const LogprobArgs& a, int r, int at, uint64_t key, const Run& t) {
+    const float x = value_of((uint32_t)(key >> 32));
+    const float L = logf(t.l);
+    // (t.l is NaN in a row with NaN or +inf)
+    a.top_logp[(int64_t)r * a.top + at] = t.l != t.l ? t.l : x == -INFINITY ? x : a.scale * (x - t.m) - L;
+    a.top_index[(int64_t)r * a.top + at] = (int)~(uint32_t)key;
+}
+
+// The `top` largest keys of n distinct ones, in order: f(rank, key).
+template <typename F>
+__device__ __forceinline__ void rank_keys(const uint64_t* keys, int n, int top, F f) {
+    for (int i = threadIdx.x; i < n; i += kThreads) {
+        const uint64_t k = keys[i];
+        int rank = 0;
+        for (int j = 0; j < n; ++j) rank += keys[j] > k;
+        if (rank < top && k) f(rank, k);
+    }
+}
+
+template <typename ST, bool ENT, bool TOP>
+__global__ __launch_bounds__(kThreads) void logprob_kernel(LogprobArgs a, int P, int per, PartBuf buf) {
+    constexpr int E = Unit<ST>::E, U = 4;
+    __shared__ Run runs[kThreads / 64];
+    __shared__ uint64_t keys[TOP ? kList : 1];
+    __shared__ uint64_t threshold;
+    __shared__ int lanes[kMaxTop], count;
+    const int r = blockIdx.x / P, part = blockIdx.x % P, tid = threadIdx.x;
+    const Row<ST> row(a.x, a.row, r, a.V);
+    const int u0 = part * per, u1 = min(row.units, u0 + per);  // (the last part may be empty)
+    const float c = a.scale * kLog2e;
+    Run t{-INFINITY, 0.f, 0.f};
+    float best = -INFINITY;
+    int unit = -1;  // the first unit that holds the lane's maximum
+    for (int u = u0 + tid; u < u1; u += U * kThreads) {
+        float x[U][E];
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            if (u + i * kThreads < u1) {
+                row.get(u + i * kThreads, x[i]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < E; ++e) x[i][e] = -INFINITY;
+            }
+        }
+        float m = t.m;
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            float w = -INFINITY;  // (NaN are left out)
+#pragma unroll
+            for (int e = 0; e < E; ++e) w = fmaxf(w, x[i][e]);
+            if constexpr (TOP) {
+                if ((w > best || unit < 0) && u + i * kThreads < u1) best = w, unit = u + i * kThreads;
+            }
+            m = fmaxf(m, w);
+        }
+        if (m > t.m) rebase<ENT>(t, m, c);
+#pragma unroll
+        for (int i = 0; i < U; ++i) add_values<ENT>(t, x[i], c);
+    }
+    t = wave_join<ENT>(t, c);
+    if ((tid & 63) == 0) runs[tid >> 6] = t;
+    if (TOP) {
+        // a lane without units: 0, below every key
+        keys[tid] = unit < 0 ? 0 : key_of(best, unit);
+        if (tid == 0) count = 0;
+    }
+    __syncthreads();
+    t = runs[0];
+#pragma unroll
+    for (int w = 1; w < kThreads / 64; ++w) t = join<ENT>(t, runs[w], c);
+    if (tid == 0) {
+        if (P > 1) buf.run[(int64_t)r * P + part] = t;
+        else write_row<ST>(a, r, t);
+    }
+    if constexpr (TOP) {
+        auto put = [&](int rank, uint64_t key) {
+            if (P > 1) buf.keys[((int64_t)r * P + part) * a.top + rank] = key;
+            else write_top(a, r, rank, key, t);
+        };
+        const uint64_t mine = keys[tid];
+        int rank = 0;
+        for (int j = 0; j < kThreads; ++j) rank += keys[j] > mine || (keys[j] == mine && j < tid);
+        if (rank < a.top) lanes[rank] = tid;
+        if (rank == a.top - 1) threshold = mine;
+        __syncthreads();
+        const uint64_t least = threshold;  // 0: every value
+        const int each = (u1 - u0 + kThreads - 1) / kThreads, total = a.top * each;
+        // the units of those lanes: f(index, value) for what is at or above the threshold
+        auto visit = [&](auto f) {
+            for (int i = tid; i < total; i += kThreads) {
+                const int u = u0 + lanes[i / each] + (i % each) * kThreads;
+                if (u >= u1) continue;
+                float x[E];
+                row.get(u, x);
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    const int j = row.first(u) + e;
+                    if (j >= 0 && j < a.V && key_of(x[e], u) >= least) f(j, x[e]);
+                }
+            }
+        };
+        __syncthreads();  // (keys are read until here)
+        visit([&](int j, float x) {
+            const int n = atomicAdd(&count, 1);
+            if (n < kList) keys[n] = key_of(x, j);
+        });
+        __syncthreads();
+        const int n = count;
+        if (n <= kList) {
+            rank_keys(keys, n, a.top, put);
+        } else {
+            uint64_t last = ~(uint64_t)0;
+            for (int k = 0; k < a.top; ++k) {
+                uint64_t next = 0;
+                visit([&](int j, float x) {
+                    const uint64_t key = key_of(x, j);
+                    if (key < last && key > next) next = key;
+                });
+                keys[tid] = next;
+                __syncthreads();
+                for (int o = kThreads / 2; o > 0; o >>= 1) {
+                    if (tid < o && keys[tid + o] > keys[tid]) keys[tid] = keys[tid + o];
+                    __syncthreads();
+                }
+                last = keys[0];
+                __syncthreads();
+                if (tid == 0) put(k, last);
+            }
+        }
+        if (P > 1) {  // a part of fewer values
+            for (int k = n + tid; k < a.top; k += kThreads) put(k, 0);
+        }
+    }
+}
+
+// The parts of a row joined.
+template <typename ST, bool ENT, bool TOP>
+__global__ __launch_bounds__(kThreads) void logprob_join_kernel(LogprobArgs a, int P, PartBuf buf) {
+    __shared__ uint64_t keys[TOP ? kList : 1];
+    const int r = blockIdx.x;
+    const float c = a.scale * kLog2e;
+    Run t = buf.run[(int64_t)r * P];
+    for (int p = 1; p < P; ++p) t = join<ENT>(t, buf.run[(int64_t)r * P + p], c);
+    if (threadIdx.x == 0) write_row<ST>(a, r, t);
+    if constexpr (TOP) {
+        const int n = P * a.top;  // (at most kList: see parts_of)
+        for (int i = threadIdx.x; i < n; i += kThreads) keys[i] = buf.keys[(int64_t)r * n + i];
+        __syncthreads();
+        rank_keys(keys, n, a.top, [&](int rank, uint64_t key) { write_top(a, r, rank, key, t); });
+    }
+}
+
+// A wave takes `per` units of a row.
+template <typename ST>
+__global__ __launch_bounds__(kThreads) void logprob_bwd_kernel(LogprobArgs a, int P, int per, int64_t waves) {
+    constexpr int E = Unit<ST>::E;
+    const int lane = threadIdx.x & 63;
+    const int64_t w = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
+    if (w >= waves) return;
+    const int r = (int)(w / P), part = (int)(w % P);
+    const Row<ST> row(a.x, a.row, r, a.V);
+    ST* out = reinterpret_cast<ST*>(a.dx) + (int64_t)r * a.drow - row.lead;
+    const bool even = ((uintptr_t)out & 15) == 0;
+    const int u0 = part * per, u1 = min(row.units, u0 + per);
+    const float M = a.stats[2 * (int64_t)r], L = a.stats[2 * (int64_t)r + 1], c = a.scale * kLog2e;
+    const bool none = M == -INFINITY && L == -INFINITY;
+    const int t = a.target ? a.target[r] : -1;
+    const bool has = a.dlogp && t >= 0 && t < a.V && !none;
+    const float g = has ? a.scale * a.dlogp[r] : 0.f, gl = a.dlse ? a.scale * a.dlse[r] : 0.f;
+    const float ge = a.dent ? a.scale * a.dent[r] : 0.f, H = a.dent ? a.entropy[r] : 0.f;
+    // dx = p (A - ge log p) + g at the target
+    const float A = gl - g - ge * H, M0 = M == -INFINITY ? 0.f : M, L0 = none ? 0.f : L;
+    const float l2 = L0 * kLog2e, gk = ge * kLn2;
+    for (int u = u0 + lane; u < u1; u += 64) {
+        float x[E];
+        row.get(u, x);
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const float d = (x[e] - M0) * c - l2, p = __builtin_amdgcn_exp2f(d);
+            x[e] = p * (A - gk * fmaxf(d, -1000.f));
+        }
+        const int j = t - row.first(u);
+        if (has && j >= 0 && j < E) {
+#pragma unroll
+            for (int e = 0; e < E; ++e) x[e] += e == j ? g : 0.f;
+        }
+        if (even && row.whole(u)) {
+            Unit<ST> o;
+            o.set(x);
+            o.store(out + (int64_t)u * E);
+        } else {
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                const int64_t i = (int64_t)row.first(u) + e;
+                if (i >= 0 && i < a.V) st1<ST>(out + (int64_t)u * E + e, x[e]);
+            }
+        }
+    }
+}
+
+// Parts of a row, and units of each: where rows are few, enough for the chip.
+struct Split {
+    int P, per;
+};
+Split parts_of(int dtype, int R, int V, int top) {
+    const int E = dtype == kBF16 ? 8 : 4;
+    const int64_t units = ((int64_t)V + 2 * E - 2) / E;  // (a row that does not start at a unit)
+    int64_t P = 1024 / R;
+    const int64_t most = units / (4 * kThreads);  // a part's reads keep its lanes busy
+    if (P > most) P = most;
+    if (top && P > kList / 2 / top) P = kList / 2 / top;
+    if (P < 1) P = 1;
+    const int64_t per = (units + P - 1) / P;
+    return {(int)((units + per - 1) / per), (int)per};
+}
+
+template <typename ST, bool ENT, bool TOP>
+int forward_t(const LogprobArgs& a, const Split& s, const PartBuf& buf, hipStream_t stream) {
+    // (a row's unit 0 may hold few of its values, so that the last part may be empty)
+    hipLaunchKernelGGL((logprob_kernel<ST, ENT, TOP>), dim3((unsigned)((int64_t)a.R * s.P)), dim3(kThreads), 0, stream, a,
+                       s.P, s.per, buf);
+    if (hipGetLastError() != hipSuccess) return -1;
+    if (s.P > 1) {
+        hipLaunchKernelGGL((logprob_join_kernel<ST, ENT, TOP>), dim3(a.R), dim3(kThreads), 0, stream, a, s.P, buf);
+        if (hipGetLastError() != hipSuccess) return -1;
+    }
+    return 0;
+}
+
+}  // namespace
+
+size_t logprob_scratch_bytes(int dtype, int R, int V, int top) {
+    const Split s = parts_of(dtype, R, V, top);
+    if (s.P == 1) return 0;
+    const size_t runs = ((size_t)R * s.P * sizeof(Run) + 255) / 256 * 256;
+    return runs + (size_t)R * s.P * top * sizeof(uint64_t);
+}
+
+int launch_logprobs(int dtype, const LogprobArgs& a, void* scratch, hipStream_t stream) {
+    const Split s = parts_of(dtype, a.R, a.V, a.top);
+    const bool top = a.top > 0 && a.top_logp;
+    PartBuf buf{};
+    if (s.P > 1) {
+        buf.run = static_cast<Run*>(scratch);
+        buf.keys = reinterpret_cast<uint64_t*>(static_cast<char*>(scratch) +
+                                               ((size_t)a.R * s.P * sizeof(Run) + 255) / 256 * 256);
+    }
+    auto go = [&](auto st) {
+        using ST = decltype(st);
+        if (top) return a.entropy ? forward_t<ST, true, true>(a, s, buf, stream) : forward_t<ST, false, true>(a, s, buf, stream);
+        return a.entropy ? forward_t<ST, true, false>(a, s, buf, stream) : forward_t<ST, false, false>(a, s, buf, stream);
+    };
+    return dtype == kBF16 ? go(uint16_t{}) : go(float{});
+}
+
+int launch_logprobs_bwd(int dtype, const LogprobArgs& a, hipStream_t stream) {
+    const int E = dtype == kBF16 ? 8 : 4;
+    const int per = 256;  // units of a wave: 4 per lane
+    const int64_t units = ((int64_t)a.V + 2 * E - 2) / E, P = (units + per - 1) / per, waves = P * a.R;
+    const int64_t blocks = (waves + kThreads / 64 - 1) / (kThreads / 64);
+    if (blocks > 0x7fffffff) return -1;
+    if (dtype == kBF16)
+        hipLaunchKernelGGL((logprob_bwd_kernel<uint16_t>), dim3((unsigned)blocks), dim3(kThreads), 0, stream, a, (int)P, per, waves);
+    else
+        hipLaunchKernelGGL((logprob_bwd_kernel<float>), dim3((unsigned)blocks), dim3(kThreads), 0, stream, a, (int)P, per, waves);
+    return hipGetLastError() == hipSuccess ? 0 : -1;
+}
+
+}  // namespace mosa

@@ -1,0 +1,369 @@
+// Products of the linear operator on the matrix cores:
+//
+//   C[M x N] = sum_k Q[M x K] P[K x N]     (fp32 accumulation), C^T = P^T Q^T by tile
+//
+// An operand lies in memory with k along its rows ("k-contiguous": x, and w^T for dx)
+// or with its own axis along them (w, and both operands of dw).  A workgroup
+// computes NT columns by MT rows of C; its waves own WTN x WTM of them.  Chunks of
+// 128 bytes of k (64 bf16, 32 fp32) go from global memory straight into LDS, STG
+// chunks in flight, one barrier per chunk; a wave's fragments of the next 32 k are
+// read while the current ones are multiplied.
+//
+// The columns are the matrix instruction's rows, so that a lane ends up with 4
+// consecutive columns of one row of C; with bf16 the two 16-column blocks of a pair
+// interleave by 4 columns, so that a lane holds 8 consecutive ones and stores 16
+// bytes.
+//
+// In LDS a k-contiguous tile is [rows][8 units of 16 bytes], unit u of row r at u ^
+// f(r), f chosen so that the 8 lanes that are served at once read 8 different unit
+// places.  The other tiles are [k][columns] as in memory; bf16 fragments are read from
+// them transposed (ds_read_b64_tr_b16), fp32 ones value by value, with units
+// permuted by k.
+#pragma once
+
+#include "block.h"
+#include "gemm2.h"
+#include "wattn_dma.h"
+
+namespace mosa {
+
+struct ProdArgs {
+    const char *p, *q;    // operands: n side (P), m side (Q)
+    int64_t prow, qrow;   // bytes from one row in memory to the next
+    int M, N, K;
+    int tm, tn;           // tiles
+    int splits, kper;     // parts of K, k of each (a multiple of the chunk)
+    float* part;          // splits > 1: [splits][M][N]
+    // epilogue: c + bias, activation, + r
+    const void* bias;
+    int act;
+    Matrix r, y, z;
+};
+
+__device__ __forceinline__ float act_of(float z, int act) {
+    if (act == kActRelu) return z > 0.f ? z : z != z ? z : 0.f;
+    if (act == kActGelu) return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
+    if (act == kActSilu) return z / (1.f + expf(-z));
+    return z;
+}
+__device__ __forceinline__ float act_slope(float z, int act) {
+    if (act == kActRelu) return z > 0.f ? 1.f : z != z ? z : 0.f;
+    if (act == kActGelu)
+        return 0.5f * (1.f + erff(z * 0.70710678118654752f)) + z * 0.39894228040143268f * expf(-0.5f * z * z);
+    const float s = 1.f / (1.f + expf(-z));
+    return s * (1.f + z * (1.f - s));
+}
+
+// Unit<ST>::E values of row m from column n on: bias, activation, residual, store.
+template <typename ST>
+__device__ __forceinline__ void finish_unit(const ProdArgs& a, int m, int n, float (&x)[Unit<ST>::E]) {
+    constexpr int E = Unit<ST>::E;
+    Unit<ST> u;
+    if (a.bias) {
+        float b[E];
+        u.load(static_cast<const ST*>(a.bias) + n);
+        u.get(b);
+#pragma unroll
+        for (int e = 0; e < E; ++e) x[e] += b[e];
+    }
+    if (a.z.p) {
+        u.set(x);
+        u.store(reinterpret_cast<ST*>(a.z.p) + (int64_t)m * a.z.row + n);
+    }
+    if (a.act) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) x[e] = act_of(x[e], a.act);
+    }
+    if (a.r.p) {
+        float b[E];
+        u.load(reinterpret_cast<const ST*>(a.r.p) + (int64_t)m * a.r.row + n);
+        u.get(b);
+#pragma unroll
+        for (int e = 0; e < E; ++e) x[e] += b[e];
+    }
+    u.set(x);
+    u.store(reinterpret_cast<ST*>(a.y.p) + (int64_t)m * a.y.row + n);
+}
+
+template <typename ST_, bool PKC_, bool QKC_, int NT_, int MT_, int WN_, int WM_, int STG_>
+struct ProdShape {
+    using ST = ST_;
+    static constexpr bool PKC = PKC_, QKC = QKC_;
+    static constexpr int NT = NT_, MT = MT_, WN = WN_, WM = WM_, STG = STG_, T = 64 * WN * WM;
+    static constexpr int ES = (int)sizeof(ST), E = 16 / ES, KC = 128 / ES, KS = KC / 32;
+    static constexpr int WTN = NT / WN, WTM = MT / WM, FN = WTN / 16, FM = WTM / 16;
+    static constexpr int PU = NT * ES / 16, QU = MT * ES / 16;  // units of a [k][columns] row
+    static constexpr int P_BYTES = NT * 128, Q_BYTES = MT * 128, STAGE = P_BYTES + Q_BYTES, LDS = STG * STAGE;
+    static constexpr int IP = P_BYTES / 16 / T, IQ = Q_BYTES / 16 / T, L = IP + IQ;  // loads per lane and chunk
+    static_assert(P_BYTES % (16 * T) == 0 && Q_BYTES % (16 * T) == 0, "whole instructions per wave");
+    static_assert(ES == 4 || FN % 2 == 0, "pairs of column blocks");
+    static_assert(LDS <= 160 * 1024 && (STG - 1) * L <= 63 && STG >= 2, "stages");
+};
+
+// Unit places of a k-contiguous tile's row; the P side's bf16 rows are read 4
+// apart in eights.
+template <typename ST, bool PSIDE>
+__device__ __forceinline__ int prod_swz(int r) {
+    return PSIDE && sizeof(ST) == 2 ? (r & 3) | ((r >> 3) & 1) << 2 : r & 7;
+}
+// Unit places of a [k][columns] tile of U units a row.
+template <typename ST, int U>
+__device__ __forceinline__ int prod_kswz(int k, int u) {
+    if constexpr (sizeof(ST) == 2) return mswz<U>(k, u);
+    else return u ^ (4 * ((k >> 3) & 3));
+}
+
+// One operand: where a lane's units come from, and its fragments.
+template <class S, bool PSIDE>
+struct ProdSide {
+    using ST = typename S::ST;
+    static constexpr bool KCON = PSIDE ? S::PKC : S::QKC;
+    static constexpr int E = S::E, U = PSIDE ? S::PU : S::QU, I = PSIDE ? S::IP : S::IQ, T = S::T;
+    static constexpr int BYTES = PSIDE ? S::P_BYTES : S::Q_BYTES;
+    const char* base;  // of the tile and the split's first k
+    int64_t row, step;
+    int left;  // columns (or rows of C) of the tile that exist, at least one unit's
+    uint32_t off[I];
+
+    // unit i of the tile -> (row in memory, unit in the row) of its source
+    static __device__ __forceinline__ void place(int i, int& r, int& u) {
+        if constexpr (KCON) {
+            r = i / 8;
+            u = (i % 8) ^ prod_swz<ST, PSIDE>(r);
+        } else {
+            r = i / U;
+            u = prod_kswz<ST, U>(r, i % U);
+        }
+    }
+    __device__ __forceinline__ ProdSide(const ProdArgs& a, int o0, int k0) {
+        const int size = PSIDE ? a.N : a.M;
+        row = PSIDE ? a.prow : a.qrow;
+        const char* p = PSIDE ? a.p : a.q;
+        base = KCON ? p + (int64_t)o0 * row + (int64_t)k0 * S::ES : p + (int64_t)k0 * row + (int64_t)o0 * S::ES;
+        step = KCON ? 128 : S::KC * row;
+        left = size - o0;
+#pragma unroll
+        for (int j = 0; j < I; ++j) {
+            int r, u;
+            place((int)threadIdx.x + j * T, r, u);
+            if constexpr (KCON) r = min(r, left - 1);
+            else u = min(u, left / E - 1);
+            off[j] = (uint32_t)(r * row) + 16 * u;
+        }
+    }
+    // Chunk c of the split into the stage at `lds` (this wave's first block); v: k of it that exist.
+    __device__ __forceinline__ void issue(int c, uint32_t lds, int v) const {
+        const char* at = uniform_ptr(base + c * step);
+        if (v >= S::KC) {
+#pragma unroll
+            for (int j = 0; j < I; ++j) lds_load16s(off[j], at, lds + 16 * T * j);
+        } else {  // what lies past the last k is another valid place's, and cleared after it has landed
+#pragma unroll
+            for (int j = 0; j < I; ++j) {
+                int r, u;
+                place((int)threadIdx.x + j * T, r, u);
+                if constexpr (KCON) r = min(r, left - 1), u = min(u, v / E - 1);
+                else r = min(r, v - 1), u = min(u, left / E - 1);
+                lds_load16s((uint32_t)(r * row) + 16 * u, at, lds + 16 * T * j);
+            }
+        }
+    }
+    __device__ __forceinline__ void clear(unsigned char* tile, int v) const {
+#pragma unroll 1
+        for (int i = threadIdx.x; i < BYTES / 16; i += T) {
+            int r, u;
+            place(i, r, u);
+            if (KCON ? u * E >= v : r >= v) *reinterpret_cast<uint4*>(tile + 16 * i) = make_uint4(0, 0, 0, 0);
+        }
+    }
+    // 16 rows (of the matrix instruction) from `o` on, 32 k from ks on.  odd: block of an interleaved pair at o.
+    static __device__ __forceinline__ Frag8<ST> frag(const unsigned char* t, int o, int odd, int ks, int g, int c16) {
+        Frag8<ST> f;
+        constexpr bool PAIR = PSIDE && sizeof(ST) == 2;
+        if constexpr (KCON) {
+            const int r = o + (PAIR ? 8 * (c16 >> 2) + (c16 & 3) + 4 * odd : c16), s = prod_swz<ST, PSIDE>(r);
+            if constexpr (sizeof(ST) == 2) {
+                f.v = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(t + r * 128 + (((ks >> 3) + g) ^ s) * 16));
+            } else {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const float4 x = *reinterpret_cast<const float4*>(t + r * 128 + ((2 * g + h) ^ s) * 16);
+                    f.v[4 * h] = x.x, f.v[4 * h + 1] = x.y, f.v[4 * h + 2] = x.z, f.v[4 * h + 3] = x.w;
+                }
+            }
+        } else if constexpr (sizeof(ST) == 2) {
+            const int col = o + (PAIR ? 8 : 4) * (c16 & 3) + 4 * odd, k = ks + 8 * g + (c16 >> 2);
+            const int u = col >> 3, half = 8 * ((col >> 2) & 1);
+            const u32x2 lo = lds_tr16(t + (k * U + prod_kswz<ST, U>(k, u)) * 16 + half);
+            const u32x2 hi = lds_tr16(t + ((k + 4) * U + prod_kswz<ST, U>(k + 4, u)) * 16 + half);
+            f.v = __builtin_bit_cast(bf16x8, u32x4{lo.x, lo.y, hi.x, hi.y});
+        } else {
+            const int col = o + c16;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int k = ks + 8 * g + e;
+                f.v[e] = *reinterpret_cast<const float*>(t + (k * U + prod_kswz<ST, U>(k, col >> 2)) * 16 + 4 * (col & 3));
+            }
+        }
+        return f;
+    }
+};
+
+template <class S>
+__global__ __launch_bounds__((S::T)) void prod_kernel(const ProdArgs a) {
+    using ST = typename S::ST;
+    constexpr int STG = S::STG, KS = S::KS, L = S::L, E = S::E;
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, c16 = lane & 15;
+    const int wn = wave % S::WN, wm = wave / S::WN;
+    // Workgroups of an XCD take tiles of 8 row blocks side by side, so that they share operands in its L2.
+    int id = xcd_logical_id(blockIdx.x, gridDim.x);
+    const int tiles = a.tm * a.tn, split = id / tiles;
+    id -= split * tiles;
+    const int band = id / (8 * a.tn), bm = min(8, a.tm - 8 * band), in = id - band * 8 * a.tn;
+    const int m0 = (8 * band + in % bm) * S::MT, n0 = (in / bm) * S::NT;
+    const int k0 = split * a.kper, klen = min(a.kper, a.K - k0), chunks = (klen + S::KC - 1) / S::KC;
+
+    const ProdSide<S, true> P(a, n0, k0);
+    const ProdSide<S, false> Q(a, m0, k0);
+    const uint32_t lds = __builtin_amdgcn_readfirstlane(lds_addr(smem) + 1024 * wave);
+    auto issue = [&](int c, int buf) {
+        const int v = klen - c * S::KC;
+        P.issue(c, lds + buf * S::STAGE, v);
+        Q.issue(c, lds + buf * S::STAGE + S::P_BYTES, v);
+    };
+    // chunk c has landed in buffer buf; k past the end are cleared
+    auto clear_tail = [&](int c, int buf) {
+        const int v = klen - c * S::KC;
+        if (v >= S::KC || v <= 0) return;
+        P.clear(smem + buf * S::STAGE, v);
+        Q.clear(smem + buf * S::STAGE + S::P_BYTES, v);
+        __syncthreads();
+    };
+
+    f32x4 acc[S::FN][S::FM];
+#pragma unroll
+    for (int j = 0; j < S::FN; ++j)
+#pragma unroll
+        for (int i = 0; i < S::FM; ++i) acc[j][i] = zero4();
+    struct Frags {
+        Frag8<ST> p[S::FN], q[S::FM];
+    };
+    auto load_frags = [&](Frags& f, int buf, int ks) {
+        const unsigned char *tp = smem + buf * S::STAGE, *tq = tp + S::P_BYTES;
+#pragma unroll
+        for (int j = 0; j < S::FN; ++j) {
+            const int o = wn * S::WTN + (sizeof(ST) == 2 ? 32 * (j >> 1) : 16 * j);
+            f.p[j] = ProdSide<S, true>::frag(tp, o, sizeof(ST) == 2 ? j & 1 : 0, ks, g, c16);
+        }
+#pragma unroll
+        for (int i = 0; i < S::FM; ++i) f.q[i] = ProdSide<S, false>::frag(tq, wm * S::WTM + 16 * i, 0, ks, g, c16);
+    };
+    constexpr int READS = (S::PKC ? (S::ES == 2 ? 1 : 2) : (S::ES == 2 ? 2 : 8)) * S::FN +
+                          (S::QKC ? (S::ES == 2 ? 1 : 2) : (S::ES == 2 ? 2 : 8)) * S::FM;
+    constexpr int MFMAS = S::FN * S::FM * (S::ES == 2 ? 1 : 8);
+
+    Frags fr[2];
+#pragma unroll
+    for (int s = 0; s < STG; ++s)
+        if (s < chunks) issue(s, s);
+    if (chunks >= STG) wait_vmcnt<(STG - 1) * L>();
+    else wait_vmcnt<0>();
+    __syncthreads();
+    clear_tail(0, 0);
+    __builtin_amdgcn_sched_barrier(0);
+    load_frags(fr[0], 0, 0);
+    constexpr int UNROLL = STG * KS % 2 == 0 ? STG : 2 * STG;
+    for (int c0 = 0;; c0 += UNROLL) {
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u) {
+            const int c = c0 + u;
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                const int cur = (u * KS + ks) & 1;
+                if (ks + 1 < KS) {
+                    load_frags(fr[cur ^ 1], u % STG, 32 * (ks + 1));
+                } else {
+                    // chunk c + 1 has landed and every wave has read chunk c: its buffer takes chunk c + STG.  The
+                    // fragments read past the last chunk are never used.
+                    if (c + STG <= chunks) wait_vmcnt<(STG - 2) * L>();
+                    else wait_vmcnt<0>();
+                    __syncthreads();
+                    if (c + STG < chunks) issue(c + STG, u % STG);
+                    clear_tail(c + 1, (u + 1) % STG);
+                    __builtin_amdgcn_sched_barrier(0);
+                    load_frags(fr[cur ^ 1], (u + 1) % STG, 0);
+                }
+#pragma unroll
+                for (int j = 0; j < S::FN; ++j)
+#pragma unroll
+                    for (int i = 0; i < S::FM; ++i) mma8(acc[j][i], fr[cur].p[j], fr[cur].q[i]);
+                sched_mix<MFMAS, READS>();
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            if (c + 1 == chunks) goto multiplied;
+        }
+    }
+multiplied:
+    mfma_drain();
+#pragma unroll
+    for (int i = 0; i < S::FM; ++i) {
+        const int m = m0 + wm * S::WTM + 16 * i + c16;
+        if (m >= a.M) continue;
+#pragma unroll
+        for (int j = 0; j < S::FN; j += E / 4) {
+            const int n = n0 + wn * S::WTN + 16 * j + E * g;
+            if (n >= a.N) continue;
+            float x[E];
+#pragma unroll
+            for (int e = 0; e < E; ++e) x[e] = acc[j + e / 4][i][e % 4];
+            if (a.splits > 1) {
+                float* to = a.part + ((int64_t)split * a.M + m) * a.N + n;
+#pragma unroll
+                for (int e = 0; e < E; e += 4) *reinterpret_cast<float4*>(to + e) = make_float4(x[e], x[e + 1], x[e + 2], x[e + 3]);
+            } else {
+                finish_unit<ST>(a, m, n, x);
+            }
+        }
+    }
+}
+
+// Parts of K added in order, and the epilogue.
+template <typename ST>
+__global__ __launch_bounds__(256) void prod_join_kernel(const ProdArgs a) {
+    constexpr int E = Unit<ST>::E;
+    const int64_t units = (int64_t)a.M * a.N / E;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < units; i += (int64_t)gridDim.x * 256) {
+        const int m = (int)(i * E / a.N), n = (int)(i * E - (int64_t)m * a.N);
+        float x[E];
+#pragma unroll
+        for (int e = 0; e < E; ++e) x[e] = 0.f;
+        const float* p = a.part + i * E;
+#pragma unroll 4
+        for (int s = 0; s < a.splits; ++s) {
+#pragma unroll
+            for (int e = 0; e < E; e += 4) {
+                const float4 v = *reinterpret_cast<const float4*>(p + (int64_t)s * a.M * a.N + e);
+                x[e] += v.x, x[e + 1] += v.y, x[e + 2] += v.z, x[e + 3] += v.w;
+            }
+        }
+        finish_unit<ST>(a, m, n, x);
+    }
+}
+
+template <class S>
+int launch_prod(const ProdArgs& a, hipStream_t stream) {
+    if (allow_lds((const void*)prod_kernel<S>, S::LDS)) return -1;
+    const int64_t blocks = (int64_t)a.tm * a.tn * a.splits;
+    hipLaunchKernelGGL((prod_kernel<S>), dim3((unsigned)blocks), dim3(S::T), S::LDS, stream, a);
+    if (hipGetLastError() != hipSuccess) return -1;
+    if (a.splits > 1) {
+        const int64_t units = (int64_t)a.M * a.N / S::E, need = (units + 255) / 256;
+        hipLaunchKernelGGL((prod_join_kernel<typename S::ST>), dim3((unsigned)(need < 4096 ? need : 4096)), dim3(256), 0,
+                           stream, a);
+        if (hipGetLastError() != hipSuccess) return -1;
+    }
+    return 0;
+}
+
+}  // namespace mosa

@@ -26,7 +26,11 @@ SYMBOLS = ("mosa_workspace_size", "mosa_saved_offsets", "mosa_forward", "mosa_ba
            # operators of the dense heads (ops.py)
            "mosa_norm_scratch_size", "mosa_qk_norm_rope", "mosa_qk_norm_rope_backward", "mosa_attn_scratch_size",
            "mosa_window_attention", "mosa_window_attention_backward", "mosa_cache4_size", "mosa_cache4_append",
-           "mosa_cache4_read", "mosa_cache4_attention")
+           "mosa_cache4_read", "mosa_cache4_attention",
+           # operators around a block (ops.py)
+           "mosa_residual_scratch_size", "mosa_residual_norm", "mosa_residual_norm_backward",
+           "mosa_linear_scratch_size", "mosa_linear", "mosa_linear_backward", "mosa_logprob_scratch_size",
+           "mosa_token_logprobs", "mosa_token_logprobs_backward")
 NOALLOC_SCRATCH_MAX = 64 << 20  # MOSA_NOALLOC_SCRATCH_MAX
 MAX_STAGES = 32
 

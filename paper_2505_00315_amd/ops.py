@@ -1,6 +1,8 @@
 """Operators of the dense heads: norm and rotation of query and key rows,
 attention with a sliding window and first tokens that stay visible, and a paged
-cache that holds keys and values in 4 bits.
+cache that holds keys and values in 4 bits.  Operators around a block: the residual
+stream with its norms and gate, products with weight matrices, log probabilities
+of tokens.
 
 Python binding of the functions that ``include/mosa.h`` declares for them:
 argument marshalling and checks only, every step runs in the HIP kernels.
@@ -8,7 +10,8 @@ argument marshalling and checks only, every step runs in the HIP kernels.
 Rows are tensors of shape [batch, heads, length, d_head] in any memory order
 whose last axis is contiguous and whose other strides are multiples of 16
 bytes: ``x.transpose(1, 2)`` of a [batch, length, heads, d_head] tensor, a slice
-of packed rows, ``mosa.saved_view(shape, saved, "Kd")``.  Work goes to the
+of packed rows, ``mosa.saved_view(shape, saved, "Kd")``.  The stream is [batch,
+seq_len, d_model] likewise, and a matrix has two axes.  Work goes to the
 current stream of the tensors' device (or ``stream``), whichever device is
 current.
 """
@@ -21,6 +24,9 @@ import torch
 from . import mosa
 
 PAIRS = {"adjacent": 0, "halves": 1}  # MOSA_PAIRS_*
+GATES = {"none": 0, "vector": 1, "sequence": 2, "token": 3}  # MOSA_GATE_*
+ACTS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}  # MOSA_ACT_*
+W_ORDERS = {"in_out": 0, "out_in": 1}  # MOSA_W_*
 
 
 class Rows(ctypes.Structure):
@@ -43,6 +49,23 @@ class CacheShape(ctypes.Structure):
                                               "max_pages")]
 
 
+class Matrix(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("row_stride", ctypes.c_int64)]
+
+
+class ResidualShape(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("batch", "seq_len", "d_model", "dtype", "post_norm", "pre_norm", "gate")] + [
+        (n, ctypes.c_float) for n in ("residual_scale", "branch_scale", "eps")]
+
+
+class LinearShape(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("rows", "d_in", "d_out", "dtype", "act", "w_order")]
+
+
+class LogprobShape(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("rows", "vocab", "dtype", "top")] + [("scale", ctypes.c_float)]
+
+
 _fn = None
 
 
@@ -53,6 +76,7 @@ def _lib():
         L = mosa.lib()
         P, V, Z = ctypes.POINTER, ctypes.c_void_p, ctypes.c_size_t
         norm, attn, cache, rows = P(NormShape), P(AttnShape), P(CacheShape), P(Rows)
+        res, lin, lp, mat = P(ResidualShape), P(LinearShape), P(LogprobShape), P(Matrix)
         table = {
             "mosa_norm_scratch_size": [norm, P(Z)],
             "mosa_qk_norm_rope": [norm, rows, rows, V, V, V, rows, rows, V],
@@ -64,6 +88,15 @@ def _lib():
             "mosa_cache4_append": [cache, V, V, V, V, ctypes.c_int, rows, rows, V],
             "mosa_cache4_read": [cache, V, V, V, V, ctypes.c_int, rows, rows, V],
             "mosa_cache4_attention": [attn, cache, rows, V, V, V, V, rows, V, V, Z, V],
+            "mosa_residual_scratch_size": [res, P(Z)],
+            "mosa_residual_norm": [res, rows, rows, V, rows, V, rows, rows, V],
+            "mosa_residual_norm_backward": [res, rows, rows, V, rows, V, rows, rows, rows, rows, V, rows, V, V, Z, V],
+            "mosa_linear_scratch_size": [lin, P(Z), P(Z)],
+            "mosa_linear": [lin, mat, mat, V, mat, mat, mat, V, Z, V],
+            "mosa_linear_backward": [lin, mat, mat, mat, mat, mat, mat, V, V, Z, V],
+            "mosa_logprob_scratch_size": [lp, P(Z)],
+            "mosa_token_logprobs": [lp, mat, V, V, V, V, V, V, V, V, Z, V],
+            "mosa_token_logprobs_backward": [lp, mat, V, V, V, V, V, V, mat, V],
         }
         for name, args in table.items():
             f = getattr(L, name)
@@ -98,6 +131,24 @@ def make_cache_shape(batch, kv_heads, d_head, pages, page_size, max_pages, dtype
     return CacheShape(batch, kv_heads, d_head, _DTYPE[dtype], pages, page_size, max_pages)
 
 
+def make_residual_shape(batch, seq_len, d_model, dtype="bf16", post_norm=False, pre_norm=True, gate="none",
+                        residual_scale=1.0, branch_scale=1.0, eps=1e-6):
+    """``gate``: "none", or how it is shared: "vector" [d_model], "sequence" [batch, d_model], "token" [batch, seq_len,
+    d_model]."""
+    return ResidualShape(batch, seq_len, d_model, _DTYPE[dtype], int(bool(post_norm)), int(bool(pre_norm)), GATES[gate],
+                         residual_scale, branch_scale, eps)
+
+
+def make_linear_shape(rows, d_in, d_out, dtype="bf16", act="none", w_order="in_out"):
+    """``w_order``: w is [d_in, d_out] ("in_out", as the layer's weights) or [d_out, d_in] ("out_in")."""
+    return LinearShape(rows, d_in, d_out, _DTYPE[dtype], ACTS[act], W_ORDERS[w_order])
+
+
+def make_logprob_shape(rows, vocab, dtype="bf16", top=0, scale=1.0):
+    """``top``: alternatives that token_logprobs lists; ``scale``: of the logits (1 / temperature)."""
+    return LogprobShape(rows, vocab, _DTYPE[dtype], top, scale)
+
+
 # ---------------------------------------------------------------------------
 # checks
 # ---------------------------------------------------------------------------
@@ -113,6 +164,22 @@ def _rows(t, what, shape, dtype, device):
     if c != 1:
         raise ValueError(f"{what}: the last axis is not contiguous")
     return Rows(t.data_ptr(), b, h, r)
+
+
+def _matrix(t, what, shape, dtype, device):
+    """The Matrix of a tensor that has to be [rows, columns] of this type on this device (None: NULL)."""
+    if t is None:
+        return None
+    if t.dtype != dtype:
+        raise TypeError(f"{what}: dtype {t.dtype}, expected {dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{what}: shape {tuple(t.shape)}, expected {shape}")
+    if t.device != device:
+        raise ValueError(f"{what}: on {t.device}, expected {device}")
+    r, c = t.stride()
+    if c != 1 and shape[1] != 1:
+        raise ValueError(f"{what}: the last axis is not contiguous")
+    return Matrix(t.data_ptr(), r)
 
 
 def _device(t, what):
@@ -359,3 +426,192 @@ def cache4_attention(shape, cache_shape, q, cache, page_table, kv_lens, q_lens=N
           _array(kv_lens, "kv_lens", torch.int32, shape.batch, dev, True), _rows(out, "out", qs, st, dev),
           _array(lse, "lse", torch.float32, qs[0] * qs[1] * qs[2], dev), at, size)
     return out
+
+
+# ---------------------------------------------------------------------------
+# the residual stream
+# ---------------------------------------------------------------------------
+def residual_scratch_size(shape):
+    n = ctypes.c_size_t()
+    mosa._check(_lib().mosa_residual_scratch_size(shape, n), "mosa_residual_scratch_size")
+    return n.value
+
+
+def alloc_residual_scratch(shape, device="cuda"):
+    return torch.empty(max(residual_scratch_size(shape), 256), dtype=torch.uint8, device=device)
+
+
+def _stream_rows(t, what, shape, device, sizes=None):
+    """The Rows of a tensor [batch, seq_len, d_model] (None: NULL)."""
+    if t is None:
+        return None
+    want = (shape.batch, shape.seq_len, shape.d_model) if sizes is None else sizes
+    if t.shape != want:
+        raise ValueError(f"{what}: shape {tuple(t.shape)}, expected {want}")
+    # the axes that a shared gate does not have, and the heads' axis
+    t = t.view((1,) * (3 - len(want)) + tuple(want)) if len(want) == 1 else t.unsqueeze(1) if len(want) == 2 else t
+    return _rows(t.unsqueeze(1), what, (t.shape[0], 1, t.shape[1], t.shape[2]), _TORCH[shape.dtype], device)
+
+
+def _gate_rows(t, what, shape, device):
+    B, T, d = shape.batch, shape.seq_len, shape.d_model
+    if t is not None and shape.gate == 0:
+        raise ValueError(f"{what}: the shape has no gate")
+    return _stream_rows(t, what, shape, device, {1: (d,), 2: (B, d), 3: (B, T, d)}.get(shape.gate))
+
+
+def residual_norm(shape, x, y, w_post=None, gate=None, w_pre=None, h_out=None, n_out=None, stream=None):
+    """The stream behind a block and what the next block reads, from the stream x
+    and the block's output y (both [B, T, d]):
+        h = residual_scale x + branch_scale gate u,  u = w_post y / rms(y) (post_norm) or y
+        n = w_pre h / rms(h)  (pre_norm)
+    w_post, w_pre [d] (None: ones).  y None: h is x, and only n is computed.
+    h_out may be x or y, and n_out y.  Returns (h, n), n None without pre_norm."""
+    dev = _device(x, "x")
+    st, d = _TORCH[shape.dtype], shape.d_model
+    h_out = _like(x, h_out, stream) if y is not None else h_out
+    n_out = _like(x, n_out, stream) if shape.pre_norm else n_out
+    _call("mosa_residual_norm", dev, stream, shape, _stream_rows(x, "x", shape, dev), _stream_rows(y, "y", shape, dev),
+          _array(w_post, "w_post", st, d, dev), _gate_rows(gate, "gate", shape, dev), _array(w_pre, "w_pre", st, d, dev),
+          _stream_rows(h_out, "h_out", shape, dev), _stream_rows(n_out, "n_out", shape, dev))
+    return (x if y is None else h_out), n_out
+
+
+def residual_norm_backward(shape, x, y, w_post=None, gate=None, w_pre=None, dh=None, dn=None, dx=None, dy=None,
+                           dw_post=None, dgate=None, dw_pre=None, scratch=None, stream=None):
+    """Gradients of residual_norm: x, y as they went in, dh and dn the outputs'
+    gradients (dh None: 0).  dw_post, dgate and dw_pre are written where given, or
+    made where the weight or the gate is.  dx may be dh or dn, and dy the other of
+    them.  Returns (dx, dy, dw_post, dgate, dw_pre)."""
+    dev = _device(x, "x")
+    st, d = _TORCH[shape.dtype], shape.d_model
+    dx = _like(x, dx, stream)
+    dy = dy if y is None else _like(y, dy, stream)
+    dw_post = dw_post if w_post is None else _like(w_post, dw_post, stream)
+    dw_pre = dw_pre if w_pre is None else _like(w_pre, dw_pre, stream)
+    if gate is not None and dgate is None:  # (a broadcast gate's gradient is one of its whole shape)
+        dgate = _new(torch.empty, stream, tuple(gate.shape), dtype=gate.dtype, device=gate.device)
+    sums = dw_post is not None or dw_pre is not None or (dgate is not None and shape.gate != GATES["token"])
+    buf, at, size = _scratch(scratch, lambda: residual_scratch_size(shape) if sums else 0, dev, stream)
+    _call("mosa_residual_norm_backward", dev, stream, shape, _stream_rows(x, "x", shape, dev),
+          _stream_rows(y, "y", shape, dev), _array(w_post, "w_post", st, d, dev), _gate_rows(gate, "gate", shape, dev),
+          _array(w_pre, "w_pre", st, d, dev), _stream_rows(dh, "dh", shape, dev), _stream_rows(dn, "dn", shape, dev),
+          _stream_rows(dx, "dx", shape, dev), _stream_rows(dy, "dy", shape, dev),
+          _array(dw_post, "dw_post", st, d, dev), _gate_rows(dgate, "dgate", shape, dev),
+          _array(dw_pre, "dw_pre", st, d, dev), at, size)
+    return dx, dy, dw_post, dgate, dw_pre
+
+
+# ---------------------------------------------------------------------------
+# products
+# ---------------------------------------------------------------------------
+def linear_scratch_size(shape):
+    """(forward, backward) bytes."""
+    f, b = ctypes.c_size_t(), ctypes.c_size_t()
+    mosa._check(_lib().mosa_linear_scratch_size(shape, f, b), "mosa_linear_scratch_size")
+    return f.value, b.value
+
+
+def alloc_linear_scratch(shape, device="cuda"):
+    """One buffer for the forward and the backward of a shape."""
+    return torch.empty(max(*linear_scratch_size(shape), 256), dtype=torch.uint8, device=device)
+
+
+def _linear_io(shape):
+    w = (shape.d_in, shape.d_out) if shape.w_order == 0 else (shape.d_out, shape.d_in)
+    return _TORCH[shape.dtype], (shape.rows, shape.d_in), w, (shape.rows, shape.d_out)
+
+
+def linear(shape, x, w, bias=None, residual=None, y=None, z=None, scratch=None, stream=None):
+    """act(x w + bias) + residual of x [rows, d_in], w [d_in, d_out] or [d_out,
+    d_in] (w_order), bias [d_out], residual [rows, d_out].  z: x w + bias is written
+    too where it is given (linear_backward reads it).  y may be residual.
+    Returns y."""
+    st, xs, ws, ys = _linear_io(shape)
+    dev = _device(x, "x")
+    if y is None:
+        y = _new(torch.empty, stream, ys, dtype=st, device=dev)
+    buf, at, size = _scratch(scratch, lambda: linear_scratch_size(shape)[0], dev, stream)
+    _call("mosa_linear", dev, stream, shape, _matrix(x, "x", xs, st, dev), _matrix(w, "w", ws, st, dev),
+          _array(bias, "bias", st, shape.d_out, dev), _matrix(residual, "residual", ys, st, dev),
+          _matrix(y, "y", ys, st, dev), _matrix(z, "z", ys, st, dev), at, size)
+    return y
+
+
+def linear_backward(shape, x, w, dy, z=None, grads="xw", dx=None, dw=None, db=None, scratch=None, stream=None):
+    """Gradients of linear from dy, that of y, and z of the forward (None without
+    an activation).  grads: those that are wanted, of "x", "w" and "b"; tensors are
+    made for them where none is given.  The residual's gradient is dy.  Returns (dx,
+    dw, db), None in the place of those not wanted."""
+    st, xs, ws, ys = _linear_io(shape)
+    dev = _device(x, "x")
+    if not set(grads) <= set("xwb"):
+        raise ValueError(f"grads: {grads!r}, expected letters of 'xwb'")
+
+    def wanted(letter, given, sizes):
+        if letter not in grads:
+            return None
+        return _new(torch.empty, stream, sizes, dtype=st, device=dev) if given is None else given
+    dx, dw, db = wanted("x", dx, xs), wanted("w", dw, ws), wanted("b", db, (shape.d_out,))
+    buf, at, size = _scratch(scratch, lambda: linear_scratch_size(shape)[1], dev, stream)
+    _call("mosa_linear_backward", dev, stream, shape, _matrix(x, "x", xs, st, dev), _matrix(w, "w", ws, st, dev),
+          _matrix(z, "z", ys, st, dev), _matrix(dy, "dy", ys, st, dev), _matrix(dx, "dx", xs, st, dev),
+          _matrix(dw, "dw", ws, st, dev), _array(db, "db", st, shape.d_out, dev), at, size)
+    return dx, dw, db
+
+
+# ---------------------------------------------------------------------------
+# log probabilities
+# ---------------------------------------------------------------------------
+def logprob_scratch_size(shape):
+    n = ctypes.c_size_t()
+    mosa._check(_lib().mosa_logprob_scratch_size(shape, n), "mosa_logprob_scratch_size")
+    return n.value
+
+
+def alloc_logprob_scratch(shape, device="cuda"):
+    return torch.empty(max(logprob_scratch_size(shape), 256), dtype=torch.uint8, device=device)
+
+
+def token_logprobs(shape, logits, targets=None, logp=None, lse=None, stats=None, entropy=None, top_logp=None,
+                   top_index=None, scratch=None, stream=None):
+    """Log probabilities of the targets (int32 [rows]; a value outside 0 .. vocab -
+    1 is no target: 0) among the rows of logits [rows, vocab], the logits times
+    scale.  Returns (logp, lse, top_logp, top_index): logp None without targets, the
+    alternatives [rows, top], most probable first, None where the shape has none.
+    entropy [rows] and stats [rows, 2] (token_logprobs_backward reads them) are
+    written where they are given."""
+    dev = _device(logits, "logits")
+    R, top = shape.rows, shape.top
+
+    def made(t, sizes, dtype=torch.float32):
+        return _new(torch.empty, stream, sizes, dtype=dtype, device=dev) if t is None else t
+    logp = made(logp, (R,)) if targets is not None else logp
+    lse = made(lse, (R,))
+    if top:
+        top_logp, top_index = made(top_logp, (R, top)), made(top_index, (R, top), torch.int32)
+    buf, at, size = _scratch(scratch, lambda: logprob_scratch_size(shape), dev, stream)
+    f32, i32 = torch.float32, torch.int32
+    _call("mosa_token_logprobs", dev, stream, shape,
+          _matrix(logits, "logits", (R, shape.vocab), _TORCH[shape.dtype], dev), _array(targets, "targets", i32, R, dev),
+          _array(logp, "logp", f32, R, dev), _array(lse, "lse", f32, R, dev), _array(stats, "stats", f32, 2 * R, dev),
+          _array(entropy, "entropy", f32, R, dev), _array(top_logp, "top_logp", f32, R * top, dev),
+          _array(top_index, "top_index", i32, R * top, dev), at, size)
+    return logp, lse, top_logp, top_index
+
+
+def token_logprobs_backward(shape, logits, targets, stats, entropy=None, d_logp=None, d_lse=None, d_entropy=None,
+                            d_logits=None, stream=None):
+    """Gradient of the logits from those of logp, lse and entropy (fp32 [rows],
+    None: 0); stats and entropy are the forward's.  d_logits may be logits.
+    Returns d_logits."""
+    dev = _device(logits, "logits")
+    R, sizes, st, f32 = shape.rows, (shape.rows, shape.vocab), _TORCH[shape.dtype], torch.float32
+    if d_logits is None:
+        d_logits = _new(torch.empty, stream, sizes, dtype=st, device=dev)
+    _call("mosa_token_logprobs_backward", dev, stream, shape, _matrix(logits, "logits", sizes, st, dev),
+          _array(targets, "targets", torch.int32, R, dev), _array(stats, "stats", f32, 2 * R, dev, required=True),
+          _array(entropy, "entropy", f32, R, dev), _array(d_logp, "d_logp", f32, R, dev),
+          _array(d_lse, "d_lse", f32, R, dev), _array(d_entropy, "d_entropy", f32, R, dev),
+          _matrix(d_logits, "d_logits", sizes, st, dev))
+    return d_logits

@@ -1,0 +1,253 @@
+"""Operators around a block: bad arguments are refused before any device work (no GPU needed)."""
+import pytest
+import torch
+
+from paper_2505_00315_amd import mosa, ops
+
+INV, UNS, WS = mosa.MOSA_ERR_INVALID_ARG, mosa.MOSA_ERR_UNSUPPORTED, mosa.MOSA_ERR_WORKSPACE
+A = 0x100000  # an aligned address that is never read
+
+
+def status(f, *args):
+    with pytest.raises(mosa.MosaError) as e:
+        mosa._check(getattr(ops._lib(), f)(*args), f)
+    return e.value.status
+
+
+def rows(**kw):
+    r = ops.Rows(A, 8 * 64, 0, 64)
+    for n, v in kw.items():
+        setattr(r, n, v)
+    return r
+
+
+def residual(kw=None, **change):
+    """Arguments of a call of mosa_residual_norm with post-norm, gate per token and pre-norm, with changes."""
+    s = ops.make_residual_shape(**{**dict(batch=2, seq_len=8, d_model=64, post_norm=True, gate="token"), **(kw or {})})
+    a = dict(x=rows(), y=rows(), w_post=A, gate=rows(), w_pre=A, h=rows(), n=rows())
+    a.update(change)
+    return ("mosa_residual_norm", s, *a.values(), None)
+
+
+def residual_back(kw=None, size=1 << 40, scratch=A, **change):
+    s = ops.make_residual_shape(**{**dict(batch=2, seq_len=8, d_model=64, post_norm=True, gate="token"), **(kw or {})})
+    a = dict(x=rows(), y=rows(), w_post=A, gate=rows(), w_pre=A, dh=rows(), dn=rows(), dx=rows(), dy=rows(), dw_post=A,
+             dgate=rows(), dw_pre=A)
+    a.update(change)
+    return ("mosa_residual_norm_backward", s, *a.values(), scratch, size, None)
+
+
+@pytest.mark.parametrize("kw,want", [
+    (dict(batch=0), INV), (dict(seq_len=0), INV), (dict(d_model=0), INV), (dict(d_model=68), UNS),
+    (dict(d_model=8200), UNS), (dict(eps=-1.0), INV), (dict(eps=float("nan")), INV), (dict(branch_scale=float("inf")), INV),
+    (dict(residual_scale=float("nan")), INV), (dict(batch=1 << 16, seq_len=1 << 15), UNS),
+])
+def test_residual_shapes(kw, want):
+    base = dict(batch=2, seq_len=8, d_model=64)
+    with pytest.raises(mosa.MosaError) as e:
+        ops.residual_scratch_size(ops.make_residual_shape(**{**base, **kw}))
+    assert e.value.status == want
+
+
+def test_residual_flags():
+    for field, v in (("post_norm", 2), ("pre_norm", -1), ("gate", 4), ("gate", -1), ("dtype", 2)):
+        s = ops.make_residual_shape(2, 8, 64)
+        setattr(s, field, v)
+        with pytest.raises(mosa.MosaError):
+            ops.residual_scratch_size(s)
+
+
+BAD_ROWS = [dict(data=None), dict(data=A + 8), dict(row_stride=-64), dict(row_stride=68), dict(batch_stride=1 << 41)]
+
+
+@pytest.mark.parametrize("bad", BAD_ROWS)
+def test_residual_rows(bad):
+    for at in ("x", "y", "gate", "h", "n"):
+        assert status(*residual(**{at: rows(**bad)})) == INV
+    for at in ("x", "y", "gate", "dh", "dn", "dx", "dy", "dgate"):
+        assert status(*residual_back(**{at: rows(**bad)})) == INV
+
+
+def test_residual_outputs_may_not_overlap():
+    for over in (dict(row_stride=0), dict(row_stride=32), dict(batch_stride=7 * 64)):
+        for at in ("h", "n"):
+            assert status(*residual(**{at: rows(**over)})) == INV
+        for at in ("dx", "dy", "dgate"):
+            assert status(*residual_back(**{at: rows(**over)})) == INV
+
+
+def test_residual_parts_that_do_not_go_together():
+    assert status(*residual(x=None)) == INV
+    assert status(*residual(gate=None)) == INV
+    assert status(*residual(dict(gate="none"))) == INV                      # a gate that the shape does not have
+    assert status(*residual(dict(pre_norm=False), w_pre=None)) == INV       # n_out without pre-norm
+    assert status(*residual(dict(pre_norm=False), n=None)) == INV           # w_pre without pre-norm
+    assert status(*residual(n=None)) == INV
+    assert status(*residual(h=None)) == INV
+    assert status(*residual(dict(post_norm=False))) == INV                  # w_post without post-norm
+    assert status(*residual(w_post=A + 4)) == INV and status(*residual(w_pre=A + 8)) == INV
+    first = dict(post_norm=False, gate="none")
+    assert status(*residual(first, y=None, w_post=None, gate=None)) == INV  # h_out without y
+    assert status(*residual(dict(gate="none"), y=None, w_post=None, gate=None, h=None)) == INV  # post-norm of nothing
+    assert status(*residual(dict(post_norm=False, gate="none", pre_norm=False), y=None, w_post=None, gate=None,
+                            w_pre=None, h=None, n=None)) == INV             # nothing to do
+
+
+def test_residual_backward_arguments():
+    assert status(*residual_back(dn=None)) == INV
+    assert status(*residual_back(dy=None)) == INV and status(*residual_back(dx=None)) == INV
+    no_pre = dict(pre_norm=False)
+    assert status(*residual_back(no_pre, w_pre=None, dn=None, dw_pre=None, dh=None)) == INV  # no gradient at all
+    assert status(*residual_back(no_pre, w_pre=None, dn=None)) == INV                        # dw_pre without pre-norm
+    assert status(*residual_back(dict(gate="none"), gate=None)) == INV                       # dgate without a gate
+    assert status(*residual_back(dw_post=A + 4)) == INV
+    assert status(*residual_back(scratch=None)) == INV and status(*residual_back(scratch=A + 16)) == INV
+    need = ops.residual_scratch_size(residual_back()[1])
+    assert status(*residual_back(size=need - 1)) == WS
+
+
+# ---------------------------------------------------------------------------
+def mat(stride=64, data=A):
+    return ops.Matrix(data, stride)
+
+
+def linear(kw=None, size=1 << 40, scratch=A, **change):
+    s = ops.make_linear_shape(**{**dict(rows=8, d_in=64, d_out=128), **(kw or {})})
+    a = dict(x=mat(64), w=mat(128), b=A, r=mat(128), y=mat(128), z=mat(128))
+    a.update(change)
+    return ("mosa_linear", s, *a.values(), scratch, size, None)
+
+
+def linear_back(kw=None, size=1 << 40, scratch=A, **change):
+    s = ops.make_linear_shape(**{**dict(rows=8, d_in=64, d_out=128, act="gelu"), **(kw or {})})
+    a = dict(x=mat(64), w=mat(128), z=mat(128), dy=mat(128), dx=mat(64), dw=mat(128), db=A)
+    a.update(change)
+    return ("mosa_linear_backward", s, *a.values(), scratch, size, None)
+
+
+@pytest.mark.parametrize("kw,want", [
+    (dict(rows=0), INV), (dict(d_in=0), INV), (dict(d_out=-8), INV), (dict(d_in=60), UNS), (dict(d_out=12), UNS),
+    (dict(d_in=(1 << 20) + 8), UNS), (dict(d_out=(1 << 20) + 8), UNS), (dict(rows=(1 << 24) + 1), UNS),
+])
+def test_linear_shapes(kw, want):
+    with pytest.raises(mosa.MosaError) as e:
+        ops.linear_scratch_size(ops.make_linear_shape(**{**dict(rows=4, d_in=64, d_out=64), **kw}))
+    assert e.value.status == want
+
+
+def test_linear_flags():
+    for field, v in (("act", 4), ("act", -1), ("w_order", 2), ("dtype", 5)):
+        s = ops.make_linear_shape(4, 64, 64)
+        setattr(s, field, v)
+        with pytest.raises(mosa.MosaError):
+            ops.linear_scratch_size(s)
+
+
+def test_linear_matrices():
+    for at in ("x", "w", "r", "y", "z"):
+        assert status(*linear(**{at: mat(data=A + 8)})) == INV
+        assert status(*linear(**{at: mat(-64)})) == INV and status(*linear(**{at: mat(132)})) == INV
+        assert status(*linear(**{at: mat(1 << 22)})) == UNS
+    for at in ("x", "w", "y"):
+        assert status(*linear(**{at: None})) == INV
+    for at in ("y", "z"):  # outputs that overlap themselves
+        assert status(*linear(**{at: mat(0)})) == INV and status(*linear(**{at: mat(120)})) == INV
+    assert status(*linear(b=A + 2)) == INV
+    for at in ("x", "w", "z", "dy", "dx", "dw"):
+        assert status(*linear_back(**{at: mat(data=A + 8)})) == INV
+    for at in ("dx", "dw"):
+        assert status(*linear_back(**{at: mat(0)})) == INV
+    for at in ("x", "w", "dy"):
+        assert status(*linear_back(**{at: None})) == INV
+    assert status(*linear_back(z=None)) == INV
+    assert status(*linear_back(dict(act="none"))) == INV  # z without an activation
+    assert status(*linear_back(db=A + 4)) == INV
+
+
+def test_linear_scratch():
+    s = dict(rows=4, d_in=8192, d_out=64)
+    need = ops.linear_scratch_size(ops.make_linear_shape(**s))[0]
+    assert need > 0
+    assert status(*linear(s, size=need - 1, x=mat(8192))) == WS
+    assert status(*linear(s, scratch=None, x=mat(8192))) == INV
+    need = ops.linear_scratch_size(linear_back()[1])[1]
+    assert need > 0 and status(*linear_back(size=need - 1)) == WS
+
+
+# ---------------------------------------------------------------------------
+def logprob(kw=None, size=1 << 40, scratch=A, **change):
+    s = ops.make_logprob_shape(**{**dict(rows=8, vocab=1000, top=4), **(kw or {})})
+    a = dict(logits=mat(1000), targets=A, logp=A, lse=A, stats=A, entropy=A, top_logp=A, top_index=A)
+    a.update(change)
+    return ("mosa_token_logprobs", s, *a.values(), scratch, size, None)
+
+
+def logprob_back(kw=None, **change):
+    s = ops.make_logprob_shape(**{**dict(rows=8, vocab=1000), **(kw or {})})
+    a = dict(logits=mat(1000), targets=A, stats=A, entropy=A, d_logp=A, d_lse=A, d_entropy=A, d_logits=mat(1000))
+    a.update(change)
+    return ("mosa_token_logprobs_backward", s, *a.values(), None)
+
+
+@pytest.mark.parametrize("kw,want", [
+    (dict(rows=0), INV), (dict(vocab=0), INV), (dict(top=-1), INV), (dict(top=1001), INV), (dict(top=33), UNS),
+    (dict(scale=0.0), INV), (dict(scale=-1.0), INV), (dict(scale=float("inf")), INV), (dict(scale=float("nan")), INV),
+    (dict(vocab=(1 << 30) + 1), UNS),
+])
+def test_logprob_shapes(kw, want):
+    with pytest.raises(mosa.MosaError) as e:
+        ops.logprob_scratch_size(ops.make_logprob_shape(**{**dict(rows=2, vocab=1000), **kw}))
+    assert e.value.status == want
+
+
+def test_logprob_arguments():
+    for f, at in ((logprob, "logits"), (logprob_back, "logits"), (logprob_back, "d_logits")):
+        for bad in (None, mat(data=A + 1), mat(999), mat(-1000), mat((1 << 40) + 1), mat(data=None)):
+            assert status(*f(**{at: bad})) == INV
+    assert status(*logprob_back(d_logits=mat(0))) == INV  # rows that overlap
+    assert status(*logprob(targets=None)) == INV
+    assert status(*logprob(top_index=None)) == INV and status(*logprob(top_logp=None)) == INV
+    assert status(*logprob(dict(top=0))) == INV
+    for at in ("targets", "logp", "lse", "stats", "entropy", "top_logp", "top_index"):
+        assert status(*logprob(**{at: A + 2})) == INV
+    for at in ("targets", "stats", "entropy", "d_logp", "d_lse", "d_entropy"):
+        assert status(*logprob_back(**{at: A + 2})) == INV
+    assert status(*logprob_back(stats=None)) == INV
+    assert status(*logprob_back(targets=None)) == INV and status(*logprob_back(entropy=None)) == INV
+
+
+def test_logprob_scratch():
+    s = dict(rows=1, vocab=200000)
+    need = ops.logprob_scratch_size(ops.make_logprob_shape(**s, top=4))
+    assert need > 0
+    assert status(*logprob(s, size=need - 1, logits=mat(200000))) == WS
+    assert status(*logprob(s, scratch=None, logits=mat(200000))) == INV
+
+
+# ---------------------------------------------------------------------------
+def test_binding_refuses_what_it_can_see():
+    cpu = torch.zeros(2, 8, 64, dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="GPU"):
+        ops.residual_norm(ops.make_residual_shape(2, 8, 64), cpu, cpu)
+    with pytest.raises(ValueError, match="GPU"):
+        ops.linear(ops.make_linear_shape(16, 64, 64), cpu.view(16, 64), cpu.view(16, 64)[:, :64])
+    with pytest.raises(ValueError, match="GPU"):
+        ops.token_logprobs(ops.make_logprob_shape(16, 64), cpu.view(16, 64))
+    with pytest.raises(KeyError):
+        ops.make_residual_shape(2, 8, 64, gate="head")
+    with pytest.raises(KeyError):
+        ops.make_linear_shape(2, 8, 64, act="tanh")
+    d = torch.device("cpu")
+    s = ops.make_residual_shape(2, 8, 64, gate="sequence")
+    with pytest.raises(ValueError, match="expected"):
+        ops._gate_rows(torch.zeros(2, 8, 64, dtype=torch.bfloat16), "gate", s, d)
+    with pytest.raises(TypeError):
+        ops._stream_rows(torch.zeros(2, 8, 64), "x", s, d)
+    with pytest.raises(ValueError, match="no gate"):
+        ops._gate_rows(torch.zeros(64, dtype=torch.bfloat16), "gate", ops.make_residual_shape(2, 8, 64), d)
+    r = ops._gate_rows(torch.zeros(2, 64, dtype=torch.bfloat16), "gate", s, d)
+    assert r.batch_stride == 64
+    with pytest.raises(ValueError, match="contiguous"):
+        ops._matrix(torch.zeros(64, 8).t(), "w", (8, 64), torch.float32, d)
+    with pytest.raises(TypeError):
+        ops._matrix(torch.zeros(8, 64), "w", (8, 64), torch.bfloat16, d)

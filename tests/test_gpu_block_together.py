@@ -1,0 +1,170 @@
+"""The operators around a block as a program runs them: the stream normed for the attention layer, the layer, the
+stream behind it, a feed-forward block, the head over a vocabulary, a loss, and all the way back."""
+import math
+
+import pytest
+import torch
+
+import workloads as wl
+from gpu_util import device_inputs, shape_of
+from paper_2505_00315_amd import mosa, ops
+
+pytestmark = pytest.mark.gpu
+B, T, D, F, V = 2, 48, 64, 136, 200
+
+
+class Model:
+    """One block with the attention layer (fixed sparse heads and a dense one, so that no selection changes) and a
+    feed-forward block, both with norms, gate and scale; logits by the embedding's rows."""
+
+    def __init__(self, dtype):
+        self.dtype, self.dt = dtype, torch.bfloat16 if dtype == "bf16" else torch.float32
+        w = wl.small(batch=B, seq_len=T, d_model=D, heads=2, d_head=32, k=12, dense_heads=1, dtype=dtype, fixed_stride=4)
+        inp = device_inputs(wl.make_inputs(w))
+        self.layer = shape_of(w)
+        self.p = {n: v for n, v in inp.items() if n in mosa.WEIGHT_NAMES and n != "Wr"}
+        g = torch.Generator().manual_seed(1)
+
+        def normal(*s, scale=1.0, one=0.0):
+            return (one + scale * torch.randn(s, generator=g)).to(self.dt).cuda()
+        self.p.update(emb=normal(V, D), n0=normal(D, scale=0.2, one=1.0), n1=normal(D, scale=0.2, one=1.0),
+                      n2=normal(D, scale=0.2, one=1.0), a1=normal(D, scale=0.2, one=1.0), g1=normal(D, scale=0.5),
+                      g2=normal(B, D, scale=0.5), w1=normal(D, F, scale=D ** -0.5), b1=normal(F, scale=0.3),
+                      w2=normal(F, D, scale=F ** -0.5), b2=normal(D, scale=0.3))
+        self.tokens = torch.randint(0, V, (B, T), generator=g).cuda()
+        self.targets = torch.randint(-1, V, (B * T,), generator=g, dtype=torch.int32).cuda()
+        mk = ops.make_residual_shape
+        self.s0 = mk(B, T, D, dtype)
+        self.s1 = mk(B, T, D, dtype, post_norm=True, gate="vector", branch_scale=0.7)
+        self.s2 = mk(B, T, D, dtype, gate="sequence", residual_scale=0.9)
+        self.l1 = ops.make_linear_shape(B * T, D, F, dtype, act="gelu")
+        self.l2 = ops.make_linear_shape(B * T, F, D, dtype)
+        self.l3 = ops.make_linear_shape(B * T, D, V, dtype, w_order="out_in")
+        self.lp = ops.make_logprob_shape(B * T, V, dtype, top=3)
+        self.d_logp = torch.linspace(-1, 1, B * T).cuda()
+        self.d_entropy = torch.full((B * T,), 0.25).cuda()
+
+    def forward(self, p):
+        k = {"x": p["emb"][self.tokens]}  # the stream
+        _, k["n"] = ops.residual_norm(self.s0, k["x"], None, w_pre=p["n0"])
+        k["y"], k["saved"], _ = mosa.forward(self.layer, k["n"], p)
+        k["h1"], k["n1"] = ops.residual_norm(self.s1, k["x"], k["y"], w_post=p["a1"], gate=p["g1"], w_pre=p["n1"])
+        k["z"] = torch.empty(B * T, F, dtype=self.dt, device="cuda")
+        k["f"] = ops.linear(self.l1, k["n1"].view(-1, D), p["w1"], bias=p["b1"], z=k["z"])
+        k["y2"] = ops.linear(self.l2, k["f"], p["w2"], bias=p["b2"]).view(B, T, D)
+        k["h2"], k["n2"] = ops.residual_norm(self.s2, k["h1"], k["y2"], gate=p["g2"], w_pre=p["n2"])
+        k["logits"] = ops.linear(self.l3, k["n2"].view(-1, D), p["emb"])
+        k["stats"], k["entropy"] = torch.empty(B * T, 2, device="cuda"), torch.empty(B * T, device="cuda")
+        k["logp"], k["lse"], k["top_logp"], k["top_index"] = ops.token_logprobs(self.lp, k["logits"], self.targets,
+                                                                                stats=k["stats"], entropy=k["entropy"])
+        return k
+
+    def loss(self, k):
+        return float((k["logp"].double() * self.d_logp.double()).sum() + (k["entropy"].double() * self.d_entropy.double()).sum())
+
+    def backward(self, p, k):
+        g = {}
+        dl = ops.token_logprobs_backward(self.lp, k["logits"], self.targets, k["stats"], entropy=k["entropy"],
+                                         d_logp=self.d_logp, d_entropy=self.d_entropy)
+        dn2, demb, _ = ops.linear_backward(self.l3, k["n2"].view(-1, D), p["emb"], dl)
+        dh1, dy2, _, g["g2"], g["n2"] = ops.residual_norm_backward(self.s2, k["h1"], k["y2"], gate=p["g2"], w_pre=p["n2"],
+                                                                   dn=dn2.view(B, T, D))
+        df, g["w2"], g["b2"] = ops.linear_backward(self.l2, k["f"], p["w2"], dy2.view(-1, D), grads="xwb")
+        dn1, g["w1"], g["b1"] = ops.linear_backward(self.l1, k["n1"].view(-1, D), p["w1"], df, z=k["z"], grads="xwb")
+        dx, dy, g["a1"], g["g1"], g["n1"] = ops.residual_norm_backward(self.s1, k["x"], k["y"], w_post=p["a1"], gate=p["g1"],
+                                                                       w_pre=p["n1"], dh=dh1, dn=dn1.view(B, T, D), dx=dh1)
+        lg = {"d" + n: torch.empty_like(v) for n, v in p.items() if n in mosa.WEIGHT_NAMES}
+        dn = mosa.backward(self.layer, k["n"], p, dy, k["saved"], lg)
+        g.update({n[1:]: v for n, v in lg.items()})
+        dx, _, _, _, g["n0"] = ops.residual_norm_backward(self.s0, k["x"], None, w_pre=p["n0"], dh=dx, dn=dn, dx=dx)
+        # the embedding's rows: as logits, and as the stream's beginning
+        rows = torch.zeros(V, D, dtype=torch.float64, device="cuda").index_add_(0, self.tokens.view(-1), dx.view(-1, D).double())
+        g["emb"] = demb.double() + rows
+        return g
+
+
+def test_gradients_are_those_of_the_loss():
+    """fp32: central differences of the whole program along a random direction of every parameter."""
+    m = Model("f32")
+    k = m.forward(m.p)
+    grads = m.backward(m.p, k)
+    gen = torch.Generator().manual_seed(2)
+    for name, v in m.p.items():
+        step = torch.randn(v.shape, generator=gen).cuda() * float(v.abs().mean())
+        eps = 2.0 ** -9
+        num = (m.loss(m.forward({**m.p, name: v + eps * step})) - m.loss(m.forward({**m.p, name: v - eps * step}))) / (2 * eps)
+        part = grads[name].double() * step.double()
+        # differences: eps^2 of third derivatives as large as the gradients, and the fp32 noise of a loss of 96 rows of
+        # size 5 (2^-24 of it a rounding, some dozens of them) over eps
+        noise = 96 * 5 * 30 * 2.0 ** -24 / eps
+        assert abs(num - float(part.sum())) < 0.01 * float(part.abs().sum()) + noise, name
+
+
+def test_bf16_is_near_fp32():
+    """The same program in bf16, from the same (rounded) parameters: 3 roundings of half a step per product and norm on
+    the way, a dozen of them."""
+    m, f = Model("bf16"), Model("f32")
+    f.p = {n: v.float() for n, v in m.p.items()}
+    a, b = m.forward(m.p), f.forward(f.p)
+    tol = 40 * 2.0 ** -8
+    for n in ("h1", "n1", "h2", "n2", "logits"):
+        err = float((a[n].double() - b[n].double()).norm() / b[n].double().norm())
+        assert err < tol, (n, err)
+    ga, gb = m.backward(m.p, a), f.backward(f.p, b)
+    for n in ga:
+        err = float((ga[n].double() - gb[n].double()).norm() / gb[n].double().norm())
+        assert err < 2 * tol, (n, err)
+
+
+def test_single_tokens_give_the_prompt():
+    """The feed-forward block, the stream and the head over one token at a time give what they give over all of them:
+    bit for bit where the same sums are taken, otherwise within fp32's rounding."""
+    m = Model("f32")
+    k = m.forward(m.p)
+    one = ops.make_residual_shape(1, 1, D, "f32", post_norm=True, gate="vector", branch_scale=0.7)
+    l1, l2 = ops.make_linear_shape(1, D, F, "f32", act="gelu"), ops.make_linear_shape(1, F, D, "f32")
+    two = ops.make_residual_shape(1, 1, D, "f32", gate="sequence", residual_scale=0.9)
+    l3, lp = ops.make_linear_shape(1, D, V, "f32", w_order="out_in"), ops.make_logprob_shape(1, V, "f32", top=3)
+    p = m.p
+    for b, t in ((0, 0), (0, T - 1), (1, 17)):
+        r = b * T + t
+        h1, n1 = ops.residual_norm(one, k["x"][b:b + 1, t:t + 1], k["y"][b:b + 1, t:t + 1], w_post=p["a1"], gate=p["g1"], w_pre=p["n1"])
+        assert torch.equal(h1[0, 0], k["h1"][b, t]) and torch.equal(n1[0, 0], k["n1"][b, t])
+        f = ops.linear(l1, n1.view(1, D), p["w1"], bias=p["b1"])
+        y2 = ops.linear(l2, f, p["w2"], bias=p["b2"])
+        h2, n2 = ops.residual_norm(two, h1, y2.view(1, 1, D), gate=p["g2"][b:b + 1], w_pre=p["n2"])
+        logp, lse, top, index = ops.token_logprobs(lp, ops.linear(l3, n2.view(1, D), p["emb"]), m.targets[r:r + 1])
+        # chains of sums of at most F terms, through a norm and a head: some hundred u of values of size 5
+        tol = 5 * 400 * 2.0 ** -24 * math.sqrt(F)
+        for x, y in ((h2[0, 0], k["h2"][b, t]), (lse, k["lse"][r:r + 1]), (logp, k["logp"][r:r + 1]), (top[0], k["top_logp"][r])):
+            assert float((x - y).abs().max()) < tol
+
+
+def test_a_step_in_a_graph():
+    """The whole step captured and replayed beside eager work gives the eager step's gradients."""
+    m = Model("bf16")
+    keep = {}
+
+    def step():
+        k = m.forward(m.p)
+        keep["out"] = [k["logp"], k["top_index"], *m.backward(m.p, k).values()]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    got = keep["out"]
+    for i in range(4):
+        m.p["w1"].mul_(1.25)
+        m.p["g2"].copy_(m.p["g2"].flip(1))
+        step()
+        want = keep["out"]
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(got[:-1], want[:-1]):
+            assert torch.equal(a, b), i
+        # (the embedding's sum is torch's, in an order of its own)
+        torch.testing.assert_close(got[-1], want[-1], rtol=1e-9, atol=1e-9)
