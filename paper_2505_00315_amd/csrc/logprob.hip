@@ -15,12 +15,12 @@
 // parts of a row by a second kernel.
 //
 // Alternatives (the `top` largest, equal ones by index): every lane also keeps the
-// first of its units that holds its maximum.  The top-th of the lanes' (maximum,
-// unit) in order is a threshold: at least `top` values are at or above it, all of
-// them in the units of the `top` lanes that reach it, which are read once more
-// (from L2).  What is at or above the threshold is ranked by counting.  Where that
-// is more than the list in LDS holds (rows of equal values), the values are taken
-// one by one instead.
+// first of its units that holds its maximum.  The lanes form 64 groups; the top-th
+// of the groups' greatest (maximum, unit) is a threshold: at least `top` values are at
+// or above it, all of them in the units of the lanes that reach it (few more than
+// `top`), which are read once more, from L2.  What is at or above the threshold is
+// ranked by counting.  Where that is more than the list in LDS holds (rows of equal
+// values), the values are taken one by one instead.
 #include <math.h>
 
 #include "block.h"
@@ -31,6 +31,19 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kList = 1024;  // values that are ranked at once
+
+// Maxima in one instruction: the compiler quiets NaN of fmaxf's arguments before each (2
+// instructions of 11 per value).  NaN are left out, as by fmaxf.
+__device__ __forceinline__ float max2(float x, float y) {
+    float r;
+    asm("v_max_f32 %0, %1, %2" : "=v"(r) : "v"(x), "v"(y));
+    return r;
+}
+__device__ __forceinline__ float max3(float x, float y, float z) {
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(x), "v"(y), "v"(z));
+    return r;
+}
 
 // Order of two values as unsigned numbers: larger first counts as larger; NaN as
 // -inf, -0 as 0.
@@ -48,39 +61,54 @@ template <typename ST>
 struct Row {
     static constexpr int E = Unit<ST>::E;
     const ST* p;  // aligned
-    int lead, V, units;
+    int lead, V, units, begin, end;  // begin .. end - 1: the units that are the row's throughout
     __device__ __forceinline__ Row(const char* base, int64_t stride, int64_t r, int V) : V(V) {
         const ST* at = reinterpret_cast<const ST*>(base) + r * stride;
         lead = (int)(((uintptr_t)at & 15) / sizeof(ST));
         p = at - lead;
         units = (int)(((int64_t)lead + V + E - 1) / E);
+        begin = lead > 0;
+        end = (int)(((int64_t)lead + V) / E);
     }
     __device__ __forceinline__ int first(int u) const { return u * E - lead; }  // index of a unit's first value
-    __device__ __forceinline__ bool whole(int u) const { return first(u) >= 0 && (int64_t)first(u) + E <= V; }
-    // values of unit u, -inf in the place of those that are not the row's
-    __device__ __forceinline__ void get(int u, float (&x)[E]) const {
-        if (whole(u)) {
-            Unit<ST> v;
-            v.load(p + (int64_t)u * E);
-            v.get(x);
-        } else {
+    __device__ __forceinline__ bool whole(int u) const { return u >= begin && u < end; }
+    // Unit u, -inf in the place of values that are not the row's: its load where it is a whole one, and after
+    // the loads of others the rest.
+    __device__ __forceinline__ void load(Unit<ST>& v, int u) const {
+        constexpr uint32_t none = sizeof(ST) == 2 ? 0xff80ff80u : 0xff800000u;
+        v.u = make_uint4(none, none, none, none);
+        if (whole(u)) v.load(p + (int64_t)u * E);
+    }
+    __device__ __forceinline__ void get(const Unit<ST>& v, int u, float (&x)[E]) const {
+        v.get(x);
+        if (u >= 0 && u < units && !whole(u)) {
 #pragma unroll
             for (int e = 0; e < E; ++e) {
                 const int64_t j = (int64_t)first(u) + e;
-                x[e] = j >= 0 && j < V ? ld1<ST>(p + (int64_t)u * E + e) : -INFINITY;
+                if (j >= 0 && j < V) x[e] = ld1<ST>(p + (int64_t)u * E + e);
             }
         }
     }
 };
 
-// Running maximum m, sum l of exp(scale (x - m)) and s of the same times the
-// exponent (in log2 units).
+// Running maximum m and sums over the values, in log2 units: l of w = 2^(x c - b)
+// and s of w (x c - b), c = scale log2(e).  b is m c rounded, one instruction per
+// value with its product exact; what the rounding adds is common to the row and is
+// taken out at the end.  Far from 0, where it would not be small, and before the
+// first value b stands for m c itself, and the exponent is (x - m) c.
 struct Run {
     float m, l, s;
 };
+constexpr float kNear = 1048576.f;  // of m c: its rounding is at most 2^-5
+constexpr float kNoWeight = -1000.f;  // an exponent of weight 0 that times 0 gives 0
+__device__ __forceinline__ bool near_base(float m, float c) { return fabsf(m * c) < kNear; }
+
+// Sums of a maximum r.m in terms of a maximum m >= r.m.
 template <bool ENT>
-__device__ __forceinline__ void rebase(Run& r, float m, float c) {  // to a maximum m >= r.m
-    const float d = r.m == m ? 0.f : fmaxf((r.m - m) * c, -1000.f);  // (no sum yet: r.m = -inf)
+__device__ __forceinline__ void rebase(Run& r, float m, float c) {
+    const bool from = near_base(r.m, c), to = near_base(m, c);
+    float d = from ? (to ? r.m * c - m * c : fmaf(-m, c, r.m * c)) : to ? fmaf(r.m, c, -(m * c)) : (r.m - m) * c;
+    d = r.m == m ? 0.f : fmaxf(d, kNoWeight);
     const float f = __builtin_amdgcn_exp2f(d);
     if constexpr (ENT) r.s = f * (r.s + d * r.l);
     r.l *= f;
@@ -88,32 +116,60 @@ __device__ __forceinline__ void rebase(Run& r, float m, float c) {  // to a maxi
 }
 template <bool ENT, int N>
 __device__ __forceinline__ void add_values(Run& r, const float (&x)[N], float c) {
-    const float m = r.m == -INFINITY ? 0.f : r.m;
+    if (near_base(r.m, c)) {
+        const float b = r.m * c;
 #pragma unroll
-    for (int e = 0; e < N; ++e) {
-        const float d = (x[e] - m) * c, w = __builtin_amdgcn_exp2f(d);
-        r.l += w;
-        if constexpr (ENT) r.s += w * fmaxf(d, -1000.f);
+        for (int e = 0; e < N; ++e) {
+            const float d = fmaf(x[e], c, -b), w = __builtin_amdgcn_exp2f(d);
+            r.l += w;
+            if constexpr (ENT) r.s += w * max2(d, kNoWeight);
+        }
+    } else {
+        const float m = r.m == -INFINITY ? 0.f : r.m;
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            const float d = (x[e] - m) * c, w = __builtin_amdgcn_exp2f(d);
+            r.l += w;
+            if constexpr (ENT) r.s += w * max2(d, kNoWeight);
+        }
     }
 }
-template <bool ENT>
-__device__ __forceinline__ Run join(Run a, Run b, float c) {
-    const float m = fmaxf(a.m, b.m);
-    rebase<ENT>(a, m, c);
-    rebase<ENT>(b, m, c);
-    return {m, a.l + b.l, a.s + b.s};
+// Over the 16 lanes of a row of the wave, then its four rows, in every lane.
+__device__ __forceinline__ float wave_max(float x) {
+    x = fmaxf(x, dpp_f32<0xB1, 0xf>(x));
+    x = fmaxf(x, dpp_f32<0x4E, 0xf>(x));
+    x = fmaxf(x, dpp_f32<0x141, 0xf>(x));
+    x = fmaxf(x, dpp_f32<0x140, 0xf>(x));
+    return rows4_max(x);
+}
+__device__ __forceinline__ float wave_sum(float x) {
+    x += dpp_f32<0xB1, 0xf>(x);
+    x += dpp_f32<0x4E, 0xf>(x);
+    x += dpp_f32<0x141, 0xf>(x);
+    x += dpp_f32<0x140, 0xf>(x);
+    return rows4_sum(x);
 }
 template <bool ENT>
 __device__ __forceinline__ Run wave_join(Run r, float c) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) {
-        Run q;
-        q.m = __shfl_xor(r.m, o, 64), q.l = __shfl_xor(r.l, o, 64), q.s = ENT ? __shfl_xor(r.s, o, 64) : 0.f;
-        // (the same order of the operands in both lanes)
-        const bool low = (threadIdx.x & o) == 0;
-        r = low ? join<ENT>(r, q, c) : join<ENT>(q, r, c);
-    }
+    rebase<ENT>(r, wave_max(r.m), c);
+    r.l = wave_sum(r.l);
+    if constexpr (ENT) r.s = wave_sum(r.s);
     return r;
+}
+template <bool ENT>
+__device__ __forceinline__ Run join_all(const Run* r, int n, float c) {
+    Run t{-INFINITY, 0.f, 0.f};
+    for (int i = 0; i < n; ++i) t.m = fmaxf(t.m, r[i].m);
+    for (int i = 0; i < n; ++i) {
+        Run q = r[i];
+        rebase<ENT>(q, t.m, c);
+        t.l += q.l, t.s += q.s;
+    }
+    return t;
+}
+// log sum exp(scale (x - m)): with b for m c, 2^(m c - b) too much.
+__device__ __forceinline__ float log_sum(const Run& t, float c) {
+    return logf(t.l) + (near_base(t.m, c) ? kLn2 * fmaf(-t.m, c, t.m * c) : 0.f);
 }
 
 // Scratch of a row's parts: their Runs, then their lists of keys.
@@ -122,15 +178,15 @@ struct PartBuf {
     uint64_t* keys;  // [R][P][top]
 };
 
-// The outputs of a row, by one lane.  x_t: the target's logit.
+// The outputs of a row, by one lane.
 template <typename ST>
-__device__ __forceinline__ void write_row(const LogprobArgs& a, int r, const Run& t) {
+__device__ __forceinline__ void write_row(const LogprobArgs& a, int r, const Run& t, float c) {
     // nothing but -inf: every weight is 0
     const bool none = t.m == -INFINITY && t.l == 0.f;
-    const float L = none ? -INFINITY : logf(t.l);
+    const float L = none ? -INFINITY : log_sum(t, c);
     if (a.stats) a.stats[2 * (int64_t)r] = t.m, a.stats[2 * (int64_t)r + 1] = L;
     if (a.lse) a.lse[r] = none ? -INFINITY : a.scale * t.m + L;
-    if (a.entropy) a.entropy[r] = none ? 0.f : L - kLn2 * t.s / t.l;
+    if (a.entropy) a.entropy[r] = none ? 0.f : logf(t.l) - kLn2 * t.s / t.l;
     if (a.logp) {
         const int j = a.target[r];
         float v = 0.f;
@@ -141,32 +197,47 @@ __device__ __forceinline__ void write_row(const LogprobArgs& a, int r, const Run
         a.logp[r] = v;
     }
 }
-__device__ __forceinline__ void write_top(const LogprobArgs& a, int r, int at, uint64_t key, const Run& t) {
+
+// The `top` largest of n distinct keys, in order, with their log p.  (t.l is NaN in a row
+// with NaN or +inf.)  put(rank, key, log p).
+template <int T, typename F>
+__device__ __forceinline__ void rank_keys(const uint64_t* keys, int n, int top, F put) {
+    for (int i = threadIdx.x; i < n; i += T) {
+        const uint64_t k = keys[i];
+        int rank = 0;
+#pragma unroll 8
+        for (int j = 0; j < n; ++j) rank += keys[j] > k;
+        if (rank < top && k) put(rank, k);
+    }
+}
+__device__ __forceinline__ void write_top(const LogprobArgs& a, int r, int at, uint64_t key, const Run& t, float L) {
     const float x = value_of((uint32_t)(key >> 32));
-    const float L = logf(t.l);
-    // (t.l is NaN in a row with NaN or +inf)
     a.top_logp[(int64_t)r * a.top + at] = t.l != t.l ? t.l : x == -INFINITY ? x : a.scale * (x - t.m) - L;
     a.top_index[(int64_t)r * a.top + at] = (int)~(uint32_t)key;
 }
 
-// The `top` largest keys of n distinct ones, in order: f(rank, key).
-template <typename F>
-__device__ __forceinline__ void rank_keys(const uint64_t* keys, int n, int top, F f) {
-    for (int i = threadIdx.x; i < n; i += kThreads) {
-        const uint64_t k = keys[i];
-        int rank = 0;
-        for (int j = 0; j < n; ++j) rank += keys[j] > k;
-        if (rank < top && k) f(rank, k);
+// The top-th largest of 64 keys, one per lane (equal keys, 0, in the order of the lanes).
+__device__ __forceinline__ uint64_t wave_kth(uint64_t key, int top) {
+    const int lane = threadIdx.x & 63;
+    int rank = 0;
+#pragma unroll
+    for (int j = 0; j < 64; ++j) {
+        const uint64_t k = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(key >> 32), j) << 32 |
+                           (uint32_t)__builtin_amdgcn_readlane((int)key, j);
+        rank += k > key || (k == key && j < lane);
     }
+    const int at = __builtin_ctzll(__ballot(rank == top - 1));
+    return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(key >> 32), at) << 32 |
+           (uint32_t)__builtin_amdgcn_readlane((int)key, at);
 }
 
-template <typename ST, bool ENT, bool TOP>
-__global__ __launch_bounds__(kThreads) void logprob_kernel(LogprobArgs a, int P, int per, PartBuf buf) {
-    constexpr int E = Unit<ST>::E, U = 4;
-    __shared__ Run runs[kThreads / 64];
+template <typename ST, bool ENT, bool TOP, int T>
+__global__ __launch_bounds__(T) void logprob_kernel(LogprobArgs a, int P, int per, PartBuf buf) {
+    constexpr int E = Unit<ST>::E, U = 4, W = T / 64;
+    __shared__ Run runs[W];
     __shared__ uint64_t keys[TOP ? kList : 1];
     __shared__ uint64_t threshold;
-    __shared__ int lanes[kMaxTop], count;
+    __shared__ int lanes[TOP ? T : 1], count[2];
     const int r = blockIdx.x / P, part = blockIdx.x % P, tid = threadIdx.x;
     const Row<ST> row(a.x, a.row, r, a.V);
     const int u0 = part * per, u1 = min(row.units, u0 + per);  // (the last part may be empty)
@@ -174,25 +245,21 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(LogprobArgs a, int P,
     Run t{-INFINITY, 0.f, 0.f};
     float best = -INFINITY;
     int unit = -1;  // the first unit that holds the lane's maximum
-    for (int u = u0 + tid; u < u1; u += U * kThreads) {
+    for (int u = u0 + tid; u < u1; u += U * T) {
+        Unit<ST> v[U];
         float x[U][E];
 #pragma unroll
-        for (int i = 0; i < U; ++i) {
-            if (u + i * kThreads < u1) {
-                row.get(u + i * kThreads, x[i]);
-            } else {
+        for (int i = 0; i < U; ++i) row.load(v[i], u + i * T < u1 ? u + i * T : -1);
 #pragma unroll
-                for (int e = 0; e < E; ++e) x[i][e] = -INFINITY;
-            }
-        }
+        for (int i = 0; i < U; ++i) row.get(v[i], u + i * T < u1 ? u + i * T : -1, x[i]);
         float m = t.m;
 #pragma unroll
         for (int i = 0; i < U; ++i) {
             float w = -INFINITY;  // (NaN are left out)
 #pragma unroll
-            for (int e = 0; e < E; ++e) w = fmaxf(w, x[i][e]);
+            for (int e = 0; e < E; e += 2) w = max3(w, x[i][e], x[i][e + 1]);
             if constexpr (TOP) {
-                if ((w > best || unit < 0) && u + i * kThreads < u1) best = w, unit = u + i * kThreads;
+                if ((w > best || unit < 0) && u + i * T < u1) best = w, unit = u + i * T;
             }
             m = fmaxf(m, w);
         }
@@ -202,39 +269,47 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(LogprobArgs a, int P,
     }
     t = wave_join<ENT>(t, c);
     if ((tid & 63) == 0) runs[tid >> 6] = t;
-    if (TOP) {
-        // a lane without units: 0, below every key
-        keys[tid] = unit < 0 ? 0 : key_of(best, unit);
-        if (tid == 0) count = 0;
+    const uint64_t mine = unit < 0 ? 0 : key_of(best, unit);  // (a lane without units: below every key)
+    if constexpr (TOP) {
+        keys[tid] = mine;
+        if (tid < 2) count[tid] = 0;
     }
     __syncthreads();
-    t = runs[0];
-#pragma unroll
-    for (int w = 1; w < kThreads / 64; ++w) t = join<ENT>(t, runs[w], c);
+    if (TOP || tid < 64) t = join_all<ENT>(runs, W, c);
     if (tid == 0) {
         if (P > 1) buf.run[(int64_t)r * P + part] = t;
-        else write_row<ST>(a, r, t);
+        else write_row<ST>(a, r, t, c);
     }
     if constexpr (TOP) {
+        const float L = P > 1 ? 0.f : log_sum(t, c);
         auto put = [&](int rank, uint64_t key) {
             if (P > 1) buf.keys[((int64_t)r * P + part) * a.top + rank] = key;
-            else write_top(a, r, rank, key, t);
+            else write_top(a, r, rank, key, t, L);
         };
-        const uint64_t mine = keys[tid];
-        int rank = 0;
-        for (int j = 0; j < kThreads; ++j) rank += keys[j] > mine || (keys[j] == mine && j < tid);
-        if (rank < a.top) lanes[rank] = tid;
-        if (rank == a.top - 1) threshold = mine;
+        if (tid < 64) {
+            uint64_t group = keys[tid];
+#pragma unroll
+            for (int w = 1; w < W; ++w) {
+                const uint64_t k = keys[tid + 64 * w];
+                group = k > group ? k : group;
+            }
+            const uint64_t k = wave_kth(group, a.top);
+            if (tid == 0) threshold = k;
+        }
         __syncthreads();
         const uint64_t least = threshold;  // 0: every value
-        const int each = (u1 - u0 + kThreads - 1) / kThreads, total = a.top * each;
+        if (mine >= least && mine) lanes[atomicAdd(&count[0], 1)] = tid;
+        __syncthreads();  // (keys are read until here)
+        const int each = (u1 - u0 + T - 1) / T, total = count[0] * each;
         // the units of those lanes: f(index, value) for what is at or above the threshold
         auto visit = [&](auto f) {
-            for (int i = tid; i < total; i += kThreads) {
-                const int u = u0 + lanes[i / each] + (i % each) * kThreads;
+            for (int i = tid; i < total; i += T) {
+                const int u = u0 + lanes[i / each] + (i % each) * T;
                 if (u >= u1) continue;
+                Unit<ST> v;
                 float x[E];
-                row.get(u, x);
+                row.load(v, u);
+                row.get(v, u, x);
 #pragma unroll
                 for (int e = 0; e < E; ++e) {
                     const int j = row.first(u) + e;
@@ -242,15 +317,14 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(LogprobArgs a, int P,
                 }
             }
         };
-        __syncthreads();  // (keys are read until here)
         visit([&](int j, float x) {
-            const int n = atomicAdd(&count, 1);
+            const int n = atomicAdd(&count[1], 1);
             if (n < kList) keys[n] = key_of(x, j);
         });
         __syncthreads();
-        const int n = count;
+        const int n = count[1];
         if (n <= kList) {
-            rank_keys(keys, n, a.top, put);
+            rank_keys<T>(keys, n, a.top, put);
         } else {
             uint64_t last = ~(uint64_t)0;
             for (int k = 0; k < a.top; ++k) {
@@ -261,7 +335,7 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(LogprobArgs a, int P,
                 });
                 keys[tid] = next;
                 __syncthreads();
-                for (int o = kThreads / 2; o > 0; o >>= 1) {
+                for (int o = T / 2; o > 0; o >>= 1) {
                     if (tid < o && keys[tid + o] > keys[tid]) keys[tid] = keys[tid + o];
                     __syncthreads();
                 }
@@ -271,7 +345,7 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(LogprobArgs a, int P,
             }
         }
         if (P > 1) {  // a part of fewer values
-            for (int k = n + tid; k < a.top; k += kThreads) put(k, 0);
+            for (int k = n + tid; k < a.top; k += T) put(k, 0);
         }
     }
 }
@@ -282,14 +356,14 @@ __global__ __launch_bounds__(kThreads) void logprob_join_kernel(LogprobArgs a, i
     __shared__ uint64_t keys[TOP ? kList : 1];
     const int r = blockIdx.x;
     const float c = a.scale * kLog2e;
-    Run t = buf.run[(int64_t)r * P];
-    for (int p = 1; p < P; ++p) t = join<ENT>(t, buf.run[(int64_t)r * P + p], c);
-    if (threadIdx.x == 0) write_row<ST>(a, r, t);
+    const Run t = join_all<ENT>(buf.run + (int64_t)r * P, P, c);
+    if (threadIdx.x == 0) write_row<ST>(a, r, t, c);
     if constexpr (TOP) {
-        const int n = P * a.top;  // (at most kList: see parts_of)
+        const int n = P * a.top;  // (at most kList / 2: see parts_of)
+        const float L = log_sum(t, c);
         for (int i = threadIdx.x; i < n; i += kThreads) keys[i] = buf.keys[(int64_t)r * n + i];
         __syncthreads();
-        rank_keys(keys, n, a.top, [&](int rank, uint64_t key) { write_top(a, r, rank, key, t); });
+        rank_keys<kThreads>(keys, n, a.top, [&](int rank, uint64_t key) { write_top(a, r, rank, key, t, L); });
     }
 }
 
@@ -315,12 +389,14 @@ __global__ __launch_bounds__(kThreads) void logprob_bwd_kernel(LogprobArgs a, in
     const float A = gl - g - ge * H, M0 = M == -INFINITY ? 0.f : M, L0 = none ? 0.f : L;
     const float l2 = L0 * kLog2e, gk = ge * kLn2;
     for (int u = u0 + lane; u < u1; u += 64) {
+        Unit<ST> v;
         float x[E];
-        row.get(u, x);
+        row.load(v, u);
+        row.get(v, u, x);
 #pragma unroll
         for (int e = 0; e < E; ++e) {
             const float d = (x[e] - M0) * c - l2, p = __builtin_amdgcn_exp2f(d);
-            x[e] = p * (A - gk * fmaxf(d, -1000.f));
+            x[e] = p * (A - gk * max2(d, kNoWeight));
         }
         const int j = t - row.first(u);
         if (has && j >= 0 && j < E) {
@@ -341,27 +417,30 @@ __global__ __launch_bounds__(kThreads) void logprob_bwd_kernel(LogprobArgs a, in
     }
 }
 
-// Parts of a row, and units of each: where rows are few, enough for the chip.
+// Lanes of a workgroup, parts of a row and units of each.  Many rows: a workgroup of
+// 256 lanes each.  Fewer than the chip holds: parts of them.  A few rows, where
+// latency counts: 1024 lanes, and parts only for rows long enough to be worth a
+// second kernel (4 us).
 struct Split {
-    int P, per;
+    int T, P, per;
 };
 Split parts_of(int dtype, int R, int V, int top) {
     const int E = dtype == kBF16 ? 8 : 4;
     const int64_t units = ((int64_t)V + 2 * E - 2) / E;  // (a row that does not start at a unit)
-    int64_t P = 1024 / R;
-    const int64_t most = units / (4 * kThreads);  // a part's reads keep its lanes busy
+    const int T = R < 128 && units > 4 * kThreads ? 1024 : kThreads;
+    int64_t P = T == 1024 ? 256 / R : 1024 / R;
+    const int64_t most = units / ((T == 1024 ? 8 : 4) * T);  // a part's reads keep its lanes busy
     if (P > most) P = most;
     if (top && P > kList / 2 / top) P = kList / 2 / top;
     if (P < 1) P = 1;
     const int64_t per = (units + P - 1) / P;
-    return {(int)((units + per - 1) / per), (int)per};
+    return {T, (int)((units + per - 1) / per), (int)per};
 }
 
 template <typename ST, bool ENT, bool TOP>
 int forward_t(const LogprobArgs& a, const Split& s, const PartBuf& buf, hipStream_t stream) {
-    // (a row's unit 0 may hold few of its values, so that the last part may be empty)
-    hipLaunchKernelGGL((logprob_kernel<ST, ENT, TOP>), dim3((unsigned)((int64_t)a.R * s.P)), dim3(kThreads), 0, stream, a,
-                       s.P, s.per, buf);
+    auto kern = s.T == 1024 ? logprob_kernel<ST, ENT, TOP, 1024> : logprob_kernel<ST, ENT, TOP, kThreads>;
+    hipLaunchKernelGGL(kern, dim3((unsigned)((int64_t)a.R * s.P)), dim3(s.T), 0, stream, a, s.P, s.per, buf);
     if (hipGetLastError() != hipSuccess) return -1;
     if (s.P > 1) {
         hipLaunchKernelGGL((logprob_join_kernel<ST, ENT, TOP>), dim3(a.R), dim3(kThreads), 0, stream, a, s.P, buf);

@@ -441,23 +441,32 @@ def alloc_residual_scratch(shape, device="cuda"):
     return torch.empty(max(residual_scratch_size(shape), 256), dtype=torch.uint8, device=device)
 
 
-def _stream_rows(t, what, shape, device, sizes=None):
-    """The Rows of a tensor [batch, seq_len, d_model] (None: NULL)."""
+def _stream_rows(t, what, sizes, dtype, device):
+    """The Rows of a tensor of these sizes, [batch, seq_len, d_model] or a gate's (None: NULL)."""
     if t is None:
         return None
-    want = (shape.batch, shape.seq_len, shape.d_model) if sizes is None else sizes
-    if t.shape != want:
-        raise ValueError(f"{what}: shape {tuple(t.shape)}, expected {want}")
-    # the axes that a shared gate does not have, and the heads' axis
-    t = t.view((1,) * (3 - len(want)) + tuple(want)) if len(want) == 1 else t.unsqueeze(1) if len(want) == 2 else t
-    return _rows(t.unsqueeze(1), what, (t.shape[0], 1, t.shape[1], t.shape[2]), _TORCH[shape.dtype], device)
+    if t.dtype != dtype:
+        raise TypeError(f"{what}: dtype {t.dtype}, expected {dtype}")
+    if t.shape != sizes:
+        raise ValueError(f"{what}: shape {tuple(t.shape)}, expected {sizes}")
+    if t.device != device:
+        raise ValueError(f"{what}: on {t.device}, expected {device}")
+    st = t.stride()
+    if st[-1] != 1:
+        raise ValueError(f"{what}: the last axis is not contiguous")
+    return Rows(t.data_ptr(), st[0] if len(st) > 1 else 0, 0, st[1] if len(st) > 2 else 0)
 
 
-def _gate_rows(t, what, shape, device):
-    B, T, d = shape.batch, shape.seq_len, shape.d_model
-    if t is not None and shape.gate == 0:
+def _residual_io(shape):
+    """(storage type, sizes of the stream, sizes of the gate)"""
+    B, T, d = sizes = shape.batch, shape.seq_len, shape.d_model
+    return _TORCH[shape.dtype], sizes, (None, (d,), (B, d), sizes)[shape.gate]
+
+
+def _gate_rows(t, what, sizes, dtype, device):
+    if t is not None and sizes is None:
         raise ValueError(f"{what}: the shape has no gate")
-    return _stream_rows(t, what, shape, device, {1: (d,), 2: (B, d), 3: (B, T, d)}.get(shape.gate))
+    return _stream_rows(t, what, sizes, dtype, device)
 
 
 def residual_norm(shape, x, y, w_post=None, gate=None, w_pre=None, h_out=None, n_out=None, stream=None):
@@ -468,12 +477,14 @@ def residual_norm(shape, x, y, w_post=None, gate=None, w_pre=None, h_out=None, n
     w_post, w_pre [d] (None: ones).  y None: h is x, and only n is computed.
     h_out may be x or y, and n_out y.  Returns (h, n), n None without pre_norm."""
     dev = _device(x, "x")
-    st, d = _TORCH[shape.dtype], shape.d_model
+    st, sizes, gs = _residual_io(shape)
+    d = sizes[2]
     h_out = _like(x, h_out, stream) if y is not None else h_out
     n_out = _like(x, n_out, stream) if shape.pre_norm else n_out
-    _call("mosa_residual_norm", dev, stream, shape, _stream_rows(x, "x", shape, dev), _stream_rows(y, "y", shape, dev),
-          _array(w_post, "w_post", st, d, dev), _gate_rows(gate, "gate", shape, dev), _array(w_pre, "w_pre", st, d, dev),
-          _stream_rows(h_out, "h_out", shape, dev), _stream_rows(n_out, "n_out", shape, dev))
+    _call("mosa_residual_norm", dev, stream, shape, _stream_rows(x, "x", sizes, st, dev),
+          _stream_rows(y, "y", sizes, st, dev), _array(w_post, "w_post", st, d, dev),
+          _gate_rows(gate, "gate", gs, st, dev), _array(w_pre, "w_pre", st, d, dev),
+          _stream_rows(h_out, "h_out", sizes, st, dev), _stream_rows(n_out, "n_out", sizes, st, dev))
     return (x if y is None else h_out), n_out
 
 
@@ -484,7 +495,8 @@ def residual_norm_backward(shape, x, y, w_post=None, gate=None, w_pre=None, dh=N
     made where the weight or the gate is.  dx may be dh or dn, and dy the other of
     them.  Returns (dx, dy, dw_post, dgate, dw_pre)."""
     dev = _device(x, "x")
-    st, d = _TORCH[shape.dtype], shape.d_model
+    st, sizes, gs = _residual_io(shape)
+    d = sizes[2]
     dx = _like(x, dx, stream)
     dy = dy if y is None else _like(y, dy, stream)
     dw_post = dw_post if w_post is None else _like(w_post, dw_post, stream)
@@ -493,11 +505,12 @@ def residual_norm_backward(shape, x, y, w_post=None, gate=None, w_pre=None, dh=N
         dgate = _new(torch.empty, stream, tuple(gate.shape), dtype=gate.dtype, device=gate.device)
     sums = dw_post is not None or dw_pre is not None or (dgate is not None and shape.gate != GATES["token"])
     buf, at, size = _scratch(scratch, lambda: residual_scratch_size(shape) if sums else 0, dev, stream)
-    _call("mosa_residual_norm_backward", dev, stream, shape, _stream_rows(x, "x", shape, dev),
-          _stream_rows(y, "y", shape, dev), _array(w_post, "w_post", st, d, dev), _gate_rows(gate, "gate", shape, dev),
-          _array(w_pre, "w_pre", st, d, dev), _stream_rows(dh, "dh", shape, dev), _stream_rows(dn, "dn", shape, dev),
-          _stream_rows(dx, "dx", shape, dev), _stream_rows(dy, "dy", shape, dev),
-          _array(dw_post, "dw_post", st, d, dev), _gate_rows(dgate, "dgate", shape, dev),
+    _call("mosa_residual_norm_backward", dev, stream, shape, _stream_rows(x, "x", sizes, st, dev),
+          _stream_rows(y, "y", sizes, st, dev), _array(w_post, "w_post", st, d, dev),
+          _gate_rows(gate, "gate", gs, st, dev), _array(w_pre, "w_pre", st, d, dev),
+          _stream_rows(dh, "dh", sizes, st, dev), _stream_rows(dn, "dn", sizes, st, dev),
+          _stream_rows(dx, "dx", sizes, st, dev), _stream_rows(dy, "dy", sizes, st, dev),
+          _array(dw_post, "dw_post", st, d, dev), _gate_rows(dgate, "dgate", gs, st, dev),
           _array(dw_pre, "dw_pre", st, d, dev), at, size)
     return dx, dy, dw_post, dgate, dw_pre
 

@@ -237,16 +237,19 @@ def test_binding_refuses_what_it_can_see():
         ops.make_residual_shape(2, 8, 64, gate="head")
     with pytest.raises(KeyError):
         ops.make_linear_shape(2, 8, 64, act="tanh")
-    d = torch.device("cpu")
-    s = ops.make_residual_shape(2, 8, 64, gate="sequence")
+    d, bf16 = torch.device("cpu"), torch.bfloat16
+    st, sizes, gate = ops._residual_io(ops.make_residual_shape(2, 8, 64, gate="sequence"))
+    assert (st, sizes, gate) == (bf16, (2, 8, 64), (2, 64))
     with pytest.raises(ValueError, match="expected"):
-        ops._gate_rows(torch.zeros(2, 8, 64, dtype=torch.bfloat16), "gate", s, d)
+        ops._gate_rows(torch.zeros(2, 8, 64, dtype=bf16), "gate", gate, st, d)
     with pytest.raises(TypeError):
-        ops._stream_rows(torch.zeros(2, 8, 64), "x", s, d)
+        ops._stream_rows(torch.zeros(2, 8, 64), "x", sizes, st, d)
+    with pytest.raises(ValueError, match="contiguous"):
+        ops._stream_rows(torch.zeros(2, 64, 8, dtype=bf16).transpose(1, 2), "x", sizes, st, d)
     with pytest.raises(ValueError, match="no gate"):
-        ops._gate_rows(torch.zeros(64, dtype=torch.bfloat16), "gate", ops.make_residual_shape(2, 8, 64), d)
-    r = ops._gate_rows(torch.zeros(2, 64, dtype=torch.bfloat16), "gate", s, d)
-    assert r.batch_stride == 64
+        ops._gate_rows(torch.zeros(64, dtype=bf16), "gate", ops._residual_io(ops.make_residual_shape(2, 8, 64))[2], st, d)
+    r = ops._gate_rows(torch.zeros(2, 64, dtype=bf16), "gate", gate, st, d)
+    assert (r.batch_stride, r.row_stride) == (64, 0)
     with pytest.raises(ValueError, match="contiguous"):
         ops._matrix(torch.zeros(64, 8).t(), "w", (8, 64), torch.float32, d)
     with pytest.raises(TypeError):
