@@ -40,102 +40,149 @@ struct ProdArgs {
     Matrix r, y, z;
 };
 
+// The normal distribution's tail Phi(-x) = erfc(x / sqrt 2) / 2, x >= 0, and e = exp(-x^2 / 2).  fp32 storage: the
+// library's erfc, to a few units of the result.  bf16: e t P(t) with t = 1 / (1 + 0.27 x) and P of degree 6, fitted
+// to erfc(x / sqrt 2) exp(x^2 / 2) / (2 t) over all x: 2e-6 of the result, for a third of the instructions (the product
+// of 8192 x 1024 by 4096 columns with this epilogue: 148 us with the library's function, 69 without any).
+template <typename ST>
+__device__ __forceinline__ float normal_tail(float x, float& e) {
+    if constexpr (sizeof(ST) == 4) {
+        e = expf(-0.5f * x * x);
+        return 0.5f * erfcf(x * 0.70710678118654752f);
+    } else {
+        e = __builtin_amdgcn_exp2f(x * x * (-0.5f * kLog2e));
+        const float t = __builtin_amdgcn_rcpf(1.f + 0.27f * x);
+        float p = -0.060080647f;
+        p = fmaf(p, t, 0.156204835f);
+        p = fmaf(p, t, -0.021565299f);
+        p = fmaf(p, t, 0.116162054f);
+        p = fmaf(p, t, 0.093170337f);
+        p = fmaf(p, t, 0.108424231f);
+        p = fmaf(p, t, 0.107685007f);
+        return e * t * p;
+    }
+}
+template <typename ST>
+__device__ __forceinline__ float sigmoid(float z) {
+    if constexpr (sizeof(ST) == 4) return 1.f / (1.f + expf(-z));
+    else return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-kLog2e * z));
+}
+template <typename ST>
 __device__ __forceinline__ float act_of(float z, int act) {
     if (act == kActRelu) return z > 0.f ? z : z != z ? z : 0.f;
-    if (act == kActGelu) return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
-    if (act == kActSilu) return z / (1.f + expf(-z));
-    return z;
+    if (act == kActSilu) return z * sigmoid<ST>(z);
+    float e;
+    const float q = normal_tail<ST>(fabsf(z), e);
+    return z * (z > 0.f ? 1.f - q : q);
 }
+template <typename ST>
 __device__ __forceinline__ float act_slope(float z, int act) {
     if (act == kActRelu) return z > 0.f ? 1.f : z != z ? z : 0.f;
-    if (act == kActGelu)
-        return 0.5f * (1.f + erff(z * 0.70710678118654752f)) + z * 0.39894228040143268f * expf(-0.5f * z * z);
-    const float s = 1.f / (1.f + expf(-z));
-    return s * (1.f + z * (1.f - s));
+    if (act == kActSilu) {
+        const float s = sigmoid<ST>(z);
+        return s * (1.f + z * (1.f - s));
+    }
+    float e;
+    const float q = normal_tail<ST>(fabsf(z), e);
+    return (z > 0.f ? 1.f - q : q) + z * e * 0.39894228040143268f;
 }
 
-// Unit<ST>::E values of row m from column n on: bias, activation, residual, store.
-template <typename ST>
-__device__ __forceinline__ void finish_unit(const ProdArgs& a, int m, int n, float (&x)[Unit<ST>::E]) {
+// The epilogue of Unit<ST>::E values from column n on in R rows m[i] (those below M): bias, activation, residual,
+// stores.  Loads come first, so that they are in flight together.
+template <typename ST, int R>
+__device__ __forceinline__ void finish_units(const ProdArgs& a, const int (&m)[R], int n, float (&x)[R][Unit<ST>::E]) {
     constexpr int E = Unit<ST>::E;
-    Unit<ST> u;
-    if (a.bias) {
-        float b[E];
-        u.load(static_cast<const ST*>(a.bias) + n);
-        u.get(b);
-#pragma unroll
-        for (int e = 0; e < E; ++e) x[e] += b[e];
-    }
-    if (a.z.p) {
-        u.set(x);
-        u.store(reinterpret_cast<ST*>(a.z.p) + (int64_t)m * a.z.row + n);
-    }
-    if (a.act) {
-#pragma unroll
-        for (int e = 0; e < E; ++e) x[e] = act_of(x[e], a.act);
-    }
+    Unit<ST> b, r[R];
+    if (a.bias) b.load(static_cast<const ST*>(a.bias) + n);
     if (a.r.p) {
-        float b[E];
-        u.load(reinterpret_cast<const ST*>(a.r.p) + (int64_t)m * a.r.row + n);
-        u.get(b);
 #pragma unroll
-        for (int e = 0; e < E; ++e) x[e] += b[e];
+        for (int i = 0; i < R; ++i)
+            if (m[i] < a.M) r[i].load(reinterpret_cast<const ST*>(a.r.p) + (int64_t)m[i] * a.r.row + n);
     }
-    u.set(x);
-    u.store(reinterpret_cast<ST*>(a.y.p) + (int64_t)m * a.y.row + n);
+    if (a.bias) {
+        float v[E];
+        b.get(v);
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+#pragma unroll
+            for (int e = 0; e < E; ++e) x[i][e] += v[e];
+    }
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        if (m[i] >= a.M) continue;
+        Unit<ST> u;
+        if (a.z.p) {
+            u.set(x[i]);
+            u.store(reinterpret_cast<ST*>(a.z.p) + (int64_t)m[i] * a.z.row + n);
+        }
+        if (a.act) {
+#pragma unroll
+            for (int e = 0; e < E; ++e) x[i][e] = act_of<ST>(x[i][e], a.act);
+        }
+        if (a.r.p) {
+            float v[E];
+            r[i].get(v);
+#pragma unroll
+            for (int e = 0; e < E; ++e) x[i][e] += v[e];
+        }
+        u.set(x[i]);
+        u.store(reinterpret_cast<ST*>(a.y.p) + (int64_t)m[i] * a.y.row + n);
+    }
 }
 
-template <typename ST_, bool PKC_, bool QKC_, int NT_, int MT_, int WN_, int WM_, int STG_>
+template <typename ST_, bool PKC_, bool QKC_, int NT_, int MT_, int WN_, int WM_, int STG_, int NH_ = 1>
 struct ProdShape {
     using ST = ST_;
     static constexpr bool PKC = PKC_, QKC = QKC_;
-    static constexpr int NT = NT_, MT = MT_, WN = WN_, WM = WM_, STG = STG_, T = 64 * WN * WM;
+    static constexpr int NT = NT_, MT = MT_, WN = WN_, WM = WM_, STG = STG_, NH = NH_, T = 64 * WN * WM;
     static constexpr int ES = (int)sizeof(ST), E = 16 / ES, KC = 128 / ES, KS = KC / 32;
     static constexpr int WTN = NT / WN, WTM = MT / WM, FN = WTN / 16, FM = WTM / 16;
     static constexpr int PU = NT * ES / 16, QU = MT * ES / 16;  // units of a [k][columns] row
     static constexpr int P_BYTES = NT * 128, Q_BYTES = MT * 128, STAGE = P_BYTES + Q_BYTES, LDS = STG * STAGE;
     static constexpr int IP = P_BYTES / 16 / T, IQ = Q_BYTES / 16 / T, L = IP + IQ;  // loads per lane and chunk
     static_assert(P_BYTES % (16 * T) == 0 && Q_BYTES % (16 * T) == 0, "whole instructions per wave");
-    static_assert(ES == 4 || FN % 2 == 0, "pairs of column blocks");
+    static constexpr bool PAIR = ES == 2 && FN > 1;  // column blocks in interleaved pairs
+    static_assert(FN % NH == 0 && (!PAIR || FN / NH % 2 == 0), "pairs of column blocks");
     static_assert(LDS <= 160 * 1024 && (STG - 1) * L <= 63 && STG >= 2, "stages");
 };
 
-// Unit places of a k-contiguous tile's row; the P side's bf16 rows are read 4
-// apart in eights.
-template <typename ST, bool PSIDE>
+// Unit places of a k-contiguous tile's row; the rows of interleaved pairs are read
+// as two runs of 4.
+template <bool PAIR>
 __device__ __forceinline__ int prod_swz(int r) {
-    return PSIDE && sizeof(ST) == 2 ? (r & 3) | ((r >> 3) & 1) << 2 : r & 7;
+    return PAIR ? (r & 3) | ((r >> 3) & 1) << 2 : r & 7;
 }
 // Unit places of a [k][columns] tile of U units a row.
 template <typename ST, int U>
 __device__ __forceinline__ int prod_kswz(int k, int u) {
     if constexpr (sizeof(ST) == 2) return mswz<U>(k, u);
-    else return u ^ (4 * ((k >> 3) & 3));
+    else return u ^ ((4 * ((k >> 3) & 3)) & (U - 1));
 }
 
 // One operand: where a lane's units come from, and its fragments.
 template <class S, bool PSIDE>
 struct ProdSide {
     using ST = typename S::ST;
-    static constexpr bool KCON = PSIDE ? S::PKC : S::QKC;
+    static constexpr bool KCON = PSIDE ? S::PKC : S::QKC, PAIR = PSIDE && S::PAIR;
     static constexpr int E = S::E, U = PSIDE ? S::PU : S::QU, I = PSIDE ? S::IP : S::IQ, T = S::T;
     static constexpr int BYTES = PSIDE ? S::P_BYTES : S::Q_BYTES;
     const char* base;  // of the tile and the split's first k
     int64_t row, step;
     int left;  // columns (or rows of C) of the tile that exist, at least one unit's
+    int tid;   // of the S::T lanes that copy a tile
     uint32_t off[I];
 
     // unit i of the tile -> (row in memory, unit in the row) of its source
     static __device__ __forceinline__ void place(int i, int& r, int& u) {
         if constexpr (KCON) {
             r = i / 8;
-            u = (i % 8) ^ prod_swz<ST, PSIDE>(r);
+            u = (i % 8) ^ prod_swz<PAIR>(r);
         } else {
             r = i / U;
             u = prod_kswz<ST, U>(r, i % U);
         }
     }
-    __device__ __forceinline__ ProdSide(const ProdArgs& a, int o0, int k0) {
+    __device__ __forceinline__ ProdSide(const ProdArgs& a, int o0, int k0, int tid) : tid(tid) {
         const int size = PSIDE ? a.N : a.M;
         row = PSIDE ? a.prow : a.qrow;
         const char* p = PSIDE ? a.p : a.q;
@@ -145,7 +192,7 @@ struct ProdSide {
 #pragma unroll
         for (int j = 0; j < I; ++j) {
             int r, u;
-            place((int)threadIdx.x + j * T, r, u);
+            place(tid + j * T, r, u);
             if constexpr (KCON) r = min(r, left - 1);
             else u = min(u, left / E - 1);
             off[j] = (uint32_t)(r * row) + 16 * u;
@@ -161,7 +208,7 @@ struct ProdSide {
 #pragma unroll
             for (int j = 0; j < I; ++j) {
                 int r, u;
-                place((int)threadIdx.x + j * T, r, u);
+                place(tid + j * T, r, u);
                 if constexpr (KCON) r = min(r, left - 1), u = min(u, v / E - 1);
                 else r = min(r, v - 1), u = min(u, left / E - 1);
                 lds_load16s((uint32_t)(r * row) + 16 * u, at, lds + 16 * T * j);
@@ -170,7 +217,7 @@ struct ProdSide {
     }
     __device__ __forceinline__ void clear(unsigned char* tile, int v) const {
 #pragma unroll 1
-        for (int i = threadIdx.x; i < BYTES / 16; i += T) {
+        for (int i = tid; i < BYTES / 16; i += T) {
             int r, u;
             place(i, r, u);
             if (KCON ? u * E >= v : r >= v) *reinterpret_cast<uint4*>(tile + 16 * i) = make_uint4(0, 0, 0, 0);
@@ -179,9 +226,8 @@ struct ProdSide {
     // 16 rows (of the matrix instruction) from `o` on, 32 k from ks on.  odd: block of an interleaved pair at o.
     static __device__ __forceinline__ Frag8<ST> frag(const unsigned char* t, int o, int odd, int ks, int g, int c16) {
         Frag8<ST> f;
-        constexpr bool PAIR = PSIDE && sizeof(ST) == 2;
         if constexpr (KCON) {
-            const int r = o + (PAIR ? 8 * (c16 >> 2) + (c16 & 3) + 4 * odd : c16), s = prod_swz<ST, PSIDE>(r);
+            const int r = o + (PAIR ? 8 * (c16 >> 2) + (c16 & 3) + 4 * odd : c16), s = prod_swz<PAIR>(r);
             if constexpr (sizeof(ST) == 2) {
                 f.v = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(t + r * 128 + (((ks >> 3) + g) ^ s) * 16));
             } else {
@@ -224,8 +270,8 @@ __global__ __launch_bounds__((S::T)) void prod_kernel(const ProdArgs a) {
     const int m0 = (8 * band + in % bm) * S::MT, n0 = (in / bm) * S::NT;
     const int k0 = split * a.kper, klen = min(a.kper, a.K - k0), chunks = (klen + S::KC - 1) / S::KC;
 
-    const ProdSide<S, true> P(a, n0, k0);
-    const ProdSide<S, false> Q(a, m0, k0);
+    const ProdSide<S, true> P(a, n0, k0, tid);
+    const ProdSide<S, false> Q(a, m0, k0, tid);
     const uint32_t lds = __builtin_amdgcn_readfirstlane(lds_addr(smem) + 1024 * wave);
     auto issue = [&](int c, int buf) {
         const int v = klen - c * S::KC;
@@ -246,24 +292,27 @@ __global__ __launch_bounds__((S::T)) void prod_kernel(const ProdArgs a) {
     for (int j = 0; j < S::FN; ++j)
 #pragma unroll
         for (int i = 0; i < S::FM; ++i) acc[j][i] = zero4();
-    struct Frags {
-        Frag8<ST> p[S::FN], q[S::FM];
-    };
-    auto load_frags = [&](Frags& f, int buf, int ks) {
-        const unsigned char *tp = smem + buf * S::STAGE, *tq = tp + S::P_BYTES;
+    // One step: HN column blocks by all row blocks over 32 k.  The fragments of the next step are read while this one
+    // is multiplied; the Q fragments last for the steps of their 32 k.
+    constexpr int NH = S::NH, HN = S::FN / NH, STEPS = KS * NH;  // steps of a chunk
+    Frag8<ST> fp[2][HN], fq[2][S::FM];
+    auto load_p = [&](Frag8<ST> (&f)[HN], int buf, int ks, int h) {
+        const unsigned char* t = smem + buf * S::STAGE;
 #pragma unroll
-        for (int j = 0; j < S::FN; ++j) {
-            const int o = wn * S::WTN + (sizeof(ST) == 2 ? 32 * (j >> 1) : 16 * j);
-            f.p[j] = ProdSide<S, true>::frag(tp, o, sizeof(ST) == 2 ? j & 1 : 0, ks, g, c16);
+        for (int jj = 0; jj < HN; ++jj) {
+            const int j = h * HN + jj, o = wn * S::WTN + (sizeof(ST) == 2 ? 32 * (j >> 1) : 16 * j);
+            f[jj] = ProdSide<S, true>::frag(t, o, sizeof(ST) == 2 ? j & 1 : 0, 32 * ks, g, c16);
         }
-#pragma unroll
-        for (int i = 0; i < S::FM; ++i) f.q[i] = ProdSide<S, false>::frag(tq, wm * S::WTM + 16 * i, 0, ks, g, c16);
     };
-    constexpr int READS = (S::PKC ? (S::ES == 2 ? 1 : 2) : (S::ES == 2 ? 2 : 8)) * S::FN +
-                          (S::QKC ? (S::ES == 2 ? 1 : 2) : (S::ES == 2 ? 2 : 8)) * S::FM;
-    constexpr int MFMAS = S::FN * S::FM * (S::ES == 2 ? 1 : 8);
+    auto load_q = [&](Frag8<ST> (&f)[S::FM], int buf, int ks) {
+        const unsigned char* t = smem + buf * S::STAGE + S::P_BYTES;
+#pragma unroll
+        for (int i = 0; i < S::FM; ++i) f[i] = ProdSide<S, false>::frag(t, wm * S::WTM + 16 * i, 0, 32 * ks, g, c16);
+    };
+    constexpr int READS_P = (S::PKC ? (S::ES == 2 ? 1 : 2) : (S::ES == 2 ? 2 : 8)) * HN;
+    constexpr int READS_Q = (S::QKC ? (S::ES == 2 ? 1 : 2) : (S::ES == 2 ? 2 : 8)) * S::FM;
+    constexpr int MFMAS = HN * S::FM * (S::ES == 2 ? 1 : 8);
 
-    Frags fr[2];
 #pragma unroll
     for (int s = 0; s < STG; ++s)
         if (s < chunks) issue(s, s);
@@ -272,17 +321,19 @@ __global__ __launch_bounds__((S::T)) void prod_kernel(const ProdArgs a) {
     __syncthreads();
     clear_tail(0, 0);
     __builtin_amdgcn_sched_barrier(0);
-    load_frags(fr[0], 0, 0);
-    constexpr int UNROLL = STG * KS % 2 == 0 ? STG : 2 * STG;
+    load_p(fp[0], 0, 0, 0);
+    load_q(fq[0], 0, 0);
+    constexpr int UNROLL = STG * KS % 2 == 0 ? STG : 2 * STG;  // (the register sets' names are constants)
     for (int c0 = 0;; c0 += UNROLL) {
 #pragma unroll
         for (int u = 0; u < UNROLL; ++u) {
             const int c = c0 + u;
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) {
-                const int cur = (u * KS + ks) & 1;
-                if (ks + 1 < KS) {
-                    load_frags(fr[cur ^ 1], u % STG, 32 * (ks + 1));
+            for (int st = 0; st < STEPS; ++st) {
+                const int h = st % NH, cp = (u * STEPS + st) & 1, cq = (u * KS + st / NH) & 1;
+                if (st + 1 < STEPS) {
+                    load_p(fp[cp ^ 1], u % STG, (st + 1) / NH, (st + 1) % NH);
+                    if (h + 1 == NH) load_q(fq[cq ^ 1], u % STG, (st + 1) / NH);
                 } else {
                     // chunk c + 1 has landed and every wave has read chunk c: its buffer takes chunk c + STG.  The
                     // fragments read past the last chunk are never used.
@@ -292,13 +343,15 @@ __global__ __launch_bounds__((S::T)) void prod_kernel(const ProdArgs a) {
                     if (c + STG < chunks) issue(c + STG, u % STG);
                     clear_tail(c + 1, (u + 1) % STG);
                     __builtin_amdgcn_sched_barrier(0);
-                    load_frags(fr[cur ^ 1], (u + 1) % STG, 0);
+                    load_p(fp[cp ^ 1], (u + 1) % STG, 0, 0);
+                    load_q(fq[cq ^ 1], (u + 1) % STG, 0);
                 }
 #pragma unroll
-                for (int j = 0; j < S::FN; ++j)
+                for (int jj = 0; jj < HN; ++jj)
 #pragma unroll
-                    for (int i = 0; i < S::FM; ++i) mma8(acc[j][i], fr[cur].p[j], fr[cur].q[i]);
-                sched_mix<MFMAS, READS>();
+                    for (int i = 0; i < S::FM; ++i) mma8(acc[h * HN + jj][i], fp[cp][jj], fq[cq][i]);
+                if (h + 1 == NH) sched_mix<MFMAS, READS_P + READS_Q>();
+                else sched_mix<MFMAS, READS_P>();
                 __builtin_amdgcn_sched_barrier(0);
             }
             if (c + 1 == chunks) goto multiplied;
@@ -306,26 +359,127 @@ __global__ __launch_bounds__((S::T)) void prod_kernel(const ProdArgs a) {
     }
 multiplied:
     mfma_drain();
+    int m[S::FM];
 #pragma unroll
-    for (int i = 0; i < S::FM; ++i) {
-        const int m = m0 + wm * S::WTM + 16 * i + c16;
-        if (m >= a.M) continue;
+    for (int i = 0; i < S::FM; ++i) m[i] = m0 + wm * S::WTM + 16 * i + c16;
+    constexpr int B = S::PAIR ? 2 : 1;  // column blocks that hold a lane's consecutive columns
 #pragma unroll
-        for (int j = 0; j < S::FN; j += E / 4) {
-            const int n = n0 + wn * S::WTN + 16 * j + E * g;
-            if (n >= a.N) continue;
-            float x[E];
+    for (int j = 0; j < S::FN; j += B) {
+        const int n = n0 + wn * S::WTN + 16 * j + 4 * B * g;
+        if (n >= a.N) continue;
+        float x[S::FM][E];
 #pragma unroll
-            for (int e = 0; e < E; ++e) x[e] = acc[j + e / 4][i][e % 4];
-            if (a.splits > 1) {
-                float* to = a.part + ((int64_t)split * a.M + m) * a.N + n;
+        for (int i = 0; i < S::FM; ++i)
 #pragma unroll
-                for (int e = 0; e < E; e += 4) *reinterpret_cast<float4*>(to + e) = make_float4(x[e], x[e + 1], x[e + 2], x[e + 3]);
-            } else {
-                finish_unit<ST>(a, m, n, x);
+            for (int e = 0; e < E; ++e) x[i][e] = acc[j + e / 4][i][e % 4];
+        if (a.splits > 1) {
+#pragma unroll
+            for (int i = 0; i < S::FM; ++i) {
+                if (m[i] >= a.M) continue;
+                float* to = a.part + ((int64_t)split * a.M + m[i]) * a.N + n;
+#pragma unroll
+                for (int e = 0; e < E; e += 4)
+                    *reinterpret_cast<float4*>(to + e) = make_float4(x[i][e], x[i][e + 1], x[i][e + 2], x[i][e + 3]);
+            }
+        } else {
+            finish_units<ST>(a, m, n, x);
+        }
+    }
+}
+
+// Few rows by a k-contiguous weight: W waves share the k of 16 columns by 16 FM rows, each with a ring of chunks of
+// its own (no barriers until the end), and their sums are added in order in LDS.  The weight's bytes bound it: 16
+// columns give every CU a part, and a CU has up to 64 KB of them in flight (1 x 16384 by 4096, weights not in a cache:
+// 25.6 us, 5.2 TB/s, against 34.5 of tiles with parts of K and their sum).  A weight with the columns along its rows
+// has 32 bytes of them side by side for 16 columns, and this kernel reads it at 2.5 TB/s: tiles of 64 columns
+// with parts of K do that better (38 us against 57 for 32 rows).
+template <typename ST, int FM>
+struct ProdRows : ProdShape<ST, true, true, 16, 16 * FM, 1, 1, FM == 1 ? 4 : 3> {};
+
+template <typename ST, int FM, int W>
+__global__ __launch_bounds__(64 * W) void prod_rows_kernel(const ProdArgs a) {
+    using S = ProdRows<ST, FM>;
+    constexpr int STG = S::STG, KS = S::KS, L = S::L, E = S::E, LDC = 16 + 4;
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, c16 = lane & 15;
+    const int n0 = xcd_logical_id(blockIdx.x, gridDim.x) * S::NT;
+    const ProdSide<S, true> P(a, n0, 0, lane);
+    const ProdSide<S, false> Q(a, 0, 0, lane);
+    unsigned char* ring = smem + wave * S::LDS;
+    const uint32_t lds = __builtin_amdgcn_readfirstlane(lds_addr(ring));
+    const int chunks = (a.K + S::KC - 1) / S::KC, mine = (chunks - wave + W - 1) / W;
+    auto issue = [&](int i, int buf) {
+        const int c = wave + i * W, v = a.K - c * S::KC;
+        P.issue(c, lds + buf * S::STAGE, v);
+        Q.issue(c, lds + buf * S::STAGE + S::P_BYTES, v);
+    };
+    f32x4 acc[FM];
+#pragma unroll
+    for (int m = 0; m < FM; ++m) acc[m] = zero4();
+#pragma unroll
+    for (int s = 0; s < STG; ++s)
+        if (s < mine) issue(s, s);
+    for (int i0 = 0; i0 < mine; i0 += STG) {
+#pragma unroll
+        for (int u = 0; u < STG; ++u) {
+            const int i = i0 + u;
+            if (i < mine) {
+                if (i + STG <= mine) wait_vmcnt<(STG - 1) * L>();
+                else wait_vmcnt<0>();
+                unsigned char *tp = ring + u * S::STAGE, *tq = tp + S::P_BYTES;
+                const int v = a.K - (wave + i * W) * S::KC;
+                if (v < S::KC) {
+                    P.clear(tp, v);
+                    Q.clear(tq, v);
+                    wave_sync();
+                }
+                __builtin_amdgcn_sched_barrier(0);
+                Frag8<ST> p[KS], q[KS][FM];
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) {
+                    p[ks] = ProdSide<S, true>::frag(tp, 0, 0, 32 * ks, g, c16);
+#pragma unroll
+                    for (int m = 0; m < FM; ++m) q[ks][m] = ProdSide<S, false>::frag(tq, 16 * m, 0, 32 * ks, g, c16);
+                }
+                lds_wait();  // read before another chunk takes their place
+                __builtin_amdgcn_sched_barrier(0);
+                if (i + STG < mine) issue(i + STG, u);
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+                    for (int m = 0; m < FM; ++m) mma8(acc[m], p[ks], q[ks][m]);
             }
         }
     }
+    mfma_drain();
+    __syncthreads();  // every wave has read its ring
+    float* sums = reinterpret_cast<float*>(smem);  // [wave][row][LDC]
+#pragma unroll
+    for (int m = 0; m < FM; ++m) *reinterpret_cast<f32x4*>(sums + ((wave * FM + m) * 16 + c16) * LDC + 4 * g) = acc[m];
+    __syncthreads();
+    for (int i = threadIdx.x; i < 16 * FM * (16 / E); i += 64 * W) {
+        const int m = i / (16 / E), n = i % (16 / E) * E;
+        if (m >= a.M || n0 + n >= a.N) continue;
+        float x[1][E];
+#pragma unroll
+        for (int e = 0; e < E; ++e) x[0][e] = 0.f;
+#pragma unroll
+        for (int w = 0; w < W; ++w)
+#pragma unroll
+            for (int e = 0; e < E; ++e) x[0][e] += sums[(w * 16 * FM + m) * LDC + n + e];
+        const int at[1] = {m};
+        finish_units<ST>(a, at, n0 + n, x);
+    }
+}
+
+template <typename ST, int FM, int W>
+int launch_prod_rows(const ProdArgs& a, hipStream_t stream) {
+    using S = ProdRows<ST, FM>;
+    constexpr int lds = W * S::LDS;
+    static_assert(lds <= 160 * 1024 && lds >= W * 16 * FM * 20 * 4, "rings, and the waves' sums in their place");
+    if (allow_lds((const void*)prod_rows_kernel<ST, FM, W>, lds)) return -1;
+    hipLaunchKernelGGL((prod_rows_kernel<ST, FM, W>), dim3((a.N + 15) / 16), dim3(64 * W), lds, stream, a);
+    return hipGetLastError() == hipSuccess ? 0 : -1;
 }
 
 // Parts of K added in order, and the epilogue.
@@ -335,19 +489,20 @@ __global__ __launch_bounds__(256) void prod_join_kernel(const ProdArgs a) {
     const int64_t units = (int64_t)a.M * a.N / E;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < units; i += (int64_t)gridDim.x * 256) {
         const int m = (int)(i * E / a.N), n = (int)(i * E - (int64_t)m * a.N);
-        float x[E];
+        float x[1][E];
 #pragma unroll
-        for (int e = 0; e < E; ++e) x[e] = 0.f;
+        for (int e = 0; e < E; ++e) x[0][e] = 0.f;
         const float* p = a.part + i * E;
 #pragma unroll 4
         for (int s = 0; s < a.splits; ++s) {
 #pragma unroll
             for (int e = 0; e < E; e += 4) {
                 const float4 v = *reinterpret_cast<const float4*>(p + (int64_t)s * a.M * a.N + e);
-                x[e] += v.x, x[e + 1] += v.y, x[e + 2] += v.z, x[e + 3] += v.w;
+                x[0][e] += v.x, x[0][e + 1] += v.y, x[0][e + 2] += v.z, x[0][e + 3] += v.w;
             }
         }
-        finish_unit<ST>(a, m, n, x);
+        const int at[1] = {m};
+        finish_units<ST>(a, at, n, x);
     }
 }
 

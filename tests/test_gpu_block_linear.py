@@ -51,7 +51,7 @@ def check(M, K, N, dtype, act, order, t):
 # one row to several tiles, edges on every side of a tile and of a chunk of k
 SIZES = [(1, 8, 8), (1, 64, 64), (2, 1024, 72), (3, 40, 72), (16, 128, 264), (17, 136, 200), (33, 2056, 64),
          (63, 72, 8), (64, 64, 64), (65, 72, 136), (100, 4104, 24), (128, 128, 128), (129, 264, 520), (300, 520, 1304),
-         (1000, 64, 8), (1025, 24, 1032)]
+         (1000, 64, 8), (1025, 24, 1032), (1, 4104, 3232), (20, 520, 3200), (32, 1096, 4104), (31, 8, 3080)]
 
 
 @pytest.mark.parametrize("order", ["in_out", "out_in"])
