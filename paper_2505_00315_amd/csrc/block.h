@@ -44,6 +44,26 @@ struct SumParts {
     void* out[3];
 };
 int launch_sum_parts(int dtype, const SumParts& s, hipStream_t stream);
+// Columns 32 block .. + 31 of vector `which`, by T lanes: T / 32 strands of parts, then the strands in order.
+// red: T doubles of LDS.
+template <typename ST, int T>
+__device__ __forceinline__ void sum_parts_columns(const SumParts& s, int which, int block, double* red) {
+    if (!s.out[which]) return;
+    const WideSum<ST>* p = static_cast<const WideSum<ST>*>(s.partial) + (size_t)which * s.cols;
+    const int c = threadIdx.x & 31, strand = threadIdx.x >> 5, col = block * 32 + c;
+    double x = 0.0;
+    if (col < s.cols) {
+#pragma unroll 8
+        for (int i = strand; i < s.parts; i += T / 32) x += p[(size_t)i * s.n * s.cols + col];
+    }
+    red[threadIdx.x] = x;
+    __syncthreads();
+    if (threadIdx.x < 32 && col < s.cols) {
+        double t = 0.0;
+        for (int i = 0; i < T / 32; ++i) t += red[32 * i + c];
+        st1<ST>(static_cast<ST*>(s.out[which]) + col, (float)t);
+    }
+}
 
 // ---------------------------------------------------------------------------
 // residual stream

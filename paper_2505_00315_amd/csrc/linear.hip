@@ -83,37 +83,71 @@ constexpr TileKind kTilesBf16[] = {{256, 1.61f, 1.61f, 7.f, 1}, {128, 0.66f, 0.4
 constexpr TileKind kTilesF32[] = {{64, 0.65f, 0.50f, 2.5f, 4}, {32, 0.36f, 0.17f, 2.5f, 4}};
 constexpr int kCus = 256;
 
+int kinds_of(int dtype) { return dtype == kBF16 ? 4 : 2; }
+const TileKind& kind_of(int dtype, int k) { return dtype == kBF16 ? kTilesBf16[k] : kTilesF32[k]; }
+int64_t tiles_of(int M, int N, int size) { return (int64_t)((M + size - 1) / size) * ((N + size - 1) / size); }
+
 // How a product is computed: kind of tiles, parts of K and k of each; rows: few rows, one launch.
 struct Plan {
     int kind, size, splits, kper;
     bool rows;
 };
-Plan plan_of(int dtype, int M, int N, int K, bool kcontig) {
-    const int kc = dtype == kBF16 ? 64 : 32, es = dtype == kBF16 ? 2 : 4;
-    const int64_t chunks = (K + kc - 1) / kc;
+// This kind and number of parts (splits 0: not one that there is).
+Plan tiled(int dtype, int M, int N, int K, int kind, int splits) {
+    const int kc = dtype == kBF16 ? 64 : 32, chunks = (K + kc - 1) / kc, per = (chunks + splits - 1) / splits;
+    if (splits > 1 && (per < 4 || (chunks + per - 1) / per != splits)) return {};
+    return {kind, kind_of(dtype, kind).size, splits, per * kc, false};
+}
+// The parts' sum: another launch, and its bytes at the rate of the last cache.
+float join_time(const Plan& p, int M, int N) { return p.splits > 1 ? 6.f + (float)p.splits * M * N * 8.f / 7e6f : 0.f; }
+
+// kcontig: the n side of the product (the weight) is k-contiguous.  time: what the plan is taken to need, us.
+Plan plan_of(int dtype, int M, int N, int K, bool kcontig, float* time = nullptr) {
+    const int kc = dtype == kBF16 ? 64 : 32;
     // Few rows by a k-contiguous weight: one launch where its workgroups are enough to read the weight at the memory's rate.
-    if (kcontig && M <= 32 && N >= 96 * 16) return {0, 0, 1, K, true};
-    const TileKind* kinds = dtype == kBF16 ? kTilesBf16 : kTilesF32;
-    const int count = dtype == kBF16 ? 4 : 2;
+    if (kcontig && M <= 32 && N >= 96 * 16) {
+        if (time) *time = 0.f;  // (never paired)
+        return {0, 0, 1, K, true};
+    }
     Plan best{};
     float least = 0.f;
-    for (int k = 0; k < count; ++k) {
-        const TileKind& t = kinds[k];
-        const int64_t tiles = (int64_t)((M + t.size - 1) / t.size) * ((N + t.size - 1) / t.size);
-        for (int splits = 1; splits <= 16; ++splits) {
-            const int64_t per = (chunks + splits - 1) / splits;
-            if (splits > 1 && (per < 4 || (chunks + per - 1) / per != splits)) continue;
+    for (int k = 0; k < kinds_of(dtype); ++k) {
+        const TileKind& t = kind_of(dtype, k);
+        const int64_t tiles = tiles_of(M, N, t.size);
+        for (const int splits : {1, 2, 3, 4, 6, 8, 12, 16}) {
+            const Plan p = tiled(dtype, M, N, K, k, splits);
+            if (!p.splits) continue;
             const int64_t n = (tiles * splits + kCus - 1) / kCus;  // workgroups of a CU
             const float chunk = t.alone > n * t.full ? t.alone : n * t.full;
-            float time = chunk * per + t.ends * ((n + t.fit - 1) / t.fit);
-            // the parts' sum: another launch, and its bytes at the rate of the last cache
-            if (splits > 1) time += 6.f + (float)splits * M * N * 8.f / 7e6f;
-            if (least == 0.f || time < least) least = time, best = {k, t.size, splits, (int)per * kc, false};
+            const float taken = chunk * (p.kper / kc) + t.ends * ((n + t.fit - 1) / t.fit) + join_time(p, M, N);
+            if (least == 0.f || taken < least) least = taken, best = p;
         }
     }
+    if (time) *time = least;
     return best;
 }
 size_t part_bytes(const Plan& p, int M, int N) { return p.splits > 1 ? (size_t)p.splits * M * N * sizeof(float) : 0; }
+
+// The tile shape of a kind.
+template <typename ST, bool PKC, bool QKC, int KIND>
+auto shape_of() {
+    if constexpr (sizeof(ST) == 2) {
+        if constexpr (KIND == 0) return ProdShape<ST, PKC, QKC, 256, 256, 2, 4, 2, 2>{};
+        else if constexpr (KIND == 1) return ProdShape<ST, PKC, QKC, 128, 128, 2, 2, 2>{};
+        else if constexpr (KIND == 2) return ProdShape<ST, PKC, QKC, 128, 128, 2, 4, 4>{};
+        else return ProdShape<ST, PKC, QKC, 64, 64, 2, 2, 4>{};
+    } else {
+        if constexpr (KIND == 0) return ProdShape<ST, PKC, QKC, 64, 64, 2, 2, 2>{};
+        else return ProdShape<ST, PKC, QKC, 32, 32, 2, 2, 2>{};
+    }
+}
+template <typename ST, bool PKC, bool QKC, int KIND>
+using ShapeOf = decltype(shape_of<ST, PKC, QKC, KIND>());
+
+void take_plan(ProdArgs& a, const Plan& p) {
+    a.tn = (a.N + p.size - 1) / p.size, a.tm = (a.M + p.size - 1) / p.size;
+    a.splits = p.splits, a.kper = p.kper;
+}
 
 template <typename ST, bool PKC, bool QKC>
 int product(ProdArgs a, const Plan& p, hipStream_t stream) {
@@ -125,19 +159,62 @@ int product(ProdArgs a, const Plan& p, hipStream_t stream) {
             return a.M <= 16 ? launch_prod_rows<ST, 1, 8>(a, stream) : launch_prod_rows<ST, 2, 8>(a, stream);
         }
     }
-    a.tn = (a.N + p.size - 1) / p.size, a.tm = (a.M + p.size - 1) / p.size;
-    a.splits = p.splits, a.kper = p.kper;
+    take_plan(a, p);
     if constexpr (sizeof(ST) == 2) {
-        switch (p.kind) {
-            case 0: return launch_prod<ProdShape<ST, PKC, QKC, 256, 256, 2, 4, 2, 2>>(a, stream);
-            case 1: return launch_prod<ProdShape<ST, PKC, QKC, 128, 128, 2, 2, 2>>(a, stream);
-            case 2: return launch_prod<ProdShape<ST, PKC, QKC, 128, 128, 2, 4, 4>>(a, stream);
-            default: return launch_prod<ProdShape<ST, PKC, QKC, 64, 64, 2, 2, 4>>(a, stream);
-        }
+        if (p.kind == 0) return launch_prod<ShapeOf<ST, PKC, QKC, 0>>(a, stream);
+        if (p.kind == 1) return launch_prod<ShapeOf<ST, PKC, QKC, 1>>(a, stream);
+        if (p.kind == 2) return launch_prod<ShapeOf<ST, PKC, QKC, 2>>(a, stream);
+        return launch_prod<ShapeOf<ST, PKC, QKC, 3>>(a, stream);
     } else {
-        if (p.kind == 0) return launch_prod<ProdShape<ST, PKC, QKC, 64, 64, 2, 2, 2>>(a, stream);
-        return launch_prod<ProdShape<ST, PKC, QKC, 32, 32, 2, 2, 2>>(a, stream);
+        if (p.kind == 0) return launch_prod<ShapeOf<ST, PKC, QKC, 0>>(a, stream);
+        return launch_prod<ShapeOf<ST, PKC, QKC, 1>>(a, stream);
     }
+}
+
+// dx and dw of a call, and the plans of both: one launch for the two (and for db's sum) where that is taken to be
+// shorter than one after the other (a launch that waits for another starts some 4 us late, and each leaves CUs idle
+// at its end).
+struct BwdPlan {
+    Plan dx, dw;    // alone
+    bool pair;
+    Plan dx2, dw2;  // in one launch
+};
+// The products' sizes: dx [M, K] over N; dw [K, N] or [N, K] over M.
+struct Size {
+    int M, N, K;
+};
+Size dx_size(const LinearArgs& a) { return {a.M, a.K, a.N}; }
+Size dw_size(const LinearArgs& a) { return a.out_in ? Size{a.N, a.K, a.M} : Size{a.K, a.N, a.M}; }
+BwdPlan plan_bwd(int dtype, const LinearArgs& a) {
+    const Size x = dx_size(a), w = dw_size(a);
+    float tx, tw;
+    BwdPlan best{plan_of(dtype, x.M, x.N, x.K, !a.out_in, &tx), plan_of(dtype, w.M, w.N, w.K, false, &tw), false, {}, {}};
+    if (best.dx.rows) return best;
+    float least = tx + tw + 6.f;
+    const int kc = dtype == kBF16 ? 64 : 32;
+    for (int k = 0; k < kinds_of(dtype); ++k) {
+        const TileKind& t = kind_of(dtype, k);
+        if (dtype == kBF16 && k % 2 == 0) continue;  // (workgroups of 4 waves; the large tiles' products are long)
+        const int64_t tx1 = tiles_of(x.M, x.N, t.size), tw1 = tiles_of(w.M, w.N, t.size);
+        for (const int sx : {1, 2, 4}) {
+            const Plan p = tiled(dtype, x.M, x.N, x.K, k, sx);
+            if (!p.splits) continue;
+            for (const int sw : {1, 2, 3, 4, 6, 8, 12, 16}) {
+                const Plan q = tiled(dtype, w.M, w.N, w.K, k, sw);
+                if (!q.splits) continue;
+                const int64_t bx = tx1 * sx, bw = tw1 * sw;
+                const float cx = (float)p.kper / kc, cw = (float)q.kper / kc, longest = cx > cw ? cx : cw;
+                const int64_t n = (bx + bw + kCus - 1) / kCus;
+                // a CU's share, in whole workgroups, and the longest workgroup
+                const float share = t.full * (bx * cx + bw * cw) / (float)(bx + bw) * n, alone = t.alone * longest;
+                const float jx = join_time(p, x.M, x.N), jw = join_time(q, w.M, w.N);
+                const float join = jx > 0.f && jw > 0.f ? jx + jw - 6.f : jx + jw;
+                const float time = (share > alone ? share : alone) + t.ends * ((n + t.fit - 1) / t.fit) + join;
+                if (time < least) least = time, best.pair = true, best.dx2 = p, best.dw2 = q;
+            }
+        }
+    }
+    return best;
 }
 
 size_t round256(size_t n) { return (n + 255) / 256 * 256; }
@@ -155,16 +232,25 @@ int forward_t(int dtype, const LinearArgs& a, void* scratch, hipStream_t stream)
 
 struct BwdScratch {  // offsets in bytes
     size_t dz, sums, part, total;
+    BwdPlan plan;
 };
 BwdScratch bwd_scratch(int dtype, const LinearArgs& a) {
     BwdScratch s{};
     const size_t es = dtype == kBF16 ? 2 : 4;
     s.sums = a.act ? round256((size_t)a.M * a.N * es) : 0;
     s.part = s.sums + round256((size_t)dz_split(dtype, a).parts * a.N * wide_sum_bytes(dtype));
-    const size_t dx = part_bytes(plan_of(dtype, a.M, a.K, a.N, !a.out_in), a.M, a.K);
-    const size_t dw = part_bytes(a.out_in ? plan_of(dtype, a.N, a.K, a.M, false) : plan_of(dtype, a.K, a.N, a.M, false), a.K, a.N);
-    s.total = s.part + (dx > dw ? dx : dw);
+    const Size x = dx_size(a), w = dw_size(a);
+    s.plan = plan_bwd(dtype, a);
+    // one product after the other, as also where a call wants one only; or both at once
+    const size_t dx = part_bytes(s.plan.dx, x.M, x.N), dw = part_bytes(s.plan.dw, w.M, w.N), one = dx > dw ? dx : dw;
+    const size_t both = s.plan.pair ? round256(part_bytes(s.plan.dx2, x.M, x.N)) + part_bytes(s.plan.dw2, w.M, w.N) : 0;
+    s.total = s.part + (both > one ? both : one);
     return s;
+}
+
+template <typename ST, bool OUT_IN, int KIND>
+int product_pair(const ProdPair& p, hipStream_t stream) {
+    return launch_prod_pair<ShapeOf<ST, !OUT_IN, true, KIND>, ShapeOf<ST, false, false, KIND>>(p, stream);
 }
 
 template <typename ST>
@@ -173,31 +259,39 @@ int backward_t(int dtype, const LinearArgs& a, void* scratch, hipStream_t stream
     const BwdScratch s = bwd_scratch(dtype, a);
     float* part = reinterpret_cast<float*>(at + s.part);
     Matrix dz = a.dy;
+    SumParts db{};
     if (a.act || a.db) {
         const DzSplit d = dz_split(dtype, a);
         WideSum<ST>* sums = a.db ? reinterpret_cast<WideSum<ST>*>(at + s.sums) : nullptr;
         ST* out = reinterpret_cast<ST*>(at + s.dz);
         hipLaunchKernelGGL((linear_dz_kernel<ST>), dim3(d.gx, d.parts), dim3(256), 0, stream, a, d.per, out, sums);
         if (hipGetLastError() != hipSuccess) return -1;
-        if (a.db && launch_sum_parts(dtype, SumParts{sums, d.parts, 1, a.N, {a.db, nullptr, nullptr}}, stream)) return -1;
         if (a.act) dz = Matrix{at + s.dz, a.N};
+        db = SumParts{sums, d.parts, a.db ? 1 : 0, a.N, {a.db, nullptr, nullptr}};
     }
     const int64_t es = sizeof(ST);
-    if (a.dx.p) {  // dz [M, N] by w^T: k is w's d_out axis
-        ProdArgs p{};
-        p.p = a.w.p, p.prow = a.w.row * es, p.q = dz.p, p.qrow = dz.row * es;
-        p.M = a.M, p.N = a.K, p.K = a.N, p.part = part, p.y = a.dx;
-        const Plan plan = plan_of(dtype, p.M, p.N, p.K, !a.out_in);
-        if (a.out_in ? product<ST, false, true>(p, plan, stream) : product<ST, true, true>(p, plan, stream)) return -1;
+    ProdArgs x{}, w{};
+    const Size sx = dx_size(a), sw = dw_size(a);
+    // dz by w^T: k is w's d_out axis
+    x.p = a.w.p, x.prow = a.w.row * es, x.q = dz.p, x.qrow = dz.row * es;
+    x.M = sx.M, x.N = sx.N, x.K = sx.K, x.part = part, x.y = a.dx;
+    // x^T dz, or dz^T x where w's rows are outputs
+    const Matrix &rows = a.out_in ? dz : a.x, &cols = a.out_in ? a.x : dz;
+    w.p = cols.p, w.prow = cols.row * es, w.q = rows.p, w.qrow = rows.row * es;
+    w.M = sw.M, w.N = sw.N, w.K = sw.K, w.part = part, w.y = a.dw;
+    if (a.dx.p && a.dw.p && s.plan.pair) {
+        const Plan &px = s.plan.dx2, &pw = s.plan.dw2;
+        take_plan(x, px), take_plan(w, pw);
+        w.part = reinterpret_cast<float*>(at + s.part + round256(part_bytes(px, x.M, x.N)));
+        const ProdPair p{x, w, db, 0, 0, false};
+        constexpr int FIRST = sizeof(ST) == 2 ? 1 : 0, SECOND = sizeof(ST) == 2 ? 3 : 1;
+        if (px.kind == FIRST) return a.out_in ? product_pair<ST, true, FIRST>(p, stream) : product_pair<ST, false, FIRST>(p, stream);
+        return a.out_in ? product_pair<ST, true, SECOND>(p, stream) : product_pair<ST, false, SECOND>(p, stream);
     }
-    if (a.dw.p) {  // x^T dz, or dz^T x where w's rows are outputs
-        const Matrix &rows = a.out_in ? dz : a.x, &cols = a.out_in ? a.x : dz;
-        ProdArgs p{};
-        p.p = cols.p, p.prow = cols.row * es, p.q = rows.p, p.qrow = rows.row * es;
-        p.M = a.out_in ? a.N : a.K, p.N = a.out_in ? a.K : a.N, p.K = a.M, p.part = part, p.y = a.dw;
-        if (product<ST, false, false>(p, plan_of(dtype, p.M, p.N, p.K, false), stream)) return -1;
-    }
-    return 0;
+    if (db.n && launch_sum_parts(dtype, db, stream)) return -1;
+    if (a.dx.p)
+        if (a.out_in ? product<ST, false, true>(x, s.plan.dx, stream) : product<ST, true, true>(x, s.plan.dx, stream)) return -1;
+    return a.dw.p ? product<ST, false, false>(w, s.plan.dw, stream) : 0;
 }
 
 }  // namespace

@@ -255,15 +255,14 @@ struct ProdSide {
     }
 };
 
+// Tile (and part of K) `id` of a product, by the whole workgroup.
 template <class S>
-__global__ __launch_bounds__((S::T)) void prod_kernel(const ProdArgs a) {
+__device__ __forceinline__ void prod_tile(const ProdArgs& a, int id, unsigned char* smem) {
     using ST = typename S::ST;
     constexpr int STG = S::STG, KS = S::KS, L = S::L, E = S::E;
-    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, c16 = lane & 15;
     const int wn = wave % S::WN, wm = wave / S::WN;
-    // Workgroups of an XCD take tiles of 8 row blocks side by side, so that they share operands in its L2.
-    int id = xcd_logical_id(blockIdx.x, gridDim.x);
+    // consecutive ids: tiles of 8 row blocks side by side, so that they share operands in an XCD's L2
     const int tiles = a.tm * a.tn, split = id / tiles;
     id -= split * tiles;
     const int band = id / (8 * a.tn), bm = min(8, a.tm - 8 * band), in = id - band * 8 * a.tn;
@@ -387,6 +386,37 @@ multiplied:
     }
 }
 
+template <class S>
+__global__ __launch_bounds__((S::T)) void prod_kernel(const ProdArgs a) {
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+    prod_tile<S>(a, xcd_logical_id(blockIdx.x, gridDim.x), smem);
+}
+
+// Two products and the sum of partials beside them in one launch: n1 and n2 workgroups (padded to multiples of 8, the
+// XCDs) for the tiles of each, the rest for 32 columns of the sums each.  The product with the longer workgroups goes
+// first (8192 x 4096 by 1024 beside 1024 x 8192 by 4096: 139 us, 175 with the others first, 160 one after the other).
+struct ProdPair {
+    ProdArgs a, b;
+    SumParts sums;
+    int n1, n2;
+    bool second_first;
+};
+template <class S1, class S2>
+__global__ __launch_bounds__((S1::T)) void prod_pair_kernel(const ProdPair p) {
+    static_assert(S1::T == S2::T, "one workgroup size");
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+    const int lead = p.second_first ? p.n2 : p.n1, b = blockIdx.x;
+    if (b >= p.n1 + p.n2) {
+        sum_parts_columns<typename S1::ST, S1::T>(p.sums, 0, b - p.n1 - p.n2, reinterpret_cast<double*>(smem));
+    } else if ((b < lead) != p.second_first) {
+        const int id = xcd_logical_id(p.second_first ? b - lead : b, p.n1);
+        if (id < p.a.tm * p.a.tn * p.a.splits) prod_tile<S1>(p.a, id, smem);
+    } else {
+        const int id = xcd_logical_id(p.second_first ? b : b - lead, p.n2);
+        if (id < p.b.tm * p.b.tn * p.b.splits) prod_tile<S2>(p.b, id, smem);
+    }
+}
+
 // Few rows by a k-contiguous weight: W waves share the k of 16 columns by 16 FM rows, each with a ring of chunks of
 // its own (no barriers until the end), and their sums are added in order in LDS.  The weight's bytes bound it: 16
 // columns give every CU a part, and a CU has up to 64 KB of them in flight (1 x 16384 by 4096, weights not in a cache:
@@ -482,10 +512,11 @@ int launch_prod_rows(const ProdArgs& a, hipStream_t stream) {
     return hipGetLastError() == hipSuccess ? 0 : -1;
 }
 
-// Parts of K added in order, and the epilogue.
+// Parts of K added in order, and the epilogue, of one product or two.
 template <typename ST>
-__global__ __launch_bounds__(256) void prod_join_kernel(const ProdArgs a) {
+__global__ __launch_bounds__(256) void prod_join_kernel(const ProdArgs first, const ProdArgs second) {
     constexpr int E = Unit<ST>::E;
+    const ProdArgs& a = blockIdx.y ? second : first;
     const int64_t units = (int64_t)a.M * a.N / E;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < units; i += (int64_t)gridDim.x * 256) {
         const int m = (int)(i * E / a.N), n = (int)(i * E - (int64_t)m * a.N);
@@ -506,18 +537,38 @@ __global__ __launch_bounds__(256) void prod_join_kernel(const ProdArgs a) {
     }
 }
 
+template <typename ST>
+int launch_prod_join(const ProdArgs& a, const ProdArgs& b, int count, hipStream_t stream) {
+    int64_t units = (int64_t)a.M * a.N;
+    if (count > 1 && (int64_t)b.M * b.N > units) units = (int64_t)b.M * b.N;
+    const int64_t need = (units / Unit<ST>::E + 255) / 256;
+    hipLaunchKernelGGL((prod_join_kernel<ST>), dim3((unsigned)(need < 4096 ? need : 4096), count), dim3(256), 0, stream, a, b);
+    return hipGetLastError() == hipSuccess ? 0 : -1;
+}
+
 template <class S>
 int launch_prod(const ProdArgs& a, hipStream_t stream) {
     if (allow_lds((const void*)prod_kernel<S>, S::LDS)) return -1;
     const int64_t blocks = (int64_t)a.tm * a.tn * a.splits;
     hipLaunchKernelGGL((prod_kernel<S>), dim3((unsigned)blocks), dim3(S::T), S::LDS, stream, a);
     if (hipGetLastError() != hipSuccess) return -1;
-    if (a.splits > 1) {
-        const int64_t units = (int64_t)a.M * a.N / S::E, need = (units + 255) / 256;
-        hipLaunchKernelGGL((prod_join_kernel<typename S::ST>), dim3((unsigned)(need < 4096 ? need : 4096)), dim3(256), 0,
-                           stream, a);
-        if (hipGetLastError() != hipSuccess) return -1;
-    }
+    return a.splits > 1 ? launch_prod_join<typename S::ST>(a, a, 1, stream) : 0;
+}
+
+// Both products with tiles of one size, their parts joined in one more launch.
+template <class S1, class S2>
+int launch_prod_pair(ProdPair p, hipStream_t stream) {
+    constexpr int lds = S1::LDS > S2::LDS ? S1::LDS : S2::LDS;
+    static_assert(lds >= S1::T * (int)sizeof(double), "the sums' place");
+    if (allow_lds((const void*)prod_pair_kernel<S1, S2>, lds)) return -1;
+    p.n1 = (p.a.tm * p.a.tn * p.a.splits + 7) / 8 * 8, p.n2 = (p.b.tm * p.b.tn * p.b.splits + 7) / 8 * 8;
+    p.second_first = p.b.kper > p.a.kper;
+    const int sums = p.sums.n ? (p.sums.cols + 31) / 32 : 0;
+    hipLaunchKernelGGL((prod_pair_kernel<S1, S2>), dim3(p.n1 + p.n2 + sums), dim3(S1::T), lds, stream, p);
+    if (hipGetLastError() != hipSuccess) return -1;
+    if (p.a.splits > 1 && p.b.splits > 1) return launch_prod_join<typename S1::ST>(p.a, p.b, 2, stream);
+    if (p.a.splits > 1) return launch_prod_join<typename S1::ST>(p.a, p.a, 1, stream);
+    if (p.b.splits > 1) return launch_prod_join<typename S1::ST>(p.b, p.b, 1, stream);
     return 0;
 }
 

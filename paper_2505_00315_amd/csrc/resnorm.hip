@@ -364,25 +364,11 @@ __global__ __launch_bounds__(256) void sequence_gate_kernel(ResidualArgs a, int 
     }
 }
 
-// 16 columns per workgroup: 64 strands of parts, then the strands in order.
+// 32 columns per workgroup (128 bytes of the partials at once): 32 strands of parts, then the strands in order.
 template <typename ST>
 __global__ __launch_bounds__(1024) void sum_parts_kernel(SumParts s) {
-    __shared__ double red[64][17];
-    if (!s.out[blockIdx.y]) return;
-    const WideSum<ST>* p = static_cast<const WideSum<ST>*>(s.partial) + (size_t)blockIdx.y * s.cols;
-    const int c = threadIdx.x & 15, strand = threadIdx.x >> 4, col = blockIdx.x * 16 + c;
-    double x = 0.0;
-    if (col < s.cols) {
-#pragma unroll 4
-        for (int i = strand; i < s.parts; i += 64) x += p[(size_t)i * s.n * s.cols + col];
-    }
-    red[strand][c] = x;
-    __syncthreads();
-    if (threadIdx.x < 16 && col < s.cols) {
-        double t = 0.0;
-        for (int i = 0; i < 64; ++i) t += red[i][c];
-        st1<ST>(static_cast<ST*>(s.out[blockIdx.y]) + col, (float)t);
-    }
+    __shared__ double red[1024];
+    sum_parts_columns<ST, 1024>(s, blockIdx.y, blockIdx.x, red);
 }
 
 // f(LPR, C) for the team of a row of d values.  One unit per lane keeps the backward's
@@ -457,7 +443,7 @@ int residual_bwd_t(const ResidualArgs& a, int dtype, void* dwpost, bool dgate, v
 }  // namespace
 
 int launch_sum_parts(int dtype, const SumParts& s, hipStream_t stream) {
-    const dim3 grid((s.cols + 15) / 16, s.n);
+    const dim3 grid((s.cols + 31) / 32, s.n);
     if (dtype == kBF16) hipLaunchKernelGGL((sum_parts_kernel<uint16_t>), grid, dim3(1024), 0, stream, s);
     else hipLaunchKernelGGL((sum_parts_kernel<float>), grid, dim3(1024), 0, stream, s);
     return hipGetLastError() == hipSuccess ? 0 : -1;
