@@ -32,8 +32,7 @@ __global__ __launch_bounds__(256) void linear_dz_kernel(LinearArgs a, int per, S
                 float z[E];
                 u.load(reinterpret_cast<const ST*>(a.z.p) + r * a.z.row + n);
                 u.get(z);
-#pragma unroll
-                for (int e = 0; e < E; ++e) d[e] *= act_slope<ST>(z[e], a.act);
+                times_slope<ST>(d, z, a.act);
                 u.set(d);
                 u.store(dz + r * a.N + n);
             }
