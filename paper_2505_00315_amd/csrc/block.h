@@ -7,6 +7,8 @@
 
 namespace mosa {
 
+constexpr int kCus = 256;  // of the chip
+
 // Sums of many terms whose result is stored.  With fp32 storage they are taken in
 // 64 bits, so that the result is rounded once; bf16 storage rounds it to 2^-8, far
 // above the error of an fp32 sum of the few dozen terms of a lane.

@@ -80,7 +80,6 @@ struct TileKind {
 constexpr TileKind kTilesBf16[] = {{256, 1.61f, 1.61f, 7.f, 1}, {128, 0.66f, 0.495f, 1.7f, 2}, {128, 0.54f, 0.54f, 2.f, 1},
                                    {64, 0.28f, 0.20f, 2.5f, 2}};
 constexpr TileKind kTilesF32[] = {{64, 0.65f, 0.50f, 2.5f, 4}, {32, 0.36f, 0.17f, 2.5f, 4}};
-constexpr int kCus = 256;
 
 int kinds_of(int dtype) { return dtype == kBF16 ? 4 : 2; }
 const TileKind& kind_of(int dtype, int k) { return dtype == kBF16 ? kTilesBf16[k] : kTilesF32[k]; }

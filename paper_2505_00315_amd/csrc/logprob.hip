@@ -417,20 +417,24 @@ __global__ __launch_bounds__(kThreads) void logprob_bwd_kernel(LogprobArgs a, in
     }
 }
 
-// Lanes of a workgroup, parts of a row and units of each.  Many rows: a workgroup of
-// 256 lanes each.  Fewer than the chip holds: parts of them.  A few rows, where
-// latency counts: 1024 lanes, and parts only for rows long enough to be worth a
-// second kernel (4 us).
+// Lanes of a workgroup, parts of a row and units of each; parts take a second kernel (4 us and the gap before it).
+// Measured (us, logits not in a cache): up to a row per CU 1024 lanes take a row at once (128 rows of 50001 fp32: 12.8
+// against 16.3 with parts for 256 lanes; 1 of 32000 bf16 with 20 alternatives: 10 against 12), in parts only very long
+// ones of a few (1 of 200000 fp32: 10.7 in 4 parts against 17.2).  More rows: 256 lanes (700 of 100000 bf16: 34 against 46),
+// and two parts where long rows are few for the chip (300 of 50001 fp32: 21.5 against 23.7; 512 of 32000 bf16: 11.4
+// without parts against 13.4).
 struct Split {
     int T, P, per;
 };
 Split parts_of(int dtype, int R, int V, int top) {
     const int E = dtype == kBF16 ? 8 : 4;
     const int64_t units = ((int64_t)V + 2 * E - 2) / E;  // (a row that does not start at a unit)
-    const int T = R < 128 && units > 4 * kThreads ? 1024 : kThreads;
-    int64_t P = T == 1024 ? 256 / R : 1024 / R;
-    const int64_t most = units / ((T == 1024 ? 8 : 4) * T);  // a part's reads keep its lanes busy
-    if (P > most) P = most;
+    int T = kThreads;
+    int64_t P = R > kCus && R < 2 * kCus && units >= 8192 ? 2 : 1;
+    if (R <= kCus && units > 4 * kThreads) {
+        T = 1024;
+        if (units >= 16 * 1024) P = kCus / R < units / 4096 ? kCus / R : units / 4096;
+    }
     if (top && P > kList / 2 / top) P = kList / 2 / top;
     if (P < 1) P = 1;
     const int64_t per = (units + P - 1) / P;

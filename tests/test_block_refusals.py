@@ -217,11 +217,11 @@ def test_logprob_arguments():
 
 
 def test_logprob_scratch():
-    s = dict(rows=1, vocab=200000)
+    s = dict(rows=1, vocab=400000)
     need = ops.logprob_scratch_size(ops.make_logprob_shape(**s, top=4))
     assert need > 0
-    assert status(*logprob(s, size=need - 1, logits=mat(200000))) == WS
-    assert status(*logprob(s, scratch=None, logits=mat(200000))) == INV
+    assert status(*logprob(s, size=need - 1, logits=mat(400000))) == WS
+    assert status(*logprob(s, scratch=None, logits=mat(400000))) == INV
 
 
 # ---------------------------------------------------------------------------

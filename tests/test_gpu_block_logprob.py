@@ -64,6 +64,13 @@ def test_sizes(R, V, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("R,V", [(1, 300007), (3, 140001), (130, 9001), (300, 66003), (600, 5000)])
+def test_parts_of_rows(R, V, dtype):
+    """Rows in parts that are joined, and one workgroup's."""
+    check(logits(R, R, V, dtype), targets_of(R, R, V), top=7)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("top,entropy", [(0, False), (0, True), (1, False), (32, True), (5, True)])
 def test_parts(top, entropy, dtype):
     for R, V in ((3, 40), (70, 3001), (2, 40000)):
@@ -72,7 +79,7 @@ def test_parts(top, entropy, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("V", [33, 5000, 70001])
+@pytest.mark.parametrize("V", [33, 5000, 70001, 262147])
 def test_equal_values(V, dtype):
     """Ties go to the lower index: rows of few different values, of one value, rising and falling."""
     g = torch.Generator().manual_seed(V)
@@ -87,7 +94,7 @@ def test_equal_values(V, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("V", [9, 700, 33333])
+@pytest.mark.parametrize("V", [9, 700, 33333, 150001])
 def test_masked(V, dtype):
     """-inf in places, in all but one, everywhere; the type's lowest value in places and everywhere; masked targets."""
     x = logits(V, 9, V, dtype)
@@ -108,7 +115,7 @@ def test_masked(V, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("V", [12, 3000, 40001])
+@pytest.mark.parametrize("V", [12, 3000, 40001, 140002])
 def test_not_finite(V, dtype):
     """A row with NaN or +inf is NaN throughout; the others are as without it; alternatives stay in order."""
     x = logits(V, 7, V, dtype)
