@@ -405,7 +405,7 @@ typedef struct mosa_matrix {
  * h is the stream behind the block and n what the next block reads.  post_norm 0:
  * u = y.  pre_norm 0: no n.  gate: none, one vector, one per sequence, or one per
  * token.  n is taken from h before h is rounded to its storage type.
- * d_model is a multiple of 8, at most 8192; batch seq_len is at most 2^31 - 1. */
+ * d_model is a multiple of 8, at most 8192; batch seq_len is below 2^30. */
 #define MOSA_GATE_NONE 0
 #define MOSA_GATE_VECTOR 1
 #define MOSA_GATE_SEQUENCE 2
@@ -474,7 +474,8 @@ int mosa_linear_backward(const mosa_linear_shape* s, const mosa_matrix* x, const
  * logp is 0 there.  Logits of -inf are tokens that cannot come (p = 0).  A row of
  * -inf alone has lse and every log p -inf, entropy 0 and gradients 0; a row with
  * +inf or NaN has NaN in all of them (its alternatives are in order, NaN as -inf).
- * vocab is at most 2^30; top is at most 32 and at most vocab; scale is positive.
+ * rows is at most 2^23, vocab at most 2^30; top is at most 32 and at most vocab;
+ * scale is positive.
  * Logits and their gradient need the alignment of one value only, and their rows
  * may lie any number of elements apart (at least vocab; logits also 0). */
 typedef struct mosa_logprob_shape {

@@ -21,7 +21,7 @@ int check_residual(const mosa_residual_shape* s) {
     if (s->gate < MOSA_GATE_NONE || s->gate > MOSA_GATE_TOKEN) return MOSA_ERR_INVALID_ARG;
     if (!scale_ok(s->residual_scale) || !scale_ok(s->branch_scale) || !(s->eps >= 0.0f && isfinite(s->eps)))
         return MOSA_ERR_INVALID_ARG;
-    if (s->d_model % 8 || s->d_model > 8192 || !rows_ok(s->batch, s->seq_len, 1)) return MOSA_ERR_UNSUPPORTED;
+    if (s->d_model % 8 || s->d_model > 8192 || !rows_ok(s->batch, s->seq_len, 2)) return MOSA_ERR_UNSUPPORTED;
     return MOSA_OK;
 }
 
@@ -98,7 +98,8 @@ int check_logprob(const mosa_logprob_shape* s) {
     if (!s || !dtype_ok(s->dtype)) return MOSA_ERR_INVALID_ARG;
     if (s->rows < 1 || s->vocab < 1 || s->top < 0 || s->top > s->vocab) return MOSA_ERR_INVALID_ARG;
     if (!(s->scale > 0.0f && isfinite(s->scale))) return MOSA_ERR_INVALID_ARG;
-    if (s->vocab > (1 << 30) || s->top > kMaxTop) return MOSA_ERR_UNSUPPORTED;
+    // (rows: a launch holds fewer than 2^32 lanes)
+    if (s->vocab > (1 << 30) || s->rows > (1 << 23) || s->top > kMaxTop) return MOSA_ERR_UNSUPPORTED;
     return MOSA_OK;
 }
 

@@ -77,7 +77,7 @@ struct TileKind {
     float alone, full, ends;
     int fit;
 };
-constexpr TileKind kTilesBf16[] = {{256, 1.61f, 1.61f, 7.f, 1}, {128, 0.66f, 0.495f, 1.7f, 2}, {128, 0.54f, 0.54f, 2.f, 1},
+constexpr TileKind kTilesBf16[] = {{256, 1.55f, 1.55f, 6.f, 1}, {128, 0.66f, 0.495f, 1.7f, 2}, {128, 0.49f, 0.49f, 4.5f, 1},
                                    {64, 0.28f, 0.20f, 2.5f, 2}};
 constexpr TileKind kTilesF32[] = {{64, 0.65f, 0.50f, 2.5f, 4}, {32, 0.36f, 0.17f, 2.5f, 4}};
 
@@ -97,7 +97,12 @@ Plan tiled(int dtype, int M, int N, int K, int kind, int splits) {
     return {kind, kind_of(dtype, kind).size, splits, per * kc, false};
 }
 // The parts' sum: another launch, and its bytes at the rate of the last cache.
-float join_time(const Plan& p, int M, int N) { return p.splits > 1 ? 6.f + (float)p.splits * M * N * 8.f / 7e6f : 0.f; }
+float join_time(const Plan& p, int M, int N) { return p.splits > 1 ? 5.f + (float)p.splits * M * N * 8.f / 5e6f : 0.f; }
+// A chunk of each of the n workgroups of a CU: two at a time, or all beside each other.
+float chunk_time(const TileKind& t, int64_t n) {
+    if (t.fit == 2) return (float)(n / 2) * 2.f * t.full + (float)(n % 2) * t.alone;
+    return t.alone > n * t.full ? t.alone : n * t.full;
+}
 
 // kcontig: the n side of the product (the weight) is k-contiguous.  time: what the plan is taken to need, us.
 Plan plan_of(int dtype, int M, int N, int K, bool kcontig, float* time = nullptr) {
@@ -116,8 +121,7 @@ Plan plan_of(int dtype, int M, int N, int K, bool kcontig, float* time = nullptr
             const Plan p = tiled(dtype, M, N, K, k, splits);
             if (!p.splits) continue;
             const int64_t n = (tiles * splits + kCus - 1) / kCus;  // workgroups of a CU
-            const float chunk = t.alone > n * t.full ? t.alone : n * t.full;
-            const float taken = chunk * (p.kper / kc) + t.ends * ((n + t.fit - 1) / t.fit) + join_time(p, M, N);
+            const float taken = chunk_time(t, n) * (p.kper / kc) + t.ends * ((n + t.fit - 1) / t.fit) + join_time(p, M, N);
             if (least == 0.f || taken < least) least = taken, best = p;
         }
     }
@@ -206,7 +210,7 @@ BwdPlan plan_bwd(int dtype, const LinearArgs& a) {
                 // a CU's share, in whole workgroups, and the longest workgroup
                 const float share = t.full * (bx * cx + bw * cw) / (float)(bx + bw) * n, alone = t.alone * longest;
                 const float jx = join_time(p, x.M, x.N), jw = join_time(q, w.M, w.N);
-                const float join = jx > 0.f && jw > 0.f ? jx + jw - 6.f : jx + jw;
+                const float join = jx > 0.f && jw > 0.f ? jx + jw - 5.f : jx + jw;
                 const float time = (share > alone ? share : alone) + t.ends * ((n + t.fit - 1) / t.fit) + join;
                 if (time < least) least = time, best.pair = true, best.dx2 = p, best.dw2 = q;
             }

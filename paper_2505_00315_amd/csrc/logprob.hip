@@ -372,46 +372,47 @@ template <typename ST>
 __global__ __launch_bounds__(kThreads) void logprob_bwd_kernel(LogprobArgs a, int P, int per, int64_t waves) {
     constexpr int E = Unit<ST>::E;
     const int lane = threadIdx.x & 63;
-    const int64_t w = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
-    if (w >= waves) return;
-    const int r = (int)(w / P), part = (int)(w % P);
-    const Row<ST> row(a.x, a.row, r, a.V);
-    ST* out = reinterpret_cast<ST*>(a.dx) + (int64_t)r * a.drow - row.lead;
-    const bool even = ((uintptr_t)out & 15) == 0;
-    const int u0 = part * per, u1 = min(row.units, u0 + per);
-    const float M = a.stats[2 * (int64_t)r], L = a.stats[2 * (int64_t)r + 1], c = a.scale * kLog2e;
-    const bool none = M == -INFINITY && L == -INFINITY;
-    const int t = a.target ? a.target[r] : -1;
-    const bool has = a.dlogp && t >= 0 && t < a.V && !none;
-    const float g = has ? a.scale * a.dlogp[r] : 0.f, gl = a.dlse ? a.scale * a.dlse[r] : 0.f;
-    const float ge = a.dent ? a.scale * a.dent[r] : 0.f, H = a.dent ? a.entropy[r] : 0.f;
-    // dx = p (A - ge log p) + g at the target
-    const float A = gl - g - ge * H, M0 = M == -INFINITY ? 0.f : M, L0 = none ? 0.f : L;
-    const float l2 = L0 * kLog2e, gk = ge * kLn2;
-    for (int u = u0 + lane; u < u1; u += 64) {
-        Unit<ST> v;
-        float x[E];
-        row.load(v, u);
-        row.get(v, u, x);
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-            const float d = (x[e] - M0) * c - l2, p = __builtin_amdgcn_exp2f(d);
-            x[e] = p * (A - gk * max2(d, kNoWeight));
-        }
-        const int j = t - row.first(u);
-        if (has && j >= 0 && j < E) {
-#pragma unroll
-            for (int e = 0; e < E; ++e) x[e] += e == j ? g : 0.f;
-        }
-        if (even && row.whole(u)) {
-            Unit<ST> o;
-            o.set(x);
-            o.store(out + (int64_t)u * E);
-        } else {
+    for (int64_t w = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6); w < waves;
+         w += (int64_t)gridDim.x * (kThreads / 64)) {
+        const int r = (int)(w / P), part = (int)(w % P);
+        const Row<ST> row(a.x, a.row, r, a.V);
+        ST* out = reinterpret_cast<ST*>(a.dx) + (int64_t)r * a.drow - row.lead;
+        const bool even = ((uintptr_t)out & 15) == 0;
+        const int u0 = part * per, u1 = min(row.units, u0 + per);
+        const float M = a.stats[2 * (int64_t)r], L = a.stats[2 * (int64_t)r + 1], c = a.scale * kLog2e;
+        const bool none = M == -INFINITY && L == -INFINITY;
+        const int t = a.target ? a.target[r] : -1;
+        const bool has = a.dlogp && t >= 0 && t < a.V && !none;
+        const float g = has ? a.scale * a.dlogp[r] : 0.f, gl = a.dlse ? a.scale * a.dlse[r] : 0.f;
+        const float ge = a.dent ? a.scale * a.dent[r] : 0.f, H = a.dent ? a.entropy[r] : 0.f;
+        // dx = p (A - ge log p) + g at the target
+        const float A = gl - g - ge * H, M0 = M == -INFINITY ? 0.f : M, L0 = none ? 0.f : L;
+        const float l2 = L0 * kLog2e, gk = ge * kLn2;
+        for (int u = u0 + lane; u < u1; u += 64) {
+            Unit<ST> v;
+            float x[E];
+            row.load(v, u);
+            row.get(v, u, x);
 #pragma unroll
             for (int e = 0; e < E; ++e) {
-                const int64_t i = (int64_t)row.first(u) + e;
-                if (i >= 0 && i < a.V) st1<ST>(out + (int64_t)u * E + e, x[e]);
+                const float d = (x[e] - M0) * c - l2, p = __builtin_amdgcn_exp2f(d);
+                x[e] = p * (A - gk * max2(d, kNoWeight));
+            }
+            const int j = t - row.first(u);
+            if (has && j >= 0 && j < E) {
+#pragma unroll
+                for (int e = 0; e < E; ++e) x[e] += e == j ? g : 0.f;
+            }
+            if (even && row.whole(u)) {
+                Unit<ST> o;
+                o.set(x);
+                o.store(out + (int64_t)u * E);
+            } else {
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    const int64_t i = (int64_t)row.first(u) + e;
+                    if (i >= 0 && i < a.V) st1<ST>(out + (int64_t)u * E + e, x[e]);
+                }
             }
         }
     }
@@ -422,14 +423,15 @@ __global__ __launch_bounds__(kThreads) void logprob_bwd_kernel(LogprobArgs a, in
 // against 16.3 with parts for 256 lanes; 1 of 32000 bf16 with 20 alternatives: 10 against 12), in parts only very long
 // ones of a few (1 of 200000 fp32: 10.7 in 4 parts against 17.2).  More rows: 256 lanes (700 of 100000 bf16: 34 against 46),
 // and two parts where long rows are few for the chip (300 of 50001 fp32: 21.5 against 23.7; 512 of 32000 bf16: 11.4
-// without parts against 13.4).
+// without parts against 13.4).  Many short rows: a wave each (8192 of 1000 bf16: 8 against 14, with 5 alternatives 19
+// against 35; of 8000: 23 against 22 and 39 against 40).
 struct Split {
     int T, P, per;
 };
 Split parts_of(int dtype, int R, int V, int top) {
     const int E = dtype == kBF16 ? 8 : 4;
     const int64_t units = ((int64_t)V + 2 * E - 2) / E;  // (a row that does not start at a unit)
-    int T = kThreads;
+    int T = R > 4 * kCus && units <= (top ? 1024 : 512) ? 64 : kThreads;
     int64_t P = R > kCus && R < 2 * kCus && units >= 8192 ? 2 : 1;
     if (R <= kCus && units > 4 * kThreads) {
         T = 1024;
@@ -443,7 +445,8 @@ Split parts_of(int dtype, int R, int V, int top) {
 
 template <typename ST, bool ENT, bool TOP>
 int forward_t(const LogprobArgs& a, const Split& s, const PartBuf& buf, hipStream_t stream) {
-    auto kern = s.T == 1024 ? logprob_kernel<ST, ENT, TOP, 1024> : logprob_kernel<ST, ENT, TOP, kThreads>;
+    auto kern = s.T == 1024 ? logprob_kernel<ST, ENT, TOP, 1024>
+                : s.T == 64 ? logprob_kernel<ST, ENT, TOP, 64> : logprob_kernel<ST, ENT, TOP, kThreads>;
     hipLaunchKernelGGL(kern, dim3((unsigned)((int64_t)a.R * s.P)), dim3(s.T), 0, stream, a, s.P, s.per, buf);
     if (hipGetLastError() != hipSuccess) return -1;
     if (s.P > 1) {
@@ -483,8 +486,7 @@ int launch_logprobs_bwd(int dtype, const LogprobArgs& a, hipStream_t stream) {
     const int E = dtype == kBF16 ? 8 : 4;
     const int per = 256;  // units of a wave: 4 per lane
     const int64_t units = ((int64_t)a.V + 2 * E - 2) / E, P = (units + per - 1) / per, waves = P * a.R;
-    const int64_t blocks = (waves + kThreads / 64 - 1) / (kThreads / 64);
-    if (blocks > 0x7fffffff) return -1;
+    const int64_t need = (waves + kThreads / 64 - 1) / (kThreads / 64), most = 1 << 22, blocks = need < most ? need : most;
     if (dtype == kBF16)
         hipLaunchKernelGGL((logprob_bwd_kernel<uint16_t>), dim3((unsigned)blocks), dim3(kThreads), 0, stream, a, (int)P, per, waves);
     else

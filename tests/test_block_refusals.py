@@ -40,7 +40,7 @@ def residual_back(kw=None, size=1 << 40, scratch=A, **change):
 @pytest.mark.parametrize("kw,want", [
     (dict(batch=0), INV), (dict(seq_len=0), INV), (dict(d_model=0), INV), (dict(d_model=68), UNS),
     (dict(d_model=8200), UNS), (dict(eps=-1.0), INV), (dict(eps=float("nan")), INV), (dict(branch_scale=float("inf")), INV),
-    (dict(residual_scale=float("nan")), INV), (dict(batch=1 << 16, seq_len=1 << 15), UNS),
+    (dict(residual_scale=float("nan")), INV), (dict(batch=1 << 15, seq_len=1 << 15), UNS),
 ])
 def test_residual_shapes(kw, want):
     base = dict(batch=2, seq_len=8, d_model=64)
@@ -192,7 +192,7 @@ def logprob_back(kw=None, **change):
 @pytest.mark.parametrize("kw,want", [
     (dict(rows=0), INV), (dict(vocab=0), INV), (dict(top=-1), INV), (dict(top=1001), INV), (dict(top=33), UNS),
     (dict(scale=0.0), INV), (dict(scale=-1.0), INV), (dict(scale=float("inf")), INV), (dict(scale=float("nan")), INV),
-    (dict(vocab=(1 << 30) + 1), UNS),
+    (dict(vocab=(1 << 30) + 1), UNS), (dict(rows=(1 << 23) + 1), UNS),
 ])
 def test_logprob_shapes(kw, want):
     with pytest.raises(mosa.MosaError) as e:

@@ -145,6 +145,25 @@ def test_relu_at_and_around_zero():
     assert torch.equal(db.isnan(), want.isnan()) and torch.equal(db.nan_to_num(9.0), want.nan_to_num(9.0))
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("act", ["gelu", "silu", "relu"])
+def test_infinities(act, dtype):
+    """An infinite product gives the activation's limit and the slope's; NaN stays."""
+    inf, nan = float("inf"), float("nan")
+    z = torch.tensor([[inf, -inf, nan, 60.0, -60.0, 3e38, -3e38, 0.0]] * 3, device="cuda").to(DT[dtype])
+    shape = ops.make_linear_shape(3, 8, 8, dtype, act=act)
+    x, w = torch.zeros(3, 8, dtype=DT[dtype], device="cuda"), torch.zeros(8, 8, dtype=DT[dtype], device="cuda")
+    y = ops.linear(shape, x, w, bias=z[0].contiguous())
+    big = float(z[0, 5])
+    want = torch.tensor([inf, 0.0, nan, 60.0, 0.0, big, 0.0, 0.0], device="cuda")
+    assert torch.equal(y[0].isnan(), want.isnan())
+    assert float((y[0].float().nan_to_num(0.0, posinf=1.0) - want.nan_to_num(0.0, posinf=1.0)).abs().max()) < 1e-15
+    _, _, db = ops.linear_backward(shape, x, w, torch.ones_like(z), z=z, grads="b")
+    half = {"gelu": 0.5, "silu": 0.5, "relu": 0.0}[act]
+    want = 3 * torch.tensor([1.0, 0.0, nan, 1.0, 0.0, 1.0, 0.0, half], device="cuda")
+    assert torch.equal(db.isnan(), want.isnan()) and float((db.float() - want).nan_to_num(0.0).abs().max()) < 1e-6
+
+
 @pytest.mark.parametrize("size", [(1, 1024, 512), (200, 520, 264), (2048, 512, 1024)])
 def test_captured(size):
     M, K, N = size

@@ -64,7 +64,8 @@ def test_sizes(R, V, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("R,V", [(1, 300007), (3, 140001), (130, 9001), (300, 66003), (600, 5000)])
+@pytest.mark.parametrize("R,V", [(1, 300007), (3, 140001), (130, 9001), (300, 66003), (600, 5000), (1500, 9), (1100, 3001),
+                                 (2000, 517)])
 def test_parts_of_rows(R, V, dtype):
     """Rows in parts that are joined, and one workgroup's."""
     check(logits(R, R, V, dtype), targets_of(R, R, V), top=7)
@@ -81,8 +82,10 @@ def test_parts(top, entropy, dtype):
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("V", [33, 5000, 70001, 262147])
 def test_equal_values(V, dtype):
-    """Ties go to the lower index: rows of few different values, of one value, rising and falling."""
+    """Ties go to the lower index: rows of few different values, of one value, rising and falling; many such rows."""
     g = torch.Generator().manual_seed(V)
+    if V < 100000:
+        check(torch.randint(-1, 2, (1100, min(V, 3000)), generator=g).to(DT[dtype]).cuda(), None, top=32, backward=False)
     x = torch.randint(-2, 3, (6, V), generator=g).float()
     x[1] = 1.5
     x[2] = torch.arange(V) / 64
