@@ -112,6 +112,9 @@ Plan plan_of(int dtype, int M, int N, int K, bool kcontig, float* time = nullptr
         if (time) *time = 0.f;  // (never paired)
         return {0, 0, 1, K, true};
     }
+    // No kind is faster than memory (a few rows by a weight of 16384 x 4096: 31 us with one workgroup for every CU, 38 with
+    // the two that would be enough for twice the products).
+    const float bytes = (float)(dtype == kBF16 ? 2 : 4) * ((float)M * K + (float)K * N + (float)M * N), floor = bytes / 5.2e6f;
     Plan best{};
     float least = 0.f;
     for (int k = 0; k < kinds_of(dtype); ++k) {
@@ -121,7 +124,8 @@ Plan plan_of(int dtype, int M, int N, int K, bool kcontig, float* time = nullptr
             const Plan p = tiled(dtype, M, N, K, k, splits);
             if (!p.splits) continue;
             const int64_t n = (tiles * splits + kCus - 1) / kCus;  // workgroups of a CU
-            const float taken = chunk_time(t, n) * (p.kper / kc) + t.ends * ((n + t.fit - 1) / t.fit) + join_time(p, M, N);
+            const float alone = chunk_time(t, n) * (p.kper / kc) + t.ends * ((n + t.fit - 1) / t.fit);
+            const float taken = (alone > floor ? alone : floor) + join_time(p, M, N);
             if (least == 0.f || taken < least) least = taken, best = p;
         }
     }

@@ -437,10 +437,10 @@ __global__ __launch_bounds__((S1::T)) void prod_pair_kernel(const ProdPair p) {
 
 // Few rows by a k-contiguous weight: W waves share the k of 16 columns by 16 FM rows, each with a ring of chunks of
 // its own (no barriers until the end), and their sums are added in order in LDS.  The weight's bytes bound it: 16
-// columns give every CU a part, and a CU has up to 64 KB of them in flight (1 x 16384 by 4096, weights not in a cache:
-// 25.6 us, 5.2 TB/s, against 34.5 of tiles with parts of K and their sum).  A weight with the columns along its rows
-// has 32 bytes of them side by side for 16 columns, and this kernel reads it at 2.5 TB/s: tiles of 64 columns
-// with parts of K do that better (38 us against 57 for 32 rows).
+// columns give every CU a part of narrow weights too, in one launch, and a CU has up to 64 KB of them in flight (weights
+// not in a cache: 1 x 4096 by 4096 8.4 us, 12.5 with tiles, parts of K and their sum; 1 x 16384 by 4096 25.5 us, 5.3
+// TB/s).  A weight with the columns along its rows has 32 bytes of them side by side for 16 columns, and this kernel
+// reads it at 2.5 TB/s: tiles of 64 columns with parts of K do that better (31 us against 57 for 32 rows by 16384 x 4096).
 template <typename ST, int FM>
 struct ProdRows : ProdShape<ST, true, true, 16, 16 * FM, 1, 1, FM == 1 ? 4 : 3> {};
 
