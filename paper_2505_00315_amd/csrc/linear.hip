@@ -3,7 +3,11 @@
 //   y = act(x w + b) + r;   dz = dy act'(z),  dx = dz w^T,  dw = x^T dz,  db = sum dz
 //
 // Three products of 2 rows d_in d_out operations each (prod.h); dz and db are one
-// pass over dy and z before them.
+// pass over dy and z before them (8192 x 4096 bf16: 48 us for 204 MB, 4.2 TB/s, with
+// gelu's slope; dy alone 29 us for 136 MB).
+//
+// Measured (bf16, 16384 rows, 8192 by 4096): forward 840 us, dx 855, dw 795, 1290 to
+// 1380 TFLOP/s (a library product of the same sizes 1375, of 8192^3 1393 and this one 1368).
 #include "prod.h"
 
 namespace mosa {
@@ -14,7 +18,7 @@ namespace {
 // 32 units of columns by 8 rows of lanes, a run of rows per workgroup.
 template <typename ST>
 __global__ __launch_bounds__(256) void linear_dz_kernel(LinearArgs a, int per, ST* __restrict__ dz, WideSum<ST>* __restrict__ part) {
-    constexpr int E = Unit<ST>::E;
+    constexpr int E = Unit<ST>::E, U = 4;
     __shared__ WideSum<ST> red[8][32 * E + 1];
     const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5, n = (blockIdx.x * 32 + tx) * E;
     const int64_t r0 = (int64_t)blockIdx.y * per, r1 = r0 + per < a.M ? r0 + per : a.M;
@@ -22,22 +26,30 @@ __global__ __launch_bounds__(256) void linear_dz_kernel(LinearArgs a, int per, S
 #pragma unroll
     for (int e = 0; e < E; ++e) s[e] = 0;
     if (n < a.N) {
-#pragma unroll 4
-        for (int64_t r = r0 + ty; r < r1; r += 8) {
-            Unit<ST> u;
-            float d[E];
-            u.load(reinterpret_cast<const ST*>(a.dy.p) + r * a.dy.row + n);
-            u.get(d);
-            if (a.act) {
-                float z[E];
-                u.load(reinterpret_cast<const ST*>(a.z.p) + r * a.z.row + n);
-                u.get(z);
-                times_slope<ST>(d, z, a.act);
-                u.set(d);
-                u.store(dz + r * a.N + n);
+        for (int64_t r = r0 + ty; r < r1; r += 8 * U) {
+            Unit<ST> y[U], z[U];  // U rows' loads together (a past row's: the last one's again)
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int64_t at = r + 8 * u < r1 ? r + 8 * u : r1 - 1;
+                y[u].load(reinterpret_cast<const ST*>(a.dy.p) + at * a.dy.row + n);
+                if (a.act) z[u].load(reinterpret_cast<const ST*>(a.z.p) + at * a.z.row + n);
             }
 #pragma unroll
-            for (int e = 0; e < E; ++e) s[e] += d[e];
+            for (int u = 0; u < U; ++u) {
+                if (r + 8 * u >= r1) break;
+                float d[E];
+                y[u].get(d);
+                if (a.act) {
+                    float v[E];
+                    z[u].get(v);
+                    times_slope<ST>(d, v, a.act);
+                    Unit<ST> o;
+                    o.set(d);
+                    o.store(dz + (r + 8 * u) * a.N + n);
+                }
+#pragma unroll
+                for (int e = 0; e < E; ++e) s[e] += d[e];
+            }
         }
     }
     if (!part) return;

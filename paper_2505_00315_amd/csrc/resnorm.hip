@@ -21,6 +21,12 @@
 // over the rows of its team, the teams of a workgroup are added in order, and the
 // workgroups' partials in a second kernel; a workgroup takes a run of rows, so a
 // sequence's gate has a partial per workgroup that its rows lie in.
+//
+// Measured (bf16, 4 x 4096 tokens of 4096, both norms, one gate): forward 105 us for
+// 537 MB, 5.1 TB/s; backward 180 us for 831 MB, 4.6 TB/s, and 6 us for the partials'
+// sum (a large copy on the same card: 5.0 to 5.2 TB/s).  The backward waits for its
+// three sums over the team one after the other; loads of the next row issued before them
+// took the registers of a wave in four and were no faster.  One token of 1024: 2.3 us.
 #include "block.h"
 
 namespace mosa {
