@@ -168,3 +168,56 @@ def test_a_step_in_a_graph():
             assert torch.equal(a, b), i
         # (the embedding's sum is torch's, in an order of its own)
         torch.testing.assert_close(got[-1], want[-1], rtol=1e-9, atol=1e-9)
+
+
+def test_on_another_stream():
+    """Work on a stream of the caller's, outputs and scratch made for it, while the current stream is busy."""
+    g = torch.Generator().manual_seed(3)
+    x, y, gate = (torch.randn(4, 300, 512, generator=g).bfloat16().cuda() for _ in range(3))
+    w = torch.randn(512, 4096, generator=g).bfloat16().cuda()
+    t = torch.randint(0, 4096, (1200,), generator=g, dtype=torch.int32).cuda()
+    rs = ops.make_residual_shape(4, 300, 512, post_norm=True, gate="token")
+    ls, ps = ops.make_linear_shape(1200, 512, 4096, act="silu"), ops.make_logprob_shape(1200, 4096, top=4)
+
+    def buffers():
+        return (torch.empty(1200, 4096, dtype=torch.bfloat16, device="cuda"), torch.empty(1200, 2, device="cuda"),
+                torch.ones(1200, device="cuda"))
+
+    def run(z, stats, ones, stream=None):
+        h, n = ops.residual_norm(rs, x, y, gate=gate, stream=stream)
+        o = ops.linear(ls, n.view(-1, 512), w, z=z, stream=stream)
+        res = ops.token_logprobs(ps, o, t, stats=stats, stream=stream)
+        d = ops.token_logprobs_backward(ps, o, t, stats, d_logp=ones, stream=stream)
+        dn, dw, db = ops.linear_backward(ls, n.view(-1, 512), w, d, z=z, grads="xwb", stream=stream)
+        dx, dy = ops.residual_norm_backward(rs, x, y, gate=gate, dn=dn.view_as(n), stream=stream)[:2]
+        return h, n, o, *res, d, dn, dw, db, dx, dy
+    want = run(*buffers())
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    mine = buffers()  # ready before the stream begins: what it reads and writes has no other work pending
+    side.wait_stream(torch.cuda.current_stream())
+    busy = torch.randn(4096, 4096, device="cuda")
+    for _ in range(3):
+        busy = busy @ busy * 1e-3
+    got = run(*mine, stream=side)
+    side.synchronize()
+    for i, (a, b) in enumerate(zip(got, want)):
+        if a is not None:
+            assert torch.equal(a, b), i
+    torch.cuda.synchronize()
+
+
+def test_a_gate_that_is_one_row():
+    """A token's gate may be one row for all of them; its gradient has every token's."""
+    g = torch.Generator().manual_seed(4)
+    x, y, dh = (torch.randn(2, 9, 72, generator=g).cuda() for _ in range(3))
+    row = torch.randn(72, generator=g).cuda()
+    token = ops.make_residual_shape(2, 9, 72, "f32", pre_norm=False, post_norm=True, gate="token")
+    vector = ops.make_residual_shape(2, 9, 72, "f32", pre_norm=False, post_norm=True, gate="vector")
+    wide = row.expand(2, 9, 72)
+    assert torch.equal(ops.residual_norm(token, x, y, gate=wide)[0], ops.residual_norm(vector, x, y, gate=row)[0])
+    a = ops.residual_norm_backward(token, x, y, gate=wide, dh=dh)
+    b = ops.residual_norm_backward(vector, x, y, gate=row, dh=dh)
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1]) and a[3].shape == (2, 9, 72)
+    # sums of 18 terms, in two orders
+    torch.testing.assert_close(a[3].double().sum((0, 1)), b[3].double(), rtol=0, atol=float(18 * 2 ** -24 * a[3].abs().max() * 18))
