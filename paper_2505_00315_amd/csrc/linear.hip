@@ -116,11 +116,26 @@ float chunk_time(const TileKind& t, int64_t n) {
     return t.alone > n * t.full ? t.alone : n * t.full;
 }
 
-// kcontig: the n side of the product (the weight) is k-contiguous.  time: what the plan is taken to need, us.
-Plan plan_of(int dtype, int M, int N, int K, bool kcontig, float* time = nullptr) {
+// Few rows by strips of a weight with its columns along its rows: us for the k of a strip, one strip of a CU after the
+// other.  Measured with 1, 16 and 32 rows (us; tiles): bf16 512 x 2048 3.4, 3.5, 3.8 (4.5, 4.6, 4.8), 1024 x 4096 6.4, 6.7,
+// 7.2 (7.3, 7.6, 8.1), 4096 x 4096 17, 18, 20 (14, 15, 13); fp32 512 x 2048 4.4, 4.7, 6.0 (9.0, 9.2, 9.3), 1024 x 4096 7.8, 8.1,
+// 10.6 (9.8, 10.9, 11.4), 4096 x 8192 30, 29, 33 (47, 47, 48), 4096 x
+// 16384 56, 58, 64 (86).
+constexpr int kStrip = 32;  // columns
+float strips_time(int dtype, int M, int N, int K) {
+    const float per_k = dtype == kBF16 ? (M <= 16 ? 0.0041f : 0.0047f) : M <= 16 ? 0.0050f : 0.0062f;
+    const int64_t strips = ((int64_t)N + kStrip - 1) / kStrip;
+    return 2.f + (float)((strips + kCus - 1) / kCus) * K * per_k;
+}
+
+// What lies k-contiguous of a product's sides: both (the weight is the n side), the m side, or neither.
+enum class Layout { kBoth, kRows, kNone };
+
+// time: what the plan is taken to need, us.
+Plan plan_of(int dtype, int M, int N, int K, Layout layout, float* time = nullptr) {
     const int kc = dtype == kBF16 ? 64 : 32;
     // Few rows by a k-contiguous weight: one launch where its workgroups are enough to read the weight at the memory's rate.
-    if (kcontig && M <= 32 && N >= 96 * 16) {
+    if (layout == Layout::kBoth && M <= 32 && N >= 96 * 16) {
         if (time) *time = 0.f;  // (never paired)
         return {0, 0, 1, K, true};
     }
@@ -141,9 +156,18 @@ Plan plan_of(int dtype, int M, int N, int K, bool kcontig, float* time = nullptr
             if (least == 0.f || taken < least) least = taken, best = p;
         }
     }
+    if (layout == Layout::kRows && M <= 32) {
+        // fp32 tiles have a quarter of the bytes of others in flight: weights of 4096 x 8192 to 16384 x 4096 at 2.9 to 3.1 TB/s.
+        if (dtype != kBF16 && least < bytes / 3.1e6f) least = bytes / 3.1e6f;
+        const float strips = strips_time(dtype, M, N, K), taken = strips > floor ? strips : floor;
+        if (taken < least) least = taken, best = {0, 0, 1, K, true};
+    }
     if (time) *time = least;
     return best;
 }
+// x w and dz w^T
+Layout forward_layout(const LinearArgs& a) { return a.out_in ? Layout::kBoth : Layout::kRows; }
+Layout dx_layout(const LinearArgs& a) { return a.out_in ? Layout::kRows : Layout::kBoth; }
 size_t part_bytes(const Plan& p, int M, int N) { return p.splits > 1 ? (size_t)p.splits * M * N * sizeof(float) : 0; }
 
 // The tile shape of a kind.
@@ -173,9 +197,16 @@ int product(ProdArgs a, const Plan& p, hipStream_t stream) {
         if (p.rows) {
             // Two workgroups of 4 waves per CU where there are enough of them: one's start and end beside the other's loads.
             if (a.N >= 2 * kCus * 16)
-                return a.M <= 16 ? launch_prod_rows<ST, 1, 4>(a, stream) : launch_prod_rows<ST, 2, 4>(a, stream);
-            return a.M <= 16 ? launch_prod_rows<ST, 1, 8>(a, stream) : launch_prod_rows<ST, 2, 8>(a, stream);
+                return a.M <= 16 ? launch_prod_rows<ProdRows<ST, true, 16, 1, 4>, 4>(a, stream)
+                                 : launch_prod_rows<ProdRows<ST, true, 16, 2, 3>, 4>(a, stream);
+            return a.M <= 16 ? launch_prod_rows<ProdRows<ST, true, 16, 1, 4>, 8>(a, stream)
+                             : launch_prod_rows<ProdRows<ST, true, 16, 2, 3>, 8>(a, stream);
         }
+    }
+    if constexpr (!PKC && QKC) {
+        if (p.rows)
+            return a.M <= 16 ? launch_prod_rows<ProdRows<ST, false, kStrip, 1, 2>, 8>(a, stream)
+                             : launch_prod_rows<ProdRows<ST, false, kStrip, 2, 2>, 8>(a, stream);
     }
     take_plan(a, p);
     if constexpr (sizeof(ST) == 2) {
@@ -206,7 +237,7 @@ Size dw_size(const LinearArgs& a) { return a.out_in ? Size{a.N, a.K, a.M} : Size
 BwdPlan plan_bwd(int dtype, const LinearArgs& a) {
     const Size x = dx_size(a), w = dw_size(a);
     float tx, tw;
-    BwdPlan best{plan_of(dtype, x.M, x.N, x.K, !a.out_in, &tx), plan_of(dtype, w.M, w.N, w.K, false, &tw), false, {}, {}};
+    BwdPlan best{plan_of(dtype, x.M, x.N, x.K, dx_layout(a), &tx), plan_of(dtype, w.M, w.N, w.K, Layout::kNone, &tw), false, {}, {}};
     if (best.dx.rows) return best;
     float least = tx + tw + 6.f;
     const int kc = dtype == kBF16 ? 64 : 32;
@@ -244,7 +275,7 @@ int forward_t(int dtype, const LinearArgs& a, void* scratch, hipStream_t stream)
     p.M = a.M, p.N = a.N, p.K = a.K;
     p.part = static_cast<float*>(scratch);
     p.bias = a.b, p.act = a.act, p.r = a.r, p.y = a.y, p.z = a.z;
-    const Plan plan = plan_of(dtype, a.M, a.N, a.K, a.out_in);
+    const Plan plan = plan_of(dtype, a.M, a.N, a.K, forward_layout(a));
     return a.out_in ? product<ST, true, true>(p, plan, stream) : product<ST, false, true>(p, plan, stream);
 }
 
@@ -314,7 +345,7 @@ int backward_t(int dtype, const LinearArgs& a, void* scratch, hipStream_t stream
 
 }  // namespace
 
-size_t linear_fwd_scratch(int dtype, const LinearArgs& a) { return part_bytes(plan_of(dtype, a.M, a.N, a.K, a.out_in), a.M, a.N); }
+size_t linear_fwd_scratch(int dtype, const LinearArgs& a) { return part_bytes(plan_of(dtype, a.M, a.N, a.K, forward_layout(a)), a.M, a.N); }
 size_t linear_bwd_scratch(int dtype, const LinearArgs& a) { return bwd_scratch(dtype, a).total; }
 
 int launch_linear(int dtype, const LinearArgs& a, void* scratch, hipStream_t stream) {

@@ -435,22 +435,24 @@ __global__ __launch_bounds__((S1::T)) void prod_pair_kernel(const ProdPair p) {
     }
 }
 
-// Few rows by a k-contiguous weight: W waves share the k of 16 columns by 16 FM rows, each with a ring of chunks of
-// its own (no barriers until the end), and their sums are added in order in LDS.  The weight's bytes bound it: 16
-// columns give every CU a part of narrow weights too, in one launch, and a CU has up to 64 KB of them in flight (weights
-// not in a cache: 1 x 4096 by 4096 8.4 us, 12.5 with tiles, parts of K and their sum; 1 x 16384 by 4096 25.5 us, 5.3
-// TB/s).  A weight with the columns along its rows has 32 bytes of them side by side for 16 columns, and this kernel
-// reads it at 2.5 TB/s: tiles of 64 columns with parts of K do that better (31 us against 57 for 32 rows by 16384 x 4096).
-template <typename ST, int FM>
-struct ProdRows : ProdShape<ST, true, true, 16, 16 * FM, 1, 1, FM == 1 ? 4 : 3> {};
+// Few rows: W waves share the k of NT columns by 16 FM rows, each with a ring of chunks of its own (no barriers until
+// the end), and their sums are added in order in LDS.  The weight's bytes bound it.  k-contiguous: 16 columns give every
+// CU a part of narrow weights too, in one launch, and a CU has up to 64 KB of them in flight (weights not in a cache: 1 x
+// 4096 by 4096 8.4 us, 12.5 with tiles, parts of K and their sum; 1 x 16384 by 4096 25.5 us, 5.3 TB/s).  A weight with
+// the columns along its rows: a CU gets some 260 of its rows per us, however wide a piece of each it takes (16, 32 and 64
+// columns, 2 to 4 chunks of each wave in flight and the strips of an XCD side by side or apart were alike), so that
+// the k of a strip bound it: 32 columns of 512 rows 3.0 us (tiles of 64 columns 4.4), of 1024 6.4 (7.3), of 4096 17
+// (14 with parts of K).
+template <typename ST, bool PKC, int NT, int FM, int STG>
+struct ProdRows : ProdShape<ST, PKC, true, NT, 16 * FM, 1, 1, STG> {};
 
-template <typename ST, int FM, int W>
+template <class S, int W>
 __global__ __launch_bounds__(64 * W) void prod_rows_kernel(const ProdArgs a) {
-    using S = ProdRows<ST, FM>;
-    constexpr int STG = S::STG, KS = S::KS, L = S::L, E = S::E, LDC = 16 + 4;
+    using ST = typename S::ST;
+    constexpr int STG = S::STG, KS = S::KS, L = S::L, E = S::E, FN = S::FN, FM = S::FM, NT = S::NT, LDC = NT + 4;
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, c16 = lane & 15;
-    const int n0 = xcd_logical_id(blockIdx.x, gridDim.x) * S::NT;
+    const int n0 = xcd_logical_id(blockIdx.x, gridDim.x) * NT;
     const ProdSide<S, true> P(a, n0, 0, lane);
     const ProdSide<S, false> Q(a, 0, 0, lane);
     unsigned char* ring = smem + wave * S::LDS;
@@ -461,9 +463,11 @@ __global__ __launch_bounds__(64 * W) void prod_rows_kernel(const ProdArgs a) {
         P.issue(c, lds + buf * S::STAGE, v);
         Q.issue(c, lds + buf * S::STAGE + S::P_BYTES, v);
     };
-    f32x4 acc[FM];
+    f32x4 acc[FN][FM];
 #pragma unroll
-    for (int m = 0; m < FM; ++m) acc[m] = zero4();
+    for (int j = 0; j < FN; ++j)
+#pragma unroll
+        for (int m = 0; m < FM; ++m) acc[j][m] = zero4();
 #pragma unroll
     for (int s = 0; s < STG; ++s)
         if (s < mine) issue(s, s);
@@ -482,10 +486,12 @@ __global__ __launch_bounds__(64 * W) void prod_rows_kernel(const ProdArgs a) {
                     wave_sync();
                 }
                 __builtin_amdgcn_sched_barrier(0);
-                Frag8<ST> p[KS], q[KS][FM];
+                Frag8<ST> p[KS][FN], q[KS][FM];
 #pragma unroll
                 for (int ks = 0; ks < KS; ++ks) {
-                    p[ks] = ProdSide<S, true>::frag(tp, 0, 0, 32 * ks, g, c16);
+#pragma unroll
+                    for (int j = 0; j < FN; ++j)
+                        p[ks][j] = ProdSide<S, true>::frag(tp, S::PAIR ? 32 * (j >> 1) : 16 * j, S::PAIR ? j & 1 : 0, 32 * ks, g, c16);
 #pragma unroll
                     for (int m = 0; m < FM; ++m) q[ks][m] = ProdSide<S, false>::frag(tq, 16 * m, 0, 32 * ks, g, c16);
                 }
@@ -495,7 +501,9 @@ __global__ __launch_bounds__(64 * W) void prod_rows_kernel(const ProdArgs a) {
 #pragma unroll
                 for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
-                    for (int m = 0; m < FM; ++m) mma8(acc[m], p[ks], q[ks][m]);
+                    for (int j = 0; j < FN; ++j)
+#pragma unroll
+                        for (int m = 0; m < FM; ++m) mma8(acc[j][m], p[ks][j], q[ks][m]);
             }
         }
     }
@@ -503,10 +511,14 @@ __global__ __launch_bounds__(64 * W) void prod_rows_kernel(const ProdArgs a) {
     __syncthreads();  // every wave has read its ring
     float* sums = reinterpret_cast<float*>(smem);  // [wave][row][LDC]
 #pragma unroll
-    for (int m = 0; m < FM; ++m) *reinterpret_cast<f32x4*>(sums + ((wave * FM + m) * 16 + c16) * LDC + 4 * g) = acc[m];
+    for (int j = 0; j < FN; ++j) {
+        const int n = S::PAIR ? 32 * (j >> 1) + 8 * g + 4 * (j & 1) : 16 * j + 4 * g;  // a lane's 4 columns of block j
+#pragma unroll
+        for (int m = 0; m < FM; ++m) *reinterpret_cast<f32x4*>(sums + ((wave * FM + m) * 16 + c16) * LDC + n) = acc[j][m];
+    }
     __syncthreads();
-    for (int i = threadIdx.x; i < 16 * FM * (16 / E); i += 64 * W) {
-        const int m = i / (16 / E), n = i % (16 / E) * E;
+    for (int i = threadIdx.x; i < 16 * FM * (NT / E); i += 64 * W) {
+        const int m = i / (NT / E), n = i % (NT / E) * E;
         if (m >= a.M || n0 + n >= a.N) continue;
         float x[1][E];
 #pragma unroll
@@ -520,13 +532,12 @@ __global__ __launch_bounds__(64 * W) void prod_rows_kernel(const ProdArgs a) {
     }
 }
 
-template <typename ST, int FM, int W>
+template <class S, int W>
 int launch_prod_rows(const ProdArgs& a, hipStream_t stream) {
-    using S = ProdRows<ST, FM>;
     constexpr int lds = W * S::LDS;
-    static_assert(lds <= 160 * 1024 && lds >= W * 16 * FM * 20 * 4, "rings, and the waves' sums in their place");
-    if (allow_lds((const void*)prod_rows_kernel<ST, FM, W>, lds)) return -1;
-    hipLaunchKernelGGL((prod_rows_kernel<ST, FM, W>), dim3((a.N + 15) / 16), dim3(64 * W), lds, stream, a);
+    static_assert(lds <= 160 * 1024 && lds >= W * S::MT * (S::NT + 4) * 4, "rings, and the waves' sums in their place");
+    if (allow_lds((const void*)prod_rows_kernel<S, W>, lds)) return -1;
+    hipLaunchKernelGGL((prod_rows_kernel<S, W>), dim3((a.N + S::NT - 1) / S::NT), dim3(64 * W), lds, stream, a);
     return hipGetLastError() == hipSuccess ? 0 : -1;
 }
 

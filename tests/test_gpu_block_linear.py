@@ -90,6 +90,16 @@ def test_large_tiles_fp32(size, order):
     check(*size, "f32", "gelu", order, make(7, *size, "f32", order))
 
 
+@pytest.mark.parametrize("order", ["in_out", "out_in"])
+@pytest.mark.parametrize("size,dtype", [((1, 1000, 2056), "bf16"), ((16, 1032, 4104), "bf16"), ((17, 520, 8200), "bf16"),
+                                        ((32, 72, 40), "bf16"), ((1, 2104, 8264), "f32"), ((15, 1000, 2056), "f32"),
+                                        ((32, 1544, 8200), "f32"), ((18, 40, 104), "f32")])
+def test_strips_of_a_few_rows(size, dtype, order):
+    """Few rows by strips of columns, forward and (with the sides exchanged) dx: ends inside a strip and a chunk."""
+    M, K, N = size if order == "in_out" else (size[0], size[2], size[1])
+    check(M, K, N, dtype, "silu", order, make(11, M, K, N, dtype, order))
+
+
 @pytest.mark.parametrize("M", [1, 3, 9, 70, 400])
 def test_rows_keep_to_themselves(M):
     """NaN in one row of x reaches that row of y and dx only; memory around the outputs stays as it is."""
