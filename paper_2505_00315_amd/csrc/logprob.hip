@@ -36,7 +36,8 @@ constexpr int kThreads = 256;
 constexpr int kList = 1024;  // values that are ranked at once
 
 // Maxima in one instruction: the compiler quiets NaN of fmaxf's arguments before each (2
-// instructions of 11 per value).  NaN are left out, as by fmaxf.
+// instructions of 11 per value).  Quiet NaN are left out, as by fmaxf; a signaling one
+// becomes the result, so that what is found by maxima is found again in rows with NaN.
 __device__ __forceinline__ float max2(float x, float y) {
     float r;
     asm("v_max_f32 %0, %1, %2" : "=v"(r) : "v"(x), "v"(y));
@@ -272,7 +273,7 @@ __global__ __launch_bounds__(T) void logprob_kernel(LogprobArgs a, int P, int pe
     }
     t = wave_join<ENT>(t, c);
     if ((tid & 63) == 0) runs[tid >> 6] = t;
-    const uint64_t mine = unit < 0 ? 0 : key_of(best, unit);  // (a lane without units: below every key)
+    uint64_t mine = unit < 0 ? 0 : key_of(best, unit);  // (a lane without units: below every key)
     if constexpr (TOP) {
         keys[tid] = mine;
         if (tid < 2) count[tid] = 0;
@@ -284,6 +285,20 @@ __global__ __launch_bounds__(T) void logprob_kernel(LogprobArgs a, int P, int pe
         else write_row<ST>(a, r, t, c);
     }
     if constexpr (TOP) {
+        if (t.l != t.l) {  // NaN (or +inf) in some lane's units: every lane's maximum without them
+            best = -INFINITY, unit = -1;
+            for (int u = u0 + tid; u < u1; u += T) {
+                Unit<ST> v;
+                float x[E], w = -INFINITY;
+                row.load(v, u);
+                row.get(v, u, x);
+#pragma unroll
+                for (int e = 0; e < E; ++e) w = x[e] > w ? x[e] : w;
+                if (w > best || unit < 0) best = w, unit = u;
+            }
+            keys[tid] = mine = unit < 0 ? 0 : key_of(best, unit);
+            __syncthreads();
+        }
         const float L = P > 1 ? 0.f : log_sum(t, c);
         auto put = [&](int rank, uint64_t key) {
             if (P > 1) buf.keys[((int64_t)r * P + part) * a.top + rank] = key;

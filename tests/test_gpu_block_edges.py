@@ -1,0 +1,53 @@
+"""Operators around a block: values and calls at the edges of what they allow."""
+import math
+
+import pytest
+import torch
+
+from block_util import logprobs64, within
+from paper_2505_00315_amd import ops
+
+pytestmark = pytest.mark.gpu
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+# NaN whose first bit of the fraction is 0, as no arithmetic makes them
+SIGNALING = {"bf16": (torch.int16, 0x7F81), "f32": (torch.int32, 0x7F800001)}
+
+
+def signaling(x, dtype, at):
+    """Signaling NaN in x at these indices of its flat values (set as bits: a copy of values may quiet them)."""
+    kind, bits = SIGNALING[dtype]
+    x.view(kind).view(-1)[torch.as_tensor(at, device=x.device)] = bits
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("R,V", [(9, 12), (9, 700), (9, 3000), (9, 40001), (9, 140002), (300, 3000), (300, 66003), (1100, 12),
+                                 (1100, 700), (1100, 9001)])
+def test_signaling_nan(R, V, dtype):
+    """A row with a signaling NaN is NaN throughout and its alternatives are in order, NaN as -inf, wherever in the row
+    the NaN lies and whatever the lane that meets it has seen before."""
+    g = torch.Generator().manual_seed(V)
+    x = (torch.randn(R, V, generator=g) * 3).to(DT[dtype]).cuda()
+    x[0] = -torch.arange(V) / 64  # falling: every lane's largest value is its first
+    x[1] = torch.arange(V) / 64
+    most = [0, V // 2, V - 1, min(V - 1, 7), min(V - 1, 3), V // 3]
+    for r in range(min(R, 8)):
+        at = {0: [0], 1: [V - 1], 2: most, 3: list(range(0, V, 2)), 4: list(range(7, V, 8)), 5: [],
+              6: list(range(V)), 7: most[1:2]}[r]
+        if at:
+            signaling(x, dtype, [r * V + i for i in at])
+    for r in range(8, R):
+        signaling(x, dtype, [r * V + int(i) for i in torch.randint(0, V, (3,), generator=g)])
+    assert bool(torch.isnan(x[4:5, 7::8]).all()) and not bool(torch.isnan(x[5]).any())
+    top = min(V, 8)
+    shape = ops.make_logprob_shape(R, V, dtype, top=top)
+    t = torch.randint(0, V, (R,), generator=g, dtype=torch.int32).cuda()
+    stats, ent = torch.empty(R, 2, device="cuda"), torch.empty(R, device="cuda")
+    ones = torch.ones(R, device="cuda")
+    # (the 64-bit form's conversion quiets NaN)
+    want = logprobs64(x, t, 1.0, top, d_logp=ones, d_entropy=ones)
+    logp, lse, top_logp, top_index = ops.token_logprobs(shape, x, t, stats=stats, entropy=ent)
+    for name, got in (("logp", logp), ("lse", lse), ("entropy", ent), ("top_logp", top_logp)):
+        within(got, *want[name], name)
+    assert torch.equal(top_index.long(), want["top_index"])
+    dx = ops.token_logprobs_backward(shape, x, t, stats, entropy=ent, d_logp=ones, d_entropy=ones)
+    within(dx, *want["dx"], "gradient")
