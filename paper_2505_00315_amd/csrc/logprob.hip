@@ -107,11 +107,19 @@ constexpr float kNear = 1048576.f;  // of m c: its rounding is at most 2^-5
 constexpr float kNoWeight = -1000.f;  // an exponent of weight 0 that times 0 gives 0
 __device__ __forceinline__ bool near_base(float m, float c) { return fabsf(m * c) < kNear; }
 
+// From the base of m0 to that of m1, both near: the difference of the rounded products that values were and are
+// taken against.  (One of them unrounded, as in a fused product and difference, would leave its rounding, up to
+// 2^-5, in the exponents.)
+__device__ __forceinline__ float base_step(float m0, float m1, float c) {
+#pragma clang fp contract(off)
+    return m0 * c - m1 * c;
+}
+
 // Sums of a maximum r.m in terms of a maximum m >= r.m.
 template <bool ENT>
 __device__ __forceinline__ void rebase(Run& r, float m, float c) {
     const bool from = near_base(r.m, c), to = near_base(m, c);
-    float d = from ? (to ? r.m * c - m * c : fmaf(-m, c, r.m * c)) : to ? fmaf(r.m, c, -(m * c)) : (r.m - m) * c;
+    float d = from ? (to ? base_step(r.m, m, c) : fmaf(-m, c, r.m * c)) : to ? fmaf(r.m, c, -(m * c)) : (r.m - m) * c;
     d = r.m == m ? 0.f : fmaxf(d, kNoWeight);
     const float f = __builtin_amdgcn_exp2f(d);
     if constexpr (ENT) r.s = f * (r.s + d * r.l);

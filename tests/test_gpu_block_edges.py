@@ -6,6 +6,7 @@ import torch
 
 from block_util import logprobs64, within
 from paper_2505_00315_amd import ops
+from test_gpu_block_logprob import check as check_logprobs
 
 pytestmark = pytest.mark.gpu
 DT = {"bf16": torch.bfloat16, "f32": torch.float32}
@@ -51,3 +52,18 @@ def test_signaling_nan(R, V, dtype):
     assert torch.equal(top_index.long(), want["top_index"])
     dx = ops.token_logprobs_backward(shape, x, t, stats, entropy=ent, d_logp=ones, d_entropy=ones)
     within(dx, *want["dx"], "gradient")
+
+
+@pytest.mark.parametrize("V", [60, 3001, 20001, 140002])
+@pytest.mark.parametrize("scale", [1.0, 0.3])
+@pytest.mark.parametrize("spread", [0.5, 40.0])
+def test_bases_at_their_limit(spread, scale, V):
+    """Rows whose largest exponent, in log2 units, lies just below, across and just above 2^20 (of either sign), with
+    weights of one size in all lanes and other maxima in each: the roundings of the lanes' bases, up to 2^-5 here,
+    leave the sums, whichever bases they are brought to."""
+    at = 2.0 ** 20 * math.log(2.0) / scale
+    g = torch.Generator().manual_seed(V)
+    shift = torch.tensor([at * f for f in (0.9, 0.999, 1.0, 1.001, 1.1, -0.9, -1.0, -1.1, 0.6)])
+    x = (torch.randn(9, V, generator=g) * spread + shift[:, None]).cuda()
+    t = torch.randint(0, V, (9,), generator=g, dtype=torch.int32).cuda()
+    check_logprobs(x, t, scale=scale, top=min(V, 5))
