@@ -475,7 +475,7 @@ int mosa_linear_backward(const mosa_linear_shape* s, const mosa_matrix* x, const
  * -inf alone has lse and every log p -inf, entropy 0 and gradients 0; a row with
  * +inf or NaN has NaN in all of them (its alternatives are in order, NaN as -inf).
  * rows is at most 2^23, vocab at most 2^30; top is at most 32 and at most vocab;
- * scale is positive.
+ * scale is positive and scale log2(e) in the range of fp32 (scale up to 2.35e38).
  * Logits and their gradient need the alignment of one value only, and their rows
  * may lie any number of elements apart (at least vocab; logits also 0). */
 typedef struct mosa_logprob_shape {

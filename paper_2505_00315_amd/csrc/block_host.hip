@@ -98,8 +98,9 @@ int check_logprob(const mosa_logprob_shape* s) {
     if (!s || !dtype_ok(s->dtype)) return MOSA_ERR_INVALID_ARG;
     if (s->rows < 1 || s->vocab < 1 || s->top < 0 || s->top > s->vocab) return MOSA_ERR_INVALID_ARG;
     if (!(s->scale > 0.0f && isfinite(s->scale))) return MOSA_ERR_INVALID_ARG;
-    // (rows: a launch holds fewer than 2^32 lanes)
-    if (s->vocab > (1 << 30) || s->rows > (1 << 23) || s->top > kMaxTop) return MOSA_ERR_UNSUPPORTED;
+    // (rows: a launch holds fewer than 2^32 lanes; scale: the kernels' exponents are powers of 2)
+    if (s->vocab > (1 << 30) || s->rows > (1 << 23) || s->top > kMaxTop || !isfinite(s->scale * kLog2e))
+        return MOSA_ERR_UNSUPPORTED;
     return MOSA_OK;
 }
 

@@ -67,3 +67,27 @@ def test_bases_at_their_limit(spread, scale, V):
     x = (torch.randn(9, V, generator=g) * spread + shift[:, None]).cuda()
     t = torch.randint(0, V, (9,), generator=g, dtype=torch.int32).cuda()
     check_logprobs(x, t, scale=scale, top=min(V, 5))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_extreme_scales(dtype):
+    """The largest scale that is taken, and one below the normal numbers."""
+    x = torch.zeros(4, 3000, dtype=DT[dtype], device="cuda")
+    x[1, 7] = 1.0
+    x[2] = torch.linspace(-1.0, 1.0, 3000).to(DT[dtype])
+    x[3] = (torch.arange(3000) % 7 * 2.0 ** -126).to(DT[dtype])
+    t = torch.tensor([0, 7, 2999, 6], dtype=torch.int32, device="cuda")
+    check_logprobs(x, t, scale=1e-40, top=3)
+    shape = ops.make_logprob_shape(4, 3000, dtype, top=3, scale=2.35e38)
+    want = logprobs64(x, t, shape.scale, 3)
+    ent = torch.empty(4, device="cuda")
+    logp, lse, top_logp, top_index = ops.token_logprobs(shape, x, t, entropy=ent)
+    assert torch.equal(top_index.long(), want["top_index"])
+    for name, got in (("logp", logp), ("lse", lse), ("entropy", ent), ("top_logp", top_logp)):
+        ref, bound = want[name]
+        if "logp" in name:
+            # The form's bound takes differences z - m up to 1e30 only (masked places are infinitely far).  Here they are up
+            # to 4.7e38 in 32 bits: a difference, a product and a difference, each off by 2^-24 of itself at most, so 3 2^-24
+            # (1.8e-7) of a log p that is all but z - m.
+            bound = bound + 3 * 2.0 ** -24 * ref.abs().clamp(max=1e39)
+        within(got, ref, bound, name)
