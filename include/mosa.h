@@ -460,8 +460,9 @@ int mosa_linear(const mosa_linear_shape* s, const mosa_matrix* x, const mosa_mat
                 const mosa_matrix* r, const mosa_matrix* y, const mosa_matrix* z, void* scratch,
                 size_t scratch_bytes, void* stream);
 /* From x, w, z (NULL with MOSA_ACT_NONE) and the gradient dy: dx, dw (rows as w's)
- * and db [d_out], each NULL where it is not needed.  The gradient of r is dy.
- * bf16 storage rounds dy act'(z) to bf16 where it enters the products. */
+ * and db [d_out], each NULL where it is not needed.  x may be NULL where dw is, w where
+ * dx is.  The gradient of r is dy.  bf16 storage rounds dy act'(z) to bf16 where it
+ * enters the products. */
 int mosa_linear_backward(const mosa_linear_shape* s, const mosa_matrix* x, const mosa_matrix* w,
                          const mosa_matrix* z, const mosa_matrix* dy, const mosa_matrix* dx, const mosa_matrix* dw,
                          void* db, void* scratch, size_t scratch_bytes, void* stream);

@@ -200,9 +200,11 @@ int mosa_linear_backward(const mosa_linear_shape* s, const mosa_matrix* x, const
     LinearArgs a = linear_args(s);
     if (!vector_ok(db) || (z != nullptr) != (s->act != MOSA_ACT_NONE)) return MOSA_ERR_INVALID_ARG;
     a.db = db;
-    // (an input that no asked gradient reads is checked all the same)
-    if (const int e = take_matrix(x, s->rows, s->d_in, s->dtype, false, &a.x)) return e;
-    if (const int e = take_weight(s, w, false, &a.w)) return e;
+    // (an input that no asked gradient reads is checked all the same where it is given)
+    if (x || dw)
+        if (const int e = take_matrix(x, s->rows, s->d_in, s->dtype, false, &a.x)) return e;
+    if (w || dx)
+        if (const int e = take_weight(s, w, false, &a.w)) return e;
     if (z)
         if (const int e = take_matrix(z, s->rows, s->d_out, s->dtype, false, &a.z)) return e;
     if (const int e = take_matrix(dy, s->rows, s->d_out, s->dtype, false, &a.dy)) return e;

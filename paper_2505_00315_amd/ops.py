@@ -554,10 +554,11 @@ def linear(shape, x, w, bias=None, residual=None, y=None, z=None, scratch=None, 
 def linear_backward(shape, x, w, dy, z=None, grads="xw", dx=None, dw=None, db=None, scratch=None, stream=None):
     """Gradients of linear from dy, that of y, and z of the forward (None without
     an activation).  grads: those that are wanted, of "x", "w" and "b"; tensors are
-    made for them where none is given.  The residual's gradient is dy.  Returns (dx,
-    dw, db), None in the place of those not wanted."""
+    made for them where none is given.  x may be None where "w" is not wanted, w where
+    "x" is not.  The residual's gradient is dy.  Returns (dx, dw, db), None in the place
+    of those not wanted."""
     st, xs, ws, ys = _linear_io(shape)
-    dev = _device(x, "x")
+    dev = _device(dy, "dy")
     if not set(grads) <= set("xwb"):
         raise ValueError(f"grads: {grads!r}, expected letters of 'xwb'")
 

@@ -5,7 +5,8 @@ import pytest
 import torch
 
 from block_util import logprobs64, within
-from paper_2505_00315_amd import ops
+from paper_2505_00315_amd import mosa, ops
+from test_gpu_block_linear import make as make_linear
 from test_gpu_block_logprob import check as check_logprobs
 
 pytestmark = pytest.mark.gpu
@@ -91,3 +92,24 @@ def test_extreme_scales(dtype):
             # (1.8e-7) of a log p that is all but z - m.
             bound = bound + 3 * 2.0 ** -24 * ref.abs().clamp(max=1e39)
         within(got, ref, bound, name)
+
+
+@pytest.mark.parametrize("order", ["in_out", "out_in"])
+@pytest.mark.parametrize("M", [3, 200])
+def test_product_gradients_without_what_they_do_not_read(M, order):
+    """dx needs no x (a frozen weight's product keeps no activations), dw no w, db neither; a missing one that is
+    read is refused."""
+    shape = ops.make_linear_shape(M, 136, 264, act="gelu", w_order=order)
+    t = make_linear(21, M, 136, 264, "bf16", order)
+    z = torch.empty_like(t["dy"])
+    ops.linear(shape, t["x"], t["w"], bias=t["bias"], z=z)
+    every = ops.linear_backward(shape, t["x"], t["w"], t["dy"], z=z, grads="xwb")
+    for grads, x, w in (("x", None, t["w"]), ("xb", None, t["w"]), ("w", t["x"], None), ("wb", t["x"], None),
+                        ("b", None, None)):
+        got = ops.linear_backward(shape, x, w, t["dy"], z=z, grads=grads)
+        for letter, a, b in zip("xwb", got, every):
+            assert (a is None) if letter not in grads else torch.equal(a, b)
+    for grads, x, w in (("w", None, t["w"]), ("xw", None, t["w"]), ("x", t["x"], None), ("xb", None, None)):
+        with pytest.raises(mosa.MosaError) as e:
+            ops.linear_backward(shape, x, w, t["dy"], z=z, grads=grads)
+        assert e.value.status == mosa.MOSA_ERR_INVALID_ARG
