@@ -113,3 +113,44 @@ def test_product_gradients_without_what_they_do_not_read(M, order):
         with pytest.raises(mosa.MosaError) as e:
             ops.linear_backward(shape, x, w, t["dy"], z=z, grads=grads)
         assert e.value.status == mosa.MOSA_ERR_INVALID_ARG
+
+
+def padded(rows, cols, dtype):
+    """A store of 7s and its middle [rows, cols], and whether what is around the middle is as it was."""
+    store = torch.full((rows + 2, cols + 16), 7.0, dtype=dtype, device="cuda")
+    around = torch.ones_like(store, dtype=torch.bool)
+    around[1:rows + 1, 8:cols + 8] = False
+    return store[1:rows + 1, 8:cols + 8], lambda: bool((store[around] == 7.0).all())
+
+
+@pytest.mark.parametrize("order", ["in_out", "out_in"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("M", [1, 3, 9, 70, 400, 2100])
+def test_product_gradients_keep_to_themselves(M, dtype, order):
+    """NaN in a row of dy or of z reaches that row of dx only, and infinities there too; dw and db are NaN in that
+    column; memory around z, dx, dw and y stays as it is."""
+    K, N = 328, 456
+    shape = ops.make_linear_shape(M, K, N, dtype, act="silu", w_order=order)
+    t = make_linear(22, M, K, N, dtype, order)
+    (y, y_ok), (z, z_ok), (dx, dx_ok), (dw, dw_ok) = (padded(*s, DT[dtype]) for s in ((M, N), (M, N), (M, K), t["w"].shape))
+    plain = torch.empty_like(t["dy"])
+    want_y = ops.linear(shape, t["x"], t["w"], bias=t["bias"], z=plain)
+    want = ops.linear_backward(shape, t["x"], t["w"], t["dy"], z=plain, grads="xwb")
+    ops.linear(shape, t["x"], t["w"], bias=t["bias"], y=y, z=z)
+    assert torch.equal(y, want_y) and torch.equal(z, plain)
+    db = torch.empty_like(want[2])
+    ops.linear_backward(shape, t["x"], t["w"], t["dy"], z=z, grads="xwb", dx=dx, dw=dw, db=db)
+    assert torch.equal(dx, want[0]) and torch.equal(dw, want[1]) and torch.equal(db, want[2])
+    r, col = M // 2, 5
+    others = torch.arange(M, device="cuda") != r
+    rest = torch.arange(N, device="cuda") != col
+    for what, bad in (("dy", float("nan")), ("z", float("nan")), ("dy", float("inf"))):
+        d = {"dy": t["dy"].clone(), "z": plain.clone()}
+        d[what][r, col] = bad
+        ops.linear_backward(shape, t["x"], t["w"], d["dy"], z=d["z"], grads="xwb", dx=dx, dw=dw, db=db)
+        assert torch.equal(dx[others], want[0][others]) and not bool(dx[r].isfinite().any())
+        by_output = dw.t() if order == "in_out" else dw  # [N, K]
+        want_dw = want[1].t() if order == "in_out" else want[1]
+        assert torch.equal(by_output[rest], want_dw[rest]) and not bool(by_output[col].isfinite().any())
+        assert torch.equal(db[rest], want[2][rest]) and not bool(db[col].isfinite())
+    assert y_ok() and z_ok() and dx_ok() and dw_ok()
