@@ -352,22 +352,46 @@ __global__ __launch_bounds__((TeamGeom<ST, LPR, C>::THREADS)) void residual_norm
     if (sums & 4) add_teams<ST, LPR, C>(cols, sg, lds, [&](int col, W v) { p[2 * a.d + col] = v; });
 }
 
-// dg of the sequences whose rows lie in several workgroups: their slots in order.
-template <typename ST>
-__global__ __launch_bounds__(256) void sequence_gate_kernel(ResidualArgs a, int per, const WideSum<ST>* __restrict__ slots) {
-    const int col = blockIdx.x * 256 + threadIdx.x;
-    if (col >= a.d) return;
+// dg of the sequences whose rows lie in several workgroups: their slots in order, by a lane per column; or, where
+// sequences are long, 32 columns by 32 strands of slots, then the strands in order.  (A sequence may have as many slots
+// as there are workgroups.  Backward of 1 x 4096 tokens of 1024, 2048 slots: 684 us with a lane per column, a memory's
+// latency per slot or so, 40 with strands; of 32 x 512 of 2048, 32 slots: 114 and 108; of 64 x 256, 16 slots: 104 and
+// 112; of 2048 x 4 of 8192, where sequences have 1 or none: 231 and 720.)
+constexpr int kManySlots = 24;
+template <typename ST, int STRANDS>
+__global__ __launch_bounds__((STRANDS == 1 ? 256 : 32 * STRANDS)) void sequence_gate_kernel(
+    ResidualArgs a, int per, const WideSum<ST>* __restrict__ slots) {
+    constexpr int COLS = STRANDS == 1 ? 256 : 32;
+    __shared__ double red[COLS * STRANDS];
+    const int c = threadIdx.x % COLS, strand = threadIdx.x / COLS, col = blockIdx.x * COLS + c;
     for (int b = blockIdx.y; b < a.B; b += gridDim.y) {
-        const int64_t r0 = (int64_t)b * a.T, r1 = r0 + a.T - 1;
-        const int k0 = (int)(r0 / per), k1 = (int)(r1 / per);
+        const int k0 = b * a.T / per, k1 = (b * a.T + a.T - 1) / per;
         if (k0 == k1) continue;
+        // the rows of the first workgroup may begin with another sequence, those of the rest begin with this one
+        const int behind = k0 * per / a.T != b;
         double s = 0.0;
-        for (int k = k0; k <= k1; ++k) {
-            const int first = (int)((int64_t)k * per / a.T);
-            s += slots[((size_t)k * 2 + (b != first)) * a.d + col];
+        if (col < a.d) {
+#pragma unroll 8
+            for (int k = k0 + strand; k <= k1; k += STRANDS) s += slots[((size_t)k * 2 + (k == k0 ? behind : 0)) * a.d + col];
         }
-        st1<ST>(row_ptr<ST>(a.dg, b, 0, 0) + col, (float)s);
+        if constexpr (STRANDS > 1) {
+            red[threadIdx.x] = s;
+            __syncthreads();
+            s = 0.0;
+            if (strand == 0) {
+                for (int i = 0; i < STRANDS; ++i) s += red[COLS * i + c];
+            }
+            __syncthreads();
+        }
+        if (strand == 0 && col < a.d) st1<ST>(row_ptr<ST>(a.dg, b, 0, 0) + col, (float)s);
     }
+}
+template <typename ST, int STRANDS>
+void launch_sequence_gate(const ResidualArgs& a, int per, const WideSum<ST>* slots, hipStream_t stream) {
+    // (a grid's second axis is bounded, and most sequences may have no slots: workgroups stride over them)
+    constexpr int COLS = STRANDS == 1 ? 256 : 32, MOST = STRANDS == 1 ? 4096 : kCus;
+    hipLaunchKernelGGL((sequence_gate_kernel<ST, STRANDS>), dim3((a.d + COLS - 1) / COLS, a.B < MOST ? a.B : MOST),
+                       dim3(COLS * STRANDS), 0, stream, a, per, slots);
 }
 
 // 32 columns per workgroup (128 bytes of the partials at once): 32 strands of parts, then the strands in order.
@@ -434,9 +458,8 @@ int residual_bwd_t(const ResidualArgs& a, int dtype, void* dwpost, bool dgate, v
     });
     if (hipGetLastError() != hipSuccess) return -1;
     if (slots && s.blocks > 1) {
-        // (a grid's second axis is bounded; its workgroups stride over the sequences)
-        hipLaunchKernelGGL((sequence_gate_kernel<ST>), dim3((a.d + 255) / 256, a.B < 4096 ? a.B : 4096), dim3(256), 0,
-                           stream, a, s.per, slots);
+        if (a.T / s.per >= kManySlots) launch_sequence_gate<ST, 32>(a, s.per, slots, stream);
+        else launch_sequence_gate<ST, 1>(a, s.per, slots, stream);
         if (hipGetLastError() != hipSuccess) return -1;
     }
     if (sums) {

@@ -8,6 +8,8 @@ from block_util import logprobs64, within
 from paper_2505_00315_amd import mosa, ops
 from test_gpu_block_linear import make as make_linear
 from test_gpu_block_logprob import check as check_logprobs
+from test_gpu_block_residual import check as check_stream
+from test_gpu_block_residual import make as make_stream
 
 pytestmark = pytest.mark.gpu
 DT = {"bf16": torch.bfloat16, "f32": torch.float32}
@@ -154,3 +156,13 @@ def test_product_gradients_keep_to_themselves(M, dtype, order):
         assert torch.equal(by_output[rest], want_dw[rest]) and not bool(by_output[col].isfinite().any())
         assert torch.equal(db[rest], want[2][rest]) and not bool(db[col].isfinite())
     assert y_ok() and z_ok() and dx_ok() and dw_ok()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("B,T,d", [(7, 23, 1032), (7, 24, 1032), (7, 25, 1032), (2, 97, 8), (5, 767, 64), (5, 768, 64),
+                                   (5, 773, 64), (3, 333, 200), (1, 2500, 1024), (40, 130, 264), (1, 24, 8192)])
+def test_gate_of_a_long_sequence(B, T, d, dtype):
+    """Sequences over few and over many workgroups' rows, that start with one and inside one: both ways of adding up
+    their parts."""
+    shape = ops.make_residual_shape(B, T, d, dtype, post_norm=True, pre_norm=True, gate="sequence")
+    check_stream(shape, "sequence", make_stream(B + T, B, T, d, dtype, True, True, "sequence"))
