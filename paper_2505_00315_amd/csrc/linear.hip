@@ -4,10 +4,10 @@
 //
 // Three products of 2 rows d_in d_out operations each (prod.h); dz and db are one
 // pass over dy and z before them (8192 x 4096 bf16: 48 us for 204 MB, 4.2 TB/s, with
-// gelu's slope; dy alone 29 us for 136 MB).
+// gelu's slope; dy alone 28 us for 136 MB).
 //
-// Measured (bf16, 16384 rows, 8192 by 4096): forward 840 us, dx 855, dw 795, 1290 to
-// 1380 TFLOP/s (a library product of the same sizes 1375, of 8192^3 1393 and this one 1368).
+// Measured (bf16, 16384 rows, 8192 by 4096): forward 885 us, dx 899, dw 839, 1220 to
+// 1310 TFLOP/s (a library product of the same sizes 1341, of 8192^3 1387).
 #include "prod.h"
 
 namespace mosa {
@@ -15,7 +15,12 @@ namespace mosa {
 namespace {
 
 // dz = dy act'(z) (where there is an activation) and partial sums of it over rows:
-// 32 units of columns by 8 rows of lanes, a run of rows per workgroup.
+// 32 units of columns by 8 rows of lanes, a run of rows per workgroup.  dz is kept in
+// storage type: with bf16 it is rounded once, as the matrix instruction takes bf16
+// operands only and two of them, dz and what its rounding leaves, would double both
+// products (some 125 us more for 8192 x 1024 by 4096).  So dx and dw are 0.0024 off
+// 64-bit results, 0.0017 without that rounding and z's, and 1.4e-4 off a form that
+// makes the two; db is the sum of dz before it is rounded.
 template <typename ST>
 __global__ __launch_bounds__(256) void linear_dz_kernel(LinearArgs a, int per, ST* __restrict__ dz, WideSum<ST>* __restrict__ part) {
     constexpr int E = Unit<ST>::E, U = 4;

@@ -4,7 +4,7 @@ import math
 import pytest
 import torch
 
-from block_util import logprobs64, within
+from block_util import U32, logprobs64, slope64, within
 from paper_2505_00315_amd import mosa, ops
 from test_gpu_block_linear import make as make_linear
 from test_gpu_block_logprob import check as check_logprobs
@@ -166,3 +166,29 @@ def test_gate_of_a_long_sequence(B, T, d, dtype):
     their parts."""
     shape = ops.make_residual_shape(B, T, d, dtype, post_norm=True, pre_norm=True, gate="sequence")
     check_stream(shape, "sequence", make_stream(B + T, B, T, d, dtype, True, True, "sequence"))
+
+
+@pytest.mark.parametrize("order", ["in_out", "out_in"])
+@pytest.mark.parametrize("act", ["gelu", "silu"])
+@pytest.mark.parametrize("M,K,N", [(33, 264, 1032), (1000, 520, 1304), (2048, 1024, 512)])
+def test_bf16_product_gradients_lose_one_rounding(M, K, N, act, order):
+    """With bf16 storage dx and dw are those of dy act'(z) rounded to bf16 once, and of nothing else that was rounded:
+    against the products of the rounded values they are off by 32-bit sums and their own rounding only."""
+    shape = ops.make_linear_shape(M, K, N, act=act, w_order=order)
+    t = make_linear(23, M, K, N, "bf16", order)
+    z = torch.empty_like(t["dy"])
+    ops.linear(shape, t["x"], t["w"], bias=t["bias"], z=z)
+    dx, dw, _ = ops.linear_backward(shape, t["x"], t["w"], t["dy"], z=z)
+    X, W = t["x"].double(), t["w"].double() if order == "in_out" else t["w"].double().t()
+    dy = t["dy"].double()
+    D = dy * slope64(z.double(), act)
+    # what 32 bits leave open of it (as in the bounds of all gradients), and of its rounding where that is near a tie
+    e = dy.abs() * 16 * U32 * (1 + z.double().abs()) + 9e-8 * dy.abs()
+    lo, hi, D = ((D + s * e).to(torch.bfloat16).double() for s in (-1, 1, 0))
+    open_ = torch.maximum((hi - D).abs(), (lo - D).abs())
+    for name, got, a, b, mag, gap in (
+            ("dx", dx, D, W.t(), D.abs() @ W.abs().t(), open_ @ W.abs().t()),
+            ("dw", dw if order == "in_out" else dw.t(), X.t(), D, X.abs().t() @ D.abs(), X.abs().t() @ open_)):
+        ref = a @ b
+        n = a.shape[1]
+        within(got, ref, 2.0 ** -8 * ref.abs() + gap + (n + 2) * U32 * mag, name)
