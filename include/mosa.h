@@ -404,7 +404,8 @@ typedef struct mosa_matrix {
  *   n = w_pre h / sqrt(mean(h^2) + eps)
  * h is the stream behind the block and n what the next block reads.  post_norm 0:
  * u = y.  pre_norm 0: no n.  gate: none, one vector, one per sequence, or one per
- * token.  n is taken from h before h is rounded to its storage type.
+ * token.  n is taken from h before h is rounded to its storage type.  The sums of
+ * d_model squares are fp32: rows where one passes its range come out as 0.
  * d_model is a multiple of 8, at most 8192; batch seq_len is below 2^30. */
 #define MOSA_GATE_NONE 0
 #define MOSA_GATE_VECTOR 1

@@ -10,8 +10,11 @@ namespace mosa {
 constexpr int kCus = 256;  // of the chip
 
 // Sums of many terms whose result is stored.  With fp32 storage they are taken in
-// 64 bits, so that the result is rounded once; bf16 storage rounds it to 2^-8, far
-// above the error of an fp32 sum of the few dozen terms of a lane.
+// 64 bits, so that the result is rounded once; with bf16 storage in fp32 by lane, in
+// order, and in 64 bits from the workgroups' partials on.  A lane's terms are the rows
+// over its workgroup's share: 32 of 16384 rows of 4096, 256 of 65536 rows of 8192, some
+// 2^15 where the longest inputs fill a card.  n terms are off by at most n 2^-24 of the
+// sum of their magnitudes, so by less than bf16's half step of 2^-8 of it even then.
 template <typename ST>
 using WideSum = std::conditional_t<sizeof(ST) == 4, double, float>;
 inline size_t wide_sum_bytes(int dtype) { return dtype == kBF16 ? sizeof(float) : sizeof(double); }

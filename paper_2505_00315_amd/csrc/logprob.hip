@@ -13,9 +13,9 @@
 // Forward: a workgroup takes a row or a part of one; every lane keeps a running
 // maximum and sum over its units of 16 bytes and they are joined at the end, the
 // parts of a row by a second kernel.  Measured (4096 rows of 131072 bf16): with entropy
-// 226 us for 1.07 GB, 4.7 TB/s, where the 10 vector instructions per value (an exponential
-// takes the time of 4) bound it; backward 357 us for 2.15 GB, 6.0 TB/s.  One row of
-// 32000 with 20 alternatives: 9.7 us, a chain of loads, sums, threshold and ranks.
+// 235 us for 1.07 GB, 4.6 TB/s, where the 10 vector instructions per value (an exponential
+// takes the time of 4) bound it; backward 388 us for 2.15 GB, 5.5 TB/s.  One row of
+// 32000 with 20 alternatives: 9.6 us, a chain of loads, sums, threshold and ranks.
 //
 // Alternatives (the `top` largest, equal ones by index): every lane also keeps the
 // first of its units that holds its maximum.  The lanes form 64 groups; the top-th

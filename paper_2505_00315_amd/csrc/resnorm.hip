@@ -23,10 +23,10 @@
 // sequence's gate has a partial per workgroup that its rows lie in.
 //
 // Measured (bf16, 4 x 4096 tokens of 4096, both norms, one gate): forward 105 us for
-// 537 MB, 5.1 TB/s; backward 180 us for 831 MB, 4.6 TB/s, and 6 us for the partials'
-// sum (a large copy on the same card: 5.0 to 5.2 TB/s).  The backward waits for its
+// 537 MB, 5.1 TB/s; backward 183 us for 831 MB, 4.5 TB/s, and 7 us for the partials'
+// sum (a large copy on the same card: 5.05 TB/s).  The backward waits for its
 // three sums over the team one after the other; loads of the next row issued before them
-// took the registers of a wave in four and were no faster.  One token of 1024: 2.3 us.
+// took the registers of a wave in four and were no faster.  One token of 1024: 2.4 us.
 #include "block.h"
 
 namespace mosa {
@@ -402,7 +402,10 @@ __global__ __launch_bounds__(1024) void sum_parts_kernel(SumParts s) {
 }
 
 // f(LPR, C) for the team of a row of d values.  One unit per lane keeps the backward's
-// sums within 125 registers, 4 waves per SIMD (two units: 224 registers, 2 waves).
+// sums within 128 registers, 4 waves per SIMD (with fp32 storage 93, 5 waves).  Rows of
+// more than 1024 units (fp32, above 4096 values) take two per lane: a workgroup of 1024
+// lanes has 128 registers for each, and 89 lie in memory (2 x 2048 tokens of 8192: backward
+// 300 us for 805 MB, 2.7 TB/s; the forward 100 us for 537 MB, 5.4).
 template <typename ST, typename F>
 int team_for(int d, F f) {
     const int units = d / Unit<ST>::E;
@@ -419,8 +422,10 @@ int team_for(int d, F f) {
     return f(std::integral_constant<int, 1024>{}, one);
 }
 
-// Workgroups of the backward and rows of each: enough to fill the chip, no more,
-// as each leaves partial sums.
+// Workgroups of the backward and rows of each: as many workgroups as the chip holds at
+// once, however few rows are left for each.  Each leaves partial sums, 3 vectors at most,
+// so that one row per workgroup (2048 rows of 1024 bf16) writes about as many bytes of
+// them as its rows have.
 struct BwdSplit {
     int blocks, per;
 };
